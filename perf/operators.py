@@ -381,8 +381,6 @@ def _own(st):
             h = R.Cache.wrap(st["K"], st["V"], st["s"], st["q"], st["n"], st["pos"], st["live"], st["t_next"], st["status"])
             if c["op"] == "tree_attend":
                 st["ws"] = torch.empty(R.roco_tree_attend_workspace_bytes(h, c["T"], c["group"]), dtype=torch.uint8, device=DEV)
-            else:
-                st["ws"] = torch.empty(R.roco_tree_commit_workspace_bytes(h, c["A"], c["group"]), dtype=torch.uint8, device=DEV)
         else:
             h = R.LinearState.wrap(st["state"], st["log_decay"], DT[c["dtype"]], st["status"])
             if c["op"] == "linear_prefill":
@@ -394,7 +392,7 @@ def _own(st):
         return {"out": st["out"], "lse": st["lse"]}
     if c["op"] == "tree_commit":
         R.roco_tree_commit(h, st["Q"], st["K_new"], st["V_new"], st["lse"], st["parent"], st["path"], st["path_len"], c["r"],
-                           st["evicted_slot"], evicted_pos=st["evicted_pos"], scale=st["scale"], workspace=st["ws"])
+                           st["evicted_slot"], evicted_pos=st["evicted_pos"], scale=st["scale"])
         return {k: st[k] for k in ("K", "V", "s", "q", "n", "pos", "live", "t_next", "evicted_slot", "evicted_pos")}
     if c["op"] == "linear_prefill":
         R.roco_linear_prefill(h, st["q"], st["k"], st["v"], st["lens"], st["out"], scale=st["scale"], workspace=st["ws"])
