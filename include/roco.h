@@ -66,7 +66,9 @@ typedef enum {
 enum {
   ROCO_DEV_WAIT_TIMEOUT = 1, /* a bounded wait on a shared-memory barrier ran out */
   ROCO_DEV_BAD_LIVE = 2,     /* live[u] outside [0, B]                            */
-  ROCO_DEV_BAD_VICTIM = 4    /* the selection produced no slot (NaN statistics)   */
+  ROCO_DEV_BAD_VICTIM = 4,   /* the selection produced no slot (NaN statistics)   */
+  ROCO_DEV_BAD_TREE = 8,     /* a node count, parent or accepted path that is none */
+  ROCO_DEV_BAD_LENS = 16     /* a prompt length outside [0, Lmax]                 */
 };
 
 /* The budgeted cache of Sec. 3/4 for S sequences x G (= layers*heads) units each; U = S*G.
@@ -365,6 +367,105 @@ roco_status roco_decode_step_cluster(roco_cache *cache, const void *q, const voi
                                      int scope_mode, int step_order, int ranks, float scale, void *attn_out,
                                      float *lse_out, int32_t *evicted_slot, int32_t *evicted_pos, void *stream);
 
+
+/*
+ * Attention of a tree of drafted tokens over the cache (speculative decoding; the paper has no counterpart).  A
+ * sequence's draft is a tree of up to T tokens: parent[i] < i is the node that node i continues, -1 a node that
+ * continues the cached prefix.  Every query head of node i attends over the unit's cached tokens, node i's ancestors
+ * and node i itself (Eq. 1 over that set):
+ *     x_ij = scale * Q_i.k_j,   lse_i = log sum_j exp x_ij,   attn_out_i = sum_j exp(x_ij - lse_i) v_j
+ * The cache and its statistics stay as they are: a verified path enters with roco_tree_commit.  One launch, two
+ * where the cached tokens are divided among several CTAs (few units).
+ *
+ *   Q            [S][G][T][group][d] (G counts key-value heads);  K_new, V_new [S][G][T][d]; cache->kv_dtype
+ *   parent       [S][T] int32 DEVICE array
+ *   nodes        [S] int32 DEVICE array, nodes of each sequence, 0..T; NULL: T everywhere.  Rows of Q, K_new and V_new
+ *                at nodes[b] and behind may hold anything, and those rows of attn_out and lse_out are left as they were
+ *   T, group     1 <= T <= ROCO_TREE_MAX_NODES, 1 <= group <= ROCO_TREE_MAX_GROUP
+ *   attn_out     [S][G][T][group][d];   lse_out [S][G][T][group] fp32, or NULL
+ *   workspace    >= roco_tree_attend_workspace_bytes(cache, T, group) device bytes (which may be 0: then NULL will do),
+ *                256-byte aligned, of this call alone while it runs
+ * What a node does not see has no influence on its row, whatever it holds: empty slots and nodes on other branches may
+ * be infinite or NaN.  A node count outside [0, T] sets ROCO_DEV_BAD_TREE and counts as 0; a parent outside [-1, i) sets
+ * it and counts as -1.
+ * On the tensor cores for kv_dtype ROCO_BF16 and a positive scale, on the CUDA cores otherwise.
+ */
+#define ROCO_TREE_MAX_NODES 64
+#define ROCO_TREE_MAX_GROUP 16
+size_t roco_tree_attend_workspace_bytes(const roco_cache *cache, int T, int group);
+roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void *K_new, const void *V_new,
+                             const int32_t *parent, const int32_t *nodes, int T, int group, float scale, void *attn_out,
+                             float *lse_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The accepted path of a draft tree enters the cache.  For a sequence that accepted a nodes path[0..a-1] (path[0] a
+ * child of the cached prefix, each next one a child of the one before), every unit of it does what a step of order
+ * ROCO_ATTEND_FIRST does for one token:
+ *   1. Statistics of Sec. 4.3 of the cached tokens j: Count += a, Acc += sum_i pbar_ij, Acc^square += sum_i pbar_ij^2 over
+ *      the accepted queries i, where pbar is the mean over the group's heads of p_ij = exp(scale * Q_i.K_j - lse_i) and
+ *      lse what roco_tree_attend returned for these Q, K_new, V_new, this scale and this cache.
+ *   2. live + a - B tokens (if positive) leave: the rule of Sec. 4.3 applied that many times on the updated statistics,
+ *      frozen, over the cached tokens (as roco_block_step does on the statistics before it).
+ *   3. The accepted tokens (positions t_next .. t_next + a - 1) take, in path order, the freed slots and then slots live,
+ *      live + 1, ..., all in increasing slot order.  Accepted token m starts with the queries that saw it, its own and
+ *      those behind it on the path: Count = a - m, Acc and Acc^square from their pbar_im.
+ * a = 0 leaves a sequence's units as they are.
+ *
+ *   Q, K_new, V_new, parent, T, group   as given to roco_tree_attend;   lse [S][G][T][group] fp32
+ *   path         [S][A] int32 DEVICE array of node indices;   path_len [S] int32 DEVICE array, 0..A
+ *   A            1 <= A <= ROCO_TREE_MAX_PATH, A <= T, r + A <= B; r >= 0 (ROCO_SCOPE_LOWEST_R: r >= 1)
+ *   evicted_slot [S][G][A] freed slots in increasing order, padded with -1;   evicted_pos likewise, or NULL
+ * A path_len outside [0, A] or a path that is not a chain of the tree from its root sets ROCO_DEV_BAD_TREE and counts
+ * as a = 0.  K_new and V_new must not overlap the cache.
+ */
+#define ROCO_TREE_MAX_PATH 16
+roco_status roco_tree_commit(roco_cache *cache, const void *Q, const void *K_new, const void *V_new, const float *lse,
+                             const int32_t *parent, const int32_t *path, const int32_t *path_len, int T, int group,
+                             int A, int r, int scope_mode, float scale, int32_t *evicted_slot, int32_t *evicted_pos,
+                             void *stream);
+
+/*
+ * Linear attention with a decay for each head (the paper has no counterpart): the other attention whose memory does not
+ * grow with the context.  A unit keeps one d x d matrix instead of cached tokens; with g = exp(log_decay) in [0, 1]
+ *     state_t = g state_{t-1} + k_t v_t^T,      out_t = scale * q_t state_t        (rows of the state belong to k)
+ * The caller owns the state, which is fp32 whatever dtype is, and zeroes it before a sequence starts.
+ */
+typedef struct {
+  int32_t dtype;          /* roco_dtype of q, k, v and out                                      */
+  int32_t S, G, d;        /* sequences, heads (of all layers of a call), head dimension 64 or 128 */
+  float *state;           /* [S][G][d][d], 16-byte aligned                                      */
+  const float *log_decay; /* [G] natural logarithm of the decay, <= 0; -inf: no memory          */
+  int32_t *status;        /* [1] device status word, zeroed by the caller                       */
+} roco_linear_state;
+
+/*
+ * A prompt, or the next piece of one: the recurrence over lens[b] tokens of every sequence, in chunks on the tensor
+ * cores for dtype ROCO_BF16, on the CUDA cores for ROCO_F32.  `state` is continued and holds state_{lens - 1} afterwards.
+ * Where the units are few the prompt is divided among several CTAs per unit, which meet in the workspace.
+ *
+ *   Q, K, V      [S][G][Lmax][d];  rows at lens[b] and behind may hold anything.  Rows before must be finite: a
+ *                NaN or infinity there may reach every output row of its unit
+ *   lens         [S] int32 DEVICE array, 0 <= lens <= Lmax; any other value sets ROCO_DEV_BAD_LENS and counts as 0.
+ *                lens 0 leaves a sequence's state as it is
+ *   out          [S][G][Lmax][d]; rows at lens[b] and behind are left as they were; must not overlap Q, K or V
+ *   workspace    >= roco_linear_prefill_workspace_bytes(state, Lmax) device bytes (which may be 0: then NULL will do),
+ *                256-byte aligned, of this call alone while it runs
+ */
+size_t roco_linear_prefill_workspace_bytes(const roco_linear_state *state, int Lmax);
+roco_status roco_linear_prefill(const roco_linear_state *state, const void *Q, const void *K, const void *V,
+                                const int32_t *lens, int Lmax, float scale, void *out, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
+ * One token for every sequence: state and out as above, one launch that reads and writes the states once.
+ *   q, k, v, out [S][G][d]
+ *   active       [S] int32 DEVICE array, or NULL (all): a sequence with 0 keeps its state and its rows of out
+ */
+roco_status roco_linear_step(const roco_linear_state *state, const void *q, const void *k, const void *v,
+                             const int32_t *active, float scale, void *out, void *stream);
+
+/* roco_device_status for the status word of a linear-attention state. */
+roco_status roco_linear_device_status(const roco_linear_state *state, void *stream, int32_t *flags_host);
 
 /*
  * Consistency of an importance score under a budget with its full-cache version (Sec. 4.3, preliminary

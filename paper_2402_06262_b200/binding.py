@@ -30,7 +30,12 @@ EXPORTS = ("roco_version", "roco_status_string", "roco_prefill_workspace_bytes",
            "roco_consistency_step", "roco_selftest_read_stream", "roco_decode_host_pipeline_staging_bytes",
            "roco_decode_step_host_begin", "roco_decode_step_host_end", "roco_gqa_block_step",
            "roco_prefill_blockwise_gqa", "roco_prefill_with_output", "roco_decode_cluster_ranks",
-           "roco_decode_step_cluster", "roco_decode_step_policy_ordered", "roco_decode_step_split_ordered")
+           "roco_decode_step_cluster", "roco_decode_step_policy_ordered", "roco_decode_step_split_ordered",
+           "roco_tree_attend_workspace_bytes", "roco_tree_attend", "roco_tree_commit",
+           "roco_linear_prefill_workspace_bytes", "roco_linear_prefill", "roco_linear_step",
+           "roco_linear_device_status")
+
+TREE_MAX_NODES, TREE_MAX_GROUP, TREE_MAX_PATH = 64, 16, 16
 
 
 class RocoError(RuntimeError):
@@ -44,6 +49,11 @@ class roco_cache(C.Structure):
                 ("K", C.c_void_p), ("V", C.c_void_p), ("s", C.c_void_p), ("q", C.c_void_p),
                 ("n", C.c_void_p), ("pos", C.c_void_p), ("live", C.c_void_p), ("t_next", C.c_void_p),
                 ("status", C.c_void_p)]
+
+
+class roco_linear_state(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("S", C.c_int32), ("G", C.c_int32), ("d", C.c_int32), ("state", C.c_void_p),
+                ("log_decay", C.c_void_p), ("status", C.c_void_p)]
 
 
 _lib = None
@@ -144,6 +154,26 @@ def lib() -> C.CDLL:
         L.roco_selftest_read_stream.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         L.roco_selftest_wait_timeout.restype = C.c_int
         L.roco_selftest_wait_timeout.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+        L.roco_tree_attend_workspace_bytes.restype = C.c_size_t
+        L.roco_tree_attend_workspace_bytes.argtypes = [C.POINTER(roco_cache), C.c_int, C.c_int]
+        L.roco_tree_attend.restype = C.c_int
+        L.roco_tree_attend.argtypes = [C.POINTER(roco_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                       C.c_void_p]
+        L.roco_tree_commit.restype = C.c_int
+        L.roco_tree_commit.argtypes = [C.POINTER(roco_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_float,
+                                       C.c_void_p, C.c_void_p, C.c_void_p]
+        L.roco_linear_prefill_workspace_bytes.restype = C.c_size_t
+        L.roco_linear_prefill_workspace_bytes.argtypes = [C.POINTER(roco_linear_state), C.c_int]
+        L.roco_linear_prefill.restype = C.c_int
+        L.roco_linear_prefill.argtypes = [C.POINTER(roco_linear_state), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.roco_linear_step.restype = C.c_int
+        L.roco_linear_step.argtypes = [C.POINTER(roco_linear_state), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_float, C.c_void_p, C.c_void_p]
+        L.roco_linear_device_status.restype = C.c_int
+        L.roco_linear_device_status.argtypes = [C.POINTER(roco_linear_state), C.c_void_p, C.c_void_p]
         L.roco_device_status.restype = C.c_int
         L.roco_device_status.argtypes = [C.POINTER(roco_cache), C.c_void_p, C.c_void_p]
         _lib = L
@@ -156,6 +186,29 @@ def status_string(code: int) -> str:
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else C.c_void_p(t.data_ptr())
+
+
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _need(what: str, name: str, t, shape, dtype):
+    """The argument checks that the C entry points cannot make: a tensor of this shape and type, contiguous, on the
+    current device."""
+    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or not t.is_contiguous()
+            or not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+        raise RocoError(1, f"{what}: {name}: a contiguous {dtype} tensor of shape {list(shape)} on the current CUDA device is "
+                           f"needed, got " + (f"{t.dtype} {list(t.shape)} on {t.device}" if isinstance(t, torch.Tensor)
+                                              else type(t).__name__))
+
+
+def _workspace(what: str, t, nbytes: int, like: torch.Tensor):
+    """The caller's workspace (checked), or one made for this call; None where none is needed."""
+    if t is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+    if not t.is_cuda or t.device != like.device or not t.is_contiguous():
+        raise RocoError(3, f"{what}: the workspace is a contiguous tensor on the arguments' device")
+    return t
 
 
 def _stream():
@@ -182,9 +235,58 @@ class Cache:
                             self.n.data_ptr(), self.pos.data_ptr(), self.live.data_ptr(), self.t_next.data_ptr(),
                             self.status.data_ptr())
 
+    @classmethod
+    def wrap(cls, K, V, s, q, n, pos, live, t_next, status) -> "Cache":
+        """A cache over tensors that the caller owns already (the shapes and types of a new Cache)."""
+        if not isinstance(K, torch.Tensor) or K.dim() != 4 or K.dtype not in (torch.float32, torch.bfloat16):
+            raise RocoError(1, "Cache.wrap: K is an fp32 or bf16 tensor [S][G][B][d]")
+        c = cls.__new__(cls)
+        c.S, c.G, c.B, c.d = K.shape
+        c.dtype = K.dtype
+        for name, t, shape, dtype in (("K", K, (c.S, c.G, c.B, c.d), K.dtype), ("V", V, (c.S, c.G, c.B, c.d), K.dtype),
+                                      ("s", s, (c.S, c.G, c.B), torch.float32), ("q", q, (c.S, c.G, c.B), torch.float32),
+                                      ("n", n, (c.S, c.G, c.B), torch.int32), ("pos", pos, (c.S, c.G, c.B), torch.int32),
+                                      ("live", live, (c.S, c.G), torch.int32), ("t_next", t_next, (c.S, c.G), torch.int32),
+                                      ("status", status, (1,), torch.int32)):
+            _need("Cache.wrap", name, t, shape, dtype)
+            setattr(c, name, t)
+        c.c = roco_cache(ROCO_F32 if c.dtype == torch.float32 else ROCO_BF16, c.S, c.G, c.d, c.B,
+                         *(getattr(c, f).data_ptr() for f in ("K", "V", "s", "q", "n", "pos", "live", "t_next", "status")))
+        return c
+
     @property
     def U(self) -> int:
         return self.S * self.G
+
+
+class LinearState:
+    """Device tensors of the decayed d x d states of S sequences x G heads, plus the C struct over them.  log_decay:
+    [G] natural logarithms of the heads' decays, <= 0."""
+
+    def __init__(self, S: int, G: int, d: int, dtype: torch.dtype, log_decay, device="cuda"):
+        self._set(torch.zeros(S, G, d, d, dtype=torch.float32, device=device),
+                  torch.as_tensor(log_decay, dtype=torch.float32).to(device).contiguous(), dtype,
+                  torch.zeros(1, dtype=torch.int32, device=device))
+
+    @classmethod
+    def wrap(cls, state, log_decay, dtype: torch.dtype, status) -> "LinearState":
+        """Over tensors that the caller owns already: state [S][G][d][d] and log_decay [G] fp32, status [1] int32."""
+        c = cls.__new__(cls)
+        c._set(state, log_decay, dtype, status)
+        return c
+
+    def _set(self, state, log_decay, dtype, status):
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise RocoError(2, "LinearState: q, k, v and out are fp32 or bf16")
+        if not isinstance(state, torch.Tensor) or state.dim() != 4:
+            raise RocoError(1, "LinearState: the state is a tensor [S][G][d][d]")
+        self.S, self.G, self.d, _ = state.shape
+        _need("LinearState", "state", state, (self.S, self.G, self.d, self.d), torch.float32)
+        _need("LinearState", "log_decay", log_decay, (self.G,), torch.float32)
+        _need("LinearState", "status", status, (1,), torch.int32)
+        self.state, self.log_decay, self.status, self.dtype = state, log_decay, status, dtype
+        self.c = roco_linear_state(ROCO_F32 if dtype == torch.float32 else ROCO_BF16, self.S, self.G, self.d,
+                                   state.data_ptr(), log_decay.data_ptr(), status.data_ptr())
 
 
 def roco_prefill_workspace_bytes(cache: Cache, Lmax: int) -> int:
@@ -457,4 +559,112 @@ def roco_device_status(cache: Cache) -> int:
     rc = lib().roco_device_status(C.byref(cache.c), _stream(), C.byref(flags))
     if rc not in (ROCO_OK, 5):
         raise RocoError(rc, "roco_device_status")
+    return int(flags.value)
+
+
+def roco_tree_attend_workspace_bytes(cache: Cache, T: int, group: int = 1) -> int:
+    return int(lib().roco_tree_attend_workspace_bytes(C.byref(cache.c), T, group))
+
+
+def _check_tree(what: str, cache: Cache, Q, K_new, V_new):
+    if not isinstance(Q, torch.Tensor) or Q.dim() != 5:
+        raise RocoError(1, f"{what}: Q is [S][G][T][group][d]")
+    S, G, d, T = cache.S, cache.G, cache.d, Q.shape[2]
+    _need(what, "Q", Q, (S, G, T, Q.shape[3], d), cache.dtype)
+    _need(what, "K_new", K_new, (S, G, T, d), cache.dtype)
+    _need(what, "V_new", V_new, (S, G, T, d), cache.dtype)
+    return T, int(Q.shape[3])
+
+
+def roco_tree_attend(cache: Cache, Q, K_new, V_new, parent, attn_out, nodes=None, lse_out=None,
+                     scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None):
+    """Every node of a tree of drafted tokens attends over the cached tokens, its ancestors and itself; the cache stays
+    as it is.  Q, attn_out [S][G][T][group][d], K_new, V_new [S][G][T][d], parent [S][T] int32 (-1: the cached prefix),
+    nodes [S] int32 (None: T), lse_out [S][G][T][group] fp32."""
+    what = "roco_tree_attend"
+    T, group = _check_tree(what, cache, Q, K_new, V_new)
+    _need(what, "parent", parent, (cache.S, T), torch.int32)
+    _need(what, "attn_out", attn_out, tuple(Q.shape), cache.dtype)
+    if nodes is not None:
+        _need(what, "nodes", nodes, (cache.S,), torch.int32)
+    if lse_out is not None:
+        _need(what, "lse_out", lse_out, tuple(Q.shape[:4]), torch.float32)
+    scale = cache.d ** -0.5 if scale is None else scale
+    ws = _workspace(what, workspace, roco_tree_attend_workspace_bytes(cache, T, group) if workspace is None else 0, Q)
+    rc = lib().roco_tree_attend(C.byref(cache.c), _at(Q), _at(K_new), _at(V_new), _at(parent), _at(nodes), T, group, scale,
+                                _at(attn_out), _at(lse_out), _at(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                _stream())
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)
+
+
+def roco_tree_commit(cache: Cache, Q, K_new, V_new, lse, parent, path, path_len, r: int, evicted_slot, evicted_pos=None,
+                     scope_mode=ROCO_SCOPE_EXCLUDE_TOP_R, scale: Optional[float] = None):
+    """The accepted path of a draft tree enters the cache: statistics of its queries, evictions to the budget, insertion.
+    Q, K_new, V_new, parent as given to roco_tree_attend, lse what it returned; path [S][A] int32 node indices from the
+    root on, path_len [S] int32; evicted_slot, evicted_pos [S][G][A] int32."""
+    what = "roco_tree_commit"
+    T, group = _check_tree(what, cache, Q, K_new, V_new)
+    if not isinstance(path, torch.Tensor) or path.dim() != 2:
+        raise RocoError(1, f"{what}: path is [S][A]")
+    S, G, A = cache.S, cache.G, path.shape[1]
+    _need(what, "lse", lse, tuple(Q.shape[:4]), torch.float32)
+    _need(what, "parent", parent, (S, T), torch.int32)
+    _need(what, "path", path, (S, A), torch.int32)
+    _need(what, "path_len", path_len, (S,), torch.int32)
+    _need(what, "evicted_slot", evicted_slot, (S, G, A), torch.int32)
+    if evicted_pos is not None:
+        _need(what, "evicted_pos", evicted_pos, (S, G, A), torch.int32)
+    scale = cache.d ** -0.5 if scale is None else scale
+    rc = lib().roco_tree_commit(C.byref(cache.c), _at(Q), _at(K_new), _at(V_new), _at(lse), _at(parent), _at(path),
+                                _at(path_len), T, group, A, r, scope_mode, scale, _at(evicted_slot), _at(evicted_pos),
+                                _stream())
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)
+
+
+def roco_linear_prefill_workspace_bytes(state: LinearState, Lmax: int) -> int:
+    return int(lib().roco_linear_prefill_workspace_bytes(C.byref(state.c), Lmax))
+
+
+def roco_linear_prefill(state: LinearState, Q, K, V, lens, out, scale: Optional[float] = None,
+                        workspace: Optional[torch.Tensor] = None):
+    """Linear attention with decay over a prompt (or its next piece); the state is continued in place.  Q, K, V, out:
+    [S][G][Lmax][d]; lens: [S] int32 device tensor."""
+    what = "roco_linear_prefill"
+    if not isinstance(Q, torch.Tensor) or Q.dim() != 4:
+        raise RocoError(1, f"{what}: Q is [S][G][Lmax][d]")
+    Lmax = Q.shape[2]
+    shape = (state.S, state.G, Lmax, state.d)
+    for name, t in (("Q", Q), ("K", K), ("V", V), ("out", out)):
+        _need(what, name, t, shape, state.dtype)
+    _need(what, "lens", lens, (state.S,), torch.int32)
+    scale = state.d ** -0.5 if scale is None else scale
+    ws = _workspace(what, workspace, roco_linear_prefill_workspace_bytes(state, Lmax) if workspace is None else 0, Q)
+    rc = lib().roco_linear_prefill(C.byref(state.c), _at(Q), _at(K), _at(V), _at(lens), Lmax, scale, _at(out), _at(ws),
+                                   0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)
+
+
+def roco_linear_step(state: LinearState, q, k, v, out, active=None, scale: Optional[float] = None):
+    """One token of linear attention with decay for every sequence (with active [S] int32: those with a non-zero entry).
+    q, k, v, out: [S][G][d]."""
+    what = "roco_linear_step"
+    shape = (state.S, state.G, state.d)
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+        _need(what, name, t, shape, state.dtype)
+    if active is not None:
+        _need(what, "active", active, (state.S,), torch.int32)
+    scale = state.d ** -0.5 if scale is None else scale
+    rc = lib().roco_linear_step(C.byref(state.c), _at(q), _at(k), _at(v), _at(active), scale, _at(out), _stream())
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)
+
+
+def roco_linear_device_status(state: LinearState) -> int:
+    flags = C.c_int32(0)
+    rc = lib().roco_linear_device_status(C.byref(state.c), _stream(), C.byref(flags))
+    if rc not in (ROCO_OK, 5):
+        raise RocoError(rc, "roco_linear_device_status")
     return int(flags.value)

@@ -6,6 +6,8 @@
 
 #include "common.cuh"
 #include "launch.h"
+#include "linear.cuh"
+#include "tree.cuh"
 
 using namespace roco;
 
@@ -96,6 +98,69 @@ HostPipe *host_pipe() {
     hp.ready = true;
   }
   return &hp;
+}
+
+// Streaming multiprocessors of the current device (148, the whole GPU, where there is none to ask).
+int device_sms() {
+  static int sm_count[kHostMaxDevices] = {};  // per device, asked once (racing first calls write the same value)
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kHostMaxDevices) {
+    (void)cudaGetLastError();
+    return 148;
+  }
+  if (sm_count[dev] == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 148;
+    sm_count[dev] = n;
+  }
+  return sm_count[dev];
+}
+
+roco_status check_tree(const roco_cache *c, int T, int group) {
+  const roco_status st = check_cache(c);
+  if (st != ROCO_OK) return st;
+  if (T < 1 || group < 1) return ROCO_ERR_INVALID_ARG;
+  if (T > ROCO_TREE_MAX_NODES || group > ROCO_TREE_MAX_GROUP) return ROCO_ERR_UNSUPPORTED;
+  return ROCO_OK;
+}
+
+// How a call of roco_tree_attend is cut up: CTAs per unit that take a range of the cached tokens each, and the
+// workspace for their partial results.
+struct TreePlan {
+  bool tc;
+  int splits;
+  size_t ml_bytes, bytes;
+};
+
+TreePlan tree_plan(const roco_cache *c, int T, int group, float scale) {
+  TreePlan t;
+  const int rows = T * group;
+  const long long U = (long long)c->S * c->G;
+  t.tc = false;
+  (void)scale;
+  const long long ctas = U * tree_simt_row_blocks(rows);
+  // CUDA cores: enough CTAs for four per SM, but no range shorter than two 64-key tiles
+  long long want = (4LL * device_sms() + ctas - 1) / ctas, most = (c->B + 127) / 128;
+  if (want > most) want = most;
+  if (want > 32) want = 32;
+  t.splits = want < 1 ? 1 : (int)want;
+  t.ml_bytes = t.splits > 1 ? align_up((size_t)U * t.splits * rows * 8, 256) : 0;
+  t.bytes = t.splits > 1 ? t.ml_bytes + align_up((size_t)U * t.splits * rows * c->d * 4, 256) : 0;
+  return t;
+}
+
+roco_status check_linear(const roco_linear_state *s) {
+  if (!s || !s->state || !s->log_decay || !s->status) return ROCO_ERR_INVALID_ARG;
+  if (s->S < 1 || s->G < 1 || !aligned16(s->state)) return ROCO_ERR_INVALID_ARG;
+  if (s->dtype != ROCO_F32 && s->dtype != ROCO_BF16) return ROCO_ERR_UNSUPPORTED;
+  if (s->d != 64 && s->d != 128) return ROCO_ERR_UNSUPPORTED;
+  if ((long long)s->S * s->G > 0x7fffffffLL / 64) return ROCO_ERR_UNSUPPORTED;
+  return ROCO_OK;
+}
+
+// Parts of every unit's prompt that different CTAs work on.
+int linear_segments(const roco_linear_state *s, int Lmax) {
+  return linear_simt_segments(s->S * s->G, s->d, Lmax, device_sms());
 }
 
 int pow2_at_least(int x) {
@@ -607,6 +672,114 @@ roco_status roco_decode_step_host_end(void) {
   const int set = (int)(hp->ended % kHostDepth);
   ++hp->ended;
   return cudaEventSynchronize(hp->set_d2h[set]) == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+}
+
+size_t roco_tree_attend_workspace_bytes(const roco_cache *cache, int T, int group) {
+  if (check_tree(cache, T, group) != ROCO_OK) return 0;
+  // the larger of the two paths' needs: the scale, which also decides, is not known yet
+  const size_t a = tree_plan(cache, T, group, 1.f).bytes, b = tree_plan(cache, T, group, 0.f).bytes;
+  return a > b ? a : b;
+}
+
+roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void *K_new, const void *V_new,
+                             const int32_t *parent, const int32_t *nodes, int T, int group, float scale, void *attn_out,
+                             float *lse_out, void *workspace, size_t workspace_bytes, void *stream) {
+  NvtxRange range("roco_tree_attend");
+  const roco_status st = check_tree(cache, T, group);
+  if (st != ROCO_OK) return st;
+  if (!Q || !K_new || !V_new || !parent || !attn_out) return ROCO_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K_new) || !aligned16(V_new) || !aligned16(attn_out)) return ROCO_ERR_INVALID_ARG;
+  const TreePlan plan = tree_plan(cache, T, group, scale);
+  const int U = cache->S * cache->G;
+  if ((long long)U * T * group * plan.splits > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
+  const size_t need = roco_tree_attend_workspace_bytes(cache, T, group);
+  if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
+    return ROCO_ERR_WORKSPACE;
+  TreeParams p;
+  p.K = static_cast<const char *>(cache->K); p.V = static_cast<const char *>(cache->V);
+  p.live = cache->live; p.status = cache->status;
+  p.Q = static_cast<const char *>(Q); p.k_new = static_cast<const char *>(K_new); p.v_new = static_cast<const char *>(V_new);
+  p.parent = parent; p.nodes = nodes;
+  p.out = static_cast<char *>(attn_out); p.lse = lse_out;
+  p.part_ml = static_cast<float *>(workspace);
+  p.part_o = plan.splits > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.ml_bytes) : nullptr;
+  p.B = cache->B; p.T = T; p.group = group; p.G = cache->G; p.rows = T * group; p.splits = plan.splits; p.scale = scale;
+  return launch_tree_attend_simt(p, cache->kv_dtype, cache->d, U, static_cast<cudaStream_t>(stream));
+}
+
+roco_status roco_tree_commit(roco_cache *cache, const void *Q, const void *K_new, const void *V_new, const float *lse,
+                             const int32_t *parent, const int32_t *path, const int32_t *path_len, int T, int group,
+                             int A, int r, int scope_mode, float scale, int32_t *evicted_slot, int32_t *evicted_pos,
+                             void *stream) {
+  NvtxRange range("roco_tree_commit");
+  roco_status st = check_tree(cache, T, group);
+  if (st != ROCO_OK) return st;
+  if (!Q || !K_new || !V_new || !lse || !parent || !path || !path_len || !evicted_slot) return ROCO_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K_new) || !aligned16(V_new)) return ROCO_ERR_INVALID_ARG;
+  if (A < 1 || A > T) return ROCO_ERR_INVALID_ARG;
+  if (A > ROCO_TREE_MAX_PATH) return ROCO_ERR_UNSUPPORTED;
+  if ((st = check_scope(r, scope_mode, cache->B, true)) != ROCO_OK) return st;
+  if (r > cache->B - A) return ROCO_ERR_INVALID_ARG;
+  CommitParams p;
+  p.K = static_cast<char *>(cache->K); p.V = static_cast<char *>(cache->V);
+  p.s = cache->s; p.q = cache->q; p.n = cache->n; p.pos = cache->pos; p.live = cache->live; p.t_next = cache->t_next;
+  p.status = cache->status;
+  p.Q = static_cast<const char *>(Q); p.k_new = static_cast<const char *>(K_new); p.v_new = static_cast<const char *>(V_new);
+  p.lse = lse; p.parent = parent; p.path = path; p.path_len = path_len;
+  p.ev_slot = evicted_slot; p.ev_pos = evicted_pos;
+  p.B = cache->B; p.T = T; p.group = group; p.G = cache->G; p.A = A; p.r = r; p.scope_mode = scope_mode; p.scale = scale;
+  return launch_tree_commit(p, cache->kv_dtype, cache->d, cache->S * cache->G, device_sms(),
+                            static_cast<cudaStream_t>(stream));
+}
+
+size_t roco_linear_prefill_workspace_bytes(const roco_linear_state *state, int Lmax) {
+  if (check_linear(state) != ROCO_OK || Lmax < 1) return 0;
+  const int n = linear_segments(state, Lmax);
+  return n > 1 ? align_up((size_t)state->S * state->G * n * state->d * state->d * 4, 256) : 0;
+}
+
+roco_status roco_linear_prefill(const roco_linear_state *state, const void *Q, const void *K, const void *V,
+                                const int32_t *lens, int Lmax, float scale, void *out, void *workspace,
+                                size_t workspace_bytes, void *stream) {
+  NvtxRange range("roco_linear_prefill");
+  const roco_status st = check_linear(state);
+  if (st != ROCO_OK) return st;
+  if (!Q || !K || !V || !lens || !out || Lmax < 1) return ROCO_ERR_INVALID_ARG;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return ROCO_ERR_INVALID_ARG;
+  const size_t need = roco_linear_prefill_workspace_bytes(state, Lmax);
+  if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
+    return ROCO_ERR_WORKSPACE;
+  LinearParams p;
+  p.state = state->state; p.log_decay = state->log_decay; p.status = state->status;
+  p.Q = static_cast<const char *>(Q); p.K = static_cast<const char *>(K); p.V = static_cast<const char *>(V);
+  p.out = static_cast<char *>(out);
+  p.lens = lens; p.G = state->G; p.Lmax = Lmax; p.scale = scale;
+  p.parts = static_cast<float *>(workspace); p.segments = linear_segments(state, Lmax);
+  if ((long long)state->S * state->G * p.segments * (state->d / 64) > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
+  return launch_linear_prefill_simt(p, state->dtype, state->d, state->S * state->G, static_cast<cudaStream_t>(stream));
+}
+
+roco_status roco_linear_step(const roco_linear_state *state, const void *q, const void *k, const void *v,
+                             const int32_t *active, float scale, void *out, void *stream) {
+  NvtxRange range("roco_linear_step");
+  const roco_status st = check_linear(state);
+  if (st != ROCO_OK) return st;
+  if (!q || !k || !v || !out) return ROCO_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return ROCO_ERR_INVALID_ARG;
+  LinearParams p;
+  p.state = state->state; p.log_decay = state->log_decay; p.status = state->status;
+  p.Q = static_cast<const char *>(q); p.K = static_cast<const char *>(k); p.V = static_cast<const char *>(v);
+  p.out = static_cast<char *>(out);
+  p.lens = nullptr; p.parts = nullptr; p.G = state->G; p.Lmax = 1; p.segments = 1; p.scale = scale;
+  return launch_linear_step(p, active, state->dtype, state->d, state->S * state->G, static_cast<cudaStream_t>(stream));
+}
+
+roco_status roco_linear_device_status(const roco_linear_state *state, void *stream, int32_t *flags_host) {
+  if (!state || !state->status || !flags_host) return ROCO_ERR_INVALID_ARG;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  if (cudaMemcpyAsync(flags_host, state->status, 4, cudaMemcpyDeviceToHost, cs) != cudaSuccess) return ROCO_ERR_CUDA;
+  if (cudaStreamSynchronize(cs) != cudaSuccess) return ROCO_ERR_CUDA;
+  return *flags_host ? ROCO_ERR_STATE : ROCO_OK;
 }
 
 roco_status roco_device_status(const roco_cache *cache, void *stream, int32_t *flags_host) {

@@ -87,4 +87,20 @@ roco_status launch_multi_step(const roco_cache &c, int M, int nb, const void *Q,
 roco_status launch_consistency_step(const roco_cache &full, const roco_cache &budgeted, int policy, int32_t *overlap,
                                     float *jaccard_sum, int32_t *samples, cudaStream_t stream);
 
+// ---- attention of a tree of drafted tokens over the cache, commit of the accepted path (tree.cuh)
+struct TreeParams;
+struct CommitParams;
+// CUDA cores; p.splits > 1: partial results to p.part_o / p.part_ml and a second launch that joins them.
+int tree_simt_row_blocks(int rows);
+roco_status launch_tree_attend_simt(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
+roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
+// Statistics of the accepted queries, then evictions and insertion (two launches).
+roco_status launch_tree_commit(const CommitParams &p, int kv_dtype, int d, int U, int sms, cudaStream_t stream);
+
+// ---- linear attention with a decay for each head (linear.cuh)
+struct LinearParams;
+roco_status launch_linear_step(const LinearParams &p, const int *active, int dtype, int d, int U, cudaStream_t stream);
+int linear_simt_segments(int U, int d, int Lmax, int sms);  // parts of the prompt that work side by side (p.segments)
+roco_status launch_linear_prefill_simt(const LinearParams &p, int dtype, int d, int U, cudaStream_t stream);
+
 }  // namespace roco

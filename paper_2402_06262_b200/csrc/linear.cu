@@ -1,0 +1,301 @@
+// Linear attention with a decay for each head on the CUDA cores: the single-token step (any dtype) and the prompt pass
+// for the dtypes and head dimensions that the tensor-core kernel does not take.
+//
+//     state_t = g state_{t-1} + k_t v_t^T,     out_t = scale * q_t state_t
+//
+// Column c of the state meets only component c of v and of the output, so a unit can be cut into slabs of columns that
+// know nothing of one another.
+#include "linear.cuh"
+
+namespace roco {
+
+constexpr int kLsThreads = 128;
+constexpr int kLsCols = 32;  // columns of the state per CTA: 128-byte rows
+
+// One CTA: 32 columns of a unit's state, eight threads (16 bytes each) across, sixteen rows at a time; every thread has
+// all of its D / 16 loads in flight before it uses the first.  Reads and writes the state once: bound by that traffic.
+template <typename T, int D>
+__global__ void __launch_bounds__(kLsThreads) linear_step_kernel(const LinearParams p, const int *active) {
+  constexpr int kSlabs = D / kLsCols, kRows = D / 16;
+  __shared__ __align__(16) float red[kLsThreads / 32][kLsCols];
+  const int u = blockIdx.x / kSlabs, c0 = (blockIdx.x % kSlabs) * kLsCols;
+  if (active && active[u / p.G] == 0) return;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, col = (tid & 7) * 4, r0 = tid >> 3;
+  float *S = p.state + (size_t)u * D * D + c0 + col;
+  float4 s[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) s[i] = *reinterpret_cast<const float4 *>(S + (size_t)(r0 + 16 * i) * D);
+  const T *q = reinterpret_cast<const T *>(p.Q) + (size_t)u * D, *k = reinterpret_cast<const T *>(p.K) + (size_t)u * D;
+  const T *v = reinterpret_cast<const T *>(p.V) + (size_t)u * D + c0 + col;
+  float kr[kRows], qr[kRows], vc[4];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) { kr[i] = Elem<T>::load(k + r0 + 16 * i); qr[i] = Elem<T>::load(q + r0 + 16 * i); }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) vc[e] = Elem<T>::load(v + e);
+  const float g = expf(p.log_decay[u % p.G]);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    s[i].x = fmaf(kr[i], vc[0], g * s[i].x);
+    s[i].y = fmaf(kr[i], vc[1], g * s[i].y);
+    s[i].z = fmaf(kr[i], vc[2], g * s[i].z);
+    s[i].w = fmaf(kr[i], vc[3], g * s[i].w);
+    *reinterpret_cast<float4 *>(S + (size_t)(r0 + 16 * i) * D) = s[i];
+    o.x = fmaf(qr[i], s[i].x, o.x);
+    o.y = fmaf(qr[i], s[i].y, o.y);
+    o.z = fmaf(qr[i], s[i].z, o.z);
+    o.w = fmaf(qr[i], s[i].w, o.w);
+  }
+#pragma unroll
+  for (int d = 8; d < 32; d <<= 1) {  // lanes 8, 16, 24 apart hold other rows of the same columns
+    o.x += __shfl_xor_sync(0xffffffffu, o.x, d);
+    o.y += __shfl_xor_sync(0xffffffffu, o.y, d);
+    o.z += __shfl_xor_sync(0xffffffffu, o.z, d);
+    o.w += __shfl_xor_sync(0xffffffffu, o.w, d);
+  }
+  if (lane < 8) *reinterpret_cast<float4 *>(&red[warp][col]) = o;
+  __syncthreads();
+  if (tid < kLsCols) {
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < kLsThreads / 32; ++w) x += red[w][tid];
+    Elem<T>::store(reinterpret_cast<T *>(p.out) + (size_t)u * D + c0 + tid, x * p.scale);
+  }
+}
+
+roco_status launch_linear_step(const LinearParams &p, const int *active, int dtype, int d, int U, cudaStream_t stream) {
+  const unsigned grid = (unsigned)U * (unsigned)(d / kLsCols);
+  if (dtype == ROCO_BF16) {
+    if (d == 128) linear_step_kernel<__nv_bfloat16, 128><<<grid, kLsThreads, 0, stream>>>(p, active);
+    else linear_step_kernel<__nv_bfloat16, 64><<<grid, kLsThreads, 0, stream>>>(p, active);
+  } else {
+    if (d == 128) linear_step_kernel<float, 128><<<grid, kLsThreads, 0, stream>>>(p, active);
+    else linear_step_kernel<float, 64><<<grid, kLsThreads, 0, stream>>>(p, active);
+  }
+  return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------- prompt pass
+
+constexpr int kLpThreads = 256;
+constexpr int kLpChunk = 32;  // tokens of a chunk
+constexpr int kLpCols = 64;   // columns of the state per CTA
+
+template <int D>
+struct LpSmem {
+  float q[kLpChunk][D + 4], k[kLpChunk][D + 4];  // pitch: eight rows read at once lie in different banks
+  float v[kLpChunk][kLpCols], s[D][kLpCols];
+  float p[kLpChunk][kLpChunk + 1];
+  float pw[kLpChunk + 1];                        // g^n
+};
+
+// In chunks of 32 tokens, with i, j counted inside the chunk and S the state before it:
+//     out_i  = g^(i+1) q_i S + sum_{j <= i} g^(i-j) (q_i.k_j) v_j
+//     S     <- g^32 S + sum_j g^(31-j) k_j^T v_j
+// Three small matrix products per chunk in place of 32 dependent updates of the state.  A CTA has 64 columns of one
+// unit's state (registers; a copy in shared memory is the operand of the first product) and one segment of the prompt.
+// All powers are at most 1: nothing overflows however fast the head forgets.
+//
+// Segments (few units): a first launch (kStates) runs every segment but the last and leaves its state in `parts`:
+// segment 0's (which starts from the unit's state) in slot 1, the others', started from zero, in the slot behind their
+// index; slot 0 takes a copy of the unit's state, which the second launch overwrites at a time of its own.  The second
+// launch starts segment i > 0 from  g^(t_i - t_1) slot_1 + sum_{m=1}^{i-1} g^(t_i - t_{m+1}) slot_{m+1}.
+template <typename T, int D, bool kStates>
+__global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const LinearParams p) {
+  constexpr int kSlabs = D / kLpCols, kRows = D / 16, kEPC = Elem<T>::kPerChunk;
+  extern __shared__ __align__(16) char lp_raw[];
+  LpSmem<D> &sm = *reinterpret_cast<LpSmem<D> *>(lp_raw);
+  const int tid = threadIdx.x;
+  const int slab = blockIdx.x % kSlabs, segs = kStates ? p.segments - 1 : p.segments;
+  const int seg = blockIdx.x / kSlabs % segs, u = blockIdx.x / (kSlabs * segs), c0 = slab * kLpCols;
+  const int len = linear_len(p, u / p.G, tid == 0 && slab == 0 && seg == 0 && (kStates || p.segments == 1));
+  if (len == 0) return;
+  const int n_chunks = (len + kLpChunk - 1) / kLpChunk;
+  const int first = linear_segment(n_chunks, p.segments, seg), last = linear_segment(n_chunks, p.segments, seg + 1);
+  const double logd = (double)p.log_decay[u % p.G];
+  if (tid <= kLpChunk) sm.pw[tid] = (float)decay_pow(logd, tid);
+  const int sr0 = (tid >> 4) * kRows, sc = (tid & 15) * 4;  // this thread's rows and columns of the state
+  float *S = p.state + (size_t)u * D * D + (size_t)sr0 * D + c0 + sc;
+  float *part = p.parts + (size_t)u * p.segments * D * D + (size_t)sr0 * D + c0 + sc;
+  float4 s[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (seg == 0) {
+    const float *src = (p.segments == 1 || kStates) ? S : part;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) s[i] = *reinterpret_cast<const float4 *>(src + (size_t)i * D);
+    if (kStates) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4 *>(part + (size_t)i * D) = s[i];
+    }
+  } else if (!kStates) {
+    for (int m = 1; m <= seg; ++m) {
+      const int t = first - linear_segment(n_chunks, p.segments, m);  // chunks between the end of segment m - 1 and here
+      const float w = (float)decay_pow(logd, (double)t * kLpChunk);
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        const float4 x = *reinterpret_cast<const float4 *>(part + (size_t)m * D * D + (size_t)i * D);
+        s[i].x = fmaf(w, x.x, s[i].x); s[i].y = fmaf(w, x.y, s[i].y);
+        s[i].z = fmaf(w, x.z, s[i].z); s[i].w = fmaf(w, x.w, s[i].w);
+      }
+    }
+  }
+  const T *Q = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.Lmax * D, *K = reinterpret_cast<const T *>(p.K) + (size_t)u * p.Lmax * D;
+  const T *V = reinterpret_cast<const T *>(p.V) + (size_t)u * p.Lmax * D + c0;
+  T *O = reinterpret_cast<T *>(p.out) + (size_t)u * p.Lmax * D + c0;
+  const int row = tid >> 3, col = (tid & 7) * 4;  // this thread's token and columns (col, col + 32) of the output
+#pragma unroll 1
+  for (int c = first; c < last; ++c) {
+    const int t0 = c * kLpChunk, nt = len - t0 < kLpChunk ? len - t0 : kLpChunk;
+    __syncthreads();  // the chunk before is used up
+    // tokens behind the last are zeros: they add nothing to the sums, and their own rows are not written
+#pragma unroll
+    for (int w = tid; w < kLpChunk * D / kEPC; w += kLpThreads) {
+      const int t = w / (D / kEPC), x = w % (D / kEPC) * kEPC;
+      uint4 qv = make_uint4(0u, 0u, 0u, 0u), kv = qv;
+      if (t < nt) {
+        if (!kStates) qv = *reinterpret_cast<const uint4 *>(Q + (size_t)(t0 + t) * D + x);
+        kv = *reinterpret_cast<const uint4 *>(K + (size_t)(t0 + t) * D + x);
+      }
+      float f[kEPC];
+      if (!kStates) {
+        Elem<T>::unpack(qv, f);
+#pragma unroll
+        for (int e = 0; e < kEPC; ++e) sm.q[t][x + e] = f[e];
+      }
+      Elem<T>::unpack(kv, f);
+#pragma unroll
+      for (int e = 0; e < kEPC; ++e) sm.k[t][x + e] = f[e];
+    }
+#pragma unroll
+    for (int w = tid; w < kLpChunk * kLpCols / kEPC; w += kLpThreads) {
+      const int t = w / (kLpCols / kEPC), x = w % (kLpCols / kEPC) * kEPC;
+      uint4 vv = make_uint4(0u, 0u, 0u, 0u);
+      if (t < nt) vv = *reinterpret_cast<const uint4 *>(V + (size_t)(t0 + t) * D + x);
+      float f[kEPC];
+      Elem<T>::unpack(vv, f);
+#pragma unroll
+      for (int e = 0; e < kEPC; ++e) sm.v[t][x + e] = f[e];
+    }
+    if (!kStates) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4 *>(&sm.s[sr0 + i][sc]) = s[i];
+    }
+    __syncthreads();
+    if (!kStates) {
+      float z[4] = {0.f, 0.f, 0.f, 0.f};
+      float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 2
+      for (int x = 0; x < D; x += 4) {
+        const float4 q4 = *reinterpret_cast<const float4 *>(&sm.q[row][x]);
+        const float qs[4] = {q4.x, q4.y, q4.z, q4.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4 k4 = *reinterpret_cast<const float4 *>(&sm.k[(tid & 7) + 8 * k][x]);
+          z[k] = fmaf(q4.x, k4.x, fmaf(q4.y, k4.y, fmaf(q4.z, k4.z, fmaf(q4.w, k4.w, z[k]))));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float4 s4 = *reinterpret_cast<const float4 *>(&sm.s[x + e][col + 32 * h]);
+            o[h].x = fmaf(qs[e], s4.x, o[h].x); o[h].y = fmaf(qs[e], s4.y, o[h].y);
+            o[h].z = fmaf(qs[e], s4.z, o[h].z); o[h].w = fmaf(qs[e], s4.w, o[h].w);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = (tid & 7) + 8 * k;
+        sm.p[row][j] = j <= row ? z[k] * sm.pw[row - j] : 0.f;
+      }
+      const float w = sm.pw[row + 1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) { o[h].x *= w; o[h].y *= w; o[h].z *= w; o[h].w *= w; }
+      __syncwarp();  // a row's scores come from eight lanes of the same warp
+      const int upto = (row | 3) + 1;  // the warp's four rows end at most here
+      for (int j = 0; j < upto; ++j) {
+        const float pj = sm.p[row][j];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 v4 = *reinterpret_cast<const float4 *>(&sm.v[j][col + 32 * h]);
+          o[h].x = fmaf(pj, v4.x, o[h].x); o[h].y = fmaf(pj, v4.y, o[h].y);
+          o[h].z = fmaf(pj, v4.z, o[h].z); o[h].w = fmaf(pj, v4.w, o[h].w);
+        }
+      }
+      if (row < nt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          T *dst = O + (size_t)(t0 + row) * D + col + 32 * h;
+          Elem<T>::store(dst, o[h].x * p.scale);
+          Elem<T>::store(dst + 1, o[h].y * p.scale);
+          Elem<T>::store(dst + 2, o[h].z * p.scale);
+          Elem<T>::store(dst + 3, o[h].w * p.scale);
+        }
+      }
+    }
+    float4 add[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) add[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int t = 0; t < nt; ++t) {
+      const float w = sm.pw[nt - 1 - t];
+      float4 v4 = *reinterpret_cast<const float4 *>(&sm.v[t][sc]);
+      v4.x *= w; v4.y *= w; v4.z *= w; v4.w *= w;
+#pragma unroll
+      for (int i = 0; i < kRows; i += 4) {
+        const float4 k4 = *reinterpret_cast<const float4 *>(&sm.k[t][sr0 + i]);
+        const float ks[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          add[i + e].x = fmaf(ks[e], v4.x, add[i + e].x); add[i + e].y = fmaf(ks[e], v4.y, add[i + e].y);
+          add[i + e].z = fmaf(ks[e], v4.z, add[i + e].z); add[i + e].w = fmaf(ks[e], v4.w, add[i + e].w);
+        }
+      }
+    }
+    const Decay2 g(decay_pow(logd, nt));
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      s[i].x = g.madd(s[i].x, add[i].x); s[i].y = g.madd(s[i].y, add[i].y);
+      s[i].z = g.madd(s[i].z, add[i].z); s[i].w = g.madd(s[i].w, add[i].w);
+    }
+  }
+  if (kStates) part += (size_t)(seg + 1) * D * D;
+  float *dst = kStates ? part : S;
+  if (!kStates && seg != p.segments - 1) return;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4 *>(dst + (size_t)i * D) = s[i];
+}
+
+template <typename T, int D>
+roco_status linear_prefill_simt_t(const LinearParams &p, int U, cudaStream_t stream) {
+  constexpr int kSmem = (int)sizeof(LpSmem<D>);
+  const unsigned slabs = (unsigned)U * (unsigned)(D / kLpCols);
+  auto states = linear_prefill_simt_kernel<T, D, true>;
+  auto whole = linear_prefill_simt_kernel<T, D, false>;
+  if (cudaFuncSetAttribute(states, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
+      cudaFuncSetAttribute(whole, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess)
+    return ROCO_ERR_CUDA;
+  if (p.segments > 1) states<<<slabs * (unsigned)(p.segments - 1), kLpThreads, kSmem, stream>>>(p);
+  whole<<<slabs * (unsigned)p.segments, kLpThreads, kSmem, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+}
+
+// Segments that fill the GPU with two CTAs per SM, none shorter than four chunks: a prompt that is divided is read
+// twice (its keys and values), which pays only while SMs would be idle.
+int linear_simt_segments(int U, int d, int Lmax, int sms) {
+  const long long ctas = (long long)U * (d / kLpCols);
+  long long n = 2LL * sms / ctas;
+  const int most = Lmax / (4 * kLpChunk);
+  if (n > most) n = most;
+  if (n > 64) n = 64;
+  return n < 2 ? 1 : (int)n;
+}
+
+roco_status launch_linear_prefill_simt(const LinearParams &p, int dtype, int d, int U, cudaStream_t stream) {
+  if (dtype == ROCO_BF16)
+    return d == 128 ? linear_prefill_simt_t<__nv_bfloat16, 128>(p, U, stream) : linear_prefill_simt_t<__nv_bfloat16, 64>(p, U, stream);
+  return d == 128 ? linear_prefill_simt_t<float, 128>(p, U, stream) : linear_prefill_simt_t<float, 64>(p, U, stream);
+}
+
+}  // namespace roco

@@ -1,0 +1,112 @@
+// Shared by the kernels of speculative decoding over the cache (attention of a tree of drafted tokens, commit of the
+// accepted path): launch parameters, the tree's ancestor sets, the check of an accepted path.
+#pragma once
+
+#include "common.cuh"
+#include "launch.h"
+
+namespace roco {
+
+struct TreeParams {
+  const char *K, *V;
+  const int *live;
+  int *status;
+  const char *Q, *k_new, *v_new;
+  const int *parent, *nodes;
+  char *out;
+  float *lse;
+  float *part_o, *part_ml;  // splits > 1: [U][splits][rows][d] unnormalised outputs, [U][splits][rows][2] (max, sum)
+  int B, T, group, G;
+  int rows;    // T * group query rows of a unit; row i is head i % group of node i / group
+  int splits;  // CTAs that share a unit's cached tokens
+  float scale;
+};
+
+constexpr int kTreeMaxNodes = ROCO_TREE_MAX_NODES;
+
+// Nodes of sequence b; a count outside [0, T] is none.
+__device__ __forceinline__ int tree_nodes(const TreeParams &p, int b, bool report) {
+  const int n = p.nodes ? p.nodes[b] : p.T;
+  if (n >= 0 && n <= p.T) return n;
+  if (report) atomicOr(p.status, ROCO_DEV_BAD_TREE);
+  return 0;
+}
+
+// Occupied slots of unit u, clipped to [0, B].
+__device__ __forceinline__ int tree_live(const int *live, int u, int B, int *status, bool report) {
+  const int n = live[u];
+  if (n >= 0 && n <= B) return n;
+  if (report) atomicOr(status, ROCO_DEV_BAD_LIVE);
+  return n < 0 ? 0 : B;
+}
+
+// anc[i] = bit set of node i's ancestors and itself, by pointer doubling (six rounds for 64 nodes).  up: scratch.  All
+// threads of the block call it; it synchronises.
+__device__ __forceinline__ void tree_ancestors(const TreeParams &p, int b, int n_nodes, unsigned long long *anc, int *up,
+                                               bool report) {
+  const int i = threadIdx.x;
+  if (i < kTreeMaxNodes) {
+    int par = -1;
+    if (i < n_nodes) {
+      par = p.parent[(size_t)b * p.T + i];
+      if (par < -1 || par >= i) {
+        if (report) atomicOr(p.status, ROCO_DEV_BAD_TREE);
+        par = -1;
+      }
+    }
+    up[i] = par;
+    anc[i] = i < n_nodes ? 1ull << i : 0ull;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int round = 0; round < 6; ++round) {
+    unsigned long long a = 0;
+    int to = -1;
+    if (i < kTreeMaxNodes) {
+      a = anc[i];
+      to = up[i];
+      if (to >= 0) {
+        a |= anc[to];
+        to = up[to];
+      }
+    }
+    __syncthreads();
+    if (i < kTreeMaxNodes) {
+      anc[i] = a;
+      up[i] = to;
+    }
+    __syncthreads();
+  }
+}
+
+struct CommitParams {
+  char *K, *V;
+  float *s, *q;
+  int *n, *pos, *live, *t_next, *status;
+  const char *Q, *k_new, *v_new;
+  const float *lse;
+  const int *parent, *path, *path_len;
+  int *ev_slot, *ev_pos;
+  int B, T, group, G, A, r, scope_mode;
+  float scale;
+};
+
+// Length of sequence b's accepted path: 0 unless path[0] hangs on the cached prefix and every next node on the one
+// before.  Called by one whole warp; every lane gets the length and lane m < a the node path[m].
+__device__ __forceinline__ int commit_path(const CommitParams &p, int b, int lane, int &node, bool report) {
+  int a = p.path_len[b];
+  bool ok = a >= 0 && a <= p.A;
+  if (!ok) a = 0;
+  node = lane < a ? p.path[(size_t)b * p.A + lane] : -1;
+  const int before = __shfl_up_sync(0xffffffffu, node, 1);
+  bool chain = true;
+  if (lane < a) chain = node >= 0 && node < p.T && p.parent[(size_t)b * p.T + node] == (lane ? before : -1);
+  ok = __all_sync(0xffffffffu, chain) && ok;
+  if (!ok) {
+    if (report && lane == 0) atomicOr(p.status, ROCO_DEV_BAD_TREE);
+    a = 0;
+  }
+  return a;
+}
+
+}  // namespace roco

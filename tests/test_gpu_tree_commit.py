@@ -1,0 +1,244 @@
+"""Commit of the accepted path of a draft tree against its definition in 64 bits: statistics, evictions, insertion."""
+import pytest
+import torch
+
+import operator_reference as ref
+import paper_2402_06262_b200 as R
+from tree_cases import CACHE_FIELDS, make
+
+pytestmark = pytest.mark.gpu
+LOW, TOP = R.ROCO_SCOPE_LOWEST_R, R.ROCO_SCOPE_EXCLUDE_TOP_R
+
+
+def commit(c, cache, paths, A, r, scope_mode=TOP, scale=None):
+    """paths: one list of node indices per sequence.  The log-sum-exp is the reference's, as fp32."""
+    scale_ = c.d ** -0.5 if scale is None else scale
+    path = torch.full((c.S, A), 99, dtype=torch.int32)
+    for b, p in enumerate(paths):
+        path[b, :len(p)] = torch.tensor(p, dtype=torch.int32)
+    lse = torch.full(c.t["Q"].shape[:4], float("nan"))
+    for b in range(c.S):
+        for g in range(c.G):
+            f = {k: c.t[k][b, g].double() for k in ("K", "V", "Q", "K_new", "V_new")}
+            lse[b, g, :c.nodes[b]] = ref.tree_attend(f["K"], f["V"], c.live[b], f["Q"], f["K_new"], f["V_new"],
+                                                     c.t["parent"][b].tolist(), c.nodes[b], scale_)[1].float()
+    ev = torch.full((c.S, c.G, A), -5, dtype=torch.int32, device="cuda")
+    ep = torch.full((c.S, c.G, A), -5, dtype=torch.int32, device="cuda")
+    R.roco_tree_commit(cache, c.dev("Q"), c.dev("K_new"), c.dev("V_new"), lse.to("cuda"), c.dev("parent"), path.to("cuda"),
+                       torch.tensor([len(p) for p in paths], dtype=torch.int32, device="cuda"), r, ev, evicted_pos=ep,
+                       scope_mode=scope_mode, scale=scale)
+    torch.cuda.synchronize()
+    return lse, ev.cpu(), ep.cpu()
+
+
+def check(c, paths, A, r, scope_mode=TOP, scale=None, least_margin=1e-5):
+    cache = c.cache()
+    lse, ev, ep = commit(c, cache, paths, A, r, scope_mode, scale)
+    got = {f: getattr(cache, f).cpu() for f in CACHE_FIELDS}
+    scale = c.d ** -0.5 if scale is None else scale
+    near_ties = 0
+    for b in range(c.S):
+        for g in range(c.G):
+            st = {f: c.t[f][b, g].clone().double() if f in ("K", "V", "s", "q") else c.t[f][b, g].clone() for f in CACHE_FIELDS}
+            st["live"], st["t_next"] = int(st["live"]), int(st["t_next"])
+            gone, gone_pos, margin, sb, qb = ref.tree_commit(
+                st, c.t["Q"][b, g].double(), c.t["K_new"][b, g].double(), c.t["V_new"][b, g].double(), lse[b, g].double(),
+                paths[b], r, scope_mode == LOW, scale)
+            if margin <= least_margin:     # a decision that fp32 statistics may take either way: the unit is counted and left out
+                near_ties += 1
+                continue
+            what = f"unit {b},{g}"
+            pad = [-1] * (A - len(gone))
+            assert ev[b, g].tolist() == gone + pad and ep[b, g].tolist() == gone_pos + pad, what
+            live = st["live"]
+            assert int(got["live"][b, g]) == live and int(got["t_next"][b, g]) == st["t_next"], what
+            for f in ("n", "pos"):
+                assert torch.equal(got[f][b, g], st[f]), f"{what}: {f}"
+            for f in ("K", "V"):                       # whole rows, the untouched ones and those behind the last too
+                assert torch.equal(got[f][b, g].double().nan_to_num(9e9), st[f].nan_to_num(9e9)), f"{what}: {f}"
+            for f, bound in (("s", sb), ("q", qb)):
+                d = (got[f][b, g, :live].double() - st[f][:live]).abs()
+                assert bool((d <= bound[:live]).all()), f"{what}: {f} off by {float((d / bound[:live]).max())} of its bound"
+                assert torch.equal(got[f][b, g, live:].nan_to_num(9e9), c.t[f][b, g, live:].nan_to_num(9e9)), f"{what}: {f} behind"
+    assert near_ties <= c.S * c.G // 4
+    assert R.roco_device_status(cache) == 0
+
+
+def chain_of(parent, node):
+    p = []
+    while node >= 0:
+        p.append(node)
+        node = int(parent[node])
+    return p[::-1]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("B,T,group,A,r,live", [
+    (2, 1, 1, 1, 0, [0, 2]),
+    (5, 3, 2, 2, 1, [5, 3]),
+    (64, 4, 1, 4, 8, [64, 62]),
+    (127, 9, 3, 5, 16, [127, 1]),
+    (130, 16, 1, 16, 40, [130, 120]),
+    (300, 12, 4, 6, 30, [300, 299]),
+    (520, 20, 16, 3, 64, [520, 518]),
+    (1100, 24, 5, 7, 64, [1100, 1094]),
+])
+def test_commit(dtype, d, B, T, group, A, r, live):
+    c = make(B * 17 + T, S=2, G=3, B=B, d=d, T=T, group=group, dtype=dtype, live=live)
+    paths = []
+    for b in range(2):   # the longest root-to-node chains of the tree, cut to A
+        longest = max((chain_of(c.t["parent"][b], i) for i in range(T)), key=len)
+        paths.append(longest[:A])
+    check(c, paths, A, r)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", [TOP, LOW])
+@pytest.mark.parametrize("r", [1, 20, 140])
+@pytest.mark.parametrize("a", [1, 2, 5, 16])
+def test_scopes(dtype, mode, r, a):
+    """Both readings of the scope, from one that leaves nearly everything in to one that leaves nearly everything out."""
+    B = 160
+    c = make(1000 + r + a, S=1, G=4, B=B, T=16, dtype=dtype, shape="chain")
+    check(c, [list(range(a))], 16, r, mode)
+
+
+def test_ragged_acceptance_and_nothing_accepted():
+    c = make(40, S=4, G=2, B=100, T=8, shape="chain", live=[100, 97, 100, 0])
+    check(c, [[0, 1, 2], [], [0], [0, 1, 2, 3, 4]], 5, 10)
+
+
+def test_equal_statistics_fall_to_the_lowest_position():
+    c = make(41, S=1, G=2, B=80, T=4, shape="chain")
+    n = torch.full_like(c.t["n"], 50)
+    c.t["n"], c.t["s"], c.t["q"] = n, torch.full_like(c.t["s"], 1e-3), torch.full_like(c.t["q"], 1e-5)
+    c.t["K"] = torch.zeros_like(c.t["K"])          # every cached token receives the same probability
+    cache = c.cache()
+    _, ev, ep = commit(c, cache, [[0, 1, 2]], 3, 10)
+    for g in range(2):
+        assert sorted(ep[0, g].tolist()) == [0, 2, 4]
+        assert ev[0, g].tolist() == sorted(ev[0, g].tolist())
+    assert R.roco_device_status(cache) == 0
+
+
+def test_long_budget():
+    c = make(42, S=1, G=2, B=8192, T=6, group=2, shape="chain", live=[8190])
+    check(c, [[0, 1, 2, 3, 4, 5]], 6, 256, least_margin=1e-6)
+
+
+def test_bad_paths_are_reported_and_change_nothing():
+    c = make(43, S=5, G=2, B=60, T=6)
+    c.t["parent"][:] = torch.tensor([-1, 0, 1, -1, 3, 4], dtype=torch.int32)
+    before = c.cache()
+    cache = c.cache()
+    # not a root; not a chain; a node twice; beyond the tree; a good one
+    _, ev, ep = commit(c, cache, [[1, 2], [0, 1, 4], [0, 0], [0, 6], [3, 4]], 3, 5)
+    assert R.roco_device_status(cache) == 8
+    for f in CACHE_FIELDS:
+        a, b = getattr(cache, f), getattr(before, f)
+        assert torch.equal(a[:4].view(torch.uint8), b[:4].view(torch.uint8)), f
+        assert f == "live" or not torch.equal(a[4].view(torch.uint8), b[4].view(torch.uint8)), f   # (the budget was full)
+    assert bool((ev[:4] == -1).all()) and bool((ep[:4] == -1).all()) and bool((ev[4, :, :2] >= 0).all())
+    for n in (-1, 4):
+        cache = c.cache()
+        ev = torch.zeros(5, 2, 3, dtype=torch.int32, device="cuda")
+        R.roco_tree_commit(cache, c.dev("Q"), c.dev("K_new"), c.dev("V_new"), torch.zeros(5, 2, 6, 1, device="cuda"),
+                           c.dev("parent"), torch.zeros(5, 3, dtype=torch.int32, device="cuda"),
+                           torch.full((5,), n, dtype=torch.int32, device="cuda"), 5, ev)
+        assert R.roco_device_status(cache) == 8 and bool((ev == -1).all())
+        assert all(torch.equal(getattr(cache, f).view(torch.uint8), getattr(before, f).view(torch.uint8)) for f in CACHE_FIELDS)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.4])
+def test_any_scale(scale):
+    check(make(44, S=1, G=2, B=90, T=5, shape="chain", key_scale=0.25), [[0, 1, 2]], 4, 9, scale=scale)
+
+
+def test_corrupt_statistics_are_reported():
+    c = make(45, S=1, G=2, B=50, T=3, shape="chain")
+    c.t["s"][:] = float("nan")
+    cache = c.cache()
+    commit(c, cache, [[0, 1]], 2, 4)
+    assert R.roco_device_status(cache) & 4
+    live = cache.live.cpu()
+    assert bool((live == 50).all())
+
+
+@pytest.mark.parametrize("dtype,group", [("bf16", 1), ("bf16", 4), ("f32", 2)])
+def test_speculative_decoding(dtype, group):
+    """Draft, attend, accept, commit, several times, with plain decode steps in between: every step against the reference
+    continued from the device's statistics."""
+    S, G, B, T, A, r = 2, 2, 96, 10, 4, 12
+    c = make(50, S=S, G=G, B=B, T=T, group=group, dtype=dtype, live=[96, 90])
+    cache = c.cache()
+    d = c.d
+    for turn in range(5):
+        new = make(60 + turn, S=S, G=G, B=B, T=T, group=group, dtype=dtype)
+        for f in CACHE_FIELDS:
+            c.t[f] = getattr(cache, f).cpu()
+        c.live = c.t["live"][:, 0].tolist()
+        for f in ("Q", "K_new", "V_new", "parent"):
+            c.t[f] = new.t[f]
+        q, k, v, par = (c.dev(f) for f in ("Q", "K_new", "V_new", "parent"))
+        out, lse = torch.zeros_like(q), torch.zeros(q.shape[:4], device="cuda")
+        R.roco_tree_attend(cache, q, k, v, par, out, lse_out=lse)
+        paths = [chain_of(c.t["parent"][b], (3 * turn + 5 * b) % T)[:A] for b in range(S)]
+        path = torch.zeros(S, A, dtype=torch.int32)
+        for b, p in enumerate(paths):
+            path[b, :len(p)] = torch.tensor(p)
+        ev = torch.zeros(S, G, A, dtype=torch.int32, device="cuda")
+        R.roco_tree_commit(cache, q, k, v, lse, par, path.to("cuda"),
+                           torch.tensor([len(p) for p in paths], dtype=torch.int32, device="cuda"), r, ev)
+        torch.cuda.synchronize()
+        for b in range(S):
+            for g in range(G):
+                f64 = {k_: c.t[k_][b, g].double() for k_ in ("K", "V", "Q", "K_new", "V_new")}
+                o, l, ob, lb = ref.tree_attend(f64["K"], f64["V"], c.live[b], f64["Q"], f64["K_new"], f64["V_new"],
+                                               c.t["parent"][b].tolist(), T, d ** -0.5, low=dtype == "bf16")
+                assert bool(((out[b, g].double().cpu() - o).abs() <= ob).all())
+                assert bool(((lse[b, g].double().cpu() - l).abs() <= lb).all())
+                st = {f: c.t[f][b, g].clone().double() if f in ("K", "V", "s", "q") else c.t[f][b, g].clone()
+                      for f in CACHE_FIELDS}
+                st["live"], st["t_next"] = int(st["live"]), int(st["t_next"])
+                gone, _, margin, sb, qb = ref.tree_commit(st, f64["Q"], f64["K_new"], f64["V_new"], lse[b, g].double().cpu(),
+                                                          paths[b], r, False, d ** -0.5)
+                assert margin > 1e-5
+                n = st["live"]
+                assert ev[b, g].tolist() == gone + [-1] * (A - len(gone))
+                assert int(cache.live[b, g]) == n and int(cache.t_next[b, g]) == st["t_next"]
+                assert torch.equal(cache.n[b, g, :n].cpu(), st["n"][:n]) and torch.equal(cache.pos[b, g, :n].cpu(), st["pos"][:n])
+                assert bool(((cache.s[b, g, :n].double().cpu() - st["s"][:n]).abs() <= sb[:n]).all())
+                assert bool(((cache.q[b, g, :n].double().cpu() - st["q"][:n]).abs() <= qb[:n]).all())
+                assert torch.equal(cache.K[b, g, :n].double().cpu(), st["K"][:n])
+        if group == 1:   # the token that the last accepted node predicts, by the ordinary step
+            g = torch.Generator()
+            g.manual_seed(90 + turn)
+            tok = [torch.randn(S, G, d, generator=g).to(c.t["K"].dtype).to("cuda") for _ in range(3)]
+            before = cache.t_next.clone()
+            R.roco_decode_step(cache, *tok, r, torch.zeros_like(tok[0]), torch.zeros(S, G, dtype=torch.int32, device="cuda"))
+            assert torch.equal(cache.t_next, before + 1) and int(cache.live.max()) <= B
+    assert R.roco_device_status(cache) == 0
+
+
+def test_in_a_graph():
+    """A captured commit, replayed with another path and another number of accepted tokens."""
+    c = make(70, S=2, G=2, B=64, T=6, shape="chain", live=[64, 60])
+    eager, graphed, warm = c.cache(), c.cache(), c.cache()
+    q, k, v, par = (c.dev(f) for f in ("Q", "K_new", "V_new", "parent"))
+    lse = torch.zeros(q.shape[:4], device="cuda")
+    R.roco_tree_attend(eager, q, k, v, par, torch.zeros_like(q), lse_out=lse)
+    path = torch.arange(4, dtype=torch.int32, device="cuda").expand(2, 4).contiguous()
+    n = torch.tensor([1, 1], dtype=torch.int32, device="cuda")
+    ev = [torch.zeros(2, 2, 4, dtype=torch.int32, device="cuda") for _ in range(2)]
+    R.roco_tree_commit(warm, q, k, v, lse, par, path, n, 5, ev[0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        R.roco_tree_commit(graphed, q, k, v, lse, par, path, n, 5, ev[1])
+    n.copy_(torch.tensor([4, 0], dtype=torch.int32))
+    R.roco_tree_commit(eager, q, k, v, lse, par, path, n, 5, ev[0])
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(ev[0], ev[1])
+    for f in CACHE_FIELDS:
+        assert torch.equal(getattr(eager, f).view(torch.uint8), getattr(graphed, f).view(torch.uint8)), f
