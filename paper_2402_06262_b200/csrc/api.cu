@@ -160,7 +160,8 @@ roco_status check_linear(const roco_linear_state *s) {
 
 // Parts of every unit's prompt that different CTAs work on.
 int linear_segments(const roco_linear_state *s, int Lmax) {
-  return linear_simt_segments(s->S * s->G, s->d, Lmax, device_sms());
+  return s->dtype == ROCO_BF16 ? linear_tc_segments(s->S * s->G, Lmax, device_sms())
+                               : linear_simt_segments(s->S * s->G, s->d, Lmax, device_sms());
 }
 
 int pow2_at_least(int x) {
@@ -756,6 +757,8 @@ roco_status roco_linear_prefill(const roco_linear_state *state, const void *Q, c
   p.lens = lens; p.G = state->G; p.Lmax = Lmax; p.scale = scale;
   p.parts = static_cast<float *>(workspace); p.segments = linear_segments(state, Lmax);
   if ((long long)state->S * state->G * p.segments * (state->d / 64) > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
+  if (state->dtype == ROCO_BF16)
+    return launch_linear_prefill_tc(p, state->d, state->S * state->G, static_cast<cudaStream_t>(stream));
   return launch_linear_prefill_simt(p, state->dtype, state->d, state->S * state->G, static_cast<cudaStream_t>(stream));
 }
 

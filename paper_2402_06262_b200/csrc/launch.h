@@ -71,6 +71,10 @@ roco_status launch_budget_select_gather(const roco_cache &c, int Lmax, const int
 // box_rows rows and the 128-byte swizzle; false when the driver entry point is unavailable or the encode fails.
 bool make_tensor_map_rows128_bf16(void *map, const void *base, unsigned long long rows, unsigned box_rows);
 
+// Tensor map over a [U][rows][d] bf16 tensor (d = 64 or 128) with boxes of 64 columns x box_rows rows x 1 unit and the
+// 128-byte swizzle; rows past `rows` read as zero and are not written.
+bool make_tensor_map_units_bf16(void *map, const void *base, int U, int rows, int d, unsigned box_rows);
+
 // Multi-query steps: nb new tokens per unit, each with M / nb query heads (M = nb * group query rows, row
 // t * group + g = head g of token t).  Block-wise evict-and-encode: group 1; grouped-query decode: nb 1.
 int multi_max_queries();
@@ -101,6 +105,9 @@ roco_status launch_tree_commit(const CommitParams &p, int kv_dtype, int d, int U
 struct LinearParams;
 roco_status launch_linear_step(const LinearParams &p, const int *active, int dtype, int d, int U, cudaStream_t stream);
 int linear_simt_segments(int U, int d, int Lmax, int sms);  // parts of the prompt that work side by side (p.segments)
+// Tensor cores (bf16).
+int linear_tc_segments(int U, int Lmax, int sms);
+roco_status launch_linear_prefill_tc(const LinearParams &p, int d, int U, cudaStream_t stream);
 roco_status launch_linear_prefill_simt(const LinearParams &p, int dtype, int d, int U, cudaStream_t stream);
 
 }  // namespace roco
