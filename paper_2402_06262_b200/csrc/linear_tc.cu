@@ -4,21 +4,24 @@
 //     out_i = scale * ( g^(i+1) q_i S + sum_{j <= i} g^(i-j) (q_i.k_j) v_j )
 //     S    <- g^C S + sum_j (g^(C-1-j) k_j)^T v_j
 // which is four products per chunk, issued by one thread, accumulators in tensor memory:
-//     S1 = Q K^T                                   both operands as TMA wrote them
-//     O  = Q bf16(S)          then, by the A warps, row i times g^(i+1)
-//     O += P V                P = S1 with the decays as bf16, from tensor memory
-//     DS = KH^T V + KL^T V    KH + KL = g^(C-1-j) k_j as the sum of two bf16, from tensor memory
+//     S1 = Q K^T              both operands as TMA wrote them
+//     O  = Q bf16(S)          then, by the A warps, row i times scale g^(i+1)
+//     O += P V                P = S1 with the decays and the scale as bf16, from tensor memory
+//     DS = (K1 + K2 + K3)^T V K1 + K2 + K3 = g^(C-1-j) k_j as the sum of three bf16, from tensor memory
 // Every power of the decay is at most 1, so nothing overflows however fast a head forgets.  The state itself stays in the
-// registers of the B warps in fp32 from the first chunk to the last: a thread keeps half a row, adds DS (which the
-// split keys make exact to 2^-16 of each term) and writes the row as the next chunk's operand.  Rounded to bf16 are the
-// operands P and S of the output, which is bf16 itself.
+// registers of the B warps in fp32 from the first chunk to the last: a thread keeps half a row, adds DS and writes the row
+// as the next chunk's operand.  Three bf16 carry the 24 bits of an fp32 key, so the state is as exact as one formed in
+// fp32 (with two, 2.4e-6 of it were lost; with one, as much as bf16 loses).  Rounded to bf16 are the operands P and S of
+// the output, which is bf16 itself.
 //
 // Warps: 0-7 (A) a token per tensor-memory lane, half of the columns each: P, the scaling of O, the output.  8-15 (B) a
-// row of the state per lane: DS, the state, KH and KL.  16 TMA loads and stores (the output of a chunk is staged where its
-// queries were), 17 the products.
+// row of the state per lane: DS, the state; and the split keys, 32 tokens at a time through two buffers, so that the next
+// tokens are split while the tensor cores work on the last.  16 TMA loads and stores (the output of a chunk is staged
+// where its queries were), 17 the products.
 //
-// What bounds it: 128 KiB cross HBM per chunk at d = 128, 3.0 us at one SM's share of the measured copy rate, against
-// 2560 tensor cycles (1.4 us); the chain DS -> state -> KH -> DS and the one S1 -> P -> O -> output run side by side.
+// What bounds it: 128 KiB cross HBM per chunk at d = 128, 3.0 us at one SM's share of the measured copy rate.  A product
+// with both operands in shared memory runs at half the tensor rate here (S1 and O: 130 cycles per instruction of
+// 128 x 128 x 16), one with an operand in tensor memory at 72: about 4400 cycles (2.3 us) per chunk.
 #include <cuda.h>
 
 #include "linear.cuh"
@@ -30,15 +33,20 @@ constexpr int kLtChunk = 128;
 constexpr int kLtAWarps = 8, kLtBWarps = 8;
 constexpr int kLtTmaWarp = kLtAWarps + kLtBWarps, kLtMmaWarp = kLtTmaWarp + 1;
 constexpr int kLtThreads = (kLtMmaWarp + 1) * 32;
-constexpr uint32_t kLtColS = 0, kLtColO = 128, kLtColDS = 256, kLtColKH = 384, kLtColKL = 448, kLtTmemCols = 512;
+constexpr int kLtSplits = 3;          // bf16 terms of a decayed key
+constexpr int kLtPiece = 32;          // tokens whose keys are split at a time
+constexpr int kLtPieceCols = kLtSplits * kLtPiece / 2;
+constexpr uint32_t kLtColS = 0, kLtColO = 128, kLtColDS = 256, kLtColK = 384, kLtTmemCols = 512;
+static_assert(kLtColK + 2 * kLtPieceCols <= kLtTmemCols, "tensor memory");
 
 template <int D>
 struct LtSmem {
   static constexpr int kTile = kLtChunk * D * 2;
   static constexpr int kSop = D * D * 2;
-  static constexpr int kBars = 24;
+  static constexpr int kBars = 26;
+  static constexpr int kTables = 256 + 128 + 32;
   static constexpr size_t bytes(bool states) {
-    return 1024 + (size_t)kTile * (states ? 4 : 6) + (states ? 0 : kSop) + 260 * 4 + kBars * 8 + 16;
+    return 1024 + (size_t)kTile * (states ? 4 : 6) + (states ? 0 : kSop) + kTables * 4 + kBars * 8 + 16;
   }
 };
 
@@ -60,6 +68,29 @@ __device__ __forceinline__ uint32_t lt_pack(float lo, float hi) {
   return *reinterpret_cast<uint32_t *>(&v);
 }
 
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t lt_pack2(f32x2 v) {
+  float a, b;
+  unpack2(v, a, b);
+  return lt_pack(a, b);
+}
+// Four 8 x 8 blocks of 16-bit elements, transposed: lane t gets of block m the elements (rows 2 (t & 3) and the next,
+// column t >> 2), rows being what the addresses of lanes 8 m .. 8 m + 7 point to.
+__device__ __forceinline__ void lt_ldsm_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// 16 tensor-memory lanes x 8 columns: lane t writes row t >> 2 (r[0], r[2]) and 8 + (t >> 2) (r[1], r[3]), columns
+// t & 3 (r[0], r[1]) and 4 + (t & 3).
+__device__ __forceinline__ void lt_st_16x8(uint32_t taddr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%0], {%1, %2, %3, %4};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+
 template <int D, bool kStates>
 __global__ void __launch_bounds__(kLtThreads, 1)
     linear_prefill_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
@@ -76,11 +107,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   char *vt = at; at += 2 * kTile;
   char *qt = at; if (!kStates) at += 2 * kTile;
   char *sop = at; if (!kStates) at += LtSmem<D>::kSop;
-  float *tbl = reinterpret_cast<float *>(at); at += 260 * 4;  // tbl[128 + n] = g^n for 0 <= n <= 128, 0 for n < 0
+  float *ptab = reinterpret_cast<float *>(at);  // ptab[128 + n] = scale g^n, 0 for n < 0
+  float *ktab = ptab + 256;                     // ktab[x] = g^(127 - x)
+  float *ctab = ktab + 128;                     // ctab[e] = g^(31 - e)
+  at += LtSmem<D>::kTables * 4;
   uint64_t *bars = reinterpret_cast<uint64_t *>(at); at += LtSmem<D>::kBars * 8;
   uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6, *q_full = bars + 8;
   uint64_t *s1_full = bars + 12, *p_ready = bars + 13, *o1_full = bars + 14, *o_scaled = bars + 15, *o_full = bars + 16;
-  uint64_t *o_free = bars + 17, *sop_ready = bars + 18, *ds_full = bars + 19, *kp_ready = bars + 20, *staged = bars + 21;
+  uint64_t *o_free = bars + 17, *sop_ready = bars + 18, *ds_full = bars + 19, *ds_free = bars + 20, *staged = bars + 21;
+  uint64_t *kp_ready = bars + 22, *kp_free = bars + 24;
   uint32_t *tmem_base = reinterpret_cast<uint32_t *>(at);
   int *abort_ptr = reinterpret_cast<int *>(at + 8);
   volatile int *abort_flag = abort_ptr;
@@ -103,11 +138,14 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     }
     mbar_init(s1_full, 1); mbar_init(p_ready, kLtAWarps); mbar_init(o1_full, 1); mbar_init(o_scaled, kLtAWarps);
     mbar_init(o_full, 1); mbar_init(o_free, kLtAWarps); mbar_init(sop_ready, kLtBWarps); mbar_init(ds_full, 1);
-    mbar_init(kp_ready, kLtBWarps); mbar_init(staged, kLtAWarps);
+    mbar_init(ds_free, kLtBWarps); mbar_init(staged, kLtAWarps);
+    for (int i = 0; i < 2; ++i) { mbar_init(&kp_ready[i], kLtBWarps); mbar_init(&kp_free[i], 1); }
     *abort_ptr = 0;
     mbar_init_fence();
   }
-  if (tid < 257) tbl[tid] = tid < 128 ? 0.f : (float)decay_pow(logd, tid - 128);
+  if (tid < 256) ptab[tid] = tid < 128 ? 0.f : (float)(decay_pow(logd, tid - 128) * (double)p.scale);
+  else if (tid < 384) ktab[tid - 256] = (float)decay_pow(logd, 127 - (tid - 256));
+  else if (tid < 416) ctab[tid - 384] = (float)decay_pow(logd, 31 - (tid - 384));
   if (warp == 0) {
     tmem_alloc(tmem_base, kLtTmemCols);
     tmem_relinquish();
@@ -166,6 +204,25 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         fence_async_smem();
         __syncwarp();
       }
+      // DS, a piece of 32 tokens
+      auto piece = [&](int q) {
+        const int bf = q & 1;
+        mbar_wait(&kp_ready[bf], (2 * c + (q >> 1)) & 1, abort_flag, p.status);
+        tc_fence_after();
+        if (lane == 0) {
+#pragma unroll
+          for (int x = 0; x < 2 * kLtSplits; ++x)  // term x >> 1, tokens 16 (x & 1) .. of the piece
+            umma_bf16_tmem_a(tmem + kLtColDS, tmem + kLtColK + (uint32_t)(bf * kLtPieceCols + (x >> 1) * (kLtPiece / 2) + 8 * (x & 1)),
+                             smem_desc_sw128_mn(v + (2 * q + (x & 1)) * 2048, kBlock), kIdescV, (q > 0 || x > 0) ? 1u : 0u);
+          umma_commit(&kp_free[bf]);
+          if (q == 3) {
+            umma_commit(ds_full);
+            umma_commit(&k_empty[sl]);
+            if (kStates) umma_commit(&v_empty[sl]);
+          }
+        }
+        __syncwarp();
+      };
       if (!kStates) {
         mbar_wait(&q_full[sl], full, abort_flag, p.status);
         tc_fence_after();
@@ -178,6 +235,12 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           umma_commit(s1_full);
         }
         __syncwarp();
+      }
+      mbar_wait(&v_full[sl], full, abort_flag, p.status);
+      if (c > 0) mbar_wait(ds_free, (c - 1) & 1, abort_flag, p.status);
+      piece(0);
+      piece(1);
+      if (!kStates) {
         mbar_wait(sop_ready, par, abort_flag, p.status);
         if (c > 0) mbar_wait(o_free, (c - 1) & 1, abort_flag, p.status);
         tc_fence_after();
@@ -190,19 +253,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         }
         __syncwarp();
       }
-      mbar_wait(kp_ready, par, abort_flag, p.status);
-      mbar_wait(&v_full[sl], full, abort_flag, p.status);
-      tc_fence_after();
-      if (lane == 0) {  // DS
-#pragma unroll
-        for (int kk = 0; kk < 16; ++kk)
-          umma_bf16_tmem_a(tmem + kLtColDS, tmem + (kk < 8 ? kLtColKH : kLtColKL) + (uint32_t)(8 * (kk & 7)),
-                           smem_desc_sw128_mn(v + (kk & 7) * 2048, kBlock), kIdescV, kk > 0 ? 1u : 0u);
-        umma_commit(ds_full);
-        umma_commit(&k_empty[sl]);
-        if (kStates) umma_commit(&v_empty[sl]);
-      }
-      __syncwarp();
+      piece(2);
+      piece(3);
       if (!kStates) {
         mbar_wait(p_ready, par, abort_flag, p.status);
         mbar_wait(o_scaled, par, abort_flag, p.status);
@@ -223,7 +275,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     if (!kStates) {
       const int wq = warp & 3, half = warp >> 2, i = wq * 32 + lane;
       const uint32_t tl = tmem + ((uint32_t)(wq * 32) << 16);
-      const float inter = tbl[128 + i + 1];
+      const float inter = (float)(decay_pow(logd, i + 1) * (double)p.scale);
+      const f32x2 inter2 = pack2(inter, inter);
       for (int c = 0; c < n; ++c) {
         const uint32_t par = c & 1;
         mbar_wait(s1_full, par, abort_flag, p.status);
@@ -238,11 +291,23 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           } else {
             uint32_t r[32];
             tmem_ld32_issue(tl + kLtColS + (uint32_t)j0, r);
-            const float *w = tbl + 128 + i - j0;
-            tmem_ld_wait(r);
+            const float *w = ptab + 128 + i - j0;  // w[-e]: column j0 + e
+            if (wq * 32 > j0) {  // wholly below the diagonal: one power per row times 32 that all rows share
+              const float base = w[-31];
+              const f32x2 b2 = pack2(base, base);
+              tmem_ld_wait(r);
 #pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              pk[e >> 1] = lt_pack(__uint_as_float(r[e]) * w[-e], __uint_as_float(r[e + 1]) * w[-e - 1]);
+              for (int e = 0; e < 32; e += 4) {
+                const float4 c4 = *reinterpret_cast<const float4 *>(ctab + e);
+                pk[e >> 1] = lt_pack2(mul2(mul2(pack2(c4.x, c4.y), b2), pack2u(r[e], r[e + 1])));
+                pk[(e >> 1) + 1] = lt_pack2(mul2(mul2(pack2(c4.z, c4.w), b2), pack2u(r[e + 2], r[e + 3])));
+              }
+            } else {  // on it: the table's zeros are the mask
+              tmem_ld_wait(r);
+#pragma unroll
+              for (int e = 0; e < 32; e += 2)
+                pk[e >> 1] = lt_pack(__uint_as_float(r[e]) * w[-e], __uint_as_float(r[e + 1]) * w[-e - 1]);
+            }
           }
           tmem_st16(tl + kLtColS + (uint32_t)(half * 64 + cc * 16), pk);
         }
@@ -260,9 +325,12 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           tmem_ld_wait(r);
           uint32_t a[16], b[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            a[e] = __float_as_uint(__uint_as_float(r[e]) * inter);
-            b[e] = __float_as_uint(__uint_as_float(r[e + 16]) * inter);
+          for (int e = 0; e < 16; e += 2) {
+            float f0, f1;
+            unpack2(mul2(pack2u(r[e], r[e + 1]), inter2), f0, f1);
+            a[e] = __float_as_uint(f0); a[e + 1] = __float_as_uint(f1);
+            unpack2(mul2(pack2u(r[e + 16], r[e + 17]), inter2), f0, f1);
+            b[e] = __float_as_uint(f0); b[e + 1] = __float_as_uint(f1);
           }
           tmem_st16(to + (uint32_t)x, a);
           tmem_st16(to + (uint32_t)x + 16u, b);
@@ -289,10 +357,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             uint4 o;
-            o.x = lt_pack(__uint_as_float(r[8 * e]) * p.scale, __uint_as_float(r[8 * e + 1]) * p.scale);
-            o.y = lt_pack(__uint_as_float(r[8 * e + 2]) * p.scale, __uint_as_float(r[8 * e + 3]) * p.scale);
-            o.z = lt_pack(__uint_as_float(r[8 * e + 4]) * p.scale, __uint_as_float(r[8 * e + 5]) * p.scale);
-            o.w = lt_pack(__uint_as_float(r[8 * e + 6]) * p.scale, __uint_as_float(r[8 * e + 7]) * p.scale);
+            o.x = lt_pack(__uint_as_float(r[8 * e]), __uint_as_float(r[8 * e + 1]));
+            o.y = lt_pack(__uint_as_float(r[8 * e + 2]), __uint_as_float(r[8 * e + 3]));
+            o.z = lt_pack(__uint_as_float(r[8 * e + 4]), __uint_as_float(r[8 * e + 5]));
+            o.w = lt_pack(__uint_as_float(r[8 * e + 6]), __uint_as_float(r[8 * e + 7]));
             const int col = half * kHalfCols + x + 8 * e, ch = (col & 63) >> 3;
             if (!partial) *reinterpret_cast<uint4 *>(stage + (col >> 6) * kBlock + i * 128 + ((ch ^ (i & 7)) << 4)) = o;
             else if (i < tail) *reinterpret_cast<uint4 *>(orow + col * 2) = o;
@@ -351,54 +419,82 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         }
       }
     };
+    // ldmatrix: lanes 8 m .. 8 m + 7 point to eight tokens' 16 bytes of 8 components; blocks 0 and 1 are 16 components of
+    // the first eight tokens, 2 and 3 of the next eight
+    const int lm_tok = ((lane >> 4) & 1) * 8 + (lane & 7), lm_ch = (lane >> 3) & 1;
     for (int c = 0; c < n; ++c) {
       const int sl = c & 1;
-      if (c > 0) add_ds(c - 1, g_chunk);
-      if (!kStates) {
-        if (c > 0) mbar_wait(o1_full, (c - 1) & 1, abort_flag, p.status);  // the operand of the chunk before is used up
-        if (mine) {
-          // row r0 of the operand: 64 columns to a block of D rows of 128 bytes
-          char *row = sop + r0 * 128;
-#pragma unroll
-          for (int x = 0; x < kHalfCols; x += 8) {
-            const int col = half * kHalfCols + x, ch = (col & 63) >> 3;
-            *reinterpret_cast<uint4 *>(row + (col >> 6) * (D * 128) + ((ch ^ (r0 & 7)) << 4)) =
-                make_uint4(lt_pack(s[x], s[x + 1]), lt_pack(s[x + 2], s[x + 3]), lt_pack(s[x + 4], s[x + 5]),
-                           lt_pack(s[x + 6], s[x + 7]));
-          }
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sop_ready);
-      }
+      const int nt = c == n - 1 ? tail : kLtChunk;
       mbar_wait(&k_full[sl], (c >> 1) & 1, abort_flag, p.status);
-      if (mine) {
-        // component r0 of 64 keys, times what is left of each at the end of the chunk, as a sum of two bf16
-        const int nt = c == n - 1 ? tail : kLtChunk;
-        const char *kcol = kt + sl * kTile + (r0 >> 6) * kBlock + (r0 & 7) * 2;
-        const int ch = (r0 & 63) >> 3;
+      const char *ktile = kt + sl * kTile + (wq >> 1) * kBlock;
 #pragma unroll 1
-        for (int tt = half * 64; tt < half * 64 + 64; tt += 16) {
-          uint32_t hi[8], lo[8];
-          const float *w = tbl + 128 + nt - 1 - tt;
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            const uint32_t ka = *reinterpret_cast<const uint16_t *>(kcol + (tt + e) * 128 + ((ch ^ (e & 7)) << 4));
-            const uint32_t kb = *reinterpret_cast<const uint16_t *>(kcol + (tt + e + 1) * 128 + ((ch ^ ((e + 1) & 7)) << 4));
-            const float fa = tt + e < nt ? __uint_as_float(ka << 16) * w[-e] : 0.f;
-            const float fb = tt + e + 1 < nt ? __uint_as_float(kb << 16) * w[-e - 1] : 0.f;
-            const uint32_t h = lt_pack(fa, fb);
-            hi[e >> 1] = h;
-            lo[e >> 1] = lt_pack(fa - __uint_as_float(h << 16), fb - __uint_as_float(h & 0xffff0000u));
+      for (int q = 0; q < 4; ++q) {
+        const int bf = q & 1;
+        if (q == 2) {
+          if (c > 0) {
+            add_ds(c - 1, g_chunk);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_free);
           }
-          tmem_st8(tl + kLtColKH + (uint32_t)(tt >> 1), hi);
-          tmem_st8(tl + kLtColKL + (uint32_t)(tt >> 1), lo);
+          if (!kStates) {
+            if (c > 0) mbar_wait(o1_full, (c - 1) & 1, abort_flag, p.status);  // the operand of the chunk before is used up
+            if (mine) {
+              // row r0 of the operand: 64 columns to a block of D rows of 128 bytes
+              char *row = sop + r0 * 128;
+#pragma unroll
+              for (int x = 0; x < kHalfCols; x += 8) {
+                const int col = half * kHalfCols + x, ch = (col & 63) >> 3;
+                *reinterpret_cast<uint4 *>(row + (col >> 6) * (D * 128) + ((ch ^ (r0 & 7)) << 4)) =
+                    make_uint4(lt_pack(s[x], s[x + 1]), lt_pack(s[x + 2], s[x + 3]), lt_pack(s[x + 4], s[x + 5]),
+                               lt_pack(s[x + 6], s[x + 7]));
+              }
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sop_ready);
+          }
         }
-        tmem_st_wait();
+        if (c > 0 || q >= 2) mbar_wait(&kp_free[bf], (2 * c + (q >> 1) - 1) & 1, abort_flag, p.status);
+        if (mine) {
+          // 16 tokens (this warp's half of the piece) of 32 components, times what is left of each token at the end of
+          // the chunk, as the sum of three bf16; a register holds two neighbouring tokens
+          const int t0 = q * kLtPiece + half * 16, tok = t0 + 2 * (lane & 3);
+          float w[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) w[x] = ktab[min(tok + (x >> 1) * 8 + (x & 1) + kLtChunk - nt, kLtChunk - 1)];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int tr = t0 + lm_tok, ch = (wq & 1) * 4 + 2 * h + lm_ch;
+            uint32_t r[4], k1[4], k2[4], k3[4];
+            lt_ldsm_t(smem_u32(ktile + tr * 128 + ((ch ^ (tr & 7)) << 4)), r);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+              const int x = m & 2;
+              if (nt < kLtChunk) {  // tokens behind the last may hold anything
+                if (tok + 4 * x >= nt) r[m] &= 0xffff0000u;
+                if (tok + 4 * x + 1 >= nt) r[m] &= 0x0000ffffu;
+              }
+              float a = __uint_as_float(r[m] << 16) * w[x], b = __uint_as_float(r[m] & 0xffff0000u) * w[x + 1];
+              k1[m] = lt_pack(a, b);
+              a -= __uint_as_float(k1[m] << 16);
+              b -= __uint_as_float(k1[m] & 0xffff0000u);
+              k2[m] = lt_pack(a, b);
+              a -= __uint_as_float(k2[m] << 16);
+              b -= __uint_as_float(k2[m] & 0xffff0000u);
+              k3[m] = lt_pack(a, b);
+            }
+            const uint32_t to = tl + ((uint32_t)(16 * h) << 16) + kLtColK + (uint32_t)(bf * kLtPieceCols + half * 8);
+            lt_st_16x8(to, k1);
+            lt_st_16x8(to + kLtPiece / 2, k2);
+            lt_st_16x8(to + kLtPiece, k3);
+          }
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&kp_ready[bf]);
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(kp_ready);
     }
     if (n > 0) add_ds(n - 1, Decay2(decay_pow(logd, tail)));
     if (mine && (kStates || seg == p.segments - 1)) {
@@ -412,6 +508,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, kLtTmemCols);
 }
+
+static_assert(LtSmem<128>::bytes(false) <= 227 * 1024, "shared memory");
 
 template <int D>
 roco_status linear_prefill_tc_t(const LinearParams &p, int U, cudaStream_t stream) {
