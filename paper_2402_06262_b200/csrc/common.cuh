@@ -84,6 +84,30 @@ __device__ __forceinline__ void mbar_wait(uint64_t *bar, uint32_t parity, volati
   if (status) atomicOr(status, ROCO_DEV_WAIT_TIMEOUT);
 }
 
+// The same with everything but the first poll out of line, for kernels with many waits: inlined, the loop costs some
+// forty instructions at every wait, and a kernel of several warp roles then outgrows the instruction cache.
+static __device__ __noinline__ void mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag, int32_t *status) {
+  const uint64_t t0 = global_timer_ns();
+  do {
+    if (*abort_flag) return;
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(kSuspendHintNs)
+        : "memory");
+    if (ok) return;
+  } while (global_timer_ns() - t0 < kWaitLimitNs);
+  *abort_flag = 1;
+  if (status) atomicOr(status, ROCO_DEV_WAIT_TIMEOUT);
+}
+__device__ __forceinline__ void mbar_wait_compact(uint64_t *bar, uint32_t parity, volatile int *abort_flag, int32_t *status) {
+  if (mbar_try_wait(bar, parity)) return;
+  mbar_wait_slow(smem_u32(bar), parity, abort_flag, status);
+}
+
 // global -> shared bulk copy completing on an mbarrier.  Both addresses 16-byte aligned, bytes % 16 == 0.
 __device__ __forceinline__ void bulk_g2s(void *dst_smem, const void *src_gmem, uint32_t bytes, uint64_t *bar) {
   asm volatile(

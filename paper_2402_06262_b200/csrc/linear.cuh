@@ -20,7 +20,8 @@ struct LinearParams {
 };
 
 // g^n for n >= 0 in 64 bits: in fp32 the rounding of g alone would be off by n 2^-24 after n tokens.
-__device__ __forceinline__ double decay_pow(double log_decay, double n) { return n == 0.0 ? 1.0 : exp(log_decay * n); }
+// (Out of line: the exponential in 64 bits is long.)
+static __device__ __noinline__ double decay_pow(double log_decay, double n) { return n == 0.0 ? 1.0 : exp(log_decay * n); }
 
 // A factor as the sum of two floats, so that applying it thousands of times in a row does not drift.
 struct Decay2 {

@@ -15,7 +15,7 @@
 // the output, which is bf16 itself.
 //
 // Warps: 0-7 (A) a token per tensor-memory lane, half of the columns each: P, the scaling of O, the output.  8-15 (B) a
-// row of the state per lane: DS, the state; and the split keys, 32 tokens at a time through two buffers, so that the next
+// row of the state per lane: DS, the state.  Both split keys, 32 tokens at a time through two buffers, so that the next
 // tokens are split while the tensor cores work on the last.  16 TMA loads and stores (the output of a chunk is staged
 // where its queries were), 17 the products.
 //
@@ -23,6 +23,8 @@
 // with both operands in shared memory runs at half the tensor rate here (S1 and O: 130 cycles per instruction of
 // 128 x 128 x 16), one with an operand in tensor memory at 72: about 4400 cycles (2.3 us) per chunk.
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "linear.cuh"
 #include "tc.cuh"
@@ -43,21 +45,13 @@ template <int D>
 struct LtSmem {
   static constexpr int kTile = kLtChunk * D * 2;
   static constexpr int kSop = D * D * 2;
-  static constexpr int kBars = 26;
+  static constexpr int kBars = 28;
   static constexpr int kTables = 256 + 128 + 32;
   static constexpr size_t bytes(bool states) {
     return 1024 + (size_t)kTile * (states ? 4 : 6) + (states ? 0 : kSop) + kTables * 4 + kBars * 8 + 16;
   }
 };
 
-__device__ __forceinline__ void umma_bf16_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                                 uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void *src, int c0, int c1, int c2) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
                ::"l"(map), "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2)
@@ -139,7 +133,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     mbar_init(s1_full, 1); mbar_init(p_ready, kLtAWarps); mbar_init(o1_full, 1); mbar_init(o_scaled, kLtAWarps);
     mbar_init(o_full, 1); mbar_init(o_free, kLtAWarps); mbar_init(sop_ready, kLtBWarps); mbar_init(ds_full, 1);
     mbar_init(ds_free, kLtBWarps); mbar_init(staged, kLtAWarps);
-    for (int i = 0; i < 2; ++i) { mbar_init(&kp_ready[i], kLtBWarps); mbar_init(&kp_free[i], 1); }
+    for (int i = 0; i < 2; ++i) mbar_init(&kp_ready[i], kLtBWarps);
+    for (int i = 0; i < 4; ++i) mbar_init(&kp_free[i], 1);
     *abort_ptr = 0;
     mbar_init_fence();
   }
@@ -155,6 +150,59 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_base;
 
+  // Keys of a piece of 32 tokens, times what is left of each token at the end of the chunk, as the sum of three bf16; by
+  // eight warps: a lane quarter's 32 components each, 16 tokens each.  A register holds two neighbouring tokens.
+  // (ldmatrix: lanes 8 m .. 8 m + 7 point to eight tokens' 16 bytes of 8 components; blocks 0 and 1 are 16 components of
+  // the first eight tokens, 2 and 3 of the next eight.)
+  const int lm_tok = ((lane >> 4) & 1) * 8 + (lane & 7), lm_ch = (lane >> 3) & 1;
+  auto split_keys = [&](int c, int q) {
+    const int wq = warp & 3, half = (warp >> 2) & 1, bf = q & 1, nt = c == n - 1 ? tail : kLtChunk;
+    const char *ktile = kt + (c & 1) * kTile + (wq >> 1) * kBlock;
+    // the buffer's last piece is used up: two pieces back (one barrier per piece of a chunk, so that whoever waits on one
+    // waits for each of its phases in turn)
+    if (c > 0 || q >= 2) mbar_wait_compact(&kp_free[q ^ 2], (q >= 2 ? c : c - 1) & 1, abort_flag, p.status);
+    if (wq * 32 < D) {  // d = 64: the upper two lane quarters hold no rows
+      const int t0 = q * kLtPiece + half * 16, tok = t0 + 2 * (lane & 3), tr = t0 + lm_tok;
+      uint32_t r[2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int ch = (wq & 1) * 4 + 2 * h + lm_ch;
+        lt_ldsm_t(smem_u32(ktile + tr * 128 + ((ch ^ (tr & 7)) << 4)), r[h]);
+      }
+      float w[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[x] = ktab[min(tok + (x >> 1) * 8 + (x & 1) + kLtChunk - nt, kLtChunk - 1)];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t k1[4], k2[4], k3[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const int x = m & 2;
+          if (nt < kLtChunk) {  // tokens behind the last may hold anything
+            if (tok + 4 * x >= nt) r[h][m] &= 0xffff0000u;
+            if (tok + 4 * x + 1 >= nt) r[h][m] &= 0x0000ffffu;
+          }
+          float a = __uint_as_float(r[h][m] << 16) * w[x], b = __uint_as_float(r[h][m] & 0xffff0000u) * w[x + 1];
+          k1[m] = lt_pack(a, b);
+          a -= __uint_as_float(k1[m] << 16);
+          b -= __uint_as_float(k1[m] & 0xffff0000u);
+          k2[m] = lt_pack(a, b);
+          a -= __uint_as_float(k2[m] << 16);
+          b -= __uint_as_float(k2[m] & 0xffff0000u);
+          k3[m] = lt_pack(a, b);
+        }
+        const uint32_t to = tmem + ((uint32_t)(wq * 32 + 16 * h) << 16) + kLtColK + (uint32_t)(bf * kLtPieceCols + half * 8);
+        lt_st_16x8(to, k1);
+        lt_st_16x8(to + kLtPiece / 2, k2);
+        lt_st_16x8(to + kLtPiece, k3);
+      }
+      tmem_st_wait();
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&kp_ready[bf]);
+  };
+
   if (warp == kLtTmaWarp) {
     if (lane == 0) {
       for (int c = 0; c < n + 2; ++c) {
@@ -165,16 +213,16 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           for (int h = 0; h < D / 64; ++h) tma_load_3d(tiles + sl * kTile + h * kBlock, map, 64 * h, row, u, &full[sl]);
         };
         if (c < n) {
-          if (c >= 2) mbar_wait(&k_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
+          if (c >= 2) mbar_wait_compact(&k_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
           load(kt, &mapK, k_full);
-          if (c >= 2) mbar_wait(&v_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
+          if (c >= 2) mbar_wait_compact(&v_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
           load(vt, &mapV, v_full);
         }
         if (!kStates) {
           // the output of the chunk before the last leaves its slot, which then takes the queries of this one (a partial
           // chunk is the segment's last and is written by the A warps)
           if (c >= 2 && !(c - 2 == n - 1 && tail < kLtChunk)) {
-            mbar_wait(staged, c & 1, abort_flag, p.status);
+            mbar_wait_compact(staged, c & 1, abort_flag, p.status);
 #pragma unroll
             for (int h = 0; h < D / 64; ++h) tma_store_3d(&mapO, qt + sl * kTile + h * kBlock, 64 * h, row - 2 * kLtChunk, u);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
@@ -186,14 +234,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
       if (!kStates) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
   } else if (warp == kLtMmaWarp) {
+    // (the accumulators sit at fixed columns: the allocation is all of tensor memory)
     for (int c = 0; c < n; ++c) {
       const int sl = c & 1;
       const uint32_t full = (c >> 1) & 1, par = c & 1;
       char *k = kt + sl * kTile, *v = vt + sl * kTile, *q = qt + sl * kTile;
-      mbar_wait(&k_full[sl], full, abort_flag, p.status);
+      mbar_wait_compact(&k_full[sl], full, abort_flag, p.status);
       if (c == n - 1 && tail < kLtChunk) {
         // rows behind the prompt may hold anything: their scores are multiplied by zero, and so are their values
-        mbar_wait(&v_full[sl], full, abort_flag, p.status);
+        mbar_wait_compact(&v_full[sl], full, abort_flag, p.status);
         for (int w = lane; w < (kLtChunk - tail) * 8; w += 32) {
 #pragma unroll
           for (int h = 0; h < D / 64; ++h) {
@@ -205,83 +254,76 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         __syncwarp();
       }
       // DS, a piece of 32 tokens
-      auto piece = [&](int q) {
-        const int bf = q & 1;
-        mbar_wait(&kp_ready[bf], (2 * c + (q >> 1)) & 1, abort_flag, p.status);
+      auto piece = [&](auto number) {
+        constexpr int q4 = decltype(number)::value, bf = q4 & 1;
+        mbar_wait_compact(&kp_ready[bf], (2 * c + (q4 >> 1)) & 1, abort_flag, p.status);
         tc_fence_after();
-        if (lane == 0) {
 #pragma unroll
-          for (int x = 0; x < 2 * kLtSplits; ++x)  // term x >> 1, tokens 16 (x & 1) .. of the piece
-            umma_bf16_tmem_a(tmem + kLtColDS, tmem + kLtColK + (uint32_t)(bf * kLtPieceCols + (x >> 1) * (kLtPiece / 2) + 8 * (x & 1)),
-                             smem_desc_sw128_mn(v + (2 * q + (x & 1)) * 2048, kBlock), kIdescV, (q > 0 || x > 0) ? 1u : 0u);
-          umma_commit(&kp_free[bf]);
-          if (q == 3) {
-            umma_commit(ds_full);
-            umma_commit(&k_empty[sl]);
-            if (kStates) umma_commit(&v_empty[sl]);
-          }
+        for (int x = 0; x < 2 * kLtSplits; ++x)  // term x >> 1, tokens 16 (x & 1) .. of the piece
+          umma_bf16_ts_w(kLtColDS, kLtColK + (uint32_t)(bf * kLtPieceCols + (x >> 1) * (kLtPiece / 2) + 8 * (x & 1)),
+                         smem_desc_sw128_mn(v + (2 * q4 + (x & 1)) * 2048, kBlock), kIdescV, (q4 > 0 || x > 0) ? 1u : 0u);
+        umma_commit_w(&kp_free[q4]);
+        if (q4 == 3) {
+          umma_commit_w(ds_full);
+          umma_commit_w(&k_empty[sl]);
+          umma_commit_w(&v_empty[sl]);
         }
-        __syncwarp();
       };
       if (!kStates) {
-        mbar_wait(&q_full[sl], full, abort_flag, p.status);
+        mbar_wait_compact(&q_full[sl], full, abort_flag, p.status);
         tc_fence_after();
-        if (lane == 0) {  // S1 (the product that read P from these columns was issued before it)
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const int off = (kk / 4) * kBlock + (kk % 4) * 32;
-            umma_bf16(tmem + kLtColS, smem_desc_sw128(q + off), smem_desc_sw128(k + off), kIdescS, kk > 0 ? 1u : 0u);
-          }
-          umma_commit(s1_full);
+        for (int kk = 0; kk < D / 16; ++kk) {  // S1 (the product that read P from these columns was issued before it)
+          const int off = (kk / 4) * kBlock + (kk % 4) * 32;
+          umma_bf16_w(kLtColS, smem_desc_sw128(q + off), smem_desc_sw128(k + off), kIdescS, kk > 0 ? 1u : 0u);
         }
-        __syncwarp();
+        umma_commit_w(s1_full);
       }
-      mbar_wait(&v_full[sl], full, abort_flag, p.status);
-      if (c > 0) mbar_wait(ds_free, (c - 1) & 1, abort_flag, p.status);
-      piece(0);
-      piece(1);
+      mbar_wait_compact(&v_full[sl], full, abort_flag, p.status);
+      if (c > 0) mbar_wait_compact(ds_free, (c - 1) & 1, abort_flag, p.status);
+      piece(std::integral_constant<int, 0>{});
+      piece(std::integral_constant<int, 1>{});
       if (!kStates) {
-        mbar_wait(sop_ready, par, abort_flag, p.status);
-        if (c > 0) mbar_wait(o_free, (c - 1) & 1, abort_flag, p.status);
+        mbar_wait_compact(sop_ready, par, abort_flag, p.status);
+        if (c > 0) mbar_wait_compact(o_free, (c - 1) & 1, abort_flag, p.status);
         tc_fence_after();
-        if (lane == 0) {  // O = Q S
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            umma_bf16(tmem + kLtColO, smem_desc_sw128(q + (kk / 4) * kBlock + (kk % 4) * 32),
+        for (int kk = 0; kk < D / 16; ++kk)  // O = Q S
+          umma_bf16_w(kLtColO, smem_desc_sw128(q + (kk / 4) * kBlock + (kk % 4) * 32),
                       smem_desc_sw128_mn(sop + kk * 2048, D * 128), kIdescV, kk > 0 ? 1u : 0u);
-          umma_commit(o1_full);
-        }
-        __syncwarp();
+        umma_commit_w(o1_full);
       }
-      piece(2);
-      piece(3);
+      piece(std::integral_constant<int, 2>{});
       if (!kStates) {
-        mbar_wait(p_ready, par, abort_flag, p.status);
-        mbar_wait(o_scaled, par, abort_flag, p.status);
+        mbar_wait_compact(p_ready, par, abort_flag, p.status);
+        mbar_wait_compact(o_scaled, par, abort_flag, p.status);
         tc_fence_after();
-        if (lane == 0) {  // O += P V
 #pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            umma_bf16_tmem_a(tmem + kLtColO, tmem + kLtColS + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8),
-                             smem_desc_sw128_mn(v + kk * 2048, kBlock), kIdescV, 1u);
-          umma_commit(o_full);
-          umma_commit(&v_empty[sl]);
-        }
-        __syncwarp();
+        for (int kk = 0; kk < 8; ++kk)  // O += P V
+          umma_bf16_ts_w(kLtColO, kLtColS + (uint32_t)((kk >> 2) * 64 + (kk & 3) * 8),
+                         smem_desc_sw128_mn(v + kk * 2048, kBlock), kIdescV, 1u);
+        umma_commit_w(o_full);
       }
+      piece(std::integral_constant<int, 3>{});
     }
   } else if (warp < kLtAWarps) {
     // ---------------------------------------------------------------- A: scores and output, a token per lane
-    if (!kStates) {
+    if (kStates) {
+      for (int c = 0; c < n; ++c) {
+        mbar_wait_compact(&k_full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+        split_keys(c, 2);
+        split_keys(c, 3);
+      }
+    } else {
       const int wq = warp & 3, half = warp >> 2, i = wq * 32 + lane;
       const uint32_t tl = tmem + ((uint32_t)(wq * 32) << 16);
       const float inter = (float)(decay_pow(logd, i + 1) * (double)p.scale);
       const f32x2 inter2 = pack2(inter, inter);
       for (int c = 0; c < n; ++c) {
         const uint32_t par = c & 1;
-        mbar_wait(s1_full, par, abort_flag, p.status);
+        mbar_wait_compact(s1_full, par, abort_flag, p.status);
         tc_fence_after();
-#pragma unroll
+#pragma unroll 1
         for (int cc = 0; cc < 2; ++cc) {
           const int j0 = half * 64 + cc * 32;
           uint32_t pk[16];
@@ -315,10 +357,12 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_ready);
-        mbar_wait(o1_full, par, abort_flag, p.status);
+        mbar_wait_compact(&k_full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+        split_keys(c, 2);
+        mbar_wait_compact(o1_full, par, abort_flag, p.status);
         tc_fence_after();
         const uint32_t to = tl + kLtColO + (uint32_t)(half * kHalfCols);
-#pragma unroll
+#pragma unroll 1
         for (int x = 0; x < kHalfCols; x += 32) {
           uint32_t r[32];
           tmem_ld32_issue(to + (uint32_t)x, r);
@@ -339,12 +383,13 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(o_scaled);
-        mbar_wait(o_full, par, abort_flag, p.status);
+        split_keys(c, 3);
+        mbar_wait_compact(o_full, par, abort_flag, p.status);
         tc_fence_after();
         const bool partial = c == n - 1 && tail < kLtChunk;
         char *stage = qt + (c & 1) * kTile;  // the products that read the queries are complete
         char *orow = p.out + (((size_t)u * p.Lmax + (size_t)(first + c) * kLtChunk + i) * D) * 2;
-#pragma unroll
+#pragma unroll 1
         for (int x = 0; x < kHalfCols; x += 32) {
           uint32_t r[32];
           tmem_ld32_issue(to + (uint32_t)x, r);
@@ -376,7 +421,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   } else {
     // ---------------------------------------------------------------- B: the state, a row per lane
     const int wq = warp & 3, half = (warp >> 2) & 1, r0 = wq * 32 + lane;
-    const bool mine = wq * 32 < D;  // d = 64: the upper two lane quarters hold no rows
+    const bool mine = wq * 32 < D;
     const uint32_t tl = tmem + ((uint32_t)(wq * 32) << 16);
     float *S = p.state + ((size_t)u * D + r0) * D + half * kHalfCols;
     float *part = p.parts + ((size_t)u * p.segments * D + r0) * D + half * kHalfCols;
@@ -405,98 +450,49 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         }
       }
     }
-    const Decay2 g_chunk(decay_pow(logd, kLtChunk));
-    auto add_ds = [&](int c, const Decay2 &g) {  // the state behind chunk c
-      mbar_wait(ds_full, c & 1, abort_flag, p.status);
-      tc_fence_after();
-      if (mine) {
-#pragma unroll
-        for (int x = 0; x < kHalfCols; x += 16) {
-          uint32_t r[16];
-          tmem_ld16(tl + kLtColDS + (uint32_t)(half * kHalfCols + x), r);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[x + e] = g.madd(s[x + e], __uint_as_float(r[e]));
-        }
-      }
-    };
-    // ldmatrix: lanes 8 m .. 8 m + 7 point to eight tokens' 16 bytes of 8 components; blocks 0 and 1 are 16 components of
-    // the first eight tokens, 2 and 3 of the next eight
-    const int lm_tok = ((lane >> 4) & 1) * 8 + (lane & 7), lm_ch = (lane >> 3) & 1;
-    for (int c = 0; c < n; ++c) {
-      const int sl = c & 1;
-      const int nt = c == n - 1 ? tail : kLtChunk;
-      mbar_wait(&k_full[sl], (c >> 1) & 1, abort_flag, p.status);
-      const char *ktile = kt + sl * kTile + (wq >> 1) * kBlock;
+    const Decay2 g_chunk(decay_pow(logd, kLtChunk)), g_tail(decay_pow(logd, tail));
+    for (int c = 0; c <= n; ++c) {
+      if (c < n) {
+        mbar_wait_compact(&k_full[c & 1], (c >> 1) & 1, abort_flag, p.status);
 #pragma unroll 1
-      for (int q = 0; q < 4; ++q) {
-        const int bf = q & 1;
-        if (q == 2) {
-          if (c > 0) {
-            add_ds(c - 1, g_chunk);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ds_free);
-          }
-          if (!kStates) {
-            if (c > 0) mbar_wait(o1_full, (c - 1) & 1, abort_flag, p.status);  // the operand of the chunk before is used up
-            if (mine) {
-              // row r0 of the operand: 64 columns to a block of D rows of 128 bytes
-              char *row = sop + r0 * 128;
-#pragma unroll
-              for (int x = 0; x < kHalfCols; x += 8) {
-                const int col = half * kHalfCols + x, ch = (col & 63) >> 3;
-                *reinterpret_cast<uint4 *>(row + (col >> 6) * (D * 128) + ((ch ^ (r0 & 7)) << 4)) =
-                    make_uint4(lt_pack(s[x], s[x + 1]), lt_pack(s[x + 2], s[x + 3]), lt_pack(s[x + 4], s[x + 5]),
-                               lt_pack(s[x + 6], s[x + 7]));
-              }
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(sop_ready);
-          }
-        }
-        if (c > 0 || q >= 2) mbar_wait(&kp_free[bf], (2 * c + (q >> 1) - 1) & 1, abort_flag, p.status);
+        for (int q = 0; q < 2; ++q) split_keys(c, q);
+      }
+      if (c > 0) {  // the state behind the chunk before
+        mbar_wait_compact(ds_full, (c - 1) & 1, abort_flag, p.status);
+        tc_fence_after();
         if (mine) {
-          // 16 tokens (this warp's half of the piece) of 32 components, times what is left of each token at the end of
-          // the chunk, as the sum of three bf16; a register holds two neighbouring tokens
-          const int t0 = q * kLtPiece + half * 16, tok = t0 + 2 * (lane & 3);
-          float w[4];
+          const float hi = c == n ? g_tail.hi : g_chunk.hi, lo = c == n ? g_tail.lo : g_chunk.lo;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) w[x] = ktab[min(tok + (x >> 1) * 8 + (x & 1) + kLtChunk - nt, kLtChunk - 1)];
+          for (int x = 0; x < kHalfCols; x += 16) {
+            uint32_t r[16];
+            tmem_ld16(tl + kLtColDS + (uint32_t)(half * kHalfCols + x), r);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int tr = t0 + lm_tok, ch = (wq & 1) * 4 + 2 * h + lm_ch;
-            uint32_t r[4], k1[4], k2[4], k3[4];
-            lt_ldsm_t(smem_u32(ktile + tr * 128 + ((ch ^ (tr & 7)) << 4)), r);
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-              const int x = m & 2;
-              if (nt < kLtChunk) {  // tokens behind the last may hold anything
-                if (tok + 4 * x >= nt) r[m] &= 0xffff0000u;
-                if (tok + 4 * x + 1 >= nt) r[m] &= 0x0000ffffu;
-              }
-              float a = __uint_as_float(r[m] << 16) * w[x], b = __uint_as_float(r[m] & 0xffff0000u) * w[x + 1];
-              k1[m] = lt_pack(a, b);
-              a -= __uint_as_float(k1[m] << 16);
-              b -= __uint_as_float(k1[m] & 0xffff0000u);
-              k2[m] = lt_pack(a, b);
-              a -= __uint_as_float(k2[m] << 16);
-              b -= __uint_as_float(k2[m] & 0xffff0000u);
-              k3[m] = lt_pack(a, b);
-            }
-            const uint32_t to = tl + ((uint32_t)(16 * h) << 16) + kLtColK + (uint32_t)(bf * kLtPieceCols + half * 8);
-            lt_st_16x8(to, k1);
-            lt_st_16x8(to + kLtPiece / 2, k2);
-            lt_st_16x8(to + kLtPiece, k3);
+            for (int e = 0; e < 16; ++e) s[x + e] = fmaf(hi, s[x + e], fmaf(lo, s[x + e], __uint_as_float(r[e])));
           }
-          tmem_st_wait();
         }
+        if (c == n) break;
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&kp_ready[bf]);
+        if (lane == 0) mbar_arrive(ds_free);
+      }
+      if (!kStates) {
+        if (c > 0) mbar_wait_compact(o1_full, (c - 1) & 1, abort_flag, p.status);  // the operand of the chunk before is used up
+        if (mine) {
+          // row r0 of the operand: 64 columns to a block of D rows of 128 bytes
+          char *row = sop + r0 * 128;
+#pragma unroll
+          for (int x = 0; x < kHalfCols; x += 8) {
+            const int col = half * kHalfCols + x, ch = (col & 63) >> 3;
+            *reinterpret_cast<uint4 *>(row + (col >> 6) * (D * 128) + ((ch ^ (r0 & 7)) << 4)) =
+                make_uint4(lt_pack(s[x], s[x + 1]), lt_pack(s[x + 2], s[x + 3]), lt_pack(s[x + 4], s[x + 5]),
+                           lt_pack(s[x + 6], s[x + 7]));
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sop_ready);
       }
     }
-    if (n > 0) add_ds(n - 1, Decay2(decay_pow(logd, tail)));
     if (mine && (kStates || seg == p.segments - 1)) {
       float *dst = kStates ? part + (size_t)(seg + 1) * D * D : S;
 #pragma unroll
