@@ -106,17 +106,18 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   float *ctab = ktab + 128;                     // ctab[e] = g^(31 - e)
   at += LtSmem<D>::kTables * 4;
   uint64_t *bars = reinterpret_cast<uint64_t *>(at); at += LtSmem<D>::kBars * 8;
-  uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6, *q_full = bars + 8;
-  uint64_t *s1_full = bars + 12, *p_ready = bars + 13, *o1_full = bars + 14, *o_scaled = bars + 15, *o_full = bars + 16;
+  uint64_t *full = bars, *kv_empty = bars + 2, *q_full = bars + 4;  // per slot: keys and values landed, used up; queries
+  uint64_t *s1_full = bars + 12, *o1_full = bars + 14, *o_scaled = bars + 15, *o_full = bars + 16;
   uint64_t *o_free = bars + 17, *sop_ready = bars + 18, *ds_full = bars + 19, *ds_free = bars + 20, *staged = bars + 21;
   uint64_t *kp_ready = bars + 22, *kp_free = bars + 24;
   uint32_t *tmem_base = reinterpret_cast<uint32_t *>(at);
   int *abort_ptr = reinterpret_cast<int *>(at + 8);
   volatile int *abort_flag = abort_ptr;
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // uniform for the compiler too, and so is what follows
   const int segs = kStates ? p.segments - 1 : p.segments, seg = blockIdx.x % segs, u = blockIdx.x / segs;
-  const int len = linear_len(p, u / p.G, tid == 0 && seg == 0 && (kStates || p.segments == 1));
+  const int len = __shfl_sync(0xffffffffu, linear_len(p, u / p.G, tid == 0 && seg == 0 && (kStates || p.segments == 1)), 0);
   if (len == 0) return;
   const int n_chunks = (len + kLtChunk - 1) / kLtChunk;
   const int first = linear_segment(n_chunks, p.segments, seg), last = linear_segment(n_chunks, p.segments, seg + 1);
@@ -126,11 +127,9 @@ __global__ void __launch_bounds__(kLtThreads, 1)
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1);
-      mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1);
-      mbar_init(&q_full[i], 1);
+      mbar_init(&full[i], 2); mbar_init(&kv_empty[i], 1); mbar_init(&q_full[i], 1);
     }
-    mbar_init(s1_full, 1); mbar_init(p_ready, kLtAWarps); mbar_init(o1_full, 1); mbar_init(o_scaled, kLtAWarps);
+    mbar_init(s1_full, 1); mbar_init(o1_full, 1); mbar_init(o_scaled, kLtAWarps);
     mbar_init(o_full, 1); mbar_init(o_free, kLtAWarps); mbar_init(sop_ready, kLtBWarps); mbar_init(ds_full, 1);
     mbar_init(ds_free, kLtBWarps); mbar_init(staged, kLtAWarps);
     for (int i = 0; i < 2; ++i) mbar_init(&kp_ready[i], kLtBWarps);
@@ -182,14 +181,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             if (tok + 4 * x >= nt) r[h][m] &= 0xffff0000u;
             if (tok + 4 * x + 1 >= nt) r[h][m] &= 0x0000ffffu;
           }
+          // cut, not rounded: the upper halves of an fp32, of what they leave, and of what those leave are all its 24 bits
           float a = __uint_as_float(r[h][m] << 16) * w[x], b = __uint_as_float(r[h][m] & 0xffff0000u) * w[x + 1];
-          k1[m] = lt_pack(a, b);
-          a -= __uint_as_float(k1[m] << 16);
-          b -= __uint_as_float(k1[m] & 0xffff0000u);
-          k2[m] = lt_pack(a, b);
-          a -= __uint_as_float(k2[m] << 16);
-          b -= __uint_as_float(k2[m] & 0xffff0000u);
-          k3[m] = lt_pack(a, b);
+          k1[m] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+          a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+          b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+          k2[m] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+          a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+          b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+          k3[m] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
         }
         const uint32_t to = tmem + ((uint32_t)(wq * 32 + 16 * h) << 16) + kLtColK + (uint32_t)(bf * kLtPieceCols + half * 8);
         lt_st_16x8(to, k1);
@@ -207,16 +207,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     if (lane == 0) {
       for (int c = 0; c < n + 2; ++c) {
         const int sl = c & 1, row = (first + c) * kLtChunk;
-        auto load = [&](char *tiles, const CUtensorMap *map, uint64_t *full) {
-          mbar_expect_tx(&full[sl], kTile);
+        auto load = [&](char *tiles, const CUtensorMap *map, uint64_t *bar) {
+          mbar_expect_tx(bar, kTile);
 #pragma unroll
-          for (int h = 0; h < D / 64; ++h) tma_load_3d(tiles + sl * kTile + h * kBlock, map, 64 * h, row, u, &full[sl]);
+          for (int h = 0; h < D / 64; ++h) tma_load_3d(tiles + sl * kTile + h * kBlock, map, 64 * h, row, u, bar);
         };
         if (c < n) {
-          if (c >= 2) mbar_wait_compact(&k_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
-          load(kt, &mapK, k_full);
-          if (c >= 2) mbar_wait_compact(&v_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
-          load(vt, &mapV, v_full);
+          if (c >= 2) mbar_wait_compact(&kv_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
+          load(kt, &mapK, &full[sl]);
+          load(vt, &mapV, &full[sl]);
         }
         if (!kStates) {
           // the output of the chunk before the last leaves its slot, which then takes the queries of this one (a partial
@@ -228,75 +227,71 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
           }
-          if (c < n) load(qt, &mapQ, q_full);
+          if (c < n) load(qt, &mapQ, &q_full[sl]);
         }
       }
       if (!kStates) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
   } else if (warp == kLtMmaWarp) {
-    // (the accumulators sit at fixed columns: the allocation is all of tensor memory)
-    for (int c = 0; c < n; ++c) {
-      const int sl = c & 1;
-      const uint32_t full = (c >> 1) & 1, par = c & 1;
-      char *k = kt + sl * kTile, *v = vt + sl * kTile, *q = qt + sl * kTile;
-      mbar_wait_compact(&k_full[sl], full, abort_flag, p.status);
+    // (The accumulators sit at fixed columns: the allocation is all of tensor memory.  The pieces are kept as a loop: the
+    // roles' code together has to stay in the instruction cache.)
+    auto tile = [&](char *tiles, int c) { return tiles + (c & 1) * kTile; };
+    auto scores = [&](int c) {  // S1 (the product that read P from these columns was issued before it)
+      const char *k = tile(kt, c), *q = tile(qt, c);
+      mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
       if (c == n - 1 && tail < kLtChunk) {
         // rows behind the prompt may hold anything: their scores are multiplied by zero, and so are their values
-        mbar_wait_compact(&v_full[sl], full, abort_flag, p.status);
         for (int w = lane; w < (kLtChunk - tail) * 8; w += 32) {
 #pragma unroll
           for (int h = 0; h < D / 64; ++h) {
-            if (!kStates) *reinterpret_cast<uint4 *>(k + h * kBlock + tail * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
-            *reinterpret_cast<uint4 *>(v + h * kBlock + tail * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
+            if (!kStates) *reinterpret_cast<uint4 *>(tile(kt, c) + h * kBlock + tail * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4 *>(tile(vt, c) + h * kBlock + tail * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
         }
         fence_async_smem();
         __syncwarp();
       }
-      // DS, a piece of 32 tokens
-      auto piece = [&](auto number) {
-        constexpr int q4 = decltype(number)::value, bf = q4 & 1;
-        mbar_wait_compact(&kp_ready[bf], (2 * c + (q4 >> 1)) & 1, abort_flag, p.status);
-        tc_fence_after();
-#pragma unroll
-        for (int x = 0; x < 2 * kLtSplits; ++x)  // term x >> 1, tokens 16 (x & 1) .. of the piece
-          umma_bf16_ts_w(kLtColDS, kLtColK + (uint32_t)(bf * kLtPieceCols + (x >> 1) * (kLtPiece / 2) + 8 * (x & 1)),
-                         smem_desc_sw128_mn(v + (2 * q4 + (x & 1)) * 2048, kBlock), kIdescV, (q4 > 0 || x > 0) ? 1u : 0u);
-        umma_commit_w(&kp_free[q4]);
-        if (q4 == 3) {
-          umma_commit_w(ds_full);
-          umma_commit_w(&k_empty[sl]);
-          umma_commit_w(&v_empty[sl]);
-        }
-      };
       if (!kStates) {
-        mbar_wait_compact(&q_full[sl], full, abort_flag, p.status);
+        mbar_wait_compact(&q_full[c & 1], (c >> 1) & 1, abort_flag, p.status);
         tc_fence_after();
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {  // S1 (the product that read P from these columns was issued before it)
+        for (int kk = 0; kk < D / 16; ++kk) {
           const int off = (kk / 4) * kBlock + (kk % 4) * 32;
           umma_bf16_w(kLtColS, smem_desc_sw128(q + off), smem_desc_sw128(k + off), kIdescS, kk > 0 ? 1u : 0u);
         }
         umma_commit_w(s1_full);
       }
-      mbar_wait_compact(&v_full[sl], full, abort_flag, p.status);
+    };
+    if (n > 0) scores(0);
+    for (int c = 0; c < n; ++c) {
+      const uint32_t par = c & 1;
+      const char *v = tile(vt, c);
       if (c > 0) mbar_wait_compact(ds_free, (c - 1) & 1, abort_flag, p.status);
-      piece(std::integral_constant<int, 0>{});
-      piece(std::integral_constant<int, 1>{});
-      if (!kStates) {
-        mbar_wait_compact(sop_ready, par, abort_flag, p.status);
-        if (c > 0) mbar_wait_compact(o_free, (c - 1) & 1, abort_flag, p.status);
+#pragma unroll 1
+      for (int q4 = 0; q4 < 4; ++q4) {
+        if (!kStates && q4 == 2) {
+          mbar_wait_compact(sop_ready, par, abort_flag, p.status);
+          if (c > 0) mbar_wait_compact(o_free, (c - 1) & 1, abort_flag, p.status);
+          tc_fence_after();
+          const char *q = tile(qt, c);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)  // O = Q S
+            umma_bf16_w(kLtColO, smem_desc_sw128(q + (kk / 4) * kBlock + (kk % 4) * 32),
+                        smem_desc_sw128_mn(sop + kk * 2048, D * 128), kIdescV, kk > 0 ? 1u : 0u);
+          umma_commit_w(o1_full);
+        }
+        // DS, a piece of 32 tokens
+        mbar_wait_compact(&kp_ready[q4 & 1], (2 * c + (q4 >> 1)) & 1, abort_flag, p.status);
         tc_fence_after();
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)  // O = Q S
-          umma_bf16_w(kLtColO, smem_desc_sw128(q + (kk / 4) * kBlock + (kk % 4) * 32),
-                      smem_desc_sw128_mn(sop + kk * 2048, D * 128), kIdescV, kk > 0 ? 1u : 0u);
-        umma_commit_w(o1_full);
+        for (int x = 0; x < 2 * kLtSplits; ++x)  // term x >> 1, tokens 16 (x & 1) .. of the piece
+          umma_bf16_ts_w(kLtColDS, kLtColK + (uint32_t)((q4 & 1) * kLtPieceCols + 8 * x),
+                         smem_desc_sw128_mn(v + (2 * q4 + (x & 1)) * 2048, kBlock), kIdescV, (q4 > 0 || x > 0) ? 1u : 0u);
+        umma_commit_w(&kp_free[q4]);
       }
-      piece(std::integral_constant<int, 2>{});
+      umma_commit_w(ds_full);
       if (!kStates) {
-        mbar_wait_compact(p_ready, par, abort_flag, p.status);
-        mbar_wait_compact(o_scaled, par, abort_flag, p.status);
+        mbar_wait_compact(o_scaled, par, abort_flag, p.status);  // and P, which the same warps wrote before
         tc_fence_after();
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)  // O += P V
@@ -304,15 +299,16 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                          smem_desc_sw128_mn(v + kk * 2048, kBlock), kIdescV, 1u);
         umma_commit_w(o_full);
       }
-      piece(std::integral_constant<int, 3>{});
+      umma_commit_w(&kv_empty[c & 1]);
+      if (c + 1 < n) scores(c + 1);
     }
   } else if (warp < kLtAWarps) {
     // ---------------------------------------------------------------- A: scores and output, a token per lane
     if (kStates) {
       for (int c = 0; c < n; ++c) {
-        mbar_wait_compact(&k_full[c & 1], (c >> 1) & 1, abort_flag, p.status);
-        split_keys(c, 2);
-        split_keys(c, 3);
+        mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+#pragma unroll 1
+        for (int q = 2; q < 4; ++q) split_keys(c, q);
       }
     } else {
       const int wq = warp & 3, half = warp >> 2, i = wq * 32 + lane;
@@ -354,11 +350,9 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           tmem_st16(tl + kLtColS + (uint32_t)(half * 64 + cc * 16), pk);
         }
         tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready);
-        mbar_wait_compact(&k_full[c & 1], (c >> 1) & 1, abort_flag, p.status);
-        split_keys(c, 2);
+        mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+#pragma unroll 1
+        for (int q = 2; q < 4; ++q) split_keys(c, q);
         mbar_wait_compact(o1_full, par, abort_flag, p.status);
         tc_fence_after();
         const uint32_t to = tl + kLtColO + (uint32_t)(half * kHalfCols);
@@ -383,7 +377,6 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(o_scaled);
-        split_keys(c, 3);
         mbar_wait_compact(o_full, par, abort_flag, p.status);
         tc_fence_after();
         const bool partial = c == n - 1 && tail < kLtChunk;
@@ -453,7 +446,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     const Decay2 g_chunk(decay_pow(logd, kLtChunk)), g_tail(decay_pow(logd, tail));
     for (int c = 0; c <= n; ++c) {
       if (c < n) {
-        mbar_wait_compact(&k_full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+        mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
 #pragma unroll 1
         for (int q = 0; q < 2; ++q) split_keys(c, q);
       }
@@ -470,13 +463,12 @@ __global__ void __launch_bounds__(kLtThreads, 1)
             for (int e = 0; e < 16; ++e) s[x + e] = fmaf(hi, s[x + e], fmaf(lo, s[x + e], __uint_as_float(r[e])));
           }
         }
-        if (c == n) break;
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(ds_free);
+        if (lane == 0 && c < n) mbar_arrive(ds_free);
       }
-      if (!kStates) {
-        if (c > 0) mbar_wait_compact(o1_full, (c - 1) & 1, abort_flag, p.status);  // the operand of the chunk before is used up
+      if (!kStates && c < n) {
+        if (c > 0) mbar_wait_compact(o1_full, (c - 1) & 1, abort_flag, p.status);  // the operand before is used up
         if (mine) {
           // row r0 of the operand: 64 columns to a block of D rows of 128 bytes
           char *row = sop + r0 * 128;
