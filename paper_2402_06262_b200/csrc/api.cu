@@ -136,11 +136,12 @@ TreePlan tree_plan(const roco_cache *c, int T, int group, float scale) {
   TreePlan t;
   const int rows = T * group;
   const long long U = (long long)c->S * c->G;
-  t.tc = false;
-  (void)scale;
-  const long long ctas = U * tree_simt_row_blocks(rows);
-  // CUDA cores: enough CTAs for four per SM, but no range shorter than two 64-key tiles
-  long long want = (4LL * device_sms() + ctas - 1) / ctas, most = (c->B + 127) / 128;
+  t.tc = c->kv_dtype == ROCO_BF16 && scale > 0.f;
+  const int row_blocks = t.tc ? (rows + tree_tc_width(rows) - 1) / tree_tc_width(rows) : tree_simt_row_blocks(rows);
+  // Tensor cores: one wave of two CTAs per SM, no range shorter than two 128-key tiles.  CUDA cores: four CTAs per SM, no
+  // range shorter than two 64-key tiles.
+  const long long ctas = U * row_blocks, slots = (t.tc ? 2LL : 4LL) * device_sms();
+  long long want = t.tc ? slots / ctas : (slots + ctas - 1) / ctas, most = (c->B + (t.tc ? 255 : 127)) / (t.tc ? 256 : 128);
   if (want > most) want = most;
   if (want > 32) want = 32;
   t.splits = want < 1 ? 1 : (int)want;
@@ -705,6 +706,7 @@ roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void 
   p.part_ml = static_cast<float *>(workspace);
   p.part_o = plan.splits > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.ml_bytes) : nullptr;
   p.B = cache->B; p.T = T; p.group = group; p.G = cache->G; p.rows = T * group; p.splits = plan.splits; p.scale = scale;
+  if (plan.tc) return launch_tree_attend_tc(p, cache->d, U, static_cast<cudaStream_t>(stream));
   return launch_tree_attend_simt(p, cache->kv_dtype, cache->d, U, static_cast<cudaStream_t>(stream));
 }
 
