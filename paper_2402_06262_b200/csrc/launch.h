@@ -102,6 +102,7 @@ int tree_tc_width(int rows);
 roco_status launch_tree_attend_tc(const TreeParams &p, int d, int U, cudaStream_t stream);
 roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
 // Statistics of the accepted queries, then evictions and insertion (two launches).
+roco_status launch_commit_stats_tc(const CommitParams &p, int d, int U, int sms, cudaStream_t stream);  // bf16
 roco_status launch_tree_commit(const CommitParams &p, int kv_dtype, int d, int U, int sms, cudaStream_t stream);
 
 // ---- linear attention with a decay for each head (linear.cuh)

@@ -315,7 +315,7 @@ roco_status commit_stats_t(const CommitParams &p, int U, int sms, cudaStream_t s
 roco_status launch_tree_commit(const CommitParams &p, int kv_dtype, int d, int U, int sms, cudaStream_t stream) {
   roco_status st;
   if (kv_dtype == ROCO_BF16)
-    st = d == 128 ? commit_stats_t<__nv_bfloat16, 128>(p, U, sms, stream) : commit_stats_t<__nv_bfloat16, 64>(p, U, sms, stream);
+    st = launch_commit_stats_tc(p, d, U, sms, stream);
   else
     st = d == 128 ? commit_stats_t<float, 128>(p, U, sms, stream) : commit_stats_t<float, 64>(p, U, sms, stream);
   if (st != ROCO_OK) return st;
