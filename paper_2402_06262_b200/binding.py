@@ -192,11 +192,18 @@ def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _need(what: str, name: str, t, shape, dtype):
+def _device() -> int:
+    """The current CUDA device; -2, which no tensor has, without a GPU."""
+    if not torch.cuda.is_initialized() and not torch.cuda.is_available():
+        return -2
+    return torch.cuda.current_device()
+
+
+def _need(what: str, name: str, t, shape, dtype, dev: int):
     """The argument checks that the C entry points cannot make: a tensor of this shape and type, contiguous, on the
     current device."""
-    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or not t.is_contiguous()
-            or not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+    if (not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != dev
+            or not t.is_contiguous()):
         raise RocoError(1, f"{what}: {name}: a contiguous {dtype} tensor of shape {list(shape)} on the current CUDA device is "
                            f"needed, got " + (f"{t.dtype} {list(t.shape)} on {t.device}" if isinstance(t, torch.Tensor)
                                               else type(t).__name__))
@@ -213,6 +220,11 @@ def _workspace(what: str, t, nbytes: int, like: torch.Tensor):
 
 def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _raw_stream(dev: int) -> int:
+    """_stream() without the Python objects around it."""
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 class Cache:
@@ -243,12 +255,13 @@ class Cache:
         c = cls.__new__(cls)
         c.S, c.G, c.B, c.d = K.shape
         c.dtype = K.dtype
+        dev = _device()
         for name, t, shape, dtype in (("K", K, (c.S, c.G, c.B, c.d), K.dtype), ("V", V, (c.S, c.G, c.B, c.d), K.dtype),
                                       ("s", s, (c.S, c.G, c.B), torch.float32), ("q", q, (c.S, c.G, c.B), torch.float32),
                                       ("n", n, (c.S, c.G, c.B), torch.int32), ("pos", pos, (c.S, c.G, c.B), torch.int32),
                                       ("live", live, (c.S, c.G), torch.int32), ("t_next", t_next, (c.S, c.G), torch.int32),
                                       ("status", status, (1,), torch.int32)):
-            _need("Cache.wrap", name, t, shape, dtype)
+            _need("Cache.wrap", name, t, shape, dtype, dev)
             setattr(c, name, t)
         c.c = roco_cache(ROCO_F32 if c.dtype == torch.float32 else ROCO_BF16, c.S, c.G, c.d, c.B,
                          *(getattr(c, f).data_ptr() for f in ("K", "V", "s", "q", "n", "pos", "live", "t_next", "status")))
@@ -281,9 +294,10 @@ class LinearState:
         if not isinstance(state, torch.Tensor) or state.dim() != 4:
             raise RocoError(1, "LinearState: the state is a tensor [S][G][d][d]")
         self.S, self.G, self.d, _ = state.shape
-        _need("LinearState", "state", state, (self.S, self.G, self.d, self.d), torch.float32)
-        _need("LinearState", "log_decay", log_decay, (self.G,), torch.float32)
-        _need("LinearState", "status", status, (1,), torch.int32)
+        dev = _device()
+        _need("LinearState", "state", state, (self.S, self.G, self.d, self.d), torch.float32, dev)
+        _need("LinearState", "log_decay", log_decay, (self.G,), torch.float32, dev)
+        _need("LinearState", "status", status, (1,), torch.int32, dev)
         self.state, self.log_decay, self.status, self.dtype = state, log_decay, status, dtype
         self.c = roco_linear_state(ROCO_F32 if dtype == torch.float32 else ROCO_BF16, self.S, self.G, self.d,
                                    state.data_ptr(), log_decay.data_ptr(), status.data_ptr())
@@ -566,13 +580,15 @@ def roco_tree_attend_workspace_bytes(cache: Cache, T: int, group: int = 1) -> in
     return int(lib().roco_tree_attend_workspace_bytes(C.byref(cache.c), T, group))
 
 
-def _check_tree(what: str, cache: Cache, Q, K_new, V_new):
+def _check_tree(what: str, cache: Cache, Q, K_new, V_new, dev: int):
     if not isinstance(Q, torch.Tensor) or Q.dim() != 5:
         raise RocoError(1, f"{what}: Q is [S][G][T][group][d]")
     S, G, d, T = cache.S, cache.G, cache.d, Q.shape[2]
-    _need(what, "Q", Q, (S, G, T, Q.shape[3], d), cache.dtype)
-    _need(what, "K_new", K_new, (S, G, T, d), cache.dtype)
-    _need(what, "V_new", V_new, (S, G, T, d), cache.dtype)
+    if cache.K.get_device() != dev:
+        raise RocoError(1, f"{what}: the cache is not on the current CUDA device")
+    _need(what, "Q", Q, (S, G, T, Q.shape[3], d), cache.dtype, dev)
+    _need(what, "K_new", K_new, (S, G, T, d), cache.dtype, dev)
+    _need(what, "V_new", V_new, (S, G, T, d), cache.dtype, dev)
     return T, int(Q.shape[3])
 
 
@@ -581,19 +597,19 @@ def roco_tree_attend(cache: Cache, Q, K_new, V_new, parent, attn_out, nodes=None
     """Every node of a tree of drafted tokens attends over the cached tokens, its ancestors and itself; the cache stays
     as it is.  Q, attn_out [S][G][T][group][d], K_new, V_new [S][G][T][d], parent [S][T] int32 (-1: the cached prefix),
     nodes [S] int32 (None: T), lse_out [S][G][T][group] fp32."""
-    what = "roco_tree_attend"
-    T, group = _check_tree(what, cache, Q, K_new, V_new)
-    _need(what, "parent", parent, (cache.S, T), torch.int32)
-    _need(what, "attn_out", attn_out, tuple(Q.shape), cache.dtype)
+    what, dev = "roco_tree_attend", _device()
+    T, group = _check_tree(what, cache, Q, K_new, V_new, dev)
+    _need(what, "parent", parent, (cache.S, T), torch.int32, dev)
+    _need(what, "attn_out", attn_out, Q.shape, cache.dtype, dev)
     if nodes is not None:
-        _need(what, "nodes", nodes, (cache.S,), torch.int32)
+        _need(what, "nodes", nodes, (cache.S,), torch.int32, dev)
     if lse_out is not None:
-        _need(what, "lse_out", lse_out, tuple(Q.shape[:4]), torch.float32)
+        _need(what, "lse_out", lse_out, Q.shape[:4], torch.float32, dev)
     scale = cache.d ** -0.5 if scale is None else scale
     ws = _workspace(what, workspace, roco_tree_attend_workspace_bytes(cache, T, group) if workspace is None else 0, Q)
     rc = lib().roco_tree_attend(C.byref(cache.c), _at(Q), _at(K_new), _at(V_new), _at(parent), _at(nodes), T, group, scale,
                                 _at(attn_out), _at(lse_out), _at(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                _stream())
+                                _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
 
@@ -603,22 +619,22 @@ def roco_tree_commit(cache: Cache, Q, K_new, V_new, lse, parent, path, path_len,
     """The accepted path of a draft tree enters the cache: statistics of its queries, evictions to the budget, insertion.
     Q, K_new, V_new, parent as given to roco_tree_attend, lse what it returned; path [S][A] int32 node indices from the
     root on, path_len [S] int32; evicted_slot, evicted_pos [S][G][A] int32."""
-    what = "roco_tree_commit"
-    T, group = _check_tree(what, cache, Q, K_new, V_new)
+    what, dev = "roco_tree_commit", _device()
+    T, group = _check_tree(what, cache, Q, K_new, V_new, dev)
     if not isinstance(path, torch.Tensor) or path.dim() != 2:
         raise RocoError(1, f"{what}: path is [S][A]")
     S, G, A = cache.S, cache.G, path.shape[1]
-    _need(what, "lse", lse, tuple(Q.shape[:4]), torch.float32)
-    _need(what, "parent", parent, (S, T), torch.int32)
-    _need(what, "path", path, (S, A), torch.int32)
-    _need(what, "path_len", path_len, (S,), torch.int32)
-    _need(what, "evicted_slot", evicted_slot, (S, G, A), torch.int32)
+    _need(what, "lse", lse, Q.shape[:4], torch.float32, dev)
+    _need(what, "parent", parent, (S, T), torch.int32, dev)
+    _need(what, "path", path, (S, A), torch.int32, dev)
+    _need(what, "path_len", path_len, (S,), torch.int32, dev)
+    _need(what, "evicted_slot", evicted_slot, (S, G, A), torch.int32, dev)
     if evicted_pos is not None:
-        _need(what, "evicted_pos", evicted_pos, (S, G, A), torch.int32)
+        _need(what, "evicted_pos", evicted_pos, (S, G, A), torch.int32, dev)
     scale = cache.d ** -0.5 if scale is None else scale
     rc = lib().roco_tree_commit(C.byref(cache.c), _at(Q), _at(K_new), _at(V_new), _at(lse), _at(parent), _at(path),
                                 _at(path_len), T, group, A, r, scope_mode, scale, _at(evicted_slot), _at(evicted_pos),
-                                _stream())
+                                _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
 
@@ -631,18 +647,20 @@ def roco_linear_prefill(state: LinearState, Q, K, V, lens, out, scale: Optional[
                         workspace: Optional[torch.Tensor] = None):
     """Linear attention with decay over a prompt (or its next piece); the state is continued in place.  Q, K, V, out:
     [S][G][Lmax][d]; lens: [S] int32 device tensor."""
-    what = "roco_linear_prefill"
+    what, dev = "roco_linear_prefill", _device()
     if not isinstance(Q, torch.Tensor) or Q.dim() != 4:
         raise RocoError(1, f"{what}: Q is [S][G][Lmax][d]")
     Lmax = Q.shape[2]
     shape = (state.S, state.G, Lmax, state.d)
+    if state.state.get_device() != dev:
+        raise RocoError(1, f"{what}: the state is not on the current CUDA device")
     for name, t in (("Q", Q), ("K", K), ("V", V), ("out", out)):
-        _need(what, name, t, shape, state.dtype)
-    _need(what, "lens", lens, (state.S,), torch.int32)
+        _need(what, name, t, shape, state.dtype, dev)
+    _need(what, "lens", lens, (state.S,), torch.int32, dev)
     scale = state.d ** -0.5 if scale is None else scale
     ws = _workspace(what, workspace, roco_linear_prefill_workspace_bytes(state, Lmax) if workspace is None else 0, Q)
     rc = lib().roco_linear_prefill(C.byref(state.c), _at(Q), _at(K), _at(V), _at(lens), Lmax, scale, _at(out), _at(ws),
-                                   0 if ws is None else ws.numel() * ws.element_size(), _stream())
+                                   0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
 
@@ -650,14 +668,16 @@ def roco_linear_prefill(state: LinearState, Q, K, V, lens, out, scale: Optional[
 def roco_linear_step(state: LinearState, q, k, v, out, active=None, scale: Optional[float] = None):
     """One token of linear attention with decay for every sequence (with active [S] int32: those with a non-zero entry).
     q, k, v, out: [S][G][d]."""
-    what = "roco_linear_step"
+    what, dev = "roco_linear_step", _device()
     shape = (state.S, state.G, state.d)
+    if state.state.get_device() != dev:
+        raise RocoError(1, f"{what}: the state is not on the current CUDA device")
     for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
-        _need(what, name, t, shape, state.dtype)
+        _need(what, name, t, shape, state.dtype, dev)
     if active is not None:
-        _need(what, "active", active, (state.S,), torch.int32)
+        _need(what, "active", active, (state.S,), torch.int32, dev)
     scale = state.d ** -0.5 if scale is None else scale
-    rc = lib().roco_linear_step(C.byref(state.c), _at(q), _at(k), _at(v), _at(active), scale, _at(out), _stream())
+    rc = lib().roco_linear_step(C.byref(state.c), _at(q), _at(k), _at(v), _at(active), scale, _at(out), _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
 

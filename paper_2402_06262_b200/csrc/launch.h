@@ -8,6 +8,20 @@
 
 namespace roco {
 
+// Raises a kernel's limit of dynamic shared memory, once per device (a static object beside the launch; racing first
+// calls set the same value).
+struct SmemLimit {
+  bool done[64] = {};
+  bool operator()(const void *kernel, size_t bytes) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    if (dev >= 0 && dev < 64 && done[dev]) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+    if (dev >= 0 && dev < 64) done[dev] = true;
+    return true;
+  }
+};
+
 roco_status launch_decode_step(const roco_cache &c, const void *q, const void *k_new, const void *v_new, int r,
                                int scope_mode, int step_order, int policy, const unsigned *rnd, float scale, void *out,
                                float *lse, int32_t *ev_slot, int32_t *ev_pos, cudaStream_t stream);

@@ -273,9 +273,8 @@ roco_status linear_prefill_simt_t(const LinearParams &p, int U, cudaStream_t str
   const unsigned slabs = (unsigned)U * (unsigned)(D / kLpCols);
   auto states = linear_prefill_simt_kernel<T, D, true>;
   auto whole = linear_prefill_simt_kernel<T, D, false>;
-  if (cudaFuncSetAttribute(states, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
-      cudaFuncSetAttribute(whole, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess)
-    return ROCO_ERR_CUDA;
+  static SmemLimit limit_states, limit_whole;
+  if (!limit_states((const void *)states, kSmem) || !limit_whole((const void *)whole, kSmem)) return ROCO_ERR_CUDA;
   if (p.segments > 1) states<<<slabs * (unsigned)(p.segments - 1), kLpThreads, kSmem, stream>>>(p);
   whole<<<slabs * (unsigned)p.segments, kLpThreads, kSmem, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;

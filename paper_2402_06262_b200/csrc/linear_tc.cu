@@ -508,9 +508,8 @@ roco_status linear_prefill_tc_t(const LinearParams &p, int U, cudaStream_t strea
   auto states = linear_prefill_tc_kernel<D, true>;
   auto whole = linear_prefill_tc_kernel<D, false>;
   constexpr size_t kB1 = LtSmem<D>::bytes(true), kB0 = LtSmem<D>::bytes(false);
-  if (cudaFuncSetAttribute(states, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kB1) != cudaSuccess ||
-      cudaFuncSetAttribute(whole, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kB0) != cudaSuccess)
-    return ROCO_ERR_CUDA;
+  static SmemLimit limit_states, limit_whole;
+  if (!limit_states((const void *)states, kB1) || !limit_whole((const void *)whole, kB0)) return ROCO_ERR_CUDA;
   if (p.segments > 1) states<<<(unsigned)U * (unsigned)(p.segments - 1), kLtThreads, kB1, stream>>>(mq, mk, mv, mo, p);
   whole<<<(unsigned)U * (unsigned)p.segments, kLtThreads, kB0, stream>>>(mq, mk, mv, mo, p);
   return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;

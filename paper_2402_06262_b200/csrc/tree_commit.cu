@@ -100,48 +100,126 @@ __global__ void __launch_bounds__(kCsThreads) commit_stats_simt_kernel(const Com
 
 // ---------------------------------------------------------------- evictions and insertion, one CTA per unit
 
-constexpr int kCiThreads = kMqPolicyThreads;  // the group that the selection routines synchronise
 constexpr int kCiMaxA = ROCO_TREE_MAX_PATH;
+constexpr int kCiShort = 64;  // candidates that are ranked one against the other
+
+struct CiScratch {
+  SelectScratch sel;
+  int ctl[64];  // 20: counter; 24 .. 39: the chosen slots (the places that lowest_r_block_victims uses)
+  int cand[kCiShort];
+  uint32_t group_min[16], threshold;
+};
 
 // The kn (<= 16) slots first in (key, position) order over keys that are bit patterns of non-negative floats below
-// infinity; their number goes to *cnt, the slots (unordered) to list.
-__device__ __forceinline__ void lowest_slots(const uint32_t *key, const int *pos, int live, int kn, int *list, int *cnt,
-                                             SelectScratch &sc, int tid) {
+// infinity, in that order to sc.ctl[24 ..]; false if there are fewer.  The threads form 16 groups: at least kn keys lie
+// at or below the kn-th smallest of the groups' minima, and few more, so those are gathered and ranked one against the
+// other.  Only where many keys are equal do they not fit; then a radix select finds the threshold and the lowest
+// positions at it.  Every thread of the CTA calls it.
+template <int NT>
+__device__ __forceinline__ bool lowest_slots(const uint32_t *key, const int *pos, int live, int kn, CiScratch &sc) {
+  const int tid = threadIdx.x;
+  int *list = sc.ctl + 24, *cnt = sc.ctl + 20;
+  constexpr uint32_t kInf = 0x7f800000u;
+  uint32_t low = 0xffffffffu;
+  for (int j = tid; j < live; j += NT) low = min(low, key[j]);
+#pragma unroll
+  for (int o = NT / 32; o > 0; o >>= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, o));  // NT / 16 neighbours
+  if (tid % (NT / 16) == 0) sc.group_min[tid / (NT / 16)] = low;
+  if (tid == 0) *cnt = 0;
+  __syncthreads();
+  if (tid < 16) {
+    int rank = 0;
+    const uint32_t mine = sc.group_min[tid];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) rank += sc.group_min[i] < mine || (sc.group_min[i] == mine && i < tid);
+    if (rank == kn - 1) sc.threshold = mine;
+  }
+  __syncthreads();
+  const uint32_t T = sc.threshold;
+  for (int j = tid; j < live; j += NT) {
+    const uint32_t k = key[j];
+    if (k <= T && k < kInf) {
+      const int at = atomicAdd(cnt, 1);
+      if (at < kCiShort) sc.cand[at] = j;
+    }
+  }
+  __syncthreads();
+  const int n = *cnt;
+  __syncthreads();
+  if (n <= kCiShort) {
+    if (tid < n) {
+      const int j = sc.cand[tid];
+      const uint32_t k = key[j];
+      const int ps = pos[j];
+      int rank = 0;
+      for (int i = 0; i < n; ++i) {
+        const int c = sc.cand[i];
+        const uint32_t kc = key[c];
+        rank += kc < k || (kc == k && pos[c] < ps);
+      }
+      if (rank < kn) list[rank] = j;
+    }
+    __syncthreads();
+    return n >= kn;
+  }
   uint32_t k_and = 0xffffffffu, k_or = 0u, rank, ties;
-  for (int j = tid; j < live; j += kCiThreads) { k_and &= key[j]; k_or |= key[j]; }
-  group_and_or(k_and, k_or, sc, tid, kCiThreads, kMqBarPolicy);
-  const uint32_t T = radix_select<uint32_t>([&](int j) { return key[j]; }, [&](int) { return true; }, live,
-                                            (uint32_t)(kn - 1), sc, tid, kCiThreads, kMqBarPolicy, &rank, &ties, k_and, k_or);
+  for (int j = tid; j < live; j += NT) { k_and &= key[j]; k_or |= key[j]; }
+  group_and_or(k_and, k_or, sc.sel, tid, NT, kMqBarPolicy);
+  const uint32_t R = radix_select<uint32_t>([&](int j) { return key[j]; }, [&](int) { return true; }, live, (uint32_t)(kn - 1),
+                                            sc.sel, tid, NT, kMqBarPolicy, &rank, &ties, k_and, k_or);
   int P = 0x7fffffff;
   if (ties != rank + 1) {  // only some of the slots tied at the threshold: lowest positions
     uint32_t r2, t2;
-    P = (int)radix_select<uint32_t>([&](int j) { return (uint32_t)pos[j]; }, [&](int j) { return key[j] == T; }, live, rank,
-                                    sc, tid, kCiThreads, kMqBarPolicy, &r2, &t2);
+    P = (int)radix_select<uint32_t>([&](int j) { return (uint32_t)pos[j]; }, [&](int j) { return key[j] == R; }, live, rank,
+                                    sc.sel, tid, NT, kMqBarPolicy, &r2, &t2);
   }
   if (tid == 0) *cnt = 0;
-  named_bar_sync(kMqBarPolicy, kCiThreads);
-  for (int j = tid; j < live; j += kCiThreads) {
+  __syncthreads();
+  for (int j = tid; j < live; j += NT) {
     const uint32_t k = key[j];
-    if (k < 0x7f800000u && (k < T || (k == T && (P == 0x7fffffff || pos[j] <= P)))) {
+    if (k < kInf && (k < R || (k == R && (P == 0x7fffffff || pos[j] <= P)))) {
       const int at = atomicAdd(cnt, 1);
       if (at < kCiMaxA) list[at] = j;
     }
   }
-  named_bar_sync(kMqBarPolicy, kCiThreads);
+  __syncthreads();
+  return *cnt == kn;
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitParams p) {
+// NT threads: the keys of a unit are formed, scanned for the lowest means and counted for the scope, each pass over shared
+// memory; what bounds it is the chain of these passes and of the first loads, so the loads of the statistics do not wait
+// for the check of the path.
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(NT) commit_insert_kernel(const CommitParams p) {
   extern __shared__ char ci_smem[];
-  __shared__ SelectScratch sel;
-  __shared__ int ctl[64], tgt[kCiMaxA], sh_node[32], sh_a;
+  __shared__ CiScratch sc;
+  __shared__ int tgt[kCiMaxA], sh_node[32], sh_a;
   __shared__ float pbar[kCiMaxA][kCiMaxA];  // [query][accepted token]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, u = blockIdx.x, b = u / p.G, A = p.A, B = p.B;
+  const size_t st = (size_t)u * B;
+  uint32_t *vkey = reinterpret_cast<uint32_t *>(ci_smem);
+  float *mkey = reinterpret_cast<float *>(vkey + B);
+  uint32_t *mbits = reinterpret_cast<uint32_t *>(mkey);
+  const int *opos = p.pos + st;
+  const int live = tree_live(p.live, u, B, p.status, false), t_new = p.t_next[u];
   if (warp == 0) {
     int node;
     const int a = commit_path(p, b, lane, node, false);
     sh_node[lane] = node;
     if (lane == 0) sh_a = a;
+  }
+  uint32_t k_and = 0xffffffffu, k_or = 0u;
+  if (live + A > B) {  // (some path could evict)
+#pragma unroll 4
+    for (int j = tid; j < live; j += NT) {
+      const float s = p.s[st + j], q = p.q[st + j];
+      const int n = p.n[st + j];
+      const uint32_t v = variance_key_fast(s, q, n);
+      vkey[j] = v;
+      mkey[j] = mean_fast(s, n);
+      k_and &= v;
+      k_or |= v;
+    }
   }
   __syncthreads();
   const int a = sh_a;
@@ -152,10 +230,8 @@ __global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitP
     }
     return;
   }
-  const int live = tree_live(p.live, u, B, p.status, false), t_new = p.t_next[u];
   const int need = live + a - B > 0 ? live + a - B : 0;
-  const size_t st = (size_t)u * B;
-  int *list = ctl + 24, *cnt = ctl + 20;
+  int *list = sc.ctl + 24;
 
   // the accepted queries against the accepted tokens, a warp per (query, token) at a time
   {
@@ -163,13 +239,14 @@ __global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitP
     const float zscale = p.scale * kLog2e;
     const T *Qu = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.T * p.group * D;
     const T *Ku = reinterpret_cast<const T *>(p.k_new) + (size_t)u * p.T * D;
-    for (int w = warp; w < a * (a + 1) / 2; w += kCiThreads / 32) {
+    for (int w = warp; w < a * (a + 1) / 2; w += NT / 32) {
       int i = 0;
       while ((i + 1) * (i + 2) / 2 <= w) ++i;
       const int m = w - i * (i + 1) / 2;  // m <= i
       float k[kN], sum = 0.f;
 #pragma unroll
       for (int c = 0; c < kN; ++c) k[c] = Elem<T>::load(Ku + (size_t)sh_node[m] * D + c * 32 + lane);
+#pragma unroll 4
       for (int g = 0; g < p.group; ++g) {
         const size_t row = (size_t)sh_node[i] * p.group + g;
         float x = 0.f;
@@ -183,34 +260,19 @@ __global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitP
   }
 
   if (need > 0) {
-    uint32_t *vkey = reinterpret_cast<uint32_t *>(ci_smem);
-    float *mkey = reinterpret_cast<float *>(vkey + B);
-    uint32_t *mbits = reinterpret_cast<uint32_t *>(mkey);
-    const int *opos = p.pos + st;
-    uint32_t k_and = 0xffffffffu, k_or = 0u;
-#pragma unroll 4
-    for (int j = tid; j < live; j += kCiThreads) {
-      const float s = p.s[st + j], q = p.q[st + j];
-      const int n = p.n[st + j];
-      const uint32_t v = variance_key_fast(s, q, n);
-      vkey[j] = v;
-      mkey[j] = mean_fast(s, n);
-      k_and &= v;
-      k_or |= v;
-    }
-    group_and_or(k_and, k_or, sel, tid, kCiThreads, kMqBarPolicy);  // publishes the keys too
     const int m = scope_size(live, p.r, p.scope_mode);
     bool ok = true;
     if (need > 1 && p.scope_mode == ROCO_SCOPE_LOWEST_R && m < live) {
-      lowest_r_block_victims(vkey, mkey, &sel, ctl, opos, p.status, p.r, live, need, m, k_and, k_or, tid);
+      group_and_or(k_and, k_or, sc.sel, tid, NT, kMqBarPolicy);
+      if (tid < kMqPolicyThreads)
+        lowest_r_block_victims(vkey, mkey, &sc.sel, sc.ctl, opos, p.status, p.r, live, need, m, k_and, k_or, tid);
     } else {
       // Frozen statistics: the m first in (variance, position) order stay the scope, and the `need` of them first in
       // (mean, position) order leave.  Those are looked for among all cached tokens first: they are all in scope if the
       // one of them last in (variance, position) order is, which one count decides; a scope that leaves out few tokens
       // nearly always contains them, and the search for its threshold is saved.
       bool done = m == live;
-      lowest_slots(mbits, opos, live, need, list, cnt, sel, tid);
-      ok = *cnt == need;
+      ok = lowest_slots<NT>(mbits, opos, live, need, sc);
       if (!done && ok) {
         uint32_t cv = 0u;
         int cp = -1;
@@ -220,33 +282,36 @@ __global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitP
           if (v > cv || (v == cv && ps > cp)) { cv = v; cp = ps; }
         }
         uint32_t before = 0;
-        for (int j = tid; j < live; j += kCiThreads) before += (vkey[j] < cv || (vkey[j] == cv && opos[j] < cp)) ? 1u : 0u;
+        for (int j = tid; j < live; j += NT) {
+          const uint32_t v = vkey[j];
+          before += (v < cv || (v == cv && opos[j] < cp)) ? 1u : 0u;
+        }
         before = __reduce_add_sync(0xffffffffu, before);
-        if (lane == 0) sel.hist[warp] = before;
-        named_bar_sync(kMqBarPolicy, kCiThreads);
+        if (lane == 0) sc.sel.hist[warp] = before;
+        __syncthreads();
         before = 0;
-        for (int w = 0; w < kCiThreads / 32; ++w) before += sel.hist[w];
+#pragma unroll
+        for (int w = 0; w < NT / 32; ++w) before += sc.sel.hist[w];
         done = before < (uint32_t)m;
-        named_bar_sync(kMqBarPolicy, kCiThreads);
+        __syncthreads();
       }
       if (!done) {
         uint32_t rank, ties;
+        group_and_or(k_and, k_or, sc.sel, tid, NT, kMqBarPolicy);
         const uint32_t Tv = radix_select<uint32_t>([&](int j) { return vkey[j]; }, [&](int) { return true; }, live,
-                                                   (uint32_t)(m - 1), sel, tid, kCiThreads, kMqBarPolicy, &rank, &ties,
-                                                   k_and, k_or);
+                                                   (uint32_t)(m - 1), sc.sel, tid, NT, kMqBarPolicy, &rank, &ties, k_and, k_or);
         int Pv = 0x7fffffff;
         if (ties != rank + 1) {
           uint32_t r2, t2;
           Pv = (int)radix_select<uint32_t>([&](int j) { return (uint32_t)opos[j]; }, [&](int j) { return vkey[j] == Tv; },
-                                           live, rank, sel, tid, kCiThreads, kMqBarPolicy, &r2, &t2);
+                                           live, rank, sc.sel, tid, NT, kMqBarPolicy, &r2, &t2);
         }
-        for (int j = tid; j < live; j += kCiThreads) {
+        for (int j = tid; j < live; j += NT) {
           const uint32_t v = vkey[j];
           if (!(v < Tv || (v == Tv && (Pv == 0x7fffffff || opos[j] <= Pv)))) mkey[j] = INFINITY;
         }
-        named_bar_sync(kMqBarPolicy, kCiThreads);
-        lowest_slots(mbits, opos, live, need, list, cnt, sel, tid);
-        ok = *cnt == need;
+        __syncthreads();
+        ok = lowest_slots<NT>(mbits, opos, live, need, sc);
       }
     }
     if (!ok && tid == 0) {  // only after corrupt statistics: distinct slots all the same
@@ -265,7 +330,7 @@ __global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitP
   if (tid < A) {
     const bool freed = tid < need;
     p.ev_slot[(size_t)u * A + tid] = freed ? tgt[tid] : -1;
-    if (p.ev_pos) p.ev_pos[(size_t)u * A + tid] = freed ? p.pos[st + tgt[tid]] : -1;
+    if (p.ev_pos) p.ev_pos[(size_t)u * A + tid] = freed ? opos[tgt[tid]] : -1;
   }
   if (tid < a) {  // the thread that reads a freed slot's position is the one that writes the new one
     const size_t at = st + tgt[tid];
@@ -284,7 +349,7 @@ __global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitP
     p.t_next[u] = t_new + a;
   }
   constexpr int kRow = D * (int)sizeof(T) / 16;
-  for (int w = tid; w < a * 2 * kRow; w += kCiThreads) {
+  for (int w = tid; w < a * 2 * kRow; w += NT) {
     const int i = w / (2 * kRow), c = w % (2 * kRow);
     const bool isv = c >= kRow;
     const int cc = isv ? c - kRow : c;
@@ -293,13 +358,18 @@ __global__ void __launch_bounds__(kCiThreads) commit_insert_kernel(const CommitP
   }
 }
 
+template <typename T, int D, int NT>
+roco_status commit_insert_nt(const CommitParams &p, int U, cudaStream_t stream) {
+  static SmemLimit limit;
+  auto kernel = commit_insert_kernel<T, D, NT>;
+  if (!limit((const void *)kernel, 8192 * 8)) return ROCO_ERR_CUDA;
+  kernel<<<U, NT, (size_t)p.B * 8, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+}
+
 template <typename T, int D>
 roco_status commit_insert_t(const CommitParams &p, int U, cudaStream_t stream) {
-  const size_t smem = (size_t)p.B * 8;
-  auto kernel = commit_insert_kernel<T, D>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return ROCO_ERR_CUDA;
-  kernel<<<U, kCiThreads, smem, stream>>>(p);
-  return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+  return p.B <= 2048 ? commit_insert_nt<T, D, 256>(p, U, stream) : commit_insert_nt<T, D, 512>(p, U, stream);
 }
 
 template <typename T, int D>

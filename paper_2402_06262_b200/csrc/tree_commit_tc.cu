@@ -170,7 +170,8 @@ roco_status commit_stats_tc_t(const CommitParams &p, int U, int sms, cudaStream_
   if (!make_tensor_map_units_bf16(&mk, p.K, U, p.B, D, kCtTile)) return ROCO_ERR_CUDA;
   auto kernel = commit_stats_tc_kernel<D, N>;
   constexpr size_t smem = CtShape<D, N>::kSmem;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return ROCO_ERR_CUDA;
+  static SmemLimit limit;
+  if (!limit((const void *)kernel, smem)) return ROCO_ERR_CUDA;
   // a unit's keys in one CTA (the queries are gathered once) unless that leaves SMs without work
   const int tiles = (p.B + kCtTile - 1) / kCtTile;
   const long long slots = (long long)CtShape<D, N>::kCtas * sms;

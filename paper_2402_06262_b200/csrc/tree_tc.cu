@@ -433,7 +433,8 @@ roco_status tree_tc_t(const TreeParams &p, int U, cudaStream_t stream) {
     return ROCO_ERR_CUDA;
   auto kernel = tree_tc_kernel<D, N>;
   constexpr size_t smem = TtShape<D, N>::kSmem;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return ROCO_ERR_CUDA;
+  static SmemLimit limit;
+  if (!limit((const void *)kernel, smem)) return ROCO_ERR_CUDA;
   kernel<<<(unsigned)U * (unsigned)((p.rows + N - 1) / N) * (unsigned)p.splits, kTtThreads, smem, stream>>>(mk, mv, mn, p);
   if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
   return p.splits > 1 ? launch_tree_join(p, ROCO_BF16, D, U, stream) : ROCO_OK;

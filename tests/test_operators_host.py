@@ -93,7 +93,7 @@ def test_binding_refuses_wrong_tensors():
     """Tensors of the wrong type, shape or place are refused before the library sees a pointer."""
     x = torch.zeros(1, 2, 3, 1, 128, dtype=torch.bfloat16)
     c = binding.Cache.__new__(binding.Cache)
-    c.S, c.G, c.B, c.d, c.dtype, c.c = 1, 2, 16, 128, torch.bfloat16, fake_cache()
+    c.S, c.G, c.B, c.d, c.dtype, c.c, c.K = 1, 2, 16, 128, torch.bfloat16, fake_cache(), torch.zeros(1)
     par = torch.full((1, 3), -1, dtype=torch.int32)
     for bad in (x, x.float(), x[:, :, :, :, ::2], x[0], None):       # (the first: right, but not on a GPU)
         with pytest.raises(R.RocoError) as e:
@@ -109,7 +109,7 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(R.RocoError):
         R.Cache.wrap(*([torch.zeros(1, 2, 16, 128)] * 9))
     s = binding.LinearState.__new__(binding.LinearState)
-    s.S, s.G, s.d, s.dtype, s.c = 1, 2, 128, torch.bfloat16, linear_state()
+    s.S, s.G, s.d, s.dtype, s.c, s.state = 1, 2, 128, torch.bfloat16, linear_state(), torch.zeros(1)
     y = torch.zeros(1, 2, 4, 128, dtype=torch.bfloat16)
     with pytest.raises(R.RocoError):
         R.roco_linear_prefill(s, y, y, y, torch.ones(1, dtype=torch.int32), y)
