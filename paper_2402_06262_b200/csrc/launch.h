@@ -105,6 +105,29 @@ roco_status launch_multi_step(const roco_cache &c, int M, int nb, const void *Q,
 roco_status launch_consistency_step(const roco_cache &full, const roco_cache &budgeted, int policy, int32_t *overlap,
                                     float *jaccard_sum, int32_t *samples, cudaStream_t stream);
 
+// Launches a kernel whose first part does not depend on the launch before it on the stream: it may start as soon as every
+// CTA of that launch has called launch_dependents (or ended), and waits for its results in wait_for_launch_before, which
+// every one of its CTAs calls.
+template <typename... Params, typename... Args>
+inline bool launch_overlapped(void (*kernel)(Params...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream,
+                              Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...) == cudaSuccess;
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+#endif
+
 // ---- attention of a tree of drafted tokens over the cache, commit of the accepted path (tree.cuh)
 struct TreeParams;
 struct CommitParams;

@@ -1,8 +1,7 @@
 // Commit of the accepted path of a draft tree: the statistics of Sec. 4.3 for the accepted queries over the cached
 // tokens (CUDA-core kernel; tensor-core kernel in tree_commit_tc.cu), then per unit the evictions on the updated
 // statistics and the insertion of the accepted tokens.
-#include "multi.cuh"
-#include "tree.cuh"
+#include "tree_insert.cuh"
 
 namespace roco {
 
@@ -23,6 +22,7 @@ __global__ void __launch_bounds__(kCsThreads) commit_stats_simt_kernel(const Com
   __shared__ __align__(16) float sq[kCsRows][4 * kPitch];
   __shared__ float slse[kCsRows];
   __shared__ int sh_a, sh_node[32];
+  launch_dependents();
   const int tid = threadIdx.x, u = blockIdx.x / key_blocks, kb = blockIdx.x % key_blocks, b = u / p.G;
   if (tid < 32) {
     int node;
@@ -100,129 +100,35 @@ __global__ void __launch_bounds__(kCsThreads) commit_stats_simt_kernel(const Com
 
 // ---------------------------------------------------------------- evictions and insertion, one CTA per unit
 
-constexpr int kCiMaxA = ROCO_TREE_MAX_PATH;
-constexpr int kCiShort = 64;  // candidates that are ranked one against the other
-
-struct CiScratch {
-  SelectScratch sel;
-  int ctl[64];  // 20: counter; 24 .. 39: the chosen slots (the places that lowest_r_block_victims uses)
-  int cand[kCiShort];
-  uint32_t group_min[16], threshold;
-};
-
-// The kn (<= 16) slots first in (key, position) order over keys that are bit patterns of non-negative floats below
-// infinity, in that order to sc.ctl[24 ..]; false if there are fewer.  The threads form 16 groups: at least kn keys lie
-// at or below the kn-th smallest of the groups' minima, and few more, so those are gathered and ranked one against the
-// other.  Only where many keys are equal do they not fit; then a radix select finds the threshold and the lowest
-// positions at it.  Every thread of the CTA calls it.
-template <int NT>
-__device__ __forceinline__ bool lowest_slots(const uint32_t *key, const int *pos, int live, int kn, CiScratch &sc) {
-  const int tid = threadIdx.x;
-  int *list = sc.ctl + 24, *cnt = sc.ctl + 20;
-  constexpr uint32_t kInf = 0x7f800000u;
-  uint32_t low = 0xffffffffu;
-  for (int j = tid; j < live; j += NT) low = min(low, key[j]);
-#pragma unroll
-  for (int o = NT / 32; o > 0; o >>= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, o));  // NT / 16 neighbours
-  if (tid % (NT / 16) == 0) sc.group_min[tid / (NT / 16)] = low;
-  if (tid == 0) *cnt = 0;
-  __syncthreads();
-  if (tid < 16) {
-    int rank = 0;
-    const uint32_t mine = sc.group_min[tid];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) rank += sc.group_min[i] < mine || (sc.group_min[i] == mine && i < tid);
-    if (rank == kn - 1) sc.threshold = mine;
-  }
-  __syncthreads();
-  const uint32_t T = sc.threshold;
-  for (int j = tid; j < live; j += NT) {
-    const uint32_t k = key[j];
-    if (k <= T && k < kInf) {
-      const int at = atomicAdd(cnt, 1);
-      if (at < kCiShort) sc.cand[at] = j;
-    }
-  }
-  __syncthreads();
-  const int n = *cnt;
-  __syncthreads();
-  if (n <= kCiShort) {
-    if (tid < n) {
-      const int j = sc.cand[tid];
-      const uint32_t k = key[j];
-      const int ps = pos[j];
-      int rank = 0;
-      for (int i = 0; i < n; ++i) {
-        const int c = sc.cand[i];
-        const uint32_t kc = key[c];
-        rank += kc < k || (kc == k && pos[c] < ps);
-      }
-      if (rank < kn) list[rank] = j;
-    }
-    __syncthreads();
-    return n >= kn;
-  }
-  uint32_t k_and = 0xffffffffu, k_or = 0u, rank, ties;
-  for (int j = tid; j < live; j += NT) { k_and &= key[j]; k_or |= key[j]; }
-  group_and_or(k_and, k_or, sc.sel, tid, NT, kMqBarPolicy);
-  const uint32_t R = radix_select<uint32_t>([&](int j) { return key[j]; }, [&](int) { return true; }, live, (uint32_t)(kn - 1),
-                                            sc.sel, tid, NT, kMqBarPolicy, &rank, &ties, k_and, k_or);
-  int P = 0x7fffffff;
-  if (ties != rank + 1) {  // only some of the slots tied at the threshold: lowest positions
-    uint32_t r2, t2;
-    P = (int)radix_select<uint32_t>([&](int j) { return (uint32_t)pos[j]; }, [&](int j) { return key[j] == R; }, live, rank,
-                                    sc.sel, tid, NT, kMqBarPolicy, &r2, &t2);
-  }
-  if (tid == 0) *cnt = 0;
-  __syncthreads();
-  for (int j = tid; j < live; j += NT) {
-    const uint32_t k = key[j];
-    if (k < kInf && (k < R || (k == R && (P == 0x7fffffff || pos[j] <= P)))) {
-      const int at = atomicAdd(cnt, 1);
-      if (at < kCiMaxA) list[at] = j;
-    }
-  }
-  __syncthreads();
-  return *cnt == kn;
-}
-
-// NT threads: the keys of a unit are formed, scanned for the lowest means and counted for the scope, each pass over shared
-// memory; what bounds it is the chain of these passes and of the first loads, so the loads of the statistics do not wait
-// for the check of the path.
+// What bounds a unit is its chain of dependent loads and of passes over shared memory.  The launch starts while the
+// statistics are still being formed, and what does not need them comes first: the path, the accepted rows, what the accepted
+// tokens start with.
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(NT) commit_insert_kernel(const CommitParams p) {
-  extern __shared__ char ci_smem[];
+  extern __shared__ __align__(16) char ci_smem[];  // keys and values of the accepted tokens [2][A][D], then the slots' keys
   __shared__ CiScratch sc;
-  __shared__ int tgt[kCiMaxA], sh_node[32], sh_a;
-  __shared__ float pbar[kCiMaxA][kCiMaxA];  // [query][accepted token]
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, u = blockIdx.x, b = u / p.G, A = p.A, B = p.B;
-  const size_t st = (size_t)u * B;
-  uint32_t *vkey = reinterpret_cast<uint32_t *>(ci_smem);
-  float *mkey = reinterpret_cast<float *>(vkey + B);
-  uint32_t *mbits = reinterpret_cast<uint32_t *>(mkey);
-  const int *opos = p.pos + st;
+  __shared__ int tgt[kCiMaxA], tgt_pos[kCiMaxA], sh_node[32], sh_a;
+  __shared__ float pbar[kCiMaxA][kCiMaxA];
+  constexpr int kRow = D * (int)sizeof(T) / 16;
+  const int tid = threadIdx.x, u = blockIdx.x, b = u / p.G, A = p.A, B = p.B;
   const int live = tree_live(p.live, u, B, p.status, false), t_new = p.t_next[u];
-  if (warp == 0) {
+  if (tid < 32) {
     int node;
-    const int a = commit_path(p, b, lane, node, false);
-    sh_node[lane] = node;
-    if (lane == 0) sh_a = a;
-  }
-  uint32_t k_and = 0xffffffffu, k_or = 0u;
-  if (live + A > B) {  // (some path could evict)
-#pragma unroll 4
-    for (int j = tid; j < live; j += NT) {
-      const float s = p.s[st + j], q = p.q[st + j];
-      const int n = p.n[st + j];
-      const uint32_t v = variance_key_fast(s, q, n);
-      vkey[j] = v;
-      mkey[j] = mean_fast(s, n);
-      k_and &= v;
-      k_or |= v;
-    }
+    const int a = commit_path(p, b, tid, node, false);
+    sh_node[tid] = node;
+    if (tid == 0) sh_a = a;
   }
   __syncthreads();
   const int a = sh_a;
+  uint4 *rows = reinterpret_cast<uint4 *>(ci_smem);
+  for (int w = tid; w < a * 2 * kRow; w += NT) {
+    const int isv = w >= a * kRow, x = w - isv * a * kRow;
+    rows[isv * A * kRow + x] =
+        reinterpret_cast<const uint4 *>(isv ? p.v_new : p.k_new)[((size_t)u * p.T + sh_node[x / kRow]) * kRow + x % kRow];
+  }
+  __syncthreads();
+  commit_new_probabilities<T, D>(p, u, a, sh_node, reinterpret_cast<const T *>(ci_smem), tid >> 5, NT / 32, tid & 31, pbar);
+  wait_for_launch_before();
   if (a == 0) {
     if (tid < A) {
       p.ev_slot[(size_t)u * A + tid] = -1;
@@ -231,108 +137,17 @@ __global__ void __launch_bounds__(NT) commit_insert_kernel(const CommitParams p)
     return;
   }
   const int need = live + a - B > 0 ? live + a - B : 0;
-  int *list = sc.ctl + 24;
-
-  // the accepted queries against the accepted tokens, a warp per (query, token) at a time
-  {
-    constexpr int kN = D / 32;
-    const float zscale = p.scale * kLog2e;
-    const T *Qu = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.T * p.group * D;
-    const T *Ku = reinterpret_cast<const T *>(p.k_new) + (size_t)u * p.T * D;
-    for (int w = warp; w < a * (a + 1) / 2; w += NT / 32) {
-      int i = 0;
-      while ((i + 1) * (i + 2) / 2 <= w) ++i;
-      const int m = w - i * (i + 1) / 2;  // m <= i
-      float k[kN], sum = 0.f;
-#pragma unroll
-      for (int c = 0; c < kN; ++c) k[c] = Elem<T>::load(Ku + (size_t)sh_node[m] * D + c * 32 + lane);
-#pragma unroll 4
-      for (int g = 0; g < p.group; ++g) {
-        const size_t row = (size_t)sh_node[i] * p.group + g;
-        float x = 0.f;
-#pragma unroll
-        for (int c = 0; c < kN; ++c) x = fmaf(Elem<T>::load(Qu + row * D + c * 32 + lane), k[c], x);
-        x = warp_sum(x);
-        sum += exp2f(fmaf(x, zscale, -p.lse[(size_t)u * p.T * p.group + row] * kLog2e));
-      }
-      if (lane == 0) pbar[i][m] = sum / (float)p.group;
-    }
-  }
-
-  if (need > 0) {
-    const int m = scope_size(live, p.r, p.scope_mode);
-    bool ok = true;
-    if (need > 1 && p.scope_mode == ROCO_SCOPE_LOWEST_R && m < live) {
-      group_and_or(k_and, k_or, sc.sel, tid, NT, kMqBarPolicy);
-      if (tid < kMqPolicyThreads)
-        lowest_r_block_victims(vkey, mkey, &sc.sel, sc.ctl, opos, p.status, p.r, live, need, m, k_and, k_or, tid);
-    } else {
-      // Frozen statistics: the m first in (variance, position) order stay the scope, and the `need` of them first in
-      // (mean, position) order leave.  Those are looked for among all cached tokens first: they are all in scope if the
-      // one of them last in (variance, position) order is, which one count decides; a scope that leaves out few tokens
-      // nearly always contains them, and the search for its threshold is saved.
-      bool done = m == live;
-      ok = lowest_slots<NT>(mbits, opos, live, need, sc);
-      if (!done && ok) {
-        uint32_t cv = 0u;
-        int cp = -1;
-        for (int e = 0; e < need; ++e) {
-          const uint32_t v = vkey[list[e]];
-          const int ps = opos[list[e]];
-          if (v > cv || (v == cv && ps > cp)) { cv = v; cp = ps; }
-        }
-        uint32_t before = 0;
-        for (int j = tid; j < live; j += NT) {
-          const uint32_t v = vkey[j];
-          before += (v < cv || (v == cv && opos[j] < cp)) ? 1u : 0u;
-        }
-        before = __reduce_add_sync(0xffffffffu, before);
-        if (lane == 0) sc.sel.hist[warp] = before;
-        __syncthreads();
-        before = 0;
-#pragma unroll
-        for (int w = 0; w < NT / 32; ++w) before += sc.sel.hist[w];
-        done = before < (uint32_t)m;
-        __syncthreads();
-      }
-      if (!done) {
-        uint32_t rank, ties;
-        group_and_or(k_and, k_or, sc.sel, tid, NT, kMqBarPolicy);
-        const uint32_t Tv = radix_select<uint32_t>([&](int j) { return vkey[j]; }, [&](int) { return true; }, live,
-                                                   (uint32_t)(m - 1), sc.sel, tid, NT, kMqBarPolicy, &rank, &ties, k_and, k_or);
-        int Pv = 0x7fffffff;
-        if (ties != rank + 1) {
-          uint32_t r2, t2;
-          Pv = (int)radix_select<uint32_t>([&](int j) { return (uint32_t)opos[j]; }, [&](int j) { return vkey[j] == Tv; },
-                                           live, rank, sc.sel, tid, NT, kMqBarPolicy, &r2, &t2);
-        }
-        for (int j = tid; j < live; j += NT) {
-          const uint32_t v = vkey[j];
-          if (!(v < Tv || (v == Tv && (Pv == 0x7fffffff || opos[j] <= Pv)))) mkey[j] = INFINITY;
-        }
-        __syncthreads();
-        ok = lowest_slots<NT>(mbits, opos, live, need, sc);
-      }
-    }
-    if (!ok && tid == 0) {  // only after corrupt statistics: distinct slots all the same
-      atomicOr(p.status, ROCO_DEV_BAD_VICTIM);
-      for (int e = 0; e < need; ++e) list[e] = e;
-    }
-    __syncthreads();
-    if (tid < need) {  // freed slots in increasing order
-      int at = 0;
-      for (int x = 0; x < need; ++x) at += list[x] < list[tid] || (list[x] == list[tid] && x < tid);
-      tgt[at] = list[tid];
-    }
-  }
-  if (tid >= need && tid < a) tgt[tid] = live + tid - need;
+  char *keys = ci_smem + (size_t)2 * A * kRow * 16;
+  uint32_t k_and = 0xffffffffu, k_or = 0u;
+  if (need > 0) commit_keys<NT>(p, u, live, keys, k_and, k_or);
+  commit_slots<NT>(p, u, a, live, need, keys, k_and, k_or, sc, tgt, tgt_pos);
   __syncthreads();
   if (tid < A) {
-    const bool freed = tid < need;
-    p.ev_slot[(size_t)u * A + tid] = freed ? tgt[tid] : -1;
-    if (p.ev_pos) p.ev_pos[(size_t)u * A + tid] = freed ? opos[tgt[tid]] : -1;
+    p.ev_slot[(size_t)u * A + tid] = tid < need ? tgt[tid] : -1;
+    if (p.ev_pos) p.ev_pos[(size_t)u * A + tid] = tid < need ? tgt_pos[tid] : -1;
   }
-  if (tid < a) {  // the thread that reads a freed slot's position is the one that writes the new one
+  const size_t st = (size_t)u * B;
+  if (tid < a) {
     const size_t at = st + tgt[tid];
     float s = 0.f, q = 0.f;
     for (int i = tid; i < a; ++i) {
@@ -348,13 +163,9 @@ __global__ void __launch_bounds__(NT) commit_insert_kernel(const CommitParams p)
     p.live[u] = live - need + a;
     p.t_next[u] = t_new + a;
   }
-  constexpr int kRow = D * (int)sizeof(T) / 16;
   for (int w = tid; w < a * 2 * kRow; w += NT) {
-    const int i = w / (2 * kRow), c = w % (2 * kRow);
-    const bool isv = c >= kRow;
-    const int cc = isv ? c - kRow : c;
-    const uint4 x = reinterpret_cast<const uint4 *>(isv ? p.v_new : p.k_new)[((size_t)u * p.T + sh_node[i]) * kRow + cc];
-    reinterpret_cast<uint4 *>(isv ? p.V : p.K)[(st + tgt[i]) * kRow + cc] = x;
+    const int isv = w >= a * kRow, x = w - isv * a * kRow;
+    reinterpret_cast<uint4 *>(isv ? p.V : p.K)[(st + tgt[x / kRow]) * kRow + x % kRow] = rows[isv * A * kRow + x];
   }
 }
 
@@ -362,13 +173,16 @@ template <typename T, int D, int NT>
 roco_status commit_insert_nt(const CommitParams &p, int U, cudaStream_t stream) {
   static SmemLimit limit;
   auto kernel = commit_insert_kernel<T, D, NT>;
-  if (!limit((const void *)kernel, 8192 * 8)) return ROCO_ERR_CUDA;
-  kernel<<<U, NT, (size_t)p.B * 8, stream>>>(p);
-  return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+  if (!limit((const void *)kernel, 8192 * 8 + 2 * kCiMaxA * D * sizeof(T))) return ROCO_ERR_CUDA;
+  const size_t smem = (size_t)p.B * 8 + (size_t)2 * p.A * D * sizeof(T);
+  return launch_overlapped(kernel, U, NT, smem, stream, p) ? ROCO_OK : ROCO_ERR_CUDA;
 }
 
+// A unit is a chain of passes and loads: with few units more threads shorten the passes, with many it is the number of
+// units in flight that counts (8192 units x B 1024: 128 threads 60 us, 256 threads 105 us).
 template <typename T, int D>
-roco_status commit_insert_t(const CommitParams &p, int U, cudaStream_t stream) {
+roco_status commit_insert_t(const CommitParams &p, int U, int sms, cudaStream_t stream) {
+  if (U >= 8 * sms) return commit_insert_nt<T, D, 128>(p, U, stream);
   return p.B <= 2048 ? commit_insert_nt<T, D, 256>(p, U, stream) : commit_insert_nt<T, D, 512>(p, U, stream);
 }
 
@@ -390,8 +204,8 @@ roco_status launch_tree_commit(const CommitParams &p, int kv_dtype, int d, int U
     st = d == 128 ? commit_stats_t<float, 128>(p, U, sms, stream) : commit_stats_t<float, 64>(p, U, sms, stream);
   if (st != ROCO_OK) return st;
   if (kv_dtype == ROCO_BF16)
-    return d == 128 ? commit_insert_t<__nv_bfloat16, 128>(p, U, stream) : commit_insert_t<__nv_bfloat16, 64>(p, U, stream);
-  return d == 128 ? commit_insert_t<float, 128>(p, U, stream) : commit_insert_t<float, 64>(p, U, stream);
+    return d == 128 ? commit_insert_t<__nv_bfloat16, 128>(p, U, sms, stream) : commit_insert_t<__nv_bfloat16, 64>(p, U, sms, stream);
+  return d == 128 ? commit_insert_t<float, 128>(p, U, sms, stream) : commit_insert_t<float, 64>(p, U, sms, stream);
 }
 
 }  // namespace roco

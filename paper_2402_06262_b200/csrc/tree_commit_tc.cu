@@ -19,7 +19,7 @@ template <int D, int N>
 struct CtShape {
   static constexpr int kTile = kCtTile * D * 2, kBlock = kCtTile * 128, kQ = N * D * 2;
   // three CTAs per SM while the queries are few, else two (one for the widest)
-  static constexpr int kCtas = N <= 32 ? 3 : (N <= 128 ? 2 : 1);
+  static constexpr int kCtas = N * D <= 16 * 128 ? 3 : (N <= 128 ? 2 : 1);
   static constexpr int kRoom = 227 * 1024 / kCtas - 2048 - kQ - N * 4 - 1024;
   static constexpr int kStages = kRoom / kTile > 6 ? 6 : kRoom / kTile;
   static constexpr int kTmemCols = 2 * N < 32 ? 32 : 2 * N;
@@ -34,6 +34,7 @@ __global__ void __launch_bounds__(kCtThreads, (CtShape<D, N>::kCtas))
   constexpr int kTile = Sh::kTile, kBlock = Sh::kBlock, kStages = Sh::kStages;
   constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24) | (((uint32_t)N >> 3) << 17);
   extern __shared__ char ct_raw[];
+  launch_dependents();
   char *at = smem_align(ct_raw, 1024);
   char *ring = at; at += kStages * kTile;
   char *qop = at; at += Sh::kQ;
@@ -168,10 +169,7 @@ template <int D, int N>
 roco_status commit_stats_tc_t(const CommitParams &p, int U, int sms, cudaStream_t stream) {
   CUtensorMap mk;
   if (!make_tensor_map_units_bf16(&mk, p.K, U, p.B, D, kCtTile)) return ROCO_ERR_CUDA;
-  auto kernel = commit_stats_tc_kernel<D, N>;
   constexpr size_t smem = CtShape<D, N>::kSmem;
-  static SmemLimit limit;
-  if (!limit((const void *)kernel, smem)) return ROCO_ERR_CUDA;
   // a unit's keys in one CTA (the queries are gathered once) unless that leaves SMs without work
   const int tiles = (p.B + kCtTile - 1) / kCtTile;
   const long long slots = (long long)CtShape<D, N>::kCtas * sms;
@@ -179,6 +177,9 @@ roco_status commit_stats_tc_t(const CommitParams &p, int U, int sms, cudaStream_
   blocks = blocks < 1 ? 1 : (blocks > tiles ? tiles : blocks);
   const int per = (tiles + blocks - 1) / blocks;
   blocks = (tiles + per - 1) / per;
+  auto kernel = commit_stats_tc_kernel<D, N>;
+  static SmemLimit limit;
+  if (!limit((const void *)kernel, smem)) return ROCO_ERR_CUDA;
   kernel<<<(unsigned)U * (unsigned)blocks, kCtThreads, smem, stream>>>(mk, p, per, blocks);
   return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
 }

@@ -1,0 +1,244 @@
+// Evictions and insertion of a commit, for one unit and a group of threads (tree_commit.cu).
+#pragma once
+
+#include "multi.cuh"
+#include "tree.cuh"
+
+namespace roco {
+
+constexpr int kCiMaxA = ROCO_TREE_MAX_PATH;
+// Named barrier of the group.  Not kMqBarPolicy: lowest_r_block_victims synchronises its 128 threads on that one while the
+// rest of a larger group already waits on this.
+constexpr int kCiBar = 3;
+static_assert(kCiBar != kMqBarPolicy, "the two groups differ in size");
+constexpr int kCiShort = 64;  // candidates that are ranked one against the other
+
+struct CiScratch {
+  SelectScratch sel;
+  int ctl[64];  // 20: counter; 24 .. 39: the chosen slots (the places that lowest_r_block_victims uses)
+  int cand[kCiShort], cand_pos[kCiShort];
+  int list_pos[kCiMaxA];  // positions of the chosen slots
+  uint32_t group_min[16], threshold;
+};
+
+// The kn (<= 16) slots first in (key, position) order over keys that are bit patterns of non-negative floats below
+// infinity, to sc.ctl[24 ..] and their positions to
+// sc.list_pos; false if there are fewer.  The threads form 16 groups: at least kn keys lie
+// at or below the kn-th smallest of the groups' minima, and few more, so those are gathered and ranked one against the
+// other.  Only where many keys are equal do they not fit; then a radix select finds the threshold and the lowest
+// positions at it.  Every thread of the group of NT calls it.
+template <int NT>
+__device__ __forceinline__ bool lowest_slots(const uint32_t *key, const int *pos, int live, int kn, CiScratch &sc) {
+  const int tid = threadIdx.x;
+  int *list = sc.ctl + 24, *cnt = sc.ctl + 20;
+  constexpr uint32_t kInf = 0x7f800000u;
+  uint32_t low = 0xffffffffu;
+  for (int j = tid; j < live; j += NT) low = min(low, key[j]);
+#pragma unroll
+  for (int o = NT / 32; o > 0; o >>= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, o));  // NT / 16 neighbours
+  if (tid % (NT / 16) == 0) sc.group_min[tid / (NT / 16)] = low;
+  if (tid == 0) *cnt = 0;
+  named_bar_sync(kCiBar, NT);
+  if (tid < 16) {
+    int rank = 0;
+    const uint32_t mine = sc.group_min[tid];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) rank += sc.group_min[i] < mine || (sc.group_min[i] == mine && i < tid);
+    if (rank == kn - 1) sc.threshold = mine;
+  }
+  named_bar_sync(kCiBar, NT);
+  const uint32_t T = sc.threshold;
+  for (int j = tid; j < live; j += NT) {
+    const uint32_t k = key[j];
+    if (k <= T && k < kInf) {
+      const int at = atomicAdd(cnt, 1);
+      if (at < kCiShort) { sc.cand[at] = j; sc.cand_pos[at] = pos[j]; }
+    }
+  }
+  named_bar_sync(kCiBar, NT);
+  const int n = *cnt;
+  named_bar_sync(kCiBar, NT);
+  if (n <= kCiShort) {
+    if (tid < n) {
+      const int j = sc.cand[tid];
+      const uint32_t k = key[j];
+      const int ps = sc.cand_pos[tid];
+      int rank = 0;
+      for (int i = 0; i < n; ++i) {
+        const uint32_t kc = key[sc.cand[i]];
+        rank += kc < k || (kc == k && sc.cand_pos[i] < ps);
+      }
+      if (rank < kn) { list[rank] = j; sc.list_pos[rank] = ps; }
+    }
+    named_bar_sync(kCiBar, NT);
+    return n >= kn;
+  }
+  uint32_t k_and = 0xffffffffu, k_or = 0u, rank, ties;
+  for (int j = tid; j < live; j += NT) { k_and &= key[j]; k_or |= key[j]; }
+  group_and_or(k_and, k_or, sc.sel, tid, NT, kCiBar);
+  const uint32_t R = radix_select<uint32_t>([&](int j) { return key[j]; }, [&](int) { return true; }, live, (uint32_t)(kn - 1),
+                                            sc.sel, tid, NT, kCiBar, &rank, &ties, k_and, k_or);
+  int P = 0x7fffffff;
+  if (ties != rank + 1) {  // only some of the slots tied at the threshold: lowest positions
+    uint32_t r2, t2;
+    P = (int)radix_select<uint32_t>([&](int j) { return (uint32_t)pos[j]; }, [&](int j) { return key[j] == R; }, live, rank,
+                                    sc.sel, tid, NT, kCiBar, &r2, &t2);
+  }
+  if (tid == 0) *cnt = 0;
+  named_bar_sync(kCiBar, NT);
+  for (int j = tid; j < live; j += NT) {
+    const uint32_t k = key[j];
+    if (k < kInf && (k < R || (k == R && (P == 0x7fffffff || pos[j] <= P)))) {
+      const int at = atomicAdd(cnt, 1);
+      if (at < kCiMaxA) { list[at] = j; sc.list_pos[at] = pos[j]; }
+    }
+  }
+  named_bar_sync(kCiBar, NT);
+  return *cnt == kn;
+}
+
+// What a unit's accepted tokens start with: pbar[i][m], the mean over the heads of accepted query i's probability of accepted
+// token m <= i, from the accepted keys in shared memory.  A warp per query head at a time, the next one's row on its way;
+// the heads' shares are added up in the order of the heads by the warp that owns the query.
+template <typename T, int D>
+__device__ __forceinline__ void commit_new_probabilities(const CommitParams &p, int u, int a, const int *path, const T *keys,
+                                                         int warp, int warps, int lane, float (*pbar)[kCiMaxA]) {
+  constexpr int kN = D / 32;
+  const float zscale = p.scale * kLog2e, share = 1.f / (float)p.group;
+  const T *Qu = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.T * p.group * D + lane;
+  const float *lse = p.lse + (size_t)u * p.T * p.group;
+  for (int i = a - 1 - warp; i >= 0; i -= warps) {  // the longest first
+    const size_t row0 = (size_t)path[i] * p.group;
+    float next[kN], nl = lse[row0];
+#pragma unroll
+    for (int c = 0; c < kN; ++c) next[c] = Elem<T>::load(Qu + row0 * D + c * 32);
+    float acc = 0.f;  // lane m: token m
+    for (int g = 0; g < p.group; ++g) {
+      float q[kN];
+      const float l = -nl * kLog2e;
+#pragma unroll
+      for (int c = 0; c < kN; ++c) q[c] = next[c];
+      if (g + 1 < p.group) {
+        nl = lse[row0 + g + 1];
+#pragma unroll
+        for (int c = 0; c < kN; ++c) next[c] = Elem<T>::load(Qu + (row0 + g + 1) * D + c * 32);
+      }
+      float mine = 0.f;
+#pragma unroll 4
+      for (int m = 0; m <= i; ++m) {
+        float x = 0.f;
+#pragma unroll
+        for (int c = 0; c < kN; ++c) x = fmaf(q[c], Elem<T>::load(keys + m * D + c * 32 + lane), x);
+        x = warp_sum(x);
+        if (lane == m) mine = x;
+      }
+      if (lane <= i) acc += exp2f(fmaf(mine, zscale, l));
+    }
+    if (lane <= i) pbar[i][lane] = acc * share;
+  }
+}
+
+// Variance and mean keys of a unit's slots (keys: 8 bytes per slot of shared memory) from its statistics as they stand.
+template <int NT>
+__device__ __forceinline__ void commit_keys(const CommitParams &p, int u, int live, char *keys, uint32_t &k_and, uint32_t &k_or) {
+  const size_t st = (size_t)u * p.B;
+  uint32_t *vkey = reinterpret_cast<uint32_t *>(keys);
+  float *mkey = reinterpret_cast<float *>(vkey + p.B);
+#pragma unroll 4
+  for (int j = threadIdx.x; j < live; j += NT) {
+    const float s = p.s[st + j], q = p.q[st + j];
+    const int n = p.n[st + j];
+    const uint32_t v = variance_key_fast(s, q, n);
+    vkey[j] = v;
+    mkey[j] = mean_fast(s, n);
+    k_and &= v;
+    k_or |= v;
+  }
+}
+
+// The slots that the a > 0 accepted tokens take, ascending, to tgt[0 .. a); the first `need` of them are evicted, their
+// positions to tgt_pos.  Called by the NT threads 0 .. NT - 1 of a CTA, which synchronise on kCiBar, with the keys in
+// place.  Each pass is over shared memory.
+template <int NT>
+__device__ __forceinline__ void commit_slots(const CommitParams &p, int u, int a, int live, int need, char *keys, uint32_t k_and,
+                                             uint32_t k_or, CiScratch &sc, int *tgt, int *tgt_pos) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, B = p.B;
+  const size_t st = (size_t)u * B;
+  uint32_t *vkey = reinterpret_cast<uint32_t *>(keys);
+  float *mkey = reinterpret_cast<float *>(vkey + B);
+  uint32_t *mbits = reinterpret_cast<uint32_t *>(mkey);
+  const int *opos = p.pos + st;
+  int *list = sc.ctl + 24;
+  if (need > 0) {
+    named_bar_sync(kCiBar, NT);  // the keys are complete
+    const int m = scope_size(live, p.r, p.scope_mode);
+    bool ok = true;
+    if (need > 1 && p.scope_mode == ROCO_SCOPE_LOWEST_R && m < live) {
+      group_and_or(k_and, k_or, sc.sel, tid, NT, kCiBar);
+      if (tid < kMqPolicyThreads)
+        lowest_r_block_victims(vkey, mkey, &sc.sel, sc.ctl, opos, p.status, p.r, live, need, m, k_and, k_or, tid);
+      if (tid < need) sc.list_pos[tid] = opos[list[tid]];
+    } else {
+      // Frozen statistics: the m first in (variance, position) order stay the scope, and the `need` of them first in
+      // (mean, position) order leave.  Those are looked for among all cached tokens first: they are all in scope if the
+      // one of them last in (variance, position) order is, which one count decides; a scope that leaves out few tokens
+      // nearly always contains them, and the search for its threshold is saved.
+      bool done = m == live;
+      ok = lowest_slots<NT>(mbits, opos, live, need, sc);
+      if (!done && ok) {
+        uint32_t cv = 0u;
+        int cp = -1;
+        for (int e = 0; e < need; ++e) {
+          const uint32_t v = vkey[list[e]];
+          const int ps = sc.list_pos[e];
+          if (v > cv || (v == cv && ps > cp)) { cv = v; cp = ps; }
+        }
+        uint32_t before = 0;
+        for (int j = tid; j < live; j += NT) {
+          const uint32_t v = vkey[j];
+          before += (v < cv || (v == cv && opos[j] < cp)) ? 1u : 0u;
+        }
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) sc.sel.hist[warp] = before;
+        named_bar_sync(kCiBar, NT);
+        before = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 32; ++w) before += sc.sel.hist[w];
+        done = before < (uint32_t)m;
+        named_bar_sync(kCiBar, NT);
+      }
+      if (!done) {
+        uint32_t rank, ties;
+        group_and_or(k_and, k_or, sc.sel, tid, NT, kCiBar);
+        const uint32_t Tv = radix_select<uint32_t>([&](int j) { return vkey[j]; }, [&](int) { return true; }, live,
+                                                   (uint32_t)(m - 1), sc.sel, tid, NT, kCiBar, &rank, &ties, k_and, k_or);
+        int Pv = 0x7fffffff;
+        if (ties != rank + 1) {
+          uint32_t r2, t2;
+          Pv = (int)radix_select<uint32_t>([&](int j) { return (uint32_t)opos[j]; }, [&](int j) { return vkey[j] == Tv; },
+                                           live, rank, sc.sel, tid, NT, kCiBar, &r2, &t2);
+        }
+        for (int j = tid; j < live; j += NT) {
+          const uint32_t v = vkey[j];
+          if (!(v < Tv || (v == Tv && (Pv == 0x7fffffff || opos[j] <= Pv)))) mkey[j] = INFINITY;
+        }
+        named_bar_sync(kCiBar, NT);
+        ok = lowest_slots<NT>(mbits, opos, live, need, sc);
+      }
+    }
+    if (!ok && tid == 0) {  // only after corrupt statistics: distinct slots all the same
+      atomicOr(p.status, ROCO_DEV_BAD_VICTIM);
+      for (int e = 0; e < need; ++e) { list[e] = e; sc.list_pos[e] = opos[e]; }
+    }
+    named_bar_sync(kCiBar, NT);
+    if (tid < need) {  // freed slots in increasing order
+      int at = 0;
+      for (int x = 0; x < need; ++x) at += list[x] < list[tid] || (list[x] == list[tid] && x < tid);
+      tgt[at] = list[tid];
+      tgt_pos[at] = sc.list_pos[tid];
+    }
+  }
+  if (tid >= need && tid < a) tgt[tid] = live + tid - need;
+}
+
+}  // namespace roco

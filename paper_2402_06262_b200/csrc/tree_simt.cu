@@ -22,6 +22,7 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
   __shared__ float sp[kTsRows][kTsKeys];
   __shared__ unsigned long long anc[kTreeMaxNodes];
   __shared__ int up[kTreeMaxNodes];
+  launch_dependents();
   const int tid = threadIdx.x, row = tid >> 4, part = tid & 15;
   const int row_blocks = (p.rows + kTsRows - 1) / kTsRows;
   const int rb = blockIdx.x % row_blocks, split = (blockIdx.x / row_blocks) % p.splits;
@@ -161,6 +162,7 @@ constexpr int kTreeJoinWarps = 4;
 template <typename T, int D>
 __global__ void __launch_bounds__(kTreeJoinWarps * 32) tree_join_kernel(const TreeParams p, int U) {
   const long long w = (long long)blockIdx.x * kTreeJoinWarps + (threadIdx.x >> 5);
+  wait_for_launch_before();
   if (w >= (long long)U * p.rows) return;
   const int lane = threadIdx.x & 31, u = (int)(w / p.rows), row = (int)(w % p.rows);
   if (row >= tree_nodes(p, u / p.G, false) * p.group) return;
@@ -191,8 +193,8 @@ __global__ void __launch_bounds__(kTreeJoinWarps * 32) tree_join_kernel(const Tr
 template <typename T, int D>
 roco_status tree_join_t(const TreeParams &p, int U, cudaStream_t stream) {
   const long long blocks = ((long long)U * p.rows + kTreeJoinWarps - 1) / kTreeJoinWarps;
-  tree_join_kernel<T, D><<<(unsigned)blocks, kTreeJoinWarps * 32, 0, stream>>>(p, U);
-  return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+  return launch_overlapped(tree_join_kernel<T, D>, (unsigned)blocks, kTreeJoinWarps * 32, 0, stream, p, U) ? ROCO_OK
+                                                                                                           : ROCO_ERR_CUDA;
 }
 
 roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream) {

@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(kTtThreads, 2)
   constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24) | (((uint32_t)N >> 3) << 17);
   constexpr uint32_t kIdescO = kIdescS | (1u << 15) | (1u << 16);  // both operands with the M / N index contiguous
   extern __shared__ char tt_raw[];
+  launch_dependents();
   char *at = smem_align(tt_raw, 1024);
   char *ring = at; at += kStages * kTile;
   char *pbuf = at; at += Sh::kP * Sh::kPBufs;
