@@ -11,68 +11,129 @@ constexpr int kCiMaxA = ROCO_TREE_MAX_PATH;
 // rest of a larger group already waits on this.
 constexpr int kCiBar = 3;
 static_assert(kCiBar != kMqBarPolicy, "the two groups differ in size");
-constexpr int kCiShort = 64;  // candidates that are ranked one against the other
+constexpr int kCiShort = 256;  // candidates that are ranked one against the other
 
 struct CiScratch {
   SelectScratch sel;
   int ctl[64];  // 20: counter; 24 .. 39: the chosen slots (the places that lowest_r_block_victims uses)
-  int cand[kCiShort], cand_pos[kCiShort];
+  int cand[kCiShort];
+  unsigned long long cand_key[kCiShort];  // key, then position
+  alignas(16) uint32_t best[512];
+  uint32_t threshold;
   int list_pos[kCiMaxA];  // positions of the chosen slots
-  uint32_t group_min[16], threshold;
 };
 
-// The kn (<= 16) slots first in (key, position) order over keys that are bit patterns of non-negative floats below
-// infinity, to sc.ctl[24 ..] and their positions to
-// sc.list_pos; false if there are fewer.  The threads form 16 groups: at least kn keys lie
-// at or below the kn-th smallest of the groups' minima, and few more, so those are gathered and ranked one against the
-// other.  Only where many keys are equal do they not fit; then a radix select finds the threshold and the lowest
-// positions at it.  Every thread of the group of NT calls it.
-template <int NT>
-__device__ __forceinline__ bool lowest_slots(const uint32_t *key, const int *pos, int live, int kn, CiScratch &sc) {
-  const int tid = threadIdx.x;
-  int *list = sc.ctl + 24, *cnt = sc.ctl + 20;
-  constexpr uint32_t kInf = 0x7f800000u;
-  uint32_t low = 0xffffffffu;
-  for (int j = tid; j < live; j += NT) low = min(low, key[j]);
-#pragma unroll
-  for (int o = NT / 32; o > 0; o >>= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, o));  // NT / 16 neighbours
-  if (tid % (NT / 16) == 0) sc.group_min[tid / (NT / 16)] = low;
-  if (tid == 0) *cnt = 0;
-  named_bar_sync(kCiBar, NT);
-  if (tid < 16) {
-    int rank = 0;
-    const uint32_t mine = sc.group_min[tid];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) rank += sc.group_min[i] < mine || (sc.group_min[i] == mine && i < tid);
-    if (rank == kn - 1) sc.threshold = mine;
-  }
-  named_bar_sync(kCiBar, NT);
+// Gathers the slots whose key is at or beyond sc.threshold; returns how many, -1 if they are too many to rank (many equal
+// keys).  Every thread of the group of NT calls it.
+template <int NT, bool kLow>
+__device__ __forceinline__ int gather_candidates(const uint32_t *key, const int *pos, int live, CiScratch &sc) {
+  const int lane = threadIdx.x & 31;
+  int *cnt = sc.ctl + 20;
   const uint32_t T = sc.threshold;
-  for (int j = tid; j < live; j += NT) {
-    const uint32_t k = key[j];
-    if (k <= T && k < kInf) {
-      const int at = atomicAdd(cnt, 1);
-      if (at < kCiShort) { sc.cand[at] = j; sc.cand_pos[at] = pos[j]; }
+  for (int j0 = threadIdx.x - lane; j0 < live; j0 += NT) {  // (the warp stays together)
+    const int j = j0 + lane;
+    const uint32_t k = j < live ? key[j] : 0u;
+    const bool take = j < live && (kLow ? k <= T && k < 0x7f800000u : k >= T);
+    const uint32_t who = __ballot_sync(0xffffffffu, take);
+    if (who) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(cnt, __popc(who));
+      at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+      if (take && at < kCiShort) {
+        sc.cand[at] = j;
+        sc.cand_key[at] = (unsigned long long)k << 32 | (uint32_t)pos[j];
+      }
     }
   }
   named_bar_sync(kCiBar, NT);
   const int n = *cnt;
+  return n > kCiShort ? -1 : n;
+}
+
+// How many of the n gathered come before (kLow) or behind this one in (key, position) order.
+template <bool kLow>
+__device__ __forceinline__ int rank_candidate(const CiScratch &sc, int n, unsigned long long mine) {
+  int rank = 0;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) rank += kLow ? sc.cand_key[i] < mine : sc.cand_key[i] > mine;
+  return rank;
+}
+
+// The kn (<= 16) slots first in (key, position) order over keys that are bit patterns of non-negative floats below
+// infinity, to sc.ctl[24 ..] and their positions to sc.list_pos.  The threads form 16 groups: at least kn keys lie at or
+// below the kn-th smallest of the groups' minima, and few more, so those are gathered and ranked one against the other.
+// Returns how many were gathered: fewer than kn if there are no more, -1 if too many to rank.
+template <int NT>
+__device__ __forceinline__ int lowest_slots(const uint32_t *key, const int *pos, int live, int kn, CiScratch &sc) {
+  const int tid = threadIdx.x;
+  uint32_t low = 0xffffffffu;
+#pragma unroll 4
+  for (int j = tid; j < live; j += NT) low = min(low, key[j]);
+#pragma unroll
+  for (int o = NT / 32; o > 0; o >>= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, o));  // NT / 16 neighbours
+  if (tid % (NT / 16) == 0) sc.best[tid / (NT / 16)] = low;
+  if (tid == 0) sc.ctl[20] = 0;
   named_bar_sync(kCiBar, NT);
-  if (n <= kCiShort) {
-    if (tid < n) {
-      const int j = sc.cand[tid];
-      const uint32_t k = key[j];
-      const int ps = sc.cand_pos[tid];
-      int rank = 0;
-      for (int i = 0; i < n; ++i) {
-        const uint32_t kc = key[sc.cand[i]];
-        rank += kc < k || (kc == k && sc.cand_pos[i] < ps);
-      }
-      if (rank < kn) { list[rank] = j; sc.list_pos[rank] = ps; }
-    }
-    named_bar_sync(kCiBar, NT);
-    return n >= kn;
+  if (tid < 16) {
+    int rank = 0;
+    const uint32_t mine = sc.best[tid];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) rank += (sc.best[i] < mine) | ((sc.best[i] == mine) & (i < tid));
+    if (rank == kn - 1) sc.threshold = mine;
   }
+  named_bar_sync(kCiBar, NT);
+  const int n = gather_candidates<NT, true>(key, pos, live, sc);
+  for (int c = tid; c < n; c += NT) {
+    const int rank = rank_candidate<true>(sc, n, sc.cand_key[c]);
+    if (rank < kn) { sc.ctl[24 + rank] = sc.cand[c]; sc.list_pos[rank] = (int)(uint32_t)sc.cand_key[c]; }
+  }
+  named_bar_sync(kCiBar, NT);
+  return n;
+}
+
+// Takes the x slots last in (variance, position) order out of the scope (their means become infinite); false if it could
+// not.  The same idea the other way round, with 128 groups for x <= 64 and a group per thread up to x = NT / 2.
+template <int NT>
+__device__ __forceinline__ bool exclude_highest(const uint32_t *vkey, float *mkey, const int *pos, int live, int x, CiScratch &sc) {
+  const int tid = threadIdx.x;
+  uint32_t high = 0u;
+#pragma unroll 4
+  for (int j = tid; j < live; j += NT) high = max(high, vkey[j]);
+  const int groups = x <= 64 ? 128 : NT;
+  if (groups < NT) {
+#pragma unroll
+    for (int o = NT / 256; o > 0; o >>= 1) high = max(high, __shfl_xor_sync(0xffffffffu, high, o));  // NT / 128 neighbours
+    if (tid % (NT / 128) == 0) sc.best[tid / (NT / 128)] = high;
+  } else {
+    sc.best[tid] = high;
+  }
+  if (tid == 0) sc.ctl[20] = 0;
+  named_bar_sync(kCiBar, NT);
+  if (tid < groups) {
+    const uint32_t mine = sc.best[tid];
+    int rank = 0;
+#pragma unroll 4
+    for (int i = 0; i < groups; i += 4) {
+      const uint4 o = *reinterpret_cast<const uint4 *>(&sc.best[i]);
+      rank += ((o.x > mine) | ((o.x == mine) & (i < tid))) + ((o.y > mine) | ((o.y == mine) & (i + 1 < tid))) +
+              ((o.z > mine) | ((o.z == mine) & (i + 2 < tid))) + ((o.w > mine) | ((o.w == mine) & (i + 3 < tid)));
+    }
+    if (rank == x - 1) sc.threshold = mine;
+  }
+  named_bar_sync(kCiBar, NT);
+  const int n = gather_candidates<NT, false>(vkey, pos, live, sc);
+  for (int c = tid; c < n; c += NT)
+    if (rank_candidate<false>(sc, n, sc.cand_key[c]) < x) mkey[sc.cand[c]] = INFINITY;
+  named_bar_sync(kCiBar, NT);
+  return n >= 0;
+}
+
+// The kn slots of lowest_slots by a radix select on the keys, whatever the ties; unordered, to sc.ctl[24 ..] and sc.list_pos; false if
+// there are fewer.
+template <int NT>
+__device__ __forceinline__ bool lowest_by_radix(const uint32_t *key, const int *pos, int live, int kn, CiScratch &sc) {
+  const int tid = threadIdx.x;
+  int *list = sc.ctl + 24, *cnt = sc.ctl + 20;
   uint32_t k_and = 0xffffffffu, k_or = 0u, rank, ties;
   for (int j = tid; j < live; j += NT) { k_and &= key[j]; k_or |= key[j]; }
   group_and_or(k_and, k_or, sc.sel, tid, NT, kCiBar);
@@ -88,7 +149,7 @@ __device__ __forceinline__ bool lowest_slots(const uint32_t *key, const int *pos
   named_bar_sync(kCiBar, NT);
   for (int j = tid; j < live; j += NT) {
     const uint32_t k = key[j];
-    if (k < kInf && (k < R || (k == R && (P == 0x7fffffff || pos[j] <= P)))) {
+    if (k < 0x7f800000u && (k < R || (k == R && (P == 0x7fffffff || pos[j] <= P)))) {
       const int at = atomicAdd(cnt, 1);
       if (at < kCiMaxA) { list[at] = j; sc.list_pos[at] = pos[j]; }
     }
@@ -162,7 +223,7 @@ __device__ __forceinline__ void commit_keys(const CommitParams &p, int u, int li
 template <int NT>
 __device__ __forceinline__ void commit_slots(const CommitParams &p, int u, int a, int live, int need, char *keys, uint32_t k_and,
                                              uint32_t k_or, CiScratch &sc, int *tgt, int *tgt_pos) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, B = p.B;
+  const int tid = threadIdx.x, B = p.B;
   const size_t st = (size_t)u * B;
   uint32_t *vkey = reinterpret_cast<uint32_t *>(keys);
   float *mkey = reinterpret_cast<float *>(vkey + B);
@@ -180,34 +241,9 @@ __device__ __forceinline__ void commit_slots(const CommitParams &p, int u, int a
       if (tid < need) sc.list_pos[tid] = opos[list[tid]];
     } else {
       // Frozen statistics: the m first in (variance, position) order stay the scope, and the `need` of them first in
-      // (mean, position) order leave.  Those are looked for among all cached tokens first: they are all in scope if the
-      // one of them last in (variance, position) order is, which one count decides; a scope that leaves out few tokens
-      // nearly always contains them, and the search for its threshold is saved.
-      bool done = m == live;
-      ok = lowest_slots<NT>(mbits, opos, live, need, sc);
-      if (!done && ok) {
-        uint32_t cv = 0u;
-        int cp = -1;
-        for (int e = 0; e < need; ++e) {
-          const uint32_t v = vkey[list[e]];
-          const int ps = sc.list_pos[e];
-          if (v > cv || (v == cv && ps > cp)) { cv = v; cp = ps; }
-        }
-        uint32_t before = 0;
-        for (int j = tid; j < live; j += NT) {
-          const uint32_t v = vkey[j];
-          before += (v < cv || (v == cv && opos[j] < cp)) ? 1u : 0u;
-        }
-        before = __reduce_add_sync(0xffffffffu, before);
-        if (lane == 0) sc.sel.hist[warp] = before;
-        named_bar_sync(kCiBar, NT);
-        before = 0;
-#pragma unroll
-        for (int w = 0; w < NT / 32; ++w) before += sc.sel.hist[w];
-        done = before < (uint32_t)m;
-        named_bar_sync(kCiBar, NT);
-      }
-      if (!done) {
+      // (mean, position) order leave.  The radix selects take a few hundred cycles per digit and barrier; they are left for
+      // a scope that leaves out many tokens and for many equal keys.
+      if (m < live && !(live - m <= NT / 2 && exclude_highest<NT>(vkey, mkey, opos, live, live - m, sc))) {
         uint32_t rank, ties;
         group_and_or(k_and, k_or, sc.sel, tid, NT, kCiBar);
         const uint32_t Tv = radix_select<uint32_t>([&](int j) { return vkey[j]; }, [&](int) { return true; }, live,
@@ -223,8 +259,9 @@ __device__ __forceinline__ void commit_slots(const CommitParams &p, int u, int a
           if (!(v < Tv || (v == Tv && (Pv == 0x7fffffff || opos[j] <= Pv)))) mkey[j] = INFINITY;
         }
         named_bar_sync(kCiBar, NT);
-        ok = lowest_slots<NT>(mbits, opos, live, need, sc);
       }
+      const int n = lowest_slots<NT>(mbits, opos, live, need, sc);
+      ok = n >= need || (n < 0 && lowest_by_radix<NT>(mbits, opos, live, need, sc));
     }
     if (!ok && tid == 0) {  // only after corrupt statistics: distinct slots all the same
       atomicOr(p.status, ROCO_DEV_BAD_VICTIM);
