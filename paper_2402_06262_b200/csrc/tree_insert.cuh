@@ -109,16 +109,20 @@ __device__ __forceinline__ bool exclude_highest(const uint32_t *vkey, float *mke
   }
   if (tid == 0) sc.ctl[20] = 0;
   named_bar_sync(kCiBar, NT);
-  if (tid < groups) {
-    const uint32_t mine = sc.best[tid];
-    int rank = 0;
-#pragma unroll 4
-    for (int i = 0; i < groups; i += 4) {
-      const uint4 o = *reinterpret_cast<const uint4 *>(&sc.best[i]);
-      rank += ((o.x > mine) | ((o.x == mine) & (i < tid))) + ((o.y > mine) | ((o.y == mine) & (i + 1 < tid))) +
-              ((o.z > mine) | ((o.z == mine) & (i + 2 < tid))) + ((o.w > mine) | ((o.w == mine) & (i + 3 < tid)));
+  if (tid < 32) {  // the x-th largest of them, bit by bit: the prefix grows by a one where enough values have it
+    uint32_t v[NT / 32], t = 0u;
+#pragma unroll
+    for (int i = 0; i < NT / 32; ++i) v[i] = 32 * i < groups ? sc.best[32 * i + tid] : 0u;
+#pragma unroll 1
+    for (int bit = 30; bit >= 0; --bit) {
+      const uint32_t cand = t | 1u << bit;
+      int have = 0;
+#pragma unroll
+      for (int i = 0; i < NT / 32; ++i)
+        if (32 * i < groups) have += __popc(__ballot_sync(0xffffffffu, v[i] >= cand));
+      if (have >= x) t = cand;
     }
-    if (rank == x - 1) sc.threshold = mine;
+    if (tid == 0) sc.threshold = t;
   }
   named_bar_sync(kCiBar, NT);
   const int n = gather_candidates<NT, false>(vkey, pos, live, sc);
@@ -199,6 +203,17 @@ __device__ __forceinline__ void commit_new_probabilities(const CommitParams &p, 
   }
 }
 
+// Keys of a token.  q n - s^2 in fp32 with the rounding errors of both products carried along (each is exact as a product and
+// its error term), so a difference that nearly cancels keeps its digits as in 64 bits; n is exact in fp32, and the two
+// quotients are products with its reciprocal, a few 2^-24 off.  Equal statistics give equal keys.
+__device__ __forceinline__ void commit_key(float s, float q, int n, uint32_t &vkey, float &mkey) {
+  const float nf = (float)n, rn = __fdividef(1.f, nf);
+  const float a = q * nf, ea = fmaf(q, nf, -a), b = s * s, eb = fmaf(s, s, -b);
+  const float num = (a - b) + (ea - eb);
+  vkey = __float_as_uint(fmaxf(num, 0.f) * (rn * rn));  // (NaN -> 0)
+  mkey = s * rn;
+}
+
 // Variance and mean keys of a unit's slots (keys: 8 bytes per slot of shared memory) from its statistics as they stand.
 template <int NT>
 __device__ __forceinline__ void commit_keys(const CommitParams &p, int u, int live, char *keys, uint32_t &k_and, uint32_t &k_or) {
@@ -209,9 +224,9 @@ __device__ __forceinline__ void commit_keys(const CommitParams &p, int u, int li
   for (int j = threadIdx.x; j < live; j += NT) {
     const float s = p.s[st + j], q = p.q[st + j];
     const int n = p.n[st + j];
-    const uint32_t v = variance_key_fast(s, q, n);
+    uint32_t v;
+    commit_key(s, q, n, v, mkey[j]);
     vkey[j] = v;
-    mkey[j] = mean_fast(s, n);
     k_and &= v;
     k_or |= v;
   }
