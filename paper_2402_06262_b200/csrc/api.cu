@@ -137,10 +137,10 @@ TreePlan tree_plan(const roco_cache *c, int T, int group, float scale) {
   const int rows = T * group;
   const long long U = (long long)c->S * c->G;
   t.tc = c->kv_dtype == ROCO_BF16 && scale > 0.f;
-  const int row_blocks = t.tc ? (rows + tree_tc_width(rows) - 1) / tree_tc_width(rows) : tree_simt_row_blocks(rows);
-  // Tensor cores: one wave of two CTAs per SM, no range shorter than two 128-key tiles.  CUDA cores: four CTAs per SM, no
+  const int row_blocks = t.tc ? (rows + tree_tc_rows(rows) - 1) / tree_tc_rows(rows) : tree_simt_row_blocks(rows);
+  // Tensor cores: one wave, no range shorter than two 128-key tiles.  CUDA cores: four CTAs per SM, no
   // range shorter than two 64-key tiles.
-  const long long ctas = U * row_blocks, slots = (t.tc ? 2LL : 4LL) * device_sms();
+  const long long ctas = U * row_blocks, slots = (t.tc ? (long long)tree_tc_ctas(rows) : 4LL) * device_sms();
   long long want = t.tc ? slots / ctas : (slots + ctas - 1) / ctas, most = (c->B + (t.tc ? 255 : 127)) / (t.tc ? 256 : 128);
   if (want > most) want = most;
   if (want > 32) want = 32;

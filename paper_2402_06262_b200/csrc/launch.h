@@ -134,8 +134,9 @@ struct CommitParams;
 // CUDA cores; p.splits > 1: partial results to p.part_o / p.part_ml and a second launch that joins them.
 int tree_simt_row_blocks(int rows);
 roco_status launch_tree_attend_simt(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
-// Tensor cores (bf16, positive scale); tree_tc_width: query rows of a CTA.
-int tree_tc_width(int rows);
+// Tensor cores (bf16, positive scale); query rows of a CTA and CTAs per SM for that many rows of a unit.
+int tree_tc_rows(int rows);
+int tree_tc_ctas(int rows);
 roco_status launch_tree_attend_tc(const TreeParams &p, int d, int U, cudaStream_t stream);
 roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
 // Statistics of the accepted queries, then evictions and insertion (two launches).

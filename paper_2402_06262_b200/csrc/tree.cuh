@@ -40,11 +40,11 @@ __device__ __forceinline__ int tree_live(const int *live, int u, int B, int *sta
   return n < 0 ? 0 : B;
 }
 
-// anc[i] = bit set of node i's ancestors and itself, by pointer doubling (six rounds for 64 nodes).  up: scratch.  All
-// threads of the block call it; it synchronises.
+// anc[i] = bit set of node i's ancestors and itself, by pointer doubling (six rounds for 64 nodes).  up: scratch.  Called by
+// a group of at least 64 threads, i being the thread's index in it, that sync() synchronises.
+template <typename SyncF>
 __device__ __forceinline__ void tree_ancestors(const TreeParams &p, int b, int n_nodes, unsigned long long *anc, int *up,
-                                               bool report) {
-  const int i = threadIdx.x;
+                                               bool report, int i, SyncF sync) {
   if (i < kTreeMaxNodes) {
     int par = -1;
     if (i < n_nodes) {
@@ -57,7 +57,7 @@ __device__ __forceinline__ void tree_ancestors(const TreeParams &p, int b, int n
     up[i] = par;
     anc[i] = i < n_nodes ? 1ull << i : 0ull;
   }
-  __syncthreads();
+  sync();
 #pragma unroll 1
   for (int round = 0; round < 6; ++round) {
     unsigned long long a = 0;
@@ -70,12 +70,12 @@ __device__ __forceinline__ void tree_ancestors(const TreeParams &p, int b, int n
         to = up[to];
       }
     }
-    __syncthreads();
+    sync();
     if (i < kTreeMaxNodes) {
       anc[i] = a;
       up[i] = to;
     }
-    __syncthreads();
+    sync();
   }
 }
 
