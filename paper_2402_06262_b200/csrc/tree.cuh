@@ -41,11 +41,13 @@ __device__ __forceinline__ int tree_live(const int *live, int u, int B, int *sta
 }
 
 // anc[i] = bit set of node i's ancestors and itself, by pointer doubling (six rounds for 64 nodes).  up: scratch.  Called by
-// a group of at least 64 threads, i being the thread's index in it, that sync() synchronises.
-template <typename SyncF>
-__device__ __forceinline__ void tree_ancestors(const TreeParams &p, int b, int n_nodes, unsigned long long *anc, int *up,
-                                               bool report, int i, SyncF sync) {
-  if (i < kTreeMaxNodes) {
+// one warp, two nodes a lane; the others synchronise with it before they use the result.
+__device__ __forceinline__ void tree_ancestors_warp(const TreeParams &p, int b, int n_nodes, unsigned long long *anc, int *up,
+                                                    bool report) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = lane + 32 * h;
     int par = -1;
     if (i < n_nodes) {
       par = p.parent[(size_t)b * p.T + i];
@@ -57,25 +59,27 @@ __device__ __forceinline__ void tree_ancestors(const TreeParams &p, int b, int n
     up[i] = par;
     anc[i] = i < n_nodes ? 1ull << i : 0ull;
   }
-  sync();
+  __syncwarp();
 #pragma unroll 1
   for (int round = 0; round < 6; ++round) {
-    unsigned long long a = 0;
-    int to = -1;
-    if (i < kTreeMaxNodes) {
-      a = anc[i];
-      to = up[i];
-      if (to >= 0) {
-        a |= anc[to];
-        to = up[to];
+    unsigned long long a[2];
+    int to[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      a[h] = anc[lane + 32 * h];
+      to[h] = up[lane + 32 * h];
+      if (to[h] >= 0) {
+        a[h] |= anc[to[h]];
+        to[h] = up[to[h]];
       }
     }
-    sync();
-    if (i < kTreeMaxNodes) {
-      anc[i] = a;
-      up[i] = to;
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      anc[lane + 32 * h] = a[h];
+      up[lane + 32 * h] = to[h];
     }
-    sync();
+    __syncwarp();
   }
 }
 

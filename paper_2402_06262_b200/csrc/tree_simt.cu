@@ -32,7 +32,8 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
   const int row0 = rb * kTsRows;
   if (row0 >= n_nodes * p.group) return;
   const int live = tree_live(p.live, u, p.B, p.status, report);
-  tree_ancestors(p, b, n_nodes, anc, up, rb == 0 && split == 0, tid, [] { __syncthreads(); });
+  if (tid < 32) tree_ancestors_warp(p, b, n_nodes, anc, up, rb == 0 && split == 0);
+  __syncthreads();
   const int grow = row0 + row;
   const bool valid = grow < n_nodes * p.group;
   const T *Qu = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.rows * D;

@@ -5,11 +5,14 @@
 //     S^T[128 keys x N] = K_tile Q^T          O^T[d x N] += V_tile^T P^T
 // One pass over the cache.  A thread owns one key of a tile: it forms p = 2^(z - m) for its N scores, keeps N partial sums
 // of its own in registers (joined over the lanes once, at the end) and writes the N probabilities as bf16, the second
-// product's operand.  The reference m of a row is the maximum of its first tile and moves only when a score comes out
-// more than 2^8 above it (one vote per tile instead of a maximum over the lanes; up to there fp32 sums and bf16
-// probabilities lose nothing): then the row's column of O^T and its sums are rescaled.
-// The drafted tokens are the last tile's keys, masked by the rows' ancestor sets; their values are added on the CUDA cores
-// with fp32 probabilities, node by node where a row sees the node, so that what lies on other branches cannot reach it.
+// product's operand.  The reference m of a row need not be its maximum: any score that the row's sum contains will do, so
+// it is that of the first cached key, and moves only when a score comes out more than 2^60 above it (fp32 and bf16 share
+// their exponents, so up to there neither sums nor probabilities lose anything; the sum holds a 1).  That costs one vote per
+// tile instead of a maximum over the lanes.  When it moves, to the tile's maximum, the row's column of O^T and its sums are
+// rescaled.
+// The drafted tokens are the last tile, masked by the rows' ancestor sets.  A product with zero keeps no NaN or infinity
+// out, so if one of their values is not finite their part of the output is formed on the CUDA cores instead, node by node
+// where a row sees the node: what lies on other branches cannot reach a row.
 //
 // What bounds it: the cache is read once; 64 KiB per tile of 128 tokens at d = 128 against about 700 cycles of
 // exponentials for N = 64.  Two CTAs per SM, so that one's prologue and epilogue run under the other's stream.
@@ -26,7 +29,7 @@ constexpr int kTtTile = 128;  // keys of a tile
 constexpr int kTtGroup = 128;            // threads of a consumer group
 constexpr int kTtBar = 1;                // named barriers of the consumer groups (kTtBar + group), of all of them, and of
 constexpr int kTtBarAll = 3, kTtBarQ = 4;  // them and the warp of the products
-constexpr float kTtMoveReference = 8.f;  // binary orders
+constexpr float kTtMoveReference = 60.f;  // binary orders above the reference at which a row moves to a new one
 
 // W groups of four consumer warps, N query rows each, share the tiles of a CTA; C CTAs per SM.
 template <int D, int N, int W, int C>
@@ -37,7 +40,7 @@ struct TtShape {
   static constexpr int kP = N * kTtTile * 2;         // P^T of a tile: 128-byte rows of 64 / N keys each
   static constexpr int kPRows = kP / 128;
   static constexpr int kPBufs = N == 64 ? 1 : 2;
-  static constexpr int kGroupFloats = 4 * N /* red */ + 2 * N /* nref, alpha */ + 2 * N /* sees */;
+  static constexpr int kGroupFloats = 4 * N /* red */ + 2 * N /* nref, alpha */ + 4 /* odd values */;
   static constexpr int kFixed = 1024 + W * (kQ + kP * kPBufs + kGroupFloats * 4) + kTreeMaxNodes * 12 + 256;
   static constexpr int kRoom = (227 / C) * 1024 - 1024 - kFixed;
   static constexpr int kStages = kRoom / kTile > 6 ? 6 : kRoom / kTile;
@@ -77,6 +80,10 @@ __device__ __forceinline__ bool tt_any(bool x, int bar) {  // over the threads o
   return r != 0;
 }
 
+__device__ __forceinline__ void prefetch_tensor_map(const CUtensorMap *map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
 __device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t *>(&v);
@@ -110,9 +117,13 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
   const int rb = blockIdx.x % row_blocks, split = blockIdx.x / row_blocks % p.splits, u = blockIdx.x / (row_blocks * p.splits);
   const int b = u / p.G, cta_row0 = rb * N * W;
   const bool report = tid == 0 && rb == 0 && split == 0;
-  const int n_nodes = __shfl_sync(0xffffffffu, tree_nodes(p, b, report), 0);
+  if (tid == 0) {  // on their way before the first load asks for them
+    prefetch_tensor_map(&mapK);
+    prefetch_tensor_map(&mapV);
+  }
+  const int n_nodes_ = tree_nodes(p, b, report), live_ = tree_live(p.live, u, p.B, p.status, report);
+  const int n_nodes = __shfl_sync(0xffffffffu, n_nodes_, 0), live = __shfl_sync(0xffffffffu, live_, 0);
   if (cta_row0 >= n_nodes * p.group) return;
-  const int live = __shfl_sync(0xffffffffu, tree_live(p.live, u, p.B, p.status, report), 0);
   const int tiles = (live + kTtTile - 1) / kTtTile;
   const int t0 = (int)((long long)tiles * split / p.splits);
   const int nt = (int)((long long)tiles * (split + 1) / p.splits) - t0;  // cached tiles of this CTA
@@ -165,16 +176,17 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
         }
         umma_commit_w(&empty[st]);
       }
-      if (t >= 1 && t <= nt) {  // output of tile t - 1
+      if (t >= 1) {  // output of tile t - 1
         const int g = 2 * t - 1, st = g % kStages, tv = t - 1;
         mbar_wait_compact(&full[st], (g / kStages) & 1, abort_flag, p.status);
         char *v = ring + st * kTile;
-        const int first_bad = live - (t0 + tv) * kTtTile;
-        if (first_bad < kTtTile) {  // slots behind the last token may hold anything (0 x NaN)
-          for (int w = lane; w < (kTtTile - first_bad) * 8; w += 32) {
+        const int keys = tv == nt ? n_nodes : live - (t0 + tv) * kTtTile;
+        const int steps = keys < kTtTile ? (keys + 15) / 16 : 8;  // of 16 keys
+        if (keys < 16 * steps) {  // what lies behind the last key may be anything (0 x NaN)
+          for (int w = lane; w < (16 * steps - keys) * 8; w += 32) {
 #pragma unroll
             for (int h = 0; h < D / 64; ++h)
-              *reinterpret_cast<uint4 *>(v + h * kBlock + first_bad * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
+              *reinterpret_cast<uint4 *>(v + h * kBlock + keys * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           fence_async_smem();
           __syncwarp();
@@ -184,11 +196,15 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           mbar_wait_compact(&p_ready[2 * w + (tv & 1)], (tv >> 1) & 1, abort_flag, p.status);
           tc_fence_after();
           const char *pb = pbuf_all + (w * Sh::kPBufs + tv % Sh::kPBufs) * Sh::kP;
+          const bool skip = tv == nt && __shfl_sync(0xffffffffu, *reinterpret_cast<const int *>(floats + w * Sh::kGroupFloats + 6 * N), 0);
+          if (!skip) {
 #pragma unroll
-          for (int kk = 0; kk < 8; ++kk)  // (d = 64: the upper 64 accumulator lanes repeat the lower, unread)
-            umma_bf16_w(tmem + w * 4 * N + 2 * N, smem_desc_sw128_mn(v + kk * 2048, D == 128 ? kBlock : 0),
-                        smem_desc_sw128_mn(pb + (16 * kk % Sh::kPRows) * 128 + (16 * kk / Sh::kPRows) * (N * 2), 16), kIdescO,
-                        (tv > 0 || kk > 0) ? 1u : 0u);
+            for (int kk = 0; kk < 8; ++kk)  // (d = 64: the upper 64 accumulator lanes repeat the lower, unread)
+              if (kk < steps)
+                umma_bf16_w(tmem + w * 4 * N + 2 * N, smem_desc_sw128_mn(v + kk * 2048, D == 128 ? kBlock : 0),
+                            smem_desc_sw128_mn(pb + (16 * kk % Sh::kPRows) * 128 + (16 * kk / Sh::kPRows) * (N * 2), 16), kIdescO,
+                            (tv > 0 || kk > 0) ? 1u : 0u);
+          }
           umma_commit_w(&pv_done[2 * w + (tv & 1)]);
         }
         umma_commit_w(&empty[st]);
@@ -199,31 +215,34 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
     const int grp = W == 1 ? 0 : warp >> 2, bar = kTtBar + grp, row0 = cta_row0 + grp * N;
     const int gt = tid - grp * kTtGroup, gw = warp - 4 * grp;
     float *red = floats + grp * Sh::kGroupFloats, *nref = red + 4 * N, *alpha = nref + N;  // nref: minus a row's reference, log2
-    const unsigned long long *sees = reinterpret_cast<unsigned long long *>(red + 6 * N);
+    int *odd = reinterpret_cast<int *>(red + 6 * N);  // the drafted values are not all finite
     // the drafted tokens' probabilities [node][N], after the stream: group 0's where their keys were, group 1's in the place
     // behind their values
     float *pd = reinterpret_cast<float *>(ring + (2 * nt + 2 * grp) % kStages * kTile);
-    const char *vn = ring + (2 * nt + 1) % kStages * kTile;
+    auto drafted_value = [&](int j) -> uint32_t {  // dimension gt of node j's value, as its 16 bits
+      const char *vn = ring + (2 * nt + 1) % kStages * kTile + (gt >> 6) * kBlock + j * 128;
+      return *reinterpret_cast<const uint16_t *>(vn + ((((gt & 63) >> 3) ^ (j & 7)) << 4) + (gt & 7) * 2);
+    };
     char *pbuf = pbuf_all + grp * Sh::kPBufs * Sh::kP;
     {  // the queries as the K-major operands of the groups; rows that do not exist are zero
       const uint4 *Qu = reinterpret_cast<const uint4 *>(p.Q) + ((size_t)u * p.rows + cta_row0) * (D / 8);
-      for (int w = tid; w < W * N * D / 8; w += W * kTtGroup) {
-        const int i = w / (D / 8) % N, c = w % (D / 8);
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (cta_row0 + w / (D / 8) < n_nodes * p.group) x = Qu[w];
-        *reinterpret_cast<uint4 *>(qop_all + w / (N * D / 8) * Sh::kQ + (c >> 3) * (N * 128) + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = x;
+      constexpr int kPieces = N * D / 8 / kTtGroup;  // 16-byte pieces per thread, all loaded before the first is stored
+      uint4 x[kPieces];
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const int w = tid + k * W * kTtGroup;
+        x[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (cta_row0 + w / (D / 8) < n_nodes * p.group) x[k] = Qu[w];
+      }
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const int w = tid + k * W * kTtGroup, i = w / (D / 8) % N, c = w % (D / 8);
+        *reinterpret_cast<uint4 *>(qop_all + w / (N * D / 8) * Sh::kQ + (c >> 3) * (N * 128) + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = x[k];
       }
       fence_async_smem();
     }
     named_bar_sync(kTtBarQ, W * kTtGroup + 32);
-    if (drafts) {
-      tree_ancestors(p, b, n_nodes, anc, up, rb == 0, tid, [] { named_bar_sync(kTtBarAll, W * kTtGroup); });
-      if (tid < N * W) {  // per query row: the nodes it sees
-        unsigned long long *of = reinterpret_cast<unsigned long long *>(floats + tid / N * Sh::kGroupFloats + 6 * N);
-        of[tid % N] = cta_row0 + tid < n_nodes * p.group ? anc[(cta_row0 + tid) / p.group] : 0ull;
-      }
-      named_bar_sync(kTtBarAll, W * kTtGroup);
-    }
+    if (drafts && warp == 0) tree_ancestors_warp(p, b, n_nodes, anc, up, rb == 0);  // under the first tile's load
     const float zs = p.scale * kLog2e;
     const f32x2 zs2 = pack2(zs, zs);
     const uint32_t tl = tmem + grp * 4 * N + ((uint32_t)(gw * 32) << 16);
@@ -237,17 +256,25 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       if (t >= 0) mbar_wait_compact(&pv_done[2 * grp + (t & 1)], (t >> 1) & 1, abort_flag, p.status);
     };
     if (gt < N) nref[gt] = 0.f;
-    unsigned long long mine = 0ull;  // the rows (bits) that see node gt
-    if (drafts && gt < n_nodes) {
-#pragma unroll 8
-      for (int i = 0; i < N; ++i) mine |= ((sees[i] >> gt) & 1ull) << i;
-    }
     named_bar_sync(bar, kTtGroup);
+    bool by_hand = false;
 
-    auto tile = [&](int t, auto draft_tag) {
-      constexpr bool kDraft = decltype(draft_tag)::value;
-      const bool held = kDraft ? gt < n_nodes : (t0 + t) * kTtTile + gt < live;
-      const bool ragged = kDraft || (t0 + t + 1) * kTtTile > live;  // some lanes hold no key
+#pragma unroll 1
+    for (int t = 0; t < ns; ++t) {
+      const bool is_draft = t == nt;
+      const int keys = is_draft ? n_nodes : live - (t0 + t) * kTtTile;  // of this tile (more: a full one)
+      unsigned long long mine = gt < keys ? ~0ull : 0ull;               // the rows (bits) that see this thread's key
+      if (is_draft) {
+        named_bar_sync(kTtBarAll, W * kTtGroup);  // the ancestor sets
+        mine = 0ull;
+        if (gt < n_nodes) {
+          const int last = min(row0 + N, n_nodes * p.group);
+          for (int node = row0 / p.group; node * p.group < last; ++node) {
+            const int r0 = max(node * p.group - row0, 0), r1 = min((node + 1) * p.group - row0, N);
+            if ((anc[node] >> gt) & 1ull) mine |= (r1 - r0 == 64 ? ~0ull : (1ull << (r1 - r0)) - 1ull) << r0;
+          }
+        }
+      }
       const uint32_t ts = tl + (t & 1) * N;
       mbar_wait_compact(&s_full[2 * grp + (t & 1)], (t >> 1) & 1, abort_flag, p.status);
       tc_fence_after();
@@ -277,21 +304,50 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           }
         }
       };
-      scores();
-      bool move = t == 0;
-      if (t > 0) {
+      auto masked_scores = [&]() {
+        scores();
+        if (keys < kTtTile) {
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            float lo, hi;
+            unpack2(d[i], lo, hi);
+            d[i] = pack2((mine >> (2 * i)) & 1ull ? lo : -INFINITY, (mine >> (2 * i + 1)) & 1ull ? hi : -INFINITY);
+          }
+        }
+      };
+      bool move = false;
+      if (t == 0) {
+        if (is_draft) {
+          move = true;  // no key that every row sees
+        } else {
+          if (gw == 0) {
+#pragma unroll 1
+            for (int x = 0; x < N; x += 16) {
+              uint32_t r[16];
+              tmem_ld16(ts + x, r);
+              if (lane == 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  const float z = __uint_as_float(r[i]) * zs;
+                  nref[x + i] = -z;
+                  move |= !(fabsf(z) < INFINITY);
+                }
+              }
+            }
+          }
+          named_bar_sync(bar, kTtGroup);
+        }
+      }
+      masked_scores();
+      {
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
           float lo, hi;
           unpack2(d[i], lo, hi);
-          if (kDraft) {
-            if (!((mine >> (2 * i)) & 1ull)) lo = -INFINITY;
-            if (!((mine >> (2 * i + 1)) & 1ull)) hi = -INFINITY;
-          }
           top = max3(top, lo, hi);
         }
-        move = held && top > kTtMoveReference;
+        move |= top > kTtMoveReference;
       }
       if (tt_any(move, bar)) {
         // new references: the tile's maxima where they are larger
@@ -300,7 +356,7 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           uint32_t r[16];
           float v[16];
           tmem_ld16(ts + x, r);
-          const uint32_t m = !held ? 0u : (kDraft ? (uint32_t)(mine >> x) : 0xffffu);
+          const uint32_t m = (uint32_t)(mine >> x);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = (m >> i) & 1u ? __uint_as_float(r[i]) * zs : -INFINITY;
           const float top = tt_lanes_reduce<true>(v, lane);
@@ -335,60 +391,54 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           }
           tmem_st_wait();
         }
-        scores();
+        masked_scores();
       }
-      if (kDraft) {
-        // the ring, where the drafts' probabilities go, is free once every group's products have read it
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-          mbar_wait_compact(&s_full[2 * w + (t & 1)], (t >> 1) & 1, abort_flag, p.status);
-          if (nt > 0) mbar_wait_compact(&pv_done[2 * w + ((nt - 1) & 1)], ((nt - 1) >> 1) & 1, abort_flag, p.status);
+      wait_pv(t - Sh::kPBufs);  // the operand's place is free
+      if (is_draft) {
+        // a thread looks at one dimension of the drafted values
+        mbar_wait_compact(&full[(2 * nt + 1) % kStages], ((2 * nt + 1) / kStages) & 1, abort_flag, p.status);
+        bool fine = true;
+        if (gt < D) {
+#pragma unroll 4
+          for (int j = 0; j < n_nodes; ++j) fine &= (drafted_value(j) & 0x7f80u) != 0x7f80u;
         }
-      } else {
-        wait_pv(t - Sh::kPBufs);  // the operand's place is free
+        by_hand = tt_any(!fine, bar);
+        if (gt == 0) *odd = by_hand;
+        if (by_hand) {
+          // the places of the ring where the probabilities go are free once every group's products have read them
+#pragma unroll
+          for (int w = 0; w < W; ++w) {
+            mbar_wait_compact(&s_full[2 * w + (t & 1)], (t >> 1) & 1, abort_flag, p.status);
+            if (nt > 0) mbar_wait_compact(&pv_done[2 * w + ((nt - 1) & 1)], ((nt - 1) >> 1) & 1, abort_flag, p.status);
+          }
+        }
       }
       char *prow_p = pbuf + (t % Sh::kPBufs) * Sh::kP + prow * 128;
 #pragma unroll
       for (int x = 0; x < N; x += 8) {
-        f32x2 e[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          e[i] = exp2_mufu2(d[x / 2 + i]);
-          if (kDraft) {
-            float lo, hi;
-            unpack2(e[i], lo, hi);
-            e[i] = pack2((mine >> (x + 2 * i)) & 1ull ? lo : 0.f, (mine >> (x + 2 * i + 1)) & 1ull ? hi : 0.f);
-          } else if (ragged && !held) {
-            e[i] = pack2(0.f, 0.f);
-          }
-          l[x / 2 + i] = add2(l[x / 2 + i], e[i]);
-        }
         float f[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) unpack2(e[i], f[2 * i], f[2 * i + 1]);
-        if (kDraft) {
-          if (gt < kTreeMaxNodes) {
-            *reinterpret_cast<float4 *>(pd + gt * N + x) = make_float4(f[0], f[1], f[2], f[3]);
-            *reinterpret_cast<float4 *>(pd + gt * N + x + 4) = make_float4(f[4], f[5], f[6], f[7]);
-          }
-        } else {
-          *reinterpret_cast<uint4 *>(prow_p + (((pc0 + x / 8) ^ (prow & 7)) << 4)) =
-              make_uint4(tt_pack(f[0], f[1]), tt_pack(f[2], f[3]), tt_pack(f[4], f[5]), tt_pack(f[6], f[7]));
+        for (int i = 0; i < 4; ++i) {
+          // (two groups: of eight pairs two on the FMA pipe, the exponential unit being the limit otherwise)
+          const f32x2 e = W == 2 && ((x / 2 + i) & 7) < 2 ? exp2_poly2(d[x / 2 + i]) : exp2_mufu2(d[x / 2 + i]);
+          l[x / 2 + i] = add2(l[x / 2 + i], e);
+          unpack2(e, f[2 * i], f[2 * i + 1]);
+        }
+        *reinterpret_cast<uint4 *>(prow_p + (((pc0 + x / 8) ^ (prow & 7)) << 4)) =
+            make_uint4(tt_pack(f[0], f[1]), tt_pack(f[2], f[3]), tt_pack(f[4], f[5]), tt_pack(f[6], f[7]));
+        if (by_hand && gt < kTreeMaxNodes) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) pd[gt * N + x + i] = (mine >> (x + i)) & 1ull ? f[i] : 0.f;
         }
       }
-      if (!kDraft) {
-        fence_async_smem();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_ready[2 * grp + (t & 1)]);
-      }
-    };
-#pragma unroll 1
-    for (int t = 0; t < nt; ++t) tile(t, std::false_type{});
-    if (drafts) tile(nt, std::true_type{});
+      fence_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_ready[2 * grp + (t & 1)]);
+    }
 
     // ---------------------------------------------------------------- the sums over the lanes, then a dimension per lane
-    wait_pv(nt - 1);
+    wait_pv(ns - 1);
     tc_fence_after();
     named_bar_sync(bar, kTtGroup);  // red is free, pd complete
 #pragma unroll
@@ -416,69 +466,39 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
     }
     named_bar_sync(bar, kTtGroup);
     if (gw * 32 < D) {
-      if (drafts) mbar_wait_compact(&full[(2 * nt + 1) % kStages], ((2 * nt + 1) / kStages) & 1, abort_flag, p.status);
-      const char *vcol = vn + (gt >> 6) * kBlock + (gt & 7) * 2;  // dimension gt of the drafted values
-      const int vch = (gt & 63) >> 3;
 #pragma unroll 1
       for (int x = 0; x < rows; x += 16) {
-        f32x2 o[8];
-        if (nt > 0) {
+        float o[16];
+        if (nt > 0 || (drafts && !by_hand)) {
           uint32_t r[16];
           tmem_ld16(tl + 2 * N + x, r);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = pack2u(r[2 * i], r[2 * i + 1]);
+          for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(r[i]);
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = pack2(0.f, 0.f);
+          for (int i = 0; i < 16; ++i) o[i] = 0.f;
         }
-        if (drafts) {
-#pragma unroll 4
-          for (int j = 0; j < n_nodes; ++j) {
-            const float v = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(vcol + j * 128 + ((vch ^ (j & 7)) << 4)));
-            const float4 *e4 = reinterpret_cast<const float4 *>(pd + j * N + x);
-            if (__all_sync(0xffffffffu, fabsf(v) < INFINITY)) {
-              const f32x2 v2 = pack2(v, v);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float4 e = e4[i];
-                o[2 * i] = fma2(pack2(e.x, e.y), v2, o[2 * i]);
-                o[2 * i + 1] = fma2(pack2(e.z, e.w), v2, o[2 * i + 1]);
-              }
-            } else {  // only the rows that see the node
+        if (by_hand) {
 #pragma unroll 1
-              for (int i = 0; i < 8; ++i) {
-                const float2 e = *reinterpret_cast<const float2 *>(pd + j * N + x + 2 * i);
+          for (int j = 0; j < n_nodes; ++j) {
+            const float v = __uint_as_float(drafted_value(j) << 16);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  if (k != i) continue;
-                  float lo, hi;
-                  unpack2(o[k], lo, hi);
-                  if (e.x != 0.f) lo = fmaf(e.x, v, lo);
-                  if (e.y != 0.f) hi = fmaf(e.y, v, hi);
-                  o[k] = pack2(lo, hi);
-                }
-              }
+            for (int i = 0; i < 16; ++i) {
+              const float e = pd[j * N + x + i];
+              if (e != 0.f) o[i] = fmaf(e, v, o[i]);
             }
           }
         }
         if (p.splits > 1) {
           float *dst = p.part_o + (((size_t)u * p.splits + split) * p.rows + row0 + x) * D + gt;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float lo, hi;
-            unpack2(o[i], lo, hi);
-            if (x + 2 * i < rows) dst[(size_t)(2 * i) * D] = lo;
-            if (x + 2 * i + 1 < rows) dst[(size_t)(2 * i + 1) * D] = hi;
-          }
+          for (int i = 0; i < 16; ++i)
+            if (x + i < rows) dst[(size_t)i * D] = o[i];
         } else {
           __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(p.out) + ((size_t)u * p.rows + row0 + x) * D + gt;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float lo, hi;
-            unpack2(o[i], lo, hi);
-            if (x + 2 * i < rows) dst[(size_t)(2 * i) * D] = __float2bfloat16_rn(lo * alpha[x + 2 * i]);
-            if (x + 2 * i + 1 < rows) dst[(size_t)(2 * i + 1) * D] = __float2bfloat16_rn(hi * alpha[x + 2 * i + 1]);
-          }
+          for (int i = 0; i < 16; ++i)
+            if (x + i < rows) dst[(size_t)i * D] = __float2bfloat16_rn(o[i] * alpha[x + i]);
         }
       }
     }
