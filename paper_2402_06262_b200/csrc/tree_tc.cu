@@ -516,7 +516,7 @@ struct TtPlan {
 TtPlan tree_tc_plan(int rows) {
   if (rows <= 16) return {16, 1, 2};
   if (rows <= 32) return {32, 1, 2};
-  if (rows <= 64) return {64, 1, 2};
+  if (rows <= 64) return {32, 2, 1};
   return {64, 2, 1};
 }
 int tree_tc_rows(int rows) { const TtPlan t = tree_tc_plan(rows); return t.n * t.w; }
@@ -542,8 +542,7 @@ template <int D>
 roco_status tree_tc_d(const TreeParams &p, int U, cudaStream_t stream) {
   const TtPlan t = tree_tc_plan(p.rows);
   if (t.n == 16) return tree_tc_t<D, 16, 1, 2>(p, U, stream);
-  if (t.n == 32) return tree_tc_t<D, 32, 1, 2>(p, U, stream);
-  if (t.w == 1) return tree_tc_t<D, 64, 1, 2>(p, U, stream);
+  if (t.n == 32) return t.w == 1 ? tree_tc_t<D, 32, 1, 2>(p, U, stream) : tree_tc_t<D, 32, 2, 1>(p, U, stream);
   return tree_tc_t<D, 64, 2, 1>(p, U, stream);
 }
 
