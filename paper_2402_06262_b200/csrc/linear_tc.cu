@@ -38,17 +38,26 @@ constexpr int kLtThreads = (kLtMmaWarp + 1) * 32;
 constexpr int kLtSplits = 3;          // bf16 terms of a decayed key
 constexpr int kLtPiece = 32;          // tokens whose keys are split at a time
 constexpr int kLtPieceCols = kLtSplits * kLtPiece / 2;
-constexpr uint32_t kLtColS = 0, kLtColO = 128, kLtColDS = 256, kLtColK = 384, kLtTmemCols = 512;
-static_assert(kLtColK + 2 * kLtPieceCols <= kLtTmemCols, "tensor memory");
+constexpr uint32_t kLtColS = 0, kLtColO = 128, kLtTmemCols = 512;
+
+// What a launch that only forms states has room for besides: a buffer per piece of a chunk and two accumulators DS, so that
+// no group waits for a product of the chunk it works on, and three slots of tiles.
+template <bool kStates>
+struct LtPlan {
+  static constexpr int kSlots = kStates ? 3 : 2, kPieceBufs = kStates ? 4 : 2;
+  static constexpr uint32_t kColK = kStates ? 256 : 384;
+  __device__ static constexpr uint32_t col_ds(int c) { return kStates ? (uint32_t)(c & 1) * 128 : 256; }
+  static_assert(kColK + kPieceBufs * kLtPieceCols <= kLtTmemCols, "tensor memory");
+};
 
 template <int D>
 struct LtSmem {
   static constexpr int kTile = kLtChunk * D * 2;
   static constexpr int kSop = D * D * 2;
-  static constexpr int kBars = 28;
+  static constexpr int kBars = 32;
   static constexpr int kTables = 256 + 128 + 32;
   static constexpr size_t bytes(bool states) {
-    return 1024 + (size_t)kTile * (states ? 4 : 6) + (states ? 0 : kSop) + kTables * 4 + kBars * 8 + 16;
+    return 1024 + (size_t)kTile * 6 + (states ? 0 : kSop) + kTables * 4 + kBars * 8 + 16;
   }
 };
 
@@ -91,14 +100,16 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                              const __grid_constant__ CUtensorMap mapV, const __grid_constant__ CUtensorMap mapO,
                              const LinearParams p) {
   constexpr int kTile = LtSmem<D>::kTile, kBlock = kLtChunk * 128;  // a 64-column block of a tile: 128 rows of 128 bytes
+  using Plan = LtPlan<kStates>;
+  constexpr int kSlots = Plan::kSlots, kPieceBufs = Plan::kPieceBufs;
   constexpr int kHalfCols = D / 2;                                  // columns of the state or output a thread works on
   constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);       // bf16, fp32 accumulator, M = 128
   constexpr uint32_t kIdescS = kIdesc | ((128u >> 3) << 17);                         // N = 128, both K-major
   constexpr uint32_t kIdescV = kIdesc | (((uint32_t)D >> 3) << 17) | (1u << 16);     // N = D, B with N contiguous
   extern __shared__ char lt_raw[];
   char *at = smem_align(lt_raw, 1024);
-  char *kt = at; at += 2 * kTile;
-  char *vt = at; at += 2 * kTile;
+  char *kt = at; at += kSlots * kTile;
+  char *vt = at; at += kSlots * kTile;
   char *qt = at; if (!kStates) at += 2 * kTile;
   char *sop = at; if (!kStates) at += LtSmem<D>::kSop;
   float *ptab = reinterpret_cast<float *>(at);  // ptab[128 + n] = scale g^n, 0 for n < 0
@@ -106,10 +117,11 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   float *ctab = ktab + 128;                     // ctab[e] = g^(31 - e)
   at += LtSmem<D>::kTables * 4;
   uint64_t *bars = reinterpret_cast<uint64_t *>(at); at += LtSmem<D>::kBars * 8;
-  uint64_t *full = bars, *kv_empty = bars + 2, *q_full = bars + 4;  // per slot: keys and values landed, used up; queries
-  uint64_t *s1_full = bars + 12, *o1_full = bars + 14, *o_scaled = bars + 15, *o_full = bars + 16;
-  uint64_t *o_free = bars + 17, *sop_ready = bars + 18, *ds_full = bars + 19, *ds_free = bars + 20, *staged = bars + 21;
-  uint64_t *kp_ready = bars + 22, *kp_free = bars + 24;
+  uint64_t *full = bars, *kv_empty = bars + 3, *q_full = bars + 6;  // per slot: keys and values landed, used up; queries
+  uint64_t *kp_ready = bars + 8, *kp_free = bars + 12;              // per piece buffer; per piece of a chunk
+  uint64_t *ds_full = bars + 16, *ds_free = bars + 18;              // per chunk parity
+  uint64_t *s1_full = bars + 20, *o1_full = bars + 21, *o_scaled = bars + 22, *o_full = bars + 23;
+  uint64_t *o_free = bars + 24, *sop_ready = bars + 25, *staged = bars + 26;
   uint32_t *tmem_base = reinterpret_cast<uint32_t *>(at);
   int *abort_ptr = reinterpret_cast<int *>(at + 8);
   volatile int *abort_flag = abort_ptr;
@@ -118,7 +130,11 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // uniform for the compiler too, and so is what follows
   const int segs = kStates ? p.segments - 1 : p.segments, seg = blockIdx.x % segs, u = blockIdx.x / segs;
   const int len = __shfl_sync(0xffffffffu, linear_len(p, u / p.G, tid == 0 && seg == 0 && (kStates || p.segments == 1)), 0);
-  if (len == 0) return;
+  if (kStates) launch_dependents();
+  if (len == 0) {
+    if (!kStates) wait_for_launch_before();
+    return;
+  }
   const int n_chunks = (len + kLtChunk - 1) / kLtChunk;
   const int first = linear_segment(n_chunks, p.segments, seg), last = linear_segment(n_chunks, p.segments, seg + 1);
   const int n = last - first;
@@ -126,14 +142,11 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   const double logd = (double)p.log_decay[u % p.G];
 
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&full[i], 2); mbar_init(&kv_empty[i], 1); mbar_init(&q_full[i], 1);
-    }
-    mbar_init(s1_full, 1); mbar_init(o1_full, 1); mbar_init(o_scaled, kLtAWarps);
-    mbar_init(o_full, 1); mbar_init(o_free, kLtAWarps); mbar_init(sop_ready, kLtBWarps); mbar_init(ds_full, 1);
-    mbar_init(ds_free, kLtBWarps); mbar_init(staged, kLtAWarps);
-    for (int i = 0; i < 2; ++i) mbar_init(&kp_ready[i], kLtBWarps);
-    for (int i = 0; i < 4; ++i) mbar_init(&kp_free[i], 1);
+    for (int i = 0; i < kSlots; ++i) { mbar_init(&full[i], 2); mbar_init(&kv_empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&q_full[i], 1); mbar_init(&ds_full[i], 1); mbar_init(&ds_free[i], kLtBWarps); }
+    for (int i = 0; i < 4; ++i) { mbar_init(&kp_ready[i], kLtBWarps); mbar_init(&kp_free[i], 1); }
+    mbar_init(s1_full, 1); mbar_init(o1_full, 1); mbar_init(o_scaled, kLtAWarps); mbar_init(o_full, 1);
+    mbar_init(o_free, kLtAWarps); mbar_init(sop_ready, kLtBWarps); mbar_init(staged, kLtAWarps);
     *abort_ptr = 0;
     mbar_init_fence();
   }
@@ -155,11 +168,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   // the first eight tokens, 2 and 3 of the next eight.)
   const int lm_tok = ((lane >> 4) & 1) * 8 + (lane & 7), lm_ch = (lane >> 3) & 1;
   auto split_keys = [&](int c, int q) {
-    const int wq = warp & 3, half = (warp >> 2) & 1, bf = q & 1, nt = c == n - 1 ? tail : kLtChunk;
-    const char *ktile = kt + (c & 1) * kTile + (wq >> 1) * kBlock;
-    // the buffer's last piece is used up: two pieces back (one barrier per piece of a chunk, so that whoever waits on one
-    // waits for each of its phases in turn)
-    if (c > 0 || q >= 2) mbar_wait_compact(&kp_free[q ^ 2], (q >= 2 ? c : c - 1) & 1, abort_flag, p.status);
+    const int wq = warp & 3, half = (warp >> 2) & 1, bf = q % kPieceBufs, nt = c == n - 1 ? tail : kLtChunk;
+    const char *ktile = kt + c % kSlots * kTile + (wq >> 1) * kBlock;
+    // the buffer's last piece is used up (one barrier per piece of a chunk, so that whoever waits on one waits for each of
+    // its phases in turn)
+    if (kPieceBufs == 4) {
+      if (c > 0) mbar_wait_compact(&kp_free[q], (c - 1) & 1, abort_flag, p.status);
+    } else if (c > 0 || q >= 2) {
+      mbar_wait_compact(&kp_free[q ^ 2], (q >= 2 ? c : c - 1) & 1, abort_flag, p.status);
+    }
     if (wq * 32 < D) {  // d = 64: the upper two lane quarters hold no rows
       const int t0 = q * kLtPiece + half * 16, tok = t0 + 2 * (lane & 3), tr = t0 + lm_tok;
       uint32_t r[2][4];
@@ -168,30 +185,36 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         const int ch = (wq & 1) * 4 + 2 * h + lm_ch;
         lt_ldsm_t(smem_u32(ktile + tr * 128 + ((ch ^ (tr & 7)) << 4)), r[h]);
       }
-      float w[4];
+      f32x2 w2[2];
 #pragma unroll
-      for (int x = 0; x < 4; ++x) w[x] = ktab[min(tok + (x >> 1) * 8 + (x & 1) + kLtChunk - nt, kLtChunk - 1)];
+      for (int x = 0; x < 2; ++x) {
+        const int at = tok + 8 * x + kLtChunk - nt;
+        w2[x] = pack2(ktab[min(at, kLtChunk - 1)], ktab[min(at + 1, kLtChunk - 1)]);
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t k1[4], k2[4], k3[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-          const int x = m & 2;
+          const int x = m & 2;  // (blocks 2 and 3 are eight tokens further)
           if (nt < kLtChunk) {  // tokens behind the last may hold anything
             if (tok + 4 * x >= nt) r[h][m] &= 0xffff0000u;
             if (tok + 4 * x + 1 >= nt) r[h][m] &= 0x0000ffffu;
           }
           // cut, not rounded: the upper halves of an fp32, of what they leave, and of what those leave are all its 24 bits
-          float a = __uint_as_float(r[h][m] << 16) * w[x], b = __uint_as_float(r[h][m] & 0xffff0000u) * w[x + 1];
+          const f32x2 minus = pack2(-1.f, -1.f);
+          f32x2 f = mul2(pack2u(r[h][m] << 16, r[h][m] & 0xffff0000u), w2[m >> 1]);
+          float a, b;
+          unpack2(f, a, b);
           k1[m] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-          a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
-          b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+          f = fma2(pack2u(__float_as_uint(a) & 0xffff0000u, __float_as_uint(b) & 0xffff0000u), minus, f);
+          unpack2(f, a, b);
           k2[m] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-          a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
-          b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+          f = fma2(pack2u(__float_as_uint(a) & 0xffff0000u, __float_as_uint(b) & 0xffff0000u), minus, f);
+          unpack2(f, a, b);
           k3[m] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
         }
-        const uint32_t to = tmem + ((uint32_t)(wq * 32 + 16 * h) << 16) + kLtColK + (uint32_t)(bf * kLtPieceCols + half * 8);
+        const uint32_t to = tmem + ((uint32_t)(wq * 32 + 16 * h) << 16) + Plan::kColK + (uint32_t)(bf * kLtPieceCols + half * 8);
         lt_st_16x8(to, k1);
         lt_st_16x8(to + kLtPiece / 2, k2);
         lt_st_16x8(to + kLtPiece, k3);
@@ -206,16 +229,16 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   if (warp == kLtTmaWarp) {
     if (lane == 0) {
       for (int c = 0; c < n + 2; ++c) {
-        const int sl = c & 1, row = (first + c) * kLtChunk;
-        auto load = [&](char *tiles, const CUtensorMap *map, uint64_t *bar) {
+        const int sl = c % kSlots, row = (first + c) * kLtChunk;
+        auto load = [&](char *tiles, int sl, const CUtensorMap *map, uint64_t *bar) {
           mbar_expect_tx(bar, kTile);
 #pragma unroll
           for (int h = 0; h < D / 64; ++h) tma_load_3d(tiles + sl * kTile + h * kBlock, map, 64 * h, row, u, bar);
         };
         if (c < n) {
-          if (c >= 2) mbar_wait_compact(&kv_empty[sl], ((c >> 1) - 1) & 1, abort_flag, p.status);
-          load(kt, &mapK, &full[sl]);
-          load(vt, &mapV, &full[sl]);
+          if (c >= kSlots) mbar_wait_compact(&kv_empty[sl], (c / kSlots - 1) & 1, abort_flag, p.status);
+          load(kt, sl, &mapK, &full[sl]);
+          load(vt, sl, &mapV, &full[sl]);
         }
         if (!kStates) {
           // the output of the chunk before the last leaves its slot, which then takes the queries of this one (a partial
@@ -223,11 +246,11 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           if (c >= 2 && !(c - 2 == n - 1 && tail < kLtChunk)) {
             mbar_wait_compact(staged, c & 1, abort_flag, p.status);
 #pragma unroll
-            for (int h = 0; h < D / 64; ++h) tma_store_3d(&mapO, qt + sl * kTile + h * kBlock, 64 * h, row - 2 * kLtChunk, u);
+            for (int h = 0; h < D / 64; ++h) tma_store_3d(&mapO, qt + (c & 1) * kTile + h * kBlock, 64 * h, row - 2 * kLtChunk, u);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
           }
-          if (c < n) load(qt, &mapQ, &q_full[sl]);
+          if (c < n) load(qt, c & 1, &mapQ, &q_full[c & 1]);
         }
       }
       if (!kStates) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -235,10 +258,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   } else if (warp == kLtMmaWarp) {
     // (The accumulators sit at fixed columns: the allocation is all of tensor memory.  The pieces are kept as a loop: the
     // roles' code together has to stay in the instruction cache.)
-    auto tile = [&](char *tiles, int c) { return tiles + (c & 1) * kTile; };
+    auto tile = [&](char *tiles, int c) { return tiles + c % kSlots * kTile; };
     auto scores = [&](int c) {  // S1 (the product that read P from these columns was issued before it)
-      const char *k = tile(kt, c), *q = tile(qt, c);
-      mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+      const char *k = tile(kt, c), *q = qt + (c & 1) * kTile;
+      mbar_wait_compact(&full[c % kSlots], (c / kSlots) & 1, abort_flag, p.status);
       if (c == n - 1 && tail < kLtChunk) {
         // rows behind the prompt may hold anything: their scores are multiplied by zero, and so are their values
         for (int w = lane; w < (kLtChunk - tail) * 8; w += 32) {
@@ -266,14 +289,18 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     for (int c = 0; c < n; ++c) {
       const uint32_t par = c & 1;
       const char *v = tile(vt, c);
-      if (c > 0) mbar_wait_compact(ds_free, (c - 1) & 1, abort_flag, p.status);
+      // the accumulator's last sum has been read
+      if (kStates ? c > 1 : c > 0) {
+        const int cb = kStates ? c - 2 : c - 1;
+        mbar_wait_compact(&ds_free[cb & 1], (cb >> 1) & 1, abort_flag, p.status);
+      }
 #pragma unroll 1
       for (int q4 = 0; q4 < 4; ++q4) {
         if (!kStates && q4 == 2) {
           mbar_wait_compact(sop_ready, par, abort_flag, p.status);
           if (c > 0) mbar_wait_compact(o_free, (c - 1) & 1, abort_flag, p.status);
           tc_fence_after();
-          const char *q = tile(qt, c);
+          const char *q = qt + (c & 1) * kTile;
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)  // O = Q S
             umma_bf16_w(kLtColO, smem_desc_sw128(q + (kk / 4) * kBlock + (kk % 4) * 32),
@@ -281,15 +308,15 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           umma_commit_w(o1_full);
         }
         // DS, a piece of 32 tokens
-        mbar_wait_compact(&kp_ready[q4 & 1], (2 * c + (q4 >> 1)) & 1, abort_flag, p.status);
+        mbar_wait_compact(&kp_ready[q4 % kPieceBufs], kPieceBufs == 4 ? c & 1 : (2 * c + (q4 >> 1)) & 1, abort_flag, p.status);
         tc_fence_after();
 #pragma unroll
         for (int x = 0; x < 2 * kLtSplits; ++x)  // term x >> 1, tokens 16 (x & 1) .. of the piece
-          umma_bf16_ts_w(kLtColDS, kLtColK + (uint32_t)((q4 & 1) * kLtPieceCols + 8 * x),
+          umma_bf16_ts_w(Plan::col_ds(c), Plan::kColK + (uint32_t)(q4 % kPieceBufs * kLtPieceCols + 8 * x),
                          smem_desc_sw128_mn(v + (2 * q4 + (x & 1)) * 2048, kBlock), kIdescV, (q4 > 0 || x > 0) ? 1u : 0u);
         umma_commit_w(&kp_free[q4]);
       }
-      umma_commit_w(ds_full);
+      umma_commit_w(&ds_full[c & 1]);
       if (!kStates) {
         mbar_wait_compact(o_scaled, par, abort_flag, p.status);  // and P, which the same warps wrote before
         tc_fence_after();
@@ -299,14 +326,14 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                          smem_desc_sw128_mn(v + kk * 2048, kBlock), kIdescV, 1u);
         umma_commit_w(o_full);
       }
-      umma_commit_w(&kv_empty[c & 1]);
+      umma_commit_w(&kv_empty[c % kSlots]);
       if (c + 1 < n) scores(c + 1);
     }
   } else if (warp < kLtAWarps) {
     // ---------------------------------------------------------------- A: scores and output, a token per lane
     if (kStates) {
       for (int c = 0; c < n; ++c) {
-        mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+        mbar_wait_compact(&full[c % kSlots], (c / kSlots) & 1, abort_flag, p.status);
 #pragma unroll 1
         for (int q = 2; q < 4; ++q) split_keys(c, q);
       }
@@ -350,7 +377,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           tmem_st16(tl + kLtColS + (uint32_t)(half * 64 + cc * 16), pk);
         }
         tmem_st_wait();
-        mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+        mbar_wait_compact(&full[c % kSlots], (c / kSlots) & 1, abort_flag, p.status);
 #pragma unroll 1
         for (int q = 2; q < 4; ++q) split_keys(c, q);
         mbar_wait_compact(o1_full, par, abort_flag, p.status);
@@ -418,16 +445,18 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     const uint32_t tl = tmem + ((uint32_t)(wq * 32) << 16);
     float *S = p.state + ((size_t)u * D + r0) * D + half * kHalfCols;
     float *part = p.parts + ((size_t)u * p.segments * D + r0) * D + half * kHalfCols;
-    float s[kHalfCols];
+    f32x2 s[kHalfCols / 2];
 #pragma unroll
-    for (int x = 0; x < kHalfCols; ++x) s[x] = 0.f;
+    for (int x = 0; x < kHalfCols / 2; ++x) s[x] = pack2(0.f, 0.f);
+    if (!kStates) wait_for_launch_before();  // the segments' states
     if (mine) {
       if (seg == 0) {
         const float *src = (kStates || p.segments == 1) ? S : part;
 #pragma unroll
         for (int x = 0; x < kHalfCols; x += 4) {
           const float4 f = *reinterpret_cast<const float4 *>(src + x);
-          s[x] = f.x; s[x + 1] = f.y; s[x + 2] = f.z; s[x + 3] = f.w;
+          s[x / 2] = pack2(f.x, f.y);
+          s[x / 2 + 1] = pack2(f.z, f.w);
           if (kStates) *reinterpret_cast<float4 *>(part + x) = f;  // the second launch starts from this copy
         }
       } else if (!kStates) {
@@ -437,8 +466,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
 #pragma unroll
           for (int x = 0; x < kHalfCols; x += 4) {
             const float4 f = *reinterpret_cast<const float4 *>(src + x);
-            s[x] = fmaf(w, f.x, s[x]); s[x + 1] = fmaf(w, f.y, s[x + 1]);
-            s[x + 2] = fmaf(w, f.z, s[x + 2]); s[x + 3] = fmaf(w, f.w, s[x + 3]);
+            s[x / 2] = fma2(pack2(w, w), pack2(f.x, f.y), s[x / 2]);
+            s[x / 2 + 1] = fma2(pack2(w, w), pack2(f.z, f.w), s[x / 2 + 1]);
           }
         }
       }
@@ -446,26 +475,30 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     const Decay2 g_chunk(decay_pow(logd, kLtChunk)), g_tail(decay_pow(logd, tail));
     for (int c = 0; c <= n; ++c) {
       if (c < n) {
-        mbar_wait_compact(&full[c & 1], (c >> 1) & 1, abort_flag, p.status);
+        mbar_wait_compact(&full[c % kSlots], (c / kSlots) & 1, abort_flag, p.status);
 #pragma unroll 1
         for (int q = 0; q < 2; ++q) split_keys(c, q);
       }
       if (c > 0) {  // the state behind the chunk before
-        mbar_wait_compact(ds_full, (c - 1) & 1, abort_flag, p.status);
+        mbar_wait_compact(&ds_full[(c - 1) & 1], ((c - 1) >> 1) & 1, abort_flag, p.status);
         tc_fence_after();
         if (mine) {
-          const float hi = c == n ? g_tail.hi : g_chunk.hi, lo = c == n ? g_tail.lo : g_chunk.lo;
+          const Decay2 &g = c == n ? g_tail : g_chunk;
+          const f32x2 hi = pack2(g.hi, g.hi), lo = pack2(g.lo, g.lo);
 #pragma unroll
           for (int x = 0; x < kHalfCols; x += 16) {
             uint32_t r[16];
-            tmem_ld16(tl + kLtColDS + (uint32_t)(half * kHalfCols + x), r);
+            tmem_ld16(tl + Plan::col_ds(c - 1) + (uint32_t)(half * kHalfCols + x), r);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[x + e] = fmaf(hi, s[x + e], fmaf(lo, s[x + e], __uint_as_float(r[e])));
+            for (int e = 0; e < 16; e += 2) {
+              f32x2 &v = s[(x + e) / 2];
+              v = fma2(hi, v, fma2(lo, v, pack2u(r[e], r[e + 1])));
+            }
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0 && c < n) mbar_arrive(ds_free);
+        if (lane == 0 && c < n) mbar_arrive(&ds_free[(c - 1) & 1]);
       }
       if (!kStates && c < n) {
         if (c > 0) mbar_wait_compact(o1_full, (c - 1) & 1, abort_flag, p.status);  // the operand before is used up
@@ -476,8 +509,7 @@ __global__ void __launch_bounds__(kLtThreads, 1)
           for (int x = 0; x < kHalfCols; x += 8) {
             const int col = half * kHalfCols + x, ch = (col & 63) >> 3;
             *reinterpret_cast<uint4 *>(row + (col >> 6) * (D * 128) + ((ch ^ (r0 & 7)) << 4)) =
-                make_uint4(lt_pack(s[x], s[x + 1]), lt_pack(s[x + 2], s[x + 3]), lt_pack(s[x + 4], s[x + 5]),
-                           lt_pack(s[x + 6], s[x + 7]));
+                make_uint4(lt_pack2(s[x / 2]), lt_pack2(s[x / 2 + 1]), lt_pack2(s[x / 2 + 2]), lt_pack2(s[x / 2 + 3]));
           }
         }
         fence_async_smem();
@@ -488,8 +520,12 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     if (mine && (kStates || seg == p.segments - 1)) {
       float *dst = kStates ? part + (size_t)(seg + 1) * D * D : S;
 #pragma unroll
-      for (int x = 0; x < kHalfCols; x += 4)
-        *reinterpret_cast<float4 *>(dst + x) = make_float4(s[x], s[x + 1], s[x + 2], s[x + 3]);
+      for (int x = 0; x < kHalfCols; x += 4) {
+        float4 f;
+        unpack2(s[x / 2], f.x, f.y);
+        unpack2(s[x / 2 + 1], f.z, f.w);
+        *reinterpret_cast<float4 *>(dst + x) = f;
+      }
     }
   }
   tc_fence_before();
@@ -511,7 +547,10 @@ roco_status linear_prefill_tc_t(const LinearParams &p, int U, cudaStream_t strea
   static SmemLimit limit_states, limit_whole;
   if (!limit_states((const void *)states, kB1) || !limit_whole((const void *)whole, kB0)) return ROCO_ERR_CUDA;
   if (p.segments > 1) states<<<(unsigned)U * (unsigned)(p.segments - 1), kLtThreads, kB1, stream>>>(mq, mk, mv, mo, p);
-  whole<<<(unsigned)U * (unsigned)p.segments, kLtThreads, kB0, stream>>>(mq, mk, mv, mo, p);
+  if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
+  const unsigned blocks = (unsigned)U * (unsigned)p.segments;
+  if (p.segments > 1) return launch_overlapped(whole, blocks, kLtThreads, kB0, stream, mq, mk, mv, mo, p) ? ROCO_OK : ROCO_ERR_CUDA;
+  whole<<<blocks, kLtThreads, kB0, stream>>>(mq, mk, mv, mo, p);
   return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
 }
 
