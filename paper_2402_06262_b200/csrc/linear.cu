@@ -108,8 +108,12 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
   const int tid = threadIdx.x;
   const int slab = blockIdx.x % kSlabs, segs = kStates ? p.segments - 1 : p.segments;
   const int seg = blockIdx.x / kSlabs % segs, u = blockIdx.x / (kSlabs * segs), c0 = slab * kLpCols;
+  if (kStates) launch_dependents();
   const int len = linear_len(p, u / p.G, tid == 0 && slab == 0 && seg == 0 && (kStates || p.segments == 1));
-  if (len == 0) return;
+  if (len == 0) {
+    if (!kStates) wait_for_launch_before();
+    return;
+  }
   const int n_chunks = (len + kLpChunk - 1) / kLpChunk;
   const int first = linear_segment(n_chunks, p.segments, seg), last = linear_segment(n_chunks, p.segments, seg + 1);
   const double logd = (double)p.log_decay[u % p.G];
@@ -120,6 +124,7 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
   float4 s[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!kStates) wait_for_launch_before();  // the segments' states
   if (seg == 0) {
     const float *src = (p.segments == 1 || kStates) ? S : part;
 #pragma unroll
@@ -144,39 +149,53 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
   const T *V = reinterpret_cast<const T *>(p.V) + (size_t)u * p.Lmax * D + c0;
   T *O = reinterpret_cast<T *>(p.out) + (size_t)u * p.Lmax * D + c0;
   const int row = tid >> 3, col = (tid & 7) * 4;  // this thread's token and columns (col, col + 32) of the output
+  const Decay2 g_chunk(decay_pow(logd, kLpChunk)), g_tail(decay_pow(logd, len - (n_chunks - 1) * kLpChunk));
+  // A chunk's loads are issued while the one before is worked on.  Tokens behind the last are zeros: they add nothing to
+  // the sums, and their own rows are not written.
+  constexpr int kPieces = kLpChunk * D / kEPC / kLpThreads, kVPieces = kLpChunk * kLpCols / kEPC / kLpThreads;
+  static_assert(kPieces >= 1 && kVPieces >= 1, "a piece of 16 bytes per thread");
+  uint4 qv[kPieces], kv[kPieces], vv[kVPieces];
+  auto load = [&](int c) {
+    const int t0 = c * kLpChunk;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int w = tid + i * kLpThreads, t = t0 + w / (D / kEPC), x = w % (D / kEPC) * kEPC;
+      qv[i] = kv[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (t < len) {
+        if (!kStates) qv[i] = *reinterpret_cast<const uint4 *>(Q + (size_t)t * D + x);
+        kv[i] = *reinterpret_cast<const uint4 *>(K + (size_t)t * D + x);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kVPieces; ++i) {
+      const int w = tid + i * kLpThreads, t = t0 + w / (kLpCols / kEPC), x = w % (kLpCols / kEPC) * kEPC;
+      vv[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (t < len) vv[i] = *reinterpret_cast<const uint4 *>(V + (size_t)t * D + x);
+    }
+  };
+  auto put = [&](float *dst, const uint4 &x) {
+    float f[kEPC];
+    Elem<T>::unpack(x, f);
+#pragma unroll
+    for (int e = 0; e < kEPC; e += 4) *reinterpret_cast<float4 *>(dst + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+  };
+  if (first < last) load(first);
 #pragma unroll 1
   for (int c = first; c < last; ++c) {
     const int t0 = c * kLpChunk, nt = len - t0 < kLpChunk ? len - t0 : kLpChunk;
     __syncthreads();  // the chunk before is used up
-    // tokens behind the last are zeros: they add nothing to the sums, and their own rows are not written
 #pragma unroll
-    for (int w = tid; w < kLpChunk * D / kEPC; w += kLpThreads) {
-      const int t = w / (D / kEPC), x = w % (D / kEPC) * kEPC;
-      uint4 qv = make_uint4(0u, 0u, 0u, 0u), kv = qv;
-      if (t < nt) {
-        if (!kStates) qv = *reinterpret_cast<const uint4 *>(Q + (size_t)(t0 + t) * D + x);
-        kv = *reinterpret_cast<const uint4 *>(K + (size_t)(t0 + t) * D + x);
-      }
-      float f[kEPC];
-      if (!kStates) {
-        Elem<T>::unpack(qv, f);
-#pragma unroll
-        for (int e = 0; e < kEPC; ++e) sm.q[t][x + e] = f[e];
-      }
-      Elem<T>::unpack(kv, f);
-#pragma unroll
-      for (int e = 0; e < kEPC; ++e) sm.k[t][x + e] = f[e];
+    for (int i = 0; i < kPieces; ++i) {
+      const int w = tid + i * kLpThreads, t = w / (D / kEPC), x = w % (D / kEPC) * kEPC;
+      if (!kStates) put(&sm.q[t][x], qv[i]);
+      put(&sm.k[t][x], kv[i]);
     }
 #pragma unroll
-    for (int w = tid; w < kLpChunk * kLpCols / kEPC; w += kLpThreads) {
-      const int t = w / (kLpCols / kEPC), x = w % (kLpCols / kEPC) * kEPC;
-      uint4 vv = make_uint4(0u, 0u, 0u, 0u);
-      if (t < nt) vv = *reinterpret_cast<const uint4 *>(V + (size_t)(t0 + t) * D + x);
-      float f[kEPC];
-      Elem<T>::unpack(vv, f);
-#pragma unroll
-      for (int e = 0; e < kEPC; ++e) sm.v[t][x + e] = f[e];
+    for (int i = 0; i < kVPieces; ++i) {
+      const int w = tid + i * kLpThreads;
+      put(&sm.v[w / (kLpCols / kEPC)][w % (kLpCols / kEPC) * kEPC], vv[i]);
     }
+    if (c + 1 < last) load(c + 1);
     if (!kStates) {
 #pragma unroll
       for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4 *>(&sm.s[sr0 + i][sc]) = s[i];
@@ -253,7 +272,7 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
         }
       }
     }
-    const Decay2 g(decay_pow(logd, nt));
+    const Decay2 &g = nt == kLpChunk ? g_chunk : g_tail;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       s[i].x = g.madd(s[i].x, add[i].x); s[i].y = g.madd(s[i].y, add[i].y);
@@ -276,16 +295,19 @@ roco_status linear_prefill_simt_t(const LinearParams &p, int U, cudaStream_t str
   static SmemLimit limit_states, limit_whole;
   if (!limit_states((const void *)states, kSmem) || !limit_whole((const void *)whole, kSmem)) return ROCO_ERR_CUDA;
   if (p.segments > 1) states<<<slabs * (unsigned)(p.segments - 1), kLpThreads, kSmem, stream>>>(p);
-  whole<<<slabs * (unsigned)p.segments, kLpThreads, kSmem, stream>>>(p);
+  if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
+  if (p.segments > 1)
+    return launch_overlapped(whole, slabs * (unsigned)p.segments, kLpThreads, kSmem, stream, p) ? ROCO_OK : ROCO_ERR_CUDA;
+  whole<<<slabs, kLpThreads, kSmem, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
 }
 
-// Segments that fill the GPU with two CTAs per SM, none shorter than four chunks: a prompt that is divided is read
+// Segments that fill the GPU with two CTAs per SM, none shorter than two chunks: a prompt that is divided is read
 // twice (its keys and values), which pays only while SMs would be idle.
 int linear_simt_segments(int U, int d, int Lmax, int sms) {
   const long long ctas = (long long)U * (d / kLpCols);
   long long n = 2LL * sms / ctas;
-  const int most = Lmax / (4 * kLpChunk);
+  const int most = Lmax / (2 * kLpChunk);
   if (n > most) n = most;
   if (n > 64) n = 64;
   return n < 2 ? 1 : (int)n;
