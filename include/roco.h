@@ -382,7 +382,7 @@ roco_status roco_decode_step_cluster(roco_cache *cache, const void *q, const voi
  *   nodes        [S] int32 DEVICE array, nodes of each sequence, 0..T; NULL: T everywhere.  Rows of Q, K_new and V_new
  *                at nodes[b] and behind may hold anything, and those rows of attn_out and lse_out are left as they were
  *   T, group     1 <= T <= ROCO_TREE_MAX_NODES, 1 <= group <= ROCO_TREE_MAX_GROUP
- *   attn_out     [S][G][T][group][d];   lse_out [S][G][T][group] fp32, or NULL
+ *   attn_out     [S][G][T][group][d];   lse_out [S][G][T][group] fp32, or NULL;   neither overlaps anything else
  *   workspace    >= roco_tree_attend_workspace_bytes(cache, T, group) device bytes (which may be 0: then NULL will do),
  *                256-byte aligned, of this call alone while it runs
  * What a node does not see has no influence on its row, whatever it holds: empty slots and nodes on other branches may
@@ -415,7 +415,8 @@ roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void 
  *   path         [S][A] int32 DEVICE array of node indices;   path_len [S] int32 DEVICE array, 0..A
  *   A            1 <= A <= ROCO_TREE_MAX_PATH, A <= T, r + A <= B; r >= 0 (ROCO_SCOPE_LOWEST_R: r >= 1)
  *   evicted_slot [S][G][A] freed slots in increasing order, padded with -1;   evicted_pos likewise, or NULL
- * A path_len outside [0, A] or a path that is not a chain of the tree from its root sets ROCO_DEV_BAD_TREE and counts
+ * A path_len outside [0, A] or a path that is not a chain of the tree from its root, every node behind its
+ * parent, sets ROCO_DEV_BAD_TREE and counts
  * as a = 0.  K_new and V_new must not overlap the cache.
  */
 #define ROCO_TREE_MAX_PATH 16
@@ -458,7 +459,7 @@ roco_status roco_linear_prefill(const roco_linear_state *state, const void *Q, c
 
 /*
  * One token for every sequence: state and out as above, one launch that reads and writes the states once.
- *   q, k, v, out [S][G][d]
+ *   q, k, v, out [S][G][d]; out must not overlap q, k or v
  *   active       [S] int32 DEVICE array, or NULL (all): a sequence with 0 keeps its state and its rows of out
  */
 roco_status roco_linear_step(const roco_linear_state *state, const void *q, const void *k, const void *v,

@@ -32,14 +32,16 @@ __global__ void __launch_bounds__(kLsThreads) linear_step_kernel(const LinearPar
   for (int i = 0; i < kRows; ++i) { kr[i] = Elem<T>::load(k + r0 + 16 * i); qr[i] = Elem<T>::load(q + r0 + 16 * i); }
 #pragma unroll
   for (int e = 0; e < 4; ++e) vc[e] = Elem<T>::load(v + e);
-  const float g = expf(p.log_decay[u % p.G]);
+  // The decay to 48 bits, as in the prompt pass: rounded to fp32 it would be off in one direction at every token, by
+  // n 2^-25 of the state after n of them.
+  const Decay2 g(decay_pow((double)p.log_decay[u % p.G], 1.0));
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    s[i].x = fmaf(kr[i], vc[0], g * s[i].x);
-    s[i].y = fmaf(kr[i], vc[1], g * s[i].y);
-    s[i].z = fmaf(kr[i], vc[2], g * s[i].z);
-    s[i].w = fmaf(kr[i], vc[3], g * s[i].w);
+    s[i].x = fmaf(g.hi, s[i].x, fmaf(kr[i], vc[0], g.lo * s[i].x));
+    s[i].y = fmaf(g.hi, s[i].y, fmaf(kr[i], vc[1], g.lo * s[i].y));
+    s[i].z = fmaf(g.hi, s[i].z, fmaf(kr[i], vc[2], g.lo * s[i].z));
+    s[i].w = fmaf(g.hi, s[i].w, fmaf(kr[i], vc[3], g.lo * s[i].w));
     *reinterpret_cast<float4 *>(S + (size_t)(r0 + 16 * i) * D) = s[i];
     o.x = fmaf(qr[i], s[i].x, o.x);
     o.y = fmaf(qr[i], s[i].y, o.y);

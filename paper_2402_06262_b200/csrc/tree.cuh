@@ -96,7 +96,7 @@ struct CommitParams {
 };
 
 // Length of sequence b's accepted path: 0 unless path[0] hangs on the cached prefix and every next node on the one
-// before.  Called by one whole warp; every lane gets the length and lane m < a the node path[m].
+// before, which has to be an earlier one (any other parent hung on the prefix when the tree was attended).  Called by one whole warp; every lane gets the length and lane m < a the node path[m].
 __device__ __forceinline__ int commit_path(const CommitParams &p, int b, int lane, int &node, bool report) {
   int a = p.path_len[b];
   bool ok = a >= 0 && a <= p.A;
@@ -104,7 +104,10 @@ __device__ __forceinline__ int commit_path(const CommitParams &p, int b, int lan
   node = lane < a ? p.path[(size_t)b * p.A + lane] : -1;
   const int before = __shfl_up_sync(0xffffffffu, node, 1);
   bool chain = true;
-  if (lane < a) chain = node >= 0 && node < p.T && p.parent[(size_t)b * p.T + node] == (lane ? before : -1);
+  if (lane < a) {
+    const int from = lane ? before : -1;
+    chain = node > from && node < p.T && p.parent[(size_t)b * p.T + node] == from;
+  }
   ok = __all_sync(0xffffffffu, chain) && ok;
   if (!ok) {
     if (report && lane == 0) atomicOr(p.status, ROCO_DEV_BAD_TREE);

@@ -135,8 +135,8 @@ def linear(state, log_decay, q, k, v, scale, low=False):
     """One unit, token by token: state [d][d], q, k, v [L][d] (64 bits).  Returns (out, state, out_bound, state_bound).
     Bounds: every term decay^(i-j) (q_i.k_j) v_j (and the one of the first state) may have been rounded a few times to fp32
     in each of its factors and once more for every token that it stayed in the state; with low, in pieces on the tensor
-    cores, the scores and the state enter one product as bf16 and the keys of a state update as the sum of two bf16
-    (which leaves 2^-16)."""
+    cores, the scores and the state enter one product as bf16; the keys of a state update are the sum of three bf16, which
+    are all of an fp32."""
     g = math.exp(log_decay) if log_decay > -math.inf else 0.0
     S, A = state.clone(), state.abs()
     outs, mags = [], []
@@ -147,7 +147,7 @@ def linear(state, log_decay, q, k, v, scale, low=False):
         mags.append(abs(scale) * (q[t].abs() @ A))
     L, d = q.shape
     n = min(L, 1 / (1 - g) if g < 1 else L) + d + 150
-    sb = A * (2 * n * U32 + (2.0 ** -16 if low else 0)) + 1e-30
+    sb = A * (2 * n * U32) + 1e-30
     out = torch.stack(outs) if outs else q.new_zeros(0, d)
     mag = torch.stack(mags) if mags else q.new_zeros(0, d)
     ob = mag * (3 * n * U32 + (2 * U16 if low else 0)) + (2 * U32 + (U16 if low else 0)) * out.abs() + 1e-30

@@ -231,3 +231,43 @@ def test_step_in_a_graph():
         g.replay()
     torch.cuda.synchronize()
     assert torch.equal(want, out) and torch.equal(a.state, b.state)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_at_once(dtype):
+    """Divided prompts of two states on two streams, bit for bit as one after the other."""
+    data = [[t.to("cuda") for t in inputs(50 + i, 1, 3, 2000 + 300 * i, 128, dtype)] for i in range(2)]
+    lens = [torch.tensor([1990 + 300 * i], dtype=torch.int32, device="cuda") for i in range(2)]
+    decay = [-0.01, -0.001, -0.3]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for at_once in (False, True):
+        st, out = [make_state(d[3], decay, dtype) for d in data], [torch.zeros_like(d[0]) for d in data]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for i in range(2):
+                with torch.cuda.stream(streams[i if at_once else 0]):
+                    R.roco_linear_prefill(st[i], *data[i][:3], lens[i], out[i])
+        torch.cuda.synchronize()
+        got.append([s.state for s in st] + out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_many_steps_do_not_drift():
+    """A decay near one, keys with one component: component 0 of the state is the sum of g^j, whose relative error stays below
+    that of its roundings (each at most 2^-24 of the state, decaying with it), n 2^-24 at most; a decay rounded to fp32 alone
+    could use that up.  A third of the bound is asserted, which random signs keep by far: the root of n terms."""
+    n, d = 2000, 64
+    tok = [torch.zeros(1, 4, d, device="cuda") for _ in range(3)]
+    for t in tok:
+        t[..., 0] = 1
+    decay = [-1e-5, -3e-5, -1.7e-4, -9.1e-4]
+    st = make_state(torch.zeros(1, 4, d, d), decay, "f32")
+    out = torch.zeros_like(tok[0])
+    for _ in range(n):
+        R.roco_linear_step(st, *tok, out, scale=1.0)
+    for g in range(4):
+        x = float(torch.tensor(decay[g]))
+        want = math.expm1(n * x) / math.expm1(x)
+        assert abs(float(st.state[0, g, 0, 0]) - want) <= n / 3 * 2.0 ** -24 * want
+        assert abs(float(out[0, g, 0]) - want) <= n / 3 * 2.0 ** -24 * want

@@ -181,3 +181,23 @@ def test_in_a_graph():
     call()
     assert torch.equal(got, out) and bool((out[:, :, 5:] == SENTINEL).all()) and not bool((out[:, :, :5] == SENTINEL).any())
     assert math.isfinite(float(lse[:, :, :5].sum()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [2, 4, 8])
+@pytest.mark.parametrize("live", [0, 1, 300])
+def test_other_branches_may_hold_anything_however_many_rows(dtype, group, live):
+    """40 to 64 and more rows, whose groups of columns share the drafted tokens; with and without cached tokens in front."""
+    T = 20
+    c = make(30 + group, S=1, G=2, B=300, T=T, group=group, dtype=dtype, live=[live])
+    par = [-1 if i < 2 else i - 2 for i in range(T)]
+    c.t["parent"][0] = torch.tensor(par, dtype=torch.int32)
+    for f in ("K_new", "V_new"):
+        c.t[f][:, :, 1::2] = float("nan")
+    _, out, lse = run(c)
+    for g in range(c.G):
+        f = {k: c.t[k][0, g].double() for k in ("K", "V", "Q", "K_new", "V_new")}
+        o, l, ob, lb = ref.tree_attend(f["K"], f["V"], c.live[0], f["Q"], f["K_new"], f["V_new"], par, T, c.d ** -0.5,
+                                       low=dtype == "bf16")
+        assert bool(((out[0, g, ::2].double().cpu() - o[::2]).abs() <= ob[::2]).all())
+        assert bool(((lse[0, g, ::2].double().cpu() - l[::2]).abs() <= lb[::2]).all())

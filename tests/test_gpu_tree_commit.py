@@ -242,3 +242,95 @@ def test_in_a_graph():
     assert torch.equal(ev[0], ev[1])
     for f in CACHE_FIELDS:
         assert torch.equal(getattr(eager, f).view(torch.uint8), getattr(graphed, f).view(torch.uint8)), f
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode,r", [(TOP, 2), (TOP, 60), (TOP, 140), (LOW, 30)])
+def test_many_units(dtype, mode, r):
+    """More units than eight per SM of any B200, scopes that leave out few, a third and nearly all."""
+    c = make(80 + r, S=1, G=1200, B=160, d=64, T=4, dtype=dtype, shape="chain", live=[159])
+    check(c, [[0, 1, 2, 3]], 4, r, mode)
+
+
+@pytest.mark.parametrize("G", [2, 1200])
+@pytest.mark.parametrize("r", [10, 300])
+def test_many_equal_statistics(G, r):
+    """More equal keys than are ranked one against the other, in the variances and in the means."""
+    c = make(81, S=1, G=G, B=400, d=64, T=4, shape="chain")
+    c.t["n"], c.t["s"], c.t["q"] = torch.full_like(c.t["n"], 50), torch.full_like(c.t["s"], 1e-3), torch.full_like(c.t["q"], 1e-5)
+    c.t["K"] = torch.zeros_like(c.t["K"])
+    cache = c.cache()
+    old = c.t["pos"].to("cuda")
+    path = torch.arange(3, dtype=torch.int32, device="cuda")[None]
+    ev = torch.zeros(1, G, 3, dtype=torch.int32, device="cuda")
+    ep = torch.zeros_like(ev)
+    lse = torch.zeros(c.t["Q"].shape[:4], device="cuda")
+    R.roco_tree_attend(cache, c.dev("Q"), c.dev("K_new"), c.dev("V_new"), c.dev("parent"), torch.zeros_like(c.dev("Q")), lse_out=lse)
+    R.roco_tree_commit(cache, c.dev("Q"), c.dev("K_new"), c.dev("V_new"), lse, c.dev("parent"), path,
+                       torch.tensor([3], dtype=torch.int32, device="cuda"), r, ev, evicted_pos=ep)
+    assert R.roco_device_status(cache) == 0
+    assert torch.equal(ep.sort(-1)[0], torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda").expand_as(ep))
+    assert torch.equal(old.gather(-1, ev.long()), ep) and bool((ev[..., 1:] > ev[..., :-1]).all())
+
+
+def test_a_parent_behind_its_node_is_no_chain():
+    """Such a node was attended as one that hangs on the prefix."""
+    c = make(82, S=2, G=2, B=60, T=6)
+    c.t["parent"][:] = torch.tensor([-1, 4, 0, -1, -1, 4], dtype=torch.int32)
+    cache = c.cache()
+    q = c.dev("Q")
+    ev = torch.zeros(2, 2, 2, dtype=torch.int32, device="cuda")
+    R.roco_tree_commit(cache, q, c.dev("K_new"), c.dev("V_new"), torch.zeros(q.shape[:4], device="cuda"), c.dev("parent"),
+                       torch.tensor([[4, 1], [4, 5]], dtype=torch.int32, device="cuda"),
+                       torch.tensor([2, 2], dtype=torch.int32, device="cuda"), 5, ev)
+    assert R.roco_device_status(cache) == 8
+    assert bool((ev[0] == -1).all()) and bool((ev[1] >= 0).all())
+    assert torch.equal(cache.t_next.cpu() - c.t["t_next"], torch.tensor([[0, 0], [2, 2]], dtype=torch.int32))
+
+
+def test_two_at_once():
+    """Attention and commit of two caches on two streams, eager and as two graphs, bit for bit as one after the other."""
+    cases = [make(90 + i, S=2, G=3, B=2100 - 7 * i, T=12, group=2 + i, live=[2090 - 7 * i, 500]) for i in range(2)]
+    dev = [{k: c.dev(k) for k in ("Q", "K_new", "V_new", "parent")} for c in cases]
+    path = torch.zeros(2, 1, dtype=torch.int32, device="cuda")   # node 0 hangs on the prefix in every tree
+    one = torch.ones(2, dtype=torch.int32, device="cuda")
+
+    def results(i):
+        q = dev[i]["Q"]
+        return cases[i].cache(), torch.zeros_like(q), torch.zeros(q.shape[:4], device="cuda"), torch.zeros(2, 3, 1, dtype=torch.int32,
+                                                                                                        device="cuda")
+
+    def work(i, cache, out, lse, ev):
+        t = dev[i]
+        R.roco_tree_attend(cache, t["Q"], t["K_new"], t["V_new"], t["parent"], out, lse_out=lse)
+        R.roco_tree_commit(cache, t["Q"], t["K_new"], t["V_new"], lse, t["parent"], path, one, 20, ev)
+
+    def same(a, b):
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(a[1:], b[1:]))
+        assert all(torch.equal(getattr(a[0], f).view(torch.uint8), getattr(b[0], f).view(torch.uint8)) for f in CACHE_FIELDS)
+
+    want = [results(i) for i in range(2)]
+    for i in range(2):
+        for _ in range(4):
+            work(i, *want[i])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    eager = [results(i) for i in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                work(i, *eager[i])
+    for i in range(2):
+        same(want[i], eager[i])
+    graphed, graphs = [results(i) for i in range(2)], [torch.cuda.CUDAGraph() for _ in range(2)]
+    for i in range(2):
+        with torch.cuda.graph(graphs[i]):
+            work(i, *graphed[i])
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                graphs[i].replay()
+    for i in range(2):
+        same(want[i], graphed[i])
