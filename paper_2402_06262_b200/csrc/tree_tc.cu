@@ -27,27 +27,30 @@ namespace roco {
 
 constexpr int kTtTile = 128;  // keys of a tile
 constexpr int kTtGroup = 128;            // threads of a consumer group
-constexpr int kTtBar = 1;                // named barriers of the consumer groups (kTtBar + group), of all of them, and of
-constexpr int kTtBarAll = 3, kTtBarQ = 4;  // them and the warp of the products
+constexpr int kTtBar = 1;     // named barriers of the consumer groups (kTtBar + group)
+constexpr int kTtBarQ = 3;    // and of all of them with the warp of the products
 constexpr float kTtMoveReference = 60.f;  // binary orders above the reference at which a row moves to a new one
 
-// W groups of four consumer warps, N query rows each, share the tiles of a CTA; C CTAs per SM.
+// W groups of four consumer warps, N query rows each, share the tiles of a CTA and the products over them, N W columns wide
+// (a product reads its 4 KiB of keys or values per 16-step once, however many columns it has); C CTAs per SM.
 template <int D, int N, int W, int C>
 struct TtShape {
   static constexpr int kThreads = W * kTtGroup + 64;
   static constexpr int kTile = kTtTile * D * 2, kBlock = kTtTile * 128;
-  static constexpr int kQ = N * D * 2;
-  static constexpr int kP = N * kTtTile * 2;         // P^T of a tile: 128-byte rows of 64 / N keys each
-  static constexpr int kPRows = kP / 128;
-  static constexpr int kPBufs = N == 64 ? 1 : 2;
-  static constexpr int kGroupFloats = 4 * N /* red */ + 2 * N /* nref, alpha */ + 4 /* odd values */;
-  static constexpr int kFixed = 1024 + W * (kQ + kP * kPBufs + kGroupFloats * 4) + kTreeMaxNodes * 12 + 256;
+  static constexpr int kCols = N * W;
+  static constexpr int kQ = kCols * D * 2;
+  // P^T of a tile: blocks of up to 64 columns, in 128-byte rows of 64 / columns keys each
+  static constexpr int kPCols = kCols < 64 ? kCols : 64, kPRows = kPCols * 2, kPBlock = kPRows * 128;
+  static constexpr int kP = kCols / kPCols * kPBlock;
+  static constexpr int kPBufs = kCols == 128 ? 1 : 2;
+  static constexpr int kGroupFloats = 4 * N /* red */ + 2 * N /* nref, alpha */;
+  static constexpr int kFixed = 1024 + kQ + kP * kPBufs + W * kGroupFloats * 4 + kTreeMaxNodes * 12 + 256;
   static constexpr int kRoom = (227 / C) * 1024 - 1024 - kFixed;
   static constexpr int kStages = kRoom / kTile > 6 ? 6 : kRoom / kTile;
-  static constexpr int kTmemCols = 4 * N * W < 32 ? 32 : 4 * N * W;  // per group S^T twice, O^T; a power of two
+  static constexpr int kTmemCols = 4 * kCols;  // S^T twice, O^T; a power of two
   static constexpr size_t kSmem = (size_t)kFixed + (size_t)kStages * kTile;
   static_assert(kStages >= 2 && kTmemCols * C <= 512, "shared and tensor memory");
-  static_assert((2 * kStages + 6 * W) * 8 + 16 <= 256, "barriers");
+  static_assert((2 * kStages + 6) * 8 + 16 <= 256, "barriers");
   // the drafted tokens' probabilities [nodes][N] of a group lie in a place of the ring once the stream is over
   static_assert(kTreeMaxNodes * N * 4 <= kTile && kStages >= W + 1, "draft probabilities");
 };
@@ -94,22 +97,23 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
     tree_tc_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                    const __grid_constant__ CUtensorMap mapKn, const __grid_constant__ CUtensorMap mapVn, const TreeParams p) {
   using Sh = TtShape<D, N, W, C>;
-  constexpr int kTile = Sh::kTile, kBlock = Sh::kBlock, kStages = Sh::kStages;
-  constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24) | (((uint32_t)N >> 3) << 17);
+  constexpr int kTile = Sh::kTile, kBlock = Sh::kBlock, kStages = Sh::kStages, kCols = Sh::kCols;
+  constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24) | (((uint32_t)kCols >> 3) << 17);
   constexpr uint32_t kIdescO = kIdescS | (1u << 15) | (1u << 16);  // both operands with the M / N index contiguous
   extern __shared__ char tt_raw[];
   launch_dependents();
   char *at = smem_align(tt_raw, 1024);
   char *ring = at; at += kStages * kTile;
-  char *pbuf_all = at; at += W * Sh::kP * Sh::kPBufs;
-  char *qop_all = at; at += W * Sh::kQ;
+  char *pbuf = at; at += Sh::kP * Sh::kPBufs;
+  char *qop = at; at += Sh::kQ;
   float *floats = reinterpret_cast<float *>(at); at += W * Sh::kGroupFloats * 4;
   unsigned long long *anc = reinterpret_cast<unsigned long long *>(at); at += kTreeMaxNodes * 8;
   int *up = reinterpret_cast<int *>(at); at += kTreeMaxNodes * 4;
   uint64_t *full = reinterpret_cast<uint64_t *>(at), *empty = full + kStages;
-  uint64_t *s_full = empty + kStages, *p_ready = s_full + 2 * W, *pv_done = p_ready + 2 * W;  // [group][tile parity]
-  uint32_t *tmem_base = reinterpret_cast<uint32_t *>(pv_done + 2 * W);
+  uint64_t *s_full = empty + kStages, *p_ready = s_full + 2, *pv_done = p_ready + 2;  // by tile parity
+  uint32_t *tmem_base = reinterpret_cast<uint32_t *>(pv_done + 2);
   int *abort_ptr = reinterpret_cast<int *>(tmem_base + 2);
+  int *odd = reinterpret_cast<int *>(tmem_base + 1);  // the drafted values are not all finite
   volatile int *abort_flag = abort_ptr;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -125,14 +129,15 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
   const int n_nodes = __shfl_sync(0xffffffffu, n_nodes_, 0), live = __shfl_sync(0xffffffffu, live_, 0);
   if (cta_row0 >= n_nodes * p.group) return;
   const int tiles = (live + kTtTile - 1) / kTtTile;
-  const int t0 = (int)((long long)tiles * split / p.splits);
-  const int nt = (int)((long long)tiles * (split + 1) / p.splits) - t0;  // cached tiles of this CTA
+  // the drafted tokens are one more tile, the last one's
+  const int t0 = (int)((long long)(tiles + 1) * split / p.splits);
+  const int ns = (int)((long long)(tiles + 1) * (split + 1) / p.splits) - t0;  // score tiles
   const bool drafts = split == p.splits - 1;
-  const int ns = nt + (drafts ? 1 : 0);  // score tiles
+  const int nt = ns - (drafts ? 1 : 0);  // cached tiles of this CTA
 
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < 2 * W; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); mbar_init(&pv_done[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4 * W); mbar_init(&pv_done[i], 1); }
     *abort_ptr = 0;
     mbar_init_fence();
   }
@@ -159,7 +164,8 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       }
     }
   } else if (warp == 4 * W + 1) {
-    named_bar_sync(kTtBarQ, W * kTtGroup + 32);  // the queries are in place
+    if (drafts) tree_ancestors_warp(p, b, n_nodes, anc, up, rb == 0);  // while the queries and the first tile are on their way
+    named_bar_sync(kTtBarQ, W * kTtGroup + 32);                        // the queries are in place
     for (int t = 0; t <= ns; ++t) {
       if (t < ns) {  // scores of tile t; what its accumulator held was read before p_ready of two tiles ago
         const int g = 2 * t, st = g % kStages;
@@ -167,13 +173,10 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
         tc_fence_after();
         const char *k = ring + st * kTile;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            umma_bf16_w(tmem + w * 4 * N + (t & 1) * N, smem_desc_sw128(k + (kk / 4) * kBlock + (kk % 4) * 32),
-                        smem_desc_sw128(qop_all + w * Sh::kQ + (kk / 4) * (N * 128) + (kk % 4) * 32), kIdescS, kk > 0 ? 1u : 0u);
-          umma_commit_w(&s_full[2 * w + (t & 1)]);
-        }
+        for (int kk = 0; kk < D / 16; ++kk)
+          umma_bf16_w(tmem + (t & 1) * kCols, smem_desc_sw128(k + (kk / 4) * kBlock + (kk % 4) * 32),
+                      smem_desc_sw128(qop + (kk / 4) * (kCols * 128) + (kk % 4) * 32), kIdescS, kk > 0 ? 1u : 0u);
+        umma_commit_w(&s_full[t & 1]);
         umma_commit_w(&empty[st]);
       }
       if (t >= 1) {  // output of tile t - 1
@@ -191,22 +194,19 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           fence_async_smem();
           __syncwarp();
         }
+        mbar_wait_compact(&p_ready[tv & 1], (tv >> 1) & 1, abort_flag, p.status);
+        tc_fence_after();
+        const char *pb = pbuf + tv % Sh::kPBufs * Sh::kP;
+        const bool skip = tv == nt && __shfl_sync(0xffffffffu, *odd, 0);
+        if (!skip) {
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-          mbar_wait_compact(&p_ready[2 * w + (tv & 1)], (tv >> 1) & 1, abort_flag, p.status);
-          tc_fence_after();
-          const char *pb = pbuf_all + (w * Sh::kPBufs + tv % Sh::kPBufs) * Sh::kP;
-          const bool skip = tv == nt && __shfl_sync(0xffffffffu, *reinterpret_cast<const int *>(floats + w * Sh::kGroupFloats + 6 * N), 0);
-          if (!skip) {
-#pragma unroll
-            for (int kk = 0; kk < 8; ++kk)  // (d = 64: the upper 64 accumulator lanes repeat the lower, unread)
-              if (kk < steps)
-                umma_bf16_w(tmem + w * 4 * N + 2 * N, smem_desc_sw128_mn(v + kk * 2048, D == 128 ? kBlock : 0),
-                            smem_desc_sw128_mn(pb + (16 * kk % Sh::kPRows) * 128 + (16 * kk / Sh::kPRows) * (N * 2), 16), kIdescO,
-                            (tv > 0 || kk > 0) ? 1u : 0u);
-          }
-          umma_commit_w(&pv_done[2 * w + (tv & 1)]);
+          for (int kk = 0; kk < 8; ++kk)  // (d = 64: the upper 64 accumulator lanes repeat the lower, unread)
+            if (kk < steps)
+              umma_bf16_w(tmem + 2 * kCols, smem_desc_sw128_mn(v + kk * 2048, D == 128 ? kBlock : 0),
+                          smem_desc_sw128_mn(pb + (16 * kk % Sh::kPRows) * 128 + (16 * kk / Sh::kPRows) * (Sh::kPCols * 2), Sh::kPBlock),
+                          kIdescO, (tv > 0 || kk > 0) ? 1u : 0u);
         }
+        umma_commit_w(&pv_done[tv & 1]);
         umma_commit_w(&empty[st]);
       }
     }
@@ -215,7 +215,6 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
     const int grp = W == 1 ? 0 : warp >> 2, bar = kTtBar + grp, row0 = cta_row0 + grp * N;
     const int gt = tid - grp * kTtGroup, gw = warp - 4 * grp;
     float *red = floats + grp * Sh::kGroupFloats, *nref = red + 4 * N, *alpha = nref + N;  // nref: minus a row's reference, log2
-    int *odd = reinterpret_cast<int *>(red + 6 * N);  // the drafted values are not all finite
     // the drafted tokens' probabilities [node][N], after the stream: group 0's where their keys were, group 1's in the place
     // behind their values
     float *pd = reinterpret_cast<float *>(ring + (2 * nt + 2 * grp) % kStages * kTile);
@@ -223,8 +222,7 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       const char *vn = ring + (2 * nt + 1) % kStages * kTile + (gt >> 6) * kBlock + j * 128;
       return *reinterpret_cast<const uint16_t *>(vn + ((((gt & 63) >> 3) ^ (j & 7)) << 4) + (gt & 7) * 2);
     };
-    char *pbuf = pbuf_all + grp * Sh::kPBufs * Sh::kP;
-    {  // the queries as the K-major operands of the groups; rows that do not exist are zero
+    {  // the queries as a K-major operand; rows that do not exist are zero
       const uint4 *Qu = reinterpret_cast<const uint4 *>(p.Q) + ((size_t)u * p.rows + cta_row0) * (D / 8);
       constexpr int kPieces = N * D / 8 / kTtGroup;  // 16-byte pieces per thread, all loaded before the first is stored
       uint4 x[kPieces];
@@ -236,24 +234,25 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       }
 #pragma unroll
       for (int k = 0; k < kPieces; ++k) {
-        const int w = tid + k * W * kTtGroup, i = w / (D / 8) % N, c = w % (D / 8);
-        *reinterpret_cast<uint4 *>(qop_all + w / (N * D / 8) * Sh::kQ + (c >> 3) * (N * 128) + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = x[k];
+        const int w = tid + k * W * kTtGroup, i = w / (D / 8), c = w % (D / 8);
+        *reinterpret_cast<uint4 *>(qop + (c >> 3) * (kCols * 128) + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = x[k];
       }
       fence_async_smem();
     }
     named_bar_sync(kTtBarQ, W * kTtGroup + 32);
-    if (drafts && warp == 0) tree_ancestors_warp(p, b, n_nodes, anc, up, rb == 0);  // under the first tile's load
     const float zs = p.scale * kLog2e;
     const f32x2 zs2 = pack2(zs, zs);
-    const uint32_t tl = tmem + grp * 4 * N + ((uint32_t)(gw * 32) << 16);
-    const int prow = gt % Sh::kPRows, pc0 = gt / Sh::kPRows * (N / 8);
+    const uint32_t tl = tmem + grp * N + ((uint32_t)(gw * 32) << 16);
+    // this thread's key and the group's columns in P^T
+    const int prow = gt % Sh::kPRows, pc0 = gt / Sh::kPRows * (Sh::kPCols / 8) + grp * N % Sh::kPCols / 8;
+    char *pgrp = pbuf + grp * N / Sh::kPCols * Sh::kPBlock + prow * 128;
     f32x2 l[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) l[i] = pack2(0.f, 0.f);
     // The output product of tile t is complete.  One barrier per tile parity: this thread is never two phases of either
     // behind, since the product of tile t + 2 waits for its own probabilities of that tile.
     auto wait_pv = [&](int t) {
-      if (t >= 0) mbar_wait_compact(&pv_done[2 * grp + (t & 1)], (t >> 1) & 1, abort_flag, p.status);
+      if (t >= 0) mbar_wait_compact(&pv_done[t & 1], (t >> 1) & 1, abort_flag, p.status);
     };
     if (gt < N) nref[gt] = 0.f;
     named_bar_sync(bar, kTtGroup);
@@ -265,7 +264,6 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       const int keys = is_draft ? n_nodes : live - (t0 + t) * kTtTile;  // of this tile (more: a full one)
       unsigned long long mine = gt < keys ? ~0ull : 0ull;               // the rows (bits) that see this thread's key
       if (is_draft) {
-        named_bar_sync(kTtBarAll, W * kTtGroup);  // the ancestor sets
         mine = 0ull;
         if (gt < n_nodes) {
           const int last = min(row0 + N, n_nodes * p.group);
@@ -275,8 +273,8 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           }
         }
       }
-      const uint32_t ts = tl + (t & 1) * N;
-      mbar_wait_compact(&s_full[2 * grp + (t & 1)], (t >> 1) & 1, abort_flag, p.status);
+      const uint32_t ts = tl + (t & 1) * kCols;
+      mbar_wait_compact(&s_full[t & 1], (t >> 1) & 1, abort_flag, p.status);
       tc_fence_after();
       f32x2 d[N / 2];  // z - m, log2
       auto scores = [&]() {
@@ -378,10 +376,10 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
 #pragma unroll
           for (int x = 0; x < N; x += 16) {
             uint32_t r[16];
-            tmem_ld16(tl + 2 * N + x, r);
+            tmem_ld16(tl + 2 * kCols + x, r);
 #pragma unroll
             for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha[x + i]);
-            tmem_st16(tl + 2 * N + x, r);
+            tmem_st16(tl + 2 * kCols + x, r);
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
               float lo, hi;
@@ -405,15 +403,12 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
         by_hand = tt_any(!fine, bar);
         if (gt == 0) *odd = by_hand;
         if (by_hand) {
-          // the places of the ring where the probabilities go are free once every group's products have read them
-#pragma unroll
-          for (int w = 0; w < W; ++w) {
-            mbar_wait_compact(&s_full[2 * w + (t & 1)], (t >> 1) & 1, abort_flag, p.status);
-            if (nt > 0) mbar_wait_compact(&pv_done[2 * w + ((nt - 1) & 1)], ((nt - 1) >> 1) & 1, abort_flag, p.status);
-          }
+          // the places of the ring where the probabilities go are free once the products have read them (the scores of this
+          // tile, which are here, and the output of the last)
+          wait_pv(nt - 1);
         }
       }
-      char *prow_p = pbuf + (t % Sh::kPBufs) * Sh::kP + prow * 128;
+      char *prow_p = pgrp + t % Sh::kPBufs * Sh::kP;
 #pragma unroll
       for (int x = 0; x < N; x += 8) {
         float f[8];
@@ -434,7 +429,7 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       fence_async_smem();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_ready[2 * grp + (t & 1)]);
+      if (lane == 0) mbar_arrive(&p_ready[t & 1]);
     }
 
     // ---------------------------------------------------------------- the sums over the lanes, then a dimension per lane
@@ -471,7 +466,7 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
         float o[16];
         if (nt > 0 || (drafts && !by_hand)) {
           uint32_t r[16];
-          tmem_ld16(tl + 2 * N + x, r);
+          tmem_ld16(tl + 2 * kCols + x, r);
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(r[i]);
         } else {
