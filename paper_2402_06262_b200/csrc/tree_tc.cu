@@ -419,12 +419,16 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           l[x / 2 + i] = add2(l[x / 2 + i], e);
           unpack2(e, f[2 * i], f[2 * i + 1]);
         }
+        if (is_draft) {  // (the polynomial ends at 2^-125, and a value that a row does not see may be as large as 2^127)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = (mine >> (x + i)) & 1ull ? f[i] : 0.f;
+          if (by_hand && gt < kTreeMaxNodes) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pd[gt * N + x + i] = f[i];
+          }
+        }
         *reinterpret_cast<uint4 *>(prow_p + (((pc0 + x / 8) ^ (prow & 7)) << 4)) =
             make_uint4(tt_pack(f[0], f[1]), tt_pack(f[2], f[3]), tt_pack(f[4], f[5]), tt_pack(f[6], f[7]));
-        if (by_hand && gt < kTreeMaxNodes) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) pd[gt * N + x + i] = (mine >> (x + i)) & 1ull ? f[i] : 0.f;
-        }
       }
       fence_async_smem();
       tc_fence_before();

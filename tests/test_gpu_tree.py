@@ -186,14 +186,15 @@ def test_in_a_graph():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("group", [2, 4, 8])
 @pytest.mark.parametrize("live", [0, 1, 300])
-def test_other_branches_may_hold_anything_however_many_rows(dtype, group, live):
+@pytest.mark.parametrize("value", [float("nan"), -3e38])
+def test_other_branches_may_hold_anything_however_many_rows(dtype, group, live, value):
     """40 to 64 and more rows, whose groups of columns share the drafted tokens; with and without cached tokens in front."""
     T = 20
     c = make(30 + group, S=1, G=2, B=300, T=T, group=group, dtype=dtype, live=[live])
     par = [-1 if i < 2 else i - 2 for i in range(T)]
     c.t["parent"][0] = torch.tensor(par, dtype=torch.int32)
     for f in ("K_new", "V_new"):
-        c.t[f][:, :, 1::2] = float("nan")
+        c.t[f][:, :, 1::2] = value
     _, out, lse = run(c)
     for g in range(c.G):
         f = {k: c.t[k][0, g].double() for k in ("K", "V", "Q", "K_new", "V_new")}
