@@ -117,30 +117,12 @@ __device__ inline ClSmem cluster_carve(char *raw, int Bc, int d, int stages, int
 
 // ---------------------------------------------------------------- cluster primitives (PTX)
 
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-
-// Address of the same shared-memory location in the CTA of rank `rank` of this cluster.
-__device__ __forceinline__ uint32_t map_to_rank(const void *local, int rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(local)), "r"(rank));
-  return r;
-}
-
 // Asynchronous store of one word into a peer's shared memory; on landing it completes 4 bytes on the peer's
 // transaction barrier `remote_bar`.
 __device__ __forceinline__ void push_u32(uint32_t remote, uint32_t v, uint32_t remote_bar) {
   asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(remote), "r"(v),
                "r"(remote_bar)
                : "memory");
-}
-
-// All threads of all CTAs of the cluster.
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // One thread group's side of the exchanges: its pair of transaction barriers and the phases it has been through.

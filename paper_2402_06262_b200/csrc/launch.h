@@ -123,6 +123,25 @@ inline bool launch_overlapped(void (*kernel)(Params...), unsigned grid, unsigned
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, Params(args)...) == cudaSuccess;
 }
+
+// Launches a kernel as clusters of `ranks` CTAs (2 to 8) that follow one another in the grid.
+template <typename... Params, typename... Args>
+inline bool launch_cluster(void (*kernel)(Params...), unsigned grid, unsigned ranks, unsigned block, size_t smem,
+                           cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = ranks;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...) == cudaSuccess;
+}
+
 #ifdef __CUDACC__
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -19,6 +19,7 @@ struct TreeParams {
   int B, T, group, G;
   int rows;    // T * group query rows of a unit; row i is head i % group of node i / group
   int splits;  // CTAs that share a unit's cached tokens
+  int cluster;  // they are a cluster and join their results themselves (tensor cores only)
   float scale;
 };
 

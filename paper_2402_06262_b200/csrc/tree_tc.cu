@@ -29,6 +29,7 @@ constexpr int kTtTile = 128;  // keys of a tile
 constexpr int kTtGroup = 128;            // threads of a consumer group
 constexpr int kTtBar = 1;     // named barriers of the consumer groups (kTtBar + group)
 constexpr int kTtBarQ = 3;    // and of all of them with the warp of the products
+constexpr int kTtMaxCluster = 8;
 constexpr float kTtMoveReference = 60.f;  // binary orders above the reference at which a row moves to a new one
 
 // W groups of four consumer warps, N query rows each, share the tiles of a CTA and the products over them, N W columns wide
@@ -50,6 +51,8 @@ struct TtShape {
   static constexpr int kTmemCols = 4 * kCols;  // S^T twice, O^T; a power of two
   static constexpr size_t kSmem = (size_t)kFixed + (size_t)kStages * kTile;
   static_assert(kStages >= 2 && kTmemCols * C <= 512, "shared and tensor memory");
+  // a cluster's results [columns][D] take the place of the operands P^T and Q
+  static_assert(kCols * D * 4 <= kP * kPBufs + kQ, "results of a cluster");
   static_assert((2 * kStages + 6) * 8 + 16 <= 256, "barriers");
   // the drafted tokens' probabilities [nodes][N] of a group lie in a place of the ring once the stream is over
   static_assert(kTreeMaxNodes * N * 4 <= kTile && kStages >= W + 1, "draft probabilities");
@@ -92,6 +95,19 @@ __device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
   return *reinterpret_cast<uint32_t *>(&v);
 }
 
+__device__ __forceinline__ float ld_cluster_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void ld_cluster_vec(uint32_t at, float (&v)[2]) {
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ld_cluster_vec(uint32_t at, float (&v)[4]) {
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at) : "memory");
+}
+
 template <int D, int N, int W, int C>
 __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
     tree_tc_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
@@ -118,7 +134,7 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
 
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int row_blocks = (p.rows + N * W - 1) / (N * W);
-  const int rb = blockIdx.x % row_blocks, split = blockIdx.x / row_blocks % p.splits, u = blockIdx.x / (row_blocks * p.splits);
+  const int split = blockIdx.x % p.splits, rb = blockIdx.x / p.splits % row_blocks, u = blockIdx.x / (row_blocks * p.splits);
   const int b = u / p.G, cta_row0 = rb * N * W;
   const bool report = tid == 0 && rb == 0 && split == 0;
   if (tid == 0) {  // on their way before the first load asks for them
@@ -452,9 +468,11 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
     const int rows = max(0, min(N, n_nodes * p.group - row0));
     if (gt < N) {
       const float sum = (red[gt] + red[N + gt]) + (red[2 * N + gt] + red[3 * N + gt]);
-      alpha[gt] = p.splits > 1 ? 1.f : 1.f / sum;
-      if (gt < rows) {
-        const float ref = ns > 0 ? -nref[gt] : -INFINITY;
+      const float ref = ns > 0 ? -nref[gt] : -INFINITY;
+      alpha[gt] = p.splits > 1 ? sum : 1.f / sum;
+      if (p.cluster) {
+        nref[gt] = -ref;
+      } else if (gt < rows) {
         if (p.splits > 1) {
           const size_t pt = ((size_t)u * p.splits + split) * p.rows + row0 + gt;
           *reinterpret_cast<float2 *>(p.part_ml + 2 * pt) = make_float2(ref, sum);
@@ -489,7 +507,8 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           }
         }
         if (p.splits > 1) {
-          float *dst = p.part_o + (((size_t)u * p.splits + split) * p.rows + row0 + x) * D + gt;
+          float *dst = p.cluster ? reinterpret_cast<float *>(pbuf) + (grp * N + x) * D + gt
+                                 : p.part_o + (((size_t)u * p.splits + split) * p.rows + row0 + x) * D + gt;
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             if (x + i < rows) dst[(size_t)i * D] = o[i];
@@ -505,6 +524,45 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
   tc_fence_before();
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, Sh::kTmemCols);
+  if (p.cluster) {
+    // Every CTA joins its share of the rows, a warp a row: with m the largest reference,
+    // o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+    cluster_sync_all();
+    const int rows = min(kCols, n_nodes * p.group - cta_row0);
+    constexpr int kN = D / 32;
+    for (int row = split + p.splits * warp; row < rows; row += p.splits * (Sh::kThreads / 32)) {
+      const float *mine = floats + row / N * Sh::kGroupFloats + 4 * N + row % N;
+      float ref = -INFINITY, sum = 0.f;
+      if (lane < p.splits) {
+        ref = -ld_cluster_f32(map_to_rank(mine, lane));
+        sum = ld_cluster_f32(map_to_rank(mine + N, lane));
+      }
+      const float *o = reinterpret_cast<const float *>(pbuf) + row * D + lane * kN;
+      float v[kTtMaxCluster][kN], acc[kN];
+#pragma unroll
+      for (int r = 0; r < kTtMaxCluster; ++r) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[r][i] = 0.f;
+        if (r < p.splits) ld_cluster_vec(map_to_rank(o, r), v[r]);
+      }
+      const float m = warp_max(ref), f = exp2f(ref - m);  // (an empty part: 0)
+      const float l = warp_sum(f * sum), inv = 1.f / l;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) acc[i] = 0.f;
+#pragma unroll
+      for (int r = 0; r < kTtMaxCluster; ++r) {
+        const float w = __shfl_sync(0xffffffffu, f, r);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) acc[i] = fmaf(w, v[r][i], acc[i]);
+      }
+      const size_t to = (size_t)u * p.rows + cta_row0 + row;
+      uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + (to * D + lane * kN) * 2);
+#pragma unroll
+      for (int i = 0; i < kN; i += 2) dst[i / 2] = tt_pack(acc[i] * inv, acc[i + 1] * inv);
+      if (lane == 0 && p.lse) p.lse[to] = (m + log2f(l)) * kLn2;
+    }
+    cluster_sync_all();  // the others have read this CTA's results
+  }
 }
 
 // How the query rows of a unit are laid out: N columns a group, W groups of a CTA that share its tiles, C CTAs per SM.  Rows
@@ -532,6 +590,7 @@ roco_status tree_tc_t(const TreeParams &p, int U, cudaStream_t stream) {
   static SmemLimit limit;
   if (!limit((const void *)kernel, Sh::kSmem)) return ROCO_ERR_CUDA;
   const unsigned blocks = (unsigned)U * (unsigned)((p.rows + N * W - 1) / (N * W)) * (unsigned)p.splits;
+  if (p.cluster) return launch_cluster(kernel, blocks, (unsigned)p.splits, Sh::kThreads, Sh::kSmem, stream, mk, mv, mn, mw, p) ? ROCO_OK : ROCO_ERR_CUDA;
   kernel<<<blocks, Sh::kThreads, Sh::kSmem, stream>>>(mk, mv, mn, mw, p);
   if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
   return p.splits > 1 ? launch_tree_join(p, ROCO_BF16, D, U, stream) : ROCO_OK;
