@@ -270,6 +270,23 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
     auto wait_pv = [&](int t) {
       if (t >= 0) mbar_wait_compact(&pv_done[t & 1], (t >> 1) & 1, abort_flag, p.status);
     };
+    // The rows (bits) of the group that see drafted token gt: its descendants and itself, each `group` rows long.  Found while
+    // the first tile is on its way, if there are registers to keep it.
+    auto rows_that_see = [&]() {
+      unsigned long long sees = 0ull;
+      if (gt < n_nodes) {
+        const uint32_t *set = reinterpret_cast<const uint32_t *>(anc) + (gt >> 5);
+        const int node0 = row0 / p.group, nodes = min((row0 + N + p.group - 1) / p.group, n_nodes) - node0;
+        const int before = row0 - node0 * p.group;  // rows of the first node that belong to the group of columns before
+        const unsigned long long run = (1ull << p.group) - 1ull;
+#pragma unroll 4
+        for (int k = 0; k < nodes; ++k) {
+          if ((set[2 * (node0 + k)] >> (gt & 31)) & 1u) sees |= k ? run << (k * p.group - before) : run >> before;
+        }
+      }
+      return sees;
+    };
+    const uint32_t early = N <= 32 && drafts ? (uint32_t)rows_that_see() : 0u;
     if (gt < N) nref[gt] = 0.f;
     named_bar_sync(bar, kTtGroup);
     bool by_hand = false;
@@ -279,16 +296,7 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       const bool is_draft = t == nt;
       const int keys = is_draft ? n_nodes : live - (t0 + t) * kTtTile;  // of this tile (more: a full one)
       unsigned long long mine = gt < keys ? ~0ull : 0ull;               // the rows (bits) that see this thread's key
-      if (is_draft) {
-        mine = 0ull;
-        if (gt < n_nodes) {
-          const int last = min(row0 + N, n_nodes * p.group);
-          for (int node = row0 / p.group; node * p.group < last; ++node) {
-            const int r0 = max(node * p.group - row0, 0), r1 = min((node + 1) * p.group - row0, N);
-            if ((anc[node] >> gt) & 1ull) mine |= (r1 - r0 == 64 ? ~0ull : (1ull << (r1 - r0)) - 1ull) << r0;
-          }
-        }
-      }
+      if (is_draft) mine = N <= 32 ? (unsigned long long)early : rows_that_see();
       const uint32_t ts = tl + (t & 1) * kCols;
       mbar_wait_compact(&s_full[t & 1], (t >> 1) & 1, abort_flag, p.status);
       tc_fence_after();
@@ -409,14 +417,21 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       }
       wait_pv(t - Sh::kPBufs);  // the operand's place is free
       if (is_draft) {
-        // a thread looks at one dimension of the drafted values
+        // are the drafted values finite?  (0 x: NaN if not)
         mbar_wait_compact(&full[(2 * nt + 1) % kStages], ((2 * nt + 1) / kStages) & 1, abort_flag, p.status);
-        bool fine = true;
-        if (gt < D) {
-#pragma unroll 4
-          for (int j = 0; j < n_nodes; ++j) fine &= (drafted_value(j) & 0x7f80u) != 0x7f80u;
+        __nv_bfloat162 zero = __float2bfloat162_rn(0.f), nil = zero;
+#pragma unroll 1
+        for (int w = gt; w < n_nodes * 8; w += kTtGroup) {
+#pragma unroll
+          for (int h = 0; h < D / 64; ++h) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(ring + (2 * nt + 1) % kStages * kTile + h * kBlock + w * 16);
+            nil = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.x), zero, nil);
+            nil = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.y), zero, nil);
+            nil = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.z), zero, nil);
+            nil = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.w), zero, nil);
+          }
         }
-        by_hand = tt_any(!fine, bar);
+        by_hand = tt_any(!(__low2float(nil) == 0.f && __high2float(nil) == 0.f), bar);
         if (gt == 0) *odd = by_hand;
         if (by_hand) {
           // the places of the ring where the probabilities go are free once the products have read them (the scores of this
