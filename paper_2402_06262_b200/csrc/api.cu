@@ -717,7 +717,7 @@ roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void 
   p.part_o = plan.bytes ? reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.ml_bytes) : nullptr;
   p.B = cache->B; p.T = T; p.group = group; p.G = cache->G; p.rows = T * group; p.splits = plan.splits;
   p.cluster = plan.cluster; p.scale = scale;
-  if (plan.tc) return launch_tree_attend_tc(p, cache->d, U, static_cast<cudaStream_t>(stream));
+  if (plan.tc) return launch_tree_attend_tc(p, cache->d, U, device_sms(), static_cast<cudaStream_t>(stream));
   return launch_tree_attend_simt(p, cache->kv_dtype, cache->d, U, static_cast<cudaStream_t>(stream));
 }
 

@@ -156,7 +156,7 @@ roco_status launch_tree_attend_simt(const TreeParams &p, int kv_dtype, int d, in
 // Tensor cores (bf16, positive scale); query rows of a CTA and CTAs per SM for that many rows of a unit.
 int tree_tc_rows(int rows);
 int tree_tc_ctas(int rows);
-roco_status launch_tree_attend_tc(const TreeParams &p, int d, int U, cudaStream_t stream);
+roco_status launch_tree_attend_tc(const TreeParams &p, int d, int U, int sms, cudaStream_t stream);
 roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
 // Statistics of the accepted queries, then evictions and insertion (two launches).
 roco_status launch_commit_stats_tc(const CommitParams &p, int d, int U, int sms, cudaStream_t stream);  // bf16

@@ -612,15 +612,20 @@ roco_status tree_tc_t(const TreeParams &p, int U, cudaStream_t stream) {
 }
 
 template <int D>
-roco_status tree_tc_d(const TreeParams &p, int U, cudaStream_t stream) {
+roco_status tree_tc_d(const TreeParams &p, int U, int sms, cudaStream_t stream) {
   const TtPlan t = tree_tc_plan(p.rows);
-  if (t.n == 16) return tree_tc_t<D, 16, 1, 2>(p, U, stream);
-  if (t.n == 32) return t.w == 1 ? tree_tc_t<D, 32, 1, 2>(p, U, stream) : tree_tc_t<D, 32, 2, 1>(p, U, stream);
+  // Few CTAs: one per SM, with a ring that holds three tiles (8 units x 8192 x 32 rows: 21.1 -> 16.5 us); not where clusters
+  // of more than four would not pack (16 of eight: 11.0 -> 16.1 us).
+  const long long ctas = (long long)U * p.splits;
+  const bool few = ctas <= sms && (!p.cluster || p.splits <= 4 || 2 * ctas <= sms);
+  if (t.n == 16) return few ? tree_tc_t<D, 16, 1, 1>(p, U, stream) : tree_tc_t<D, 16, 1, 2>(p, U, stream);
+  if (t.n == 32 && t.w == 1) return few ? tree_tc_t<D, 32, 1, 1>(p, U, stream) : tree_tc_t<D, 32, 1, 2>(p, U, stream);
+  if (t.n == 32) return tree_tc_t<D, 32, 2, 1>(p, U, stream);
   return tree_tc_t<D, 64, 2, 1>(p, U, stream);
 }
 
-roco_status launch_tree_attend_tc(const TreeParams &p, int d, int U, cudaStream_t stream) {
-  return d == 128 ? tree_tc_d<128>(p, U, stream) : tree_tc_d<64>(p, U, stream);
+roco_status launch_tree_attend_tc(const TreeParams &p, int d, int U, int sms, cudaStream_t stream) {
+  return d == 128 ? tree_tc_d<128>(p, U, sms, stream) : tree_tc_d<64>(p, U, sms, stream);
 }
 
 }  // namespace roco
