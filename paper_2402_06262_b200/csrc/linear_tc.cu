@@ -15,13 +15,17 @@
 // the output, which is bf16 itself.
 //
 // Warps: 0-7 (A) a token per tensor-memory lane, half of the columns each: P, the scaling of O, the output.  8-15 (B) a
-// row of the state per lane: DS, the state.  Both split keys, 32 tokens at a time through two buffers, so that the next
-// tokens are split while the tensor cores work on the last.  16 TMA loads and stores (the output of a chunk is staged
-// where its queries were), 17 the products.
+// row of the state per lane: DS, the state.  Both split keys, 32 tokens at a time through two buffers: A the first half of
+// the next chunk's while its product P V runs, B the other half behind its operand, so that the tensor cores never wait
+// for keys.  16 TMA loads and stores (the output of a chunk is staged where its queries were), 17 the products.
 //
-// What bounds it: 128 KiB cross HBM per chunk at d = 128, 3.0 us at one SM's share of the measured copy rate.  A product
-// with both operands in shared memory runs at half the tensor rate here (S1 and O: 130 cycles per instruction of
-// 128 x 128 x 16), one with an operand in tensor memory at 72: about 4400 cycles (2.3 us) per chunk.
+// What bounds it.  A chunk at d = 128 moves 128 KiB through HBM (3.0 us at one SM's share of the measured copy rate) and
+// takes 48 products of 128 x 128 x 16, 3200 cycles at the tensor cores' rate (67 a product).  They follow one another without
+// a gap, at 127 cycles each: operands from shared memory (two per product for S1 and O, 8 KiB per 64 cycles, one for the
+// others) share its ports with the tiles that arrive and leave, and the chip is at its power limit (1.97 GHz falls to 1.4
+// within milliseconds, 1.0 kW).  1024 units x 8192 tokens: 2.15 ms, 770 Tflop/s and 4.1 TB/s at the same time, 0.63 of the
+// copy rate (1.83 ms before the clock falls).  Two terms per key instead of three would be 8 percent faster at five times
+// the error of the state (2.4e-6).
 #include <cuda.h>
 
 #include <type_traits>
@@ -342,99 +346,108 @@ __global__ void __launch_bounds__(kLtThreads, 1)
       const uint32_t tl = tmem + ((uint32_t)(wq * 32) << 16);
       const float inter = (float)(decay_pow(logd, i + 1) * (double)p.scale);
       const f32x2 inter2 = pack2(inter, inter);
-      for (int c = 0; c < n; ++c) {
-        const uint32_t par = c & 1;
-        mbar_wait_compact(s1_full, par, abort_flag, p.status);
-        tc_fence_after();
 #pragma unroll 1
-        for (int cc = 0; cc < 2; ++cc) {
-          const int j0 = half * 64 + cc * 32;
-          uint32_t pk[16];
-          if (wq * 32 + 31 < j0) {  // the whole block lies behind the diagonal
+      for (int c = -1; c < n; ++c) {
+        if (c >= 0) {
+          const uint32_t par = c & 1;
+          mbar_wait_compact(s1_full, par, abort_flag, p.status);
+          tc_fence_after();
+#pragma unroll 1
+          for (int cc = 0; cc < 2; ++cc) {
+            const int j0 = half * 64 + cc * 32;
+            uint32_t pk[16];
+            if (wq * 32 + 31 < j0) {  // the whole block lies behind the diagonal
 #pragma unroll
-            for (int e = 0; e < 16; ++e) pk[e] = 0u;
-          } else {
-            uint32_t r[32];
-            tmem_ld32_issue(tl + kLtColS + (uint32_t)j0, r);
-            const float *w = ptab + 128 + i - j0;  // w[-e]: column j0 + e
-            if (wq * 32 > j0) {  // wholly below the diagonal: one power per row times 32 that all rows share
-              const float base = w[-31];
-              const f32x2 b2 = pack2(base, base);
-              tmem_ld_wait(r);
+              for (int e = 0; e < 16; ++e) pk[e] = 0u;
+            } else {
+              uint32_t r[32];
+              tmem_ld32_issue(tl + kLtColS + (uint32_t)j0, r);
+              const float *w = ptab + 128 + i - j0;  // w[-e]: column j0 + e
+              if (wq * 32 > j0) {  // wholly below the diagonal: one power per row times 32 that all rows share
+                const float base = w[-31];
+                const f32x2 b2 = pack2(base, base);
+                tmem_ld_wait(r);
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 c4 = *reinterpret_cast<const float4 *>(ctab + e);
-                pk[e >> 1] = lt_pack2(mul2(mul2(pack2(c4.x, c4.y), b2), pack2u(r[e], r[e + 1])));
-                pk[(e >> 1) + 1] = lt_pack2(mul2(mul2(pack2(c4.z, c4.w), b2), pack2u(r[e + 2], r[e + 3])));
+                for (int e = 0; e < 32; e += 4) {
+                  const float4 c4 = *reinterpret_cast<const float4 *>(ctab + e);
+                  pk[e >> 1] = lt_pack2(mul2(mul2(pack2(c4.x, c4.y), b2), pack2u(r[e], r[e + 1])));
+                  pk[(e >> 1) + 1] = lt_pack2(mul2(mul2(pack2(c4.z, c4.w), b2), pack2u(r[e + 2], r[e + 3])));
+                }
+              } else {  // on it: the table's zeros are the mask
+                tmem_ld_wait(r);
+#pragma unroll
+                for (int e = 0; e < 32; e += 2)
+                  pk[e >> 1] = lt_pack(__uint_as_float(r[e]) * w[-e], __uint_as_float(r[e + 1]) * w[-e - 1]);
               }
-            } else {  // on it: the table's zeros are the mask
-              tmem_ld_wait(r);
+            }
+            tmem_st16(tl + kLtColS + (uint32_t)(half * 64 + cc * 16), pk);
+          }
+          tmem_st_wait();
+          mbar_wait_compact(o1_full, par, abort_flag, p.status);
+          tc_fence_after();
+          const uint32_t to = tl + kLtColO + (uint32_t)(half * kHalfCols);
+#pragma unroll 1
+          for (int x = 0; x < kHalfCols; x += 32) {
+            uint32_t r[32];
+            tmem_ld32_issue(to + (uint32_t)x, r);
+            tmem_ld_wait(r);
+            uint32_t a[16], b[16];
 #pragma unroll
-              for (int e = 0; e < 32; e += 2)
-                pk[e >> 1] = lt_pack(__uint_as_float(r[e]) * w[-e], __uint_as_float(r[e + 1]) * w[-e - 1]);
+            for (int e = 0; e < 16; e += 2) {
+              float f0, f1;
+              unpack2(mul2(pack2u(r[e], r[e + 1]), inter2), f0, f1);
+              a[e] = __float_as_uint(f0); a[e + 1] = __float_as_uint(f1);
+              unpack2(mul2(pack2u(r[e + 16], r[e + 17]), inter2), f0, f1);
+              b[e] = __float_as_uint(f0); b[e + 1] = __float_as_uint(f1);
+            }
+            tmem_st16(to + (uint32_t)x, a);
+            tmem_st16(to + (uint32_t)x + 16u, b);
+          }
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(o_scaled);
+        }
+        if (c + 1 < n) {  // while the product P V runs: half of the next chunk's keys
+          mbar_wait_compact(&full[(c + 1) % kSlots], ((c + 1) / kSlots) & 1, abort_flag, p.status);
+#pragma unroll 1
+          for (int q = 0; q < 2; ++q) split_keys(c + 1, q);
+        }
+        if (c >= 0) {
+          const uint32_t par = c & 1;
+          const uint32_t to = tl + kLtColO + (uint32_t)(half * kHalfCols);
+          mbar_wait_compact(o_full, par, abort_flag, p.status);
+          tc_fence_after();
+          const bool partial = c == n - 1 && tail < kLtChunk;
+          char *stage = qt + (c & 1) * kTile;  // the products that read the queries are complete
+          char *orow = p.out + (((size_t)u * p.Lmax + (size_t)(first + c) * kLtChunk + i) * D) * 2;
+#pragma unroll 1
+          for (int x = 0; x < kHalfCols; x += 32) {
+            uint32_t r[32];
+            tmem_ld32_issue(to + (uint32_t)x, r);
+            tmem_ld_wait(r);
+            if (x + 32 >= kHalfCols) {  // the accumulator may take the next chunk's product
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(o_free);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint4 o;
+              o.x = lt_pack(__uint_as_float(r[8 * e]), __uint_as_float(r[8 * e + 1]));
+              o.y = lt_pack(__uint_as_float(r[8 * e + 2]), __uint_as_float(r[8 * e + 3]));
+              o.z = lt_pack(__uint_as_float(r[8 * e + 4]), __uint_as_float(r[8 * e + 5]));
+              o.w = lt_pack(__uint_as_float(r[8 * e + 6]), __uint_as_float(r[8 * e + 7]));
+              const int col = half * kHalfCols + x + 8 * e, ch = (col & 63) >> 3;
+              if (!partial) *reinterpret_cast<uint4 *>(stage + (col >> 6) * kBlock + i * 128 + ((ch ^ (i & 7)) << 4)) = o;
+              else if (i < tail) *reinterpret_cast<uint4 *>(orow + col * 2) = o;
             }
           }
-          tmem_st16(tl + kLtColS + (uint32_t)(half * 64 + cc * 16), pk);
-        }
-        tmem_st_wait();
-        mbar_wait_compact(&full[c % kSlots], (c / kSlots) & 1, abort_flag, p.status);
-#pragma unroll 1
-        for (int q = 2; q < 4; ++q) split_keys(c, q);
-        mbar_wait_compact(o1_full, par, abort_flag, p.status);
-        tc_fence_after();
-        const uint32_t to = tl + kLtColO + (uint32_t)(half * kHalfCols);
-#pragma unroll 1
-        for (int x = 0; x < kHalfCols; x += 32) {
-          uint32_t r[32];
-          tmem_ld32_issue(to + (uint32_t)x, r);
-          tmem_ld_wait(r);
-          uint32_t a[16], b[16];
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            float f0, f1;
-            unpack2(mul2(pack2u(r[e], r[e + 1]), inter2), f0, f1);
-            a[e] = __float_as_uint(f0); a[e + 1] = __float_as_uint(f1);
-            unpack2(mul2(pack2u(r[e + 16], r[e + 17]), inter2), f0, f1);
-            b[e] = __float_as_uint(f0); b[e + 1] = __float_as_uint(f1);
-          }
-          tmem_st16(to + (uint32_t)x, a);
-          tmem_st16(to + (uint32_t)x + 16u, b);
-        }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(o_scaled);
-        mbar_wait_compact(o_full, par, abort_flag, p.status);
-        tc_fence_after();
-        const bool partial = c == n - 1 && tail < kLtChunk;
-        char *stage = qt + (c & 1) * kTile;  // the products that read the queries are complete
-        char *orow = p.out + (((size_t)u * p.Lmax + (size_t)(first + c) * kLtChunk + i) * D) * 2;
-#pragma unroll 1
-        for (int x = 0; x < kHalfCols; x += 32) {
-          uint32_t r[32];
-          tmem_ld32_issue(to + (uint32_t)x, r);
-          tmem_ld_wait(r);
-          if (x + 32 >= kHalfCols) {  // the accumulator may take the next chunk's product
-            tc_fence_before();
+          if (!partial) {
+            fence_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(o_free);
+            if (lane == 0) mbar_arrive(staged);
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint4 o;
-            o.x = lt_pack(__uint_as_float(r[8 * e]), __uint_as_float(r[8 * e + 1]));
-            o.y = lt_pack(__uint_as_float(r[8 * e + 2]), __uint_as_float(r[8 * e + 3]));
-            o.z = lt_pack(__uint_as_float(r[8 * e + 4]), __uint_as_float(r[8 * e + 5]));
-            o.w = lt_pack(__uint_as_float(r[8 * e + 6]), __uint_as_float(r[8 * e + 7]));
-            const int col = half * kHalfCols + x + 8 * e, ch = (col & 63) >> 3;
-            if (!partial) *reinterpret_cast<uint4 *>(stage + (col >> 6) * kBlock + i * 128 + ((ch ^ (i & 7)) << 4)) = o;
-            else if (i < tail) *reinterpret_cast<uint4 *>(orow + col * 2) = o;
-          }
-        }
-        if (!partial) {
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(staged);
         }
       }
     }
@@ -476,8 +489,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
     for (int c = 0; c <= n; ++c) {
       if (c < n) {
         mbar_wait_compact(&full[c % kSlots], (c / kSlots) & 1, abort_flag, p.status);
+        if (kStates) {
 #pragma unroll 1
-        for (int q = 0; q < 2; ++q) split_keys(c, q);
+          for (int q = 0; q < 2; ++q) split_keys(c, q);
+        }
       }
       if (c > 0) {  // the state behind the chunk before
         mbar_wait_compact(&ds_full[(c - 1) & 1], ((c - 1) >> 1) & 1, abort_flag, p.status);
@@ -515,6 +530,8 @@ __global__ void __launch_bounds__(kLtThreads, 1)
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(sop_ready);
+#pragma unroll 1
+        for (int q = 2; q < 4; ++q) split_keys(c, q);
       }
     }
     if (mine && (kStates || seg == p.segments - 1)) {
