@@ -19,7 +19,7 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
   constexpr int kVec = D / 64;   // float4 pieces of the output per thread
   __shared__ __align__(16) float sq[kTsRows * kPitch];
   __shared__ __align__(16) float skv[kTsKeys * kPitch];
-  __shared__ float sp[kTsRows][kTsKeys];
+  __shared__ __align__(16) float sp[kTsRows][kTsKeys + 4];
   __shared__ unsigned long long anc[kTreeMaxNodes];
   __shared__ int up[kTreeMaxNodes];
   launch_dependents();
@@ -32,8 +32,8 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
   const int row0 = rb * kTsRows;
   if (row0 >= n_nodes * p.group) return;
   const int live = tree_live(p.live, u, p.B, p.status, report);
-  if (tid < 32) tree_ancestors_warp(p, b, n_nodes, anc, up, rb == 0 && split == 0);
-  __syncthreads();
+  const bool drafts = split == p.splits - 1;
+  if (drafts && tid < 32) tree_ancestors_warp(p, b, n_nodes, anc, up, rb == 0);
   const int grow = row0 + row;
   const bool valid = grow < n_nodes * p.group;
   const T *Qu = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.rows * D;
@@ -47,23 +47,30 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
     for (int e = 0; e < kEPC; ++e) sq[rr * kPitch + c * kEPC + e] = f[e];
   }
   const int tiles = (live + kTsKeys - 1) / kTsKeys;
-  const int t0 = (int)((long long)tiles * split / p.splits), t1 = (int)((long long)tiles * (split + 1) / p.splits);
-  const bool drafts = split == p.splits - 1;
+  // the drafted tokens are one more tile, the last one's
+  const int t0 = (int)((long long)(tiles + 1) * split / p.splits), t_end = (int)((long long)(tiles + 1) * (split + 1) / p.splits);
   const float zscale = p.scale * kLog2e;
-  const unsigned long long sees = valid ? anc[grow / p.group] : 0ull;
   float m = -INFINITY, l = 0.f;
   float4 acc[kVec];
 #pragma unroll
   for (int c = 0; c < kVec; ++c) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
 
-  // rows [0, count) of a key or value tile as fp32, the others zero
-  auto stage = [&](const T *src, int count) {
-    for (int w = tid; w < kTsKeys * D / kEPC; w += kTsThreads) {
-      const int j = w / (D / kEPC), c = w % (D / kEPC);
+  // rows [0, count) of a key or value tile, the others zero; to shared memory as fp32
+  constexpr int kPieces = kTsKeys * D / kEPC / kTsThreads;
+  auto fetch = [&](const T *src, int count, uint4 (&x)[kPieces]) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int w = tid + i * kTsThreads, j = w / (D / kEPC), c = w % (D / kEPC);
+      x[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (j < count) x[i] = reinterpret_cast<const uint4 *>(src + (size_t)j * D)[c];
+    }
+  };
+  auto stage = [&](const uint4 (&x)[kPieces]) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int w = tid + i * kTsThreads, j = w / (D / kEPC), c = w % (D / kEPC);
       float f[kEPC];
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (j < count) x = reinterpret_cast<const uint4 *>(src + (size_t)j * D)[c];
-      Elem<T>::unpack(x, f);
+      Elem<T>::unpack(x[i], f);
 #pragma unroll
       for (int e = 0; e < kEPC; e += 4)
         *reinterpret_cast<float4 *>(&skv[j * kPitch + c * kEPC + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
@@ -71,16 +78,20 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
   };
 
 #pragma unroll 1
-  for (int t = t0; t < t1 + (drafts ? 1 : 0); ++t) {
-    const bool is_draft = t == t1;
+  for (int t = t0; t < t_end; ++t) {
+    const bool is_draft = t == tiles;
     const int count = is_draft ? n_nodes : (live - t * kTsKeys < kTsKeys ? live - t * kTsKeys : kTsKeys);
     const T *ks = is_draft ? reinterpret_cast<const T *>(p.k_new) + (size_t)u * p.T * D
                            : reinterpret_cast<const T *>(p.K) + ((size_t)u * p.B + (size_t)t * kTsKeys) * D;
     const T *vs = is_draft ? reinterpret_cast<const T *>(p.v_new) + (size_t)u * p.T * D
                            : reinterpret_cast<const T *>(p.V) + ((size_t)u * p.B + (size_t)t * kTsKeys) * D;
-    __syncthreads();  // the tile before is used up (and, the first time, the queries are in place)
-    stage(ks, count);
+    uint4 x[kPieces], v[kPieces];
+    fetch(ks, count, x);
+    fetch(vs, count, v);  // on their way during the scores
+    __syncthreads();      // the tile before is used up (and, the first time, queries and ancestor sets are in place)
+    stage(x);
     __syncthreads();
+    const unsigned long long sees = is_draft && valid ? anc[grow / p.group] : 0ull;
     float z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int c = 0; c < D; c += 4) {
@@ -116,21 +127,35 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
     l = fmaf(l, alpha, sum);
     m = m_new;
     __syncthreads();  // the keys are used up, the probabilities in place
-    stage(vs, count);
+    stage(v);
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < kVec; ++c) { acc[c].x *= alpha; acc[c].y *= alpha; acc[c].z *= alpha; acc[c].w *= alpha; }
+    if (is_draft) {  // what a row does not see may be infinite or NaN
 #pragma unroll 2
-    for (int j = 0; j < count; ++j) {
-      const float pj = sp[row][j];
-      if (pj != 0.f) {
+      for (int j = 0; j < count; ++j) {
+        if ((sees >> j) & 1ull) {
+          const float pj = sp[row][j];
 #pragma unroll
-        for (int c = 0; c < kVec; ++c) {
-          const float4 v = *reinterpret_cast<const float4 *>(&skv[j * kPitch + c * 64 + part * 4]);
-          acc[c].x = fmaf(pj, v.x, acc[c].x);
-          acc[c].y = fmaf(pj, v.y, acc[c].y);
-          acc[c].z = fmaf(pj, v.z, acc[c].z);
-          acc[c].w = fmaf(pj, v.w, acc[c].w);
+          for (int c = 0; c < kVec; ++c) {
+            const float4 w = *reinterpret_cast<const float4 *>(&skv[j * kPitch + c * 64 + part * 4]);
+            acc[c] = make_float4(fmaf(pj, w.x, acc[c].x), fmaf(pj, w.y, acc[c].y), fmaf(pj, w.z, acc[c].z), fmaf(pj, w.w, acc[c].w));
+          }
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int j = 0; j < kTsKeys; j += 4) {  // (rows behind the last are zero)
+        const float4 p4 = *reinterpret_cast<const float4 *>(&sp[row][j]);
+        const float pj[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+#pragma unroll
+          for (int c = 0; c < kVec; ++c) {
+            const float4 w = *reinterpret_cast<const float4 *>(&skv[(j + k) * kPitch + c * 64 + part * 4]);
+            acc[c] = make_float4(fmaf(pj[k], w.x, acc[c].x), fmaf(pj[k], w.y, acc[c].y), fmaf(pj[k], w.z, acc[c].z),
+                                 fmaf(pj[k], w.w, acc[c].w));
+          }
         }
       }
     }
