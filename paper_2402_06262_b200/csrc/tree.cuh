@@ -19,7 +19,7 @@ struct TreeParams {
   int B, T, group, G;
   int rows;    // T * group query rows of a unit; row i is head i % group of node i / group
   int splits;  // CTAs that share a unit's cached tokens
-  int cluster;  // they are a cluster and join their results themselves (tensor cores only)
+  int cluster;  // they are a cluster and join their results themselves
   float scale;
 };
 
@@ -82,6 +82,67 @@ __device__ __forceinline__ void tree_ancestors_warp(const TreeParams &p, int b, 
     }
     __syncwarp();
   }
+}
+
+constexpr int kTreeMaxCluster = 8;  // CTAs of a cluster
+
+__device__ __forceinline__ float ld_cluster_f32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void ld_cluster_vec(uint32_t at, float (&v)[2]) {
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ld_cluster_vec(uint32_t at, float (&v)[4]) {
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at) : "memory");
+}
+
+// The CTAs of a cluster join what each has found over its range of the cached tokens, for `rows` rows from row0 on: CTA `split`
+// those of index split, split + splits, ..., a warp a row.  With m the largest reference of the parts,
+//     o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+// In the shared memory of each: o[row][D], at(row) a row's reference and l `to_sum` floats behind it.  Called by all threads of
+// all CTAs.
+template <typename T, int D, typename At>
+__device__ __forceinline__ void tree_cluster_join(const TreeParams &p, int u, int row0, int rows, int split, int warp, int warps,
+                                                  int lane, const float *o, At at, int to_sum) {
+  cluster_sync_all();
+  constexpr int kN = D / 32;
+  for (int row = split + p.splits * warp; row < rows; row += p.splits * warps) {
+    const float *mine = at(row);
+    float ref = -INFINITY, sum = 0.f;
+    if (lane < p.splits) {
+      ref = ld_cluster_f32(map_to_rank(mine, lane));
+      sum = ld_cluster_f32(map_to_rank(mine + to_sum, lane));
+    }
+    float v[kTreeMaxCluster][kN], acc[kN];
+#pragma unroll
+    for (int r = 0; r < kTreeMaxCluster; ++r) {
+#pragma unroll
+      for (int i = 0; i < kN; ++i) v[r][i] = 0.f;
+      if (r < p.splits) ld_cluster_vec(map_to_rank(o + row * D + lane * kN, r), v[r]);
+    }
+    const float m = warp_max(ref), f = exp2f(ref - m);  // (an empty part: 0)
+    const float l = warp_sum(f * sum), inv = 1.f / l;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) acc[i] = 0.f;
+#pragma unroll
+    for (int r = 0; r < kTreeMaxCluster; ++r) {
+      const float w = __shfl_sync(0xffffffffu, f, r);
+#pragma unroll
+      for (int i = 0; i < kN; ++i) acc[i] = fmaf(w, v[r][i], acc[i]);
+    }
+    const size_t to = (size_t)u * p.rows + row0 + row;
+    T *out = reinterpret_cast<T *>(p.out) + to * D + lane * kN;
+#pragma unroll
+    for (int i = 0; i < kN; i += 2) {
+      if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162 *>(out + i) = __floats2bfloat162_rn(acc[i] * inv, acc[i + 1] * inv);
+      else *reinterpret_cast<float2 *>(out + i) = make_float2(acc[i] * inv, acc[i + 1] * inv);
+    }
+    if (lane == 0 && p.lse) p.lse[to] = (m + log2f(l)) * kLn2;
+  }
+  cluster_sync_all();  // the others have read this CTA's results
 }
 
 struct CommitParams {

@@ -11,7 +11,7 @@ constexpr int kTsKeys = 64;  // keys of a tile; the drafted nodes are one more t
 // One CTA: kTsRows query rows of a unit against one range of its cached tokens (the last range also against the
 // drafted nodes), one pass with a running maximum and sum per row.  Sixteen threads share a row: each forms four of the
 // tile's 64 scores, then owns D / 16 of the row's output dimensions.  A key that a row does not see has probability
-// zero and is left out of the sums, so what lies in its value does not matter.
+// zero; a drafted one is left out of the sums too, so what lies in its value does not matter.
 template <typename T, int D>
 __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams p) {
   constexpr int kPitch = D + 4;  // float4 reads of 16 different rows hit different banks
@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
   launch_dependents();
   const int tid = threadIdx.x, row = tid >> 4, part = tid & 15;
   const int row_blocks = (p.rows + kTsRows - 1) / kTsRows;
-  const int rb = blockIdx.x % row_blocks, split = (blockIdx.x / row_blocks) % p.splits;
+  const int split = blockIdx.x % p.splits, rb = blockIdx.x / p.splits % row_blocks;
   const int u = blockIdx.x / (row_blocks * p.splits), b = u / p.G;
   const bool report = tid == 0 && rb == 0 && split == 0;
   const int n_nodes = tree_nodes(p, b, report);
@@ -160,6 +160,15 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
       }
     }
   }
+  if (p.cluster) {
+    __syncthreads();  // the last values are used up
+#pragma unroll
+    for (int c = 0; c < kVec; ++c) *reinterpret_cast<float4 *>(&skv[row * D + c * 64 + part * 4]) = acc[c];
+    if (part == 0) { sp[row][0] = m; sp[row][1] = l; }
+    tree_cluster_join<T, D>(p, u, row0, min(kTsRows, n_nodes * p.group - row0), split, tid >> 5, kTsThreads / 32, tid & 31, skv,
+                            [&](int r) { return &sp[r][0]; }, 1);
+    return;
+  }
   if (!valid) return;
   if (p.splits > 1) {
     const size_t at = ((size_t)u * p.splits + split) * p.rows + grow;
@@ -231,17 +240,20 @@ roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cu
 
 int tree_simt_row_blocks(int rows) { return (rows + kTsRows - 1) / kTsRows; }
 
-roco_status launch_tree_attend_simt(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream) {
+template <typename T, int D>
+roco_status tree_simt_t(const TreeParams &p, int U, cudaStream_t stream) {
   const unsigned grid = (unsigned)U * (unsigned)tree_simt_row_blocks(p.rows) * (unsigned)p.splits;
-  if (kv_dtype == ROCO_BF16) {
-    if (d == 128) tree_simt_kernel<__nv_bfloat16, 128><<<grid, kTsThreads, 0, stream>>>(p);
-    else tree_simt_kernel<__nv_bfloat16, 64><<<grid, kTsThreads, 0, stream>>>(p);
-  } else {
-    if (d == 128) tree_simt_kernel<float, 128><<<grid, kTsThreads, 0, stream>>>(p);
-    else tree_simt_kernel<float, 64><<<grid, kTsThreads, 0, stream>>>(p);
-  }
+  if (p.cluster)
+    return launch_cluster(tree_simt_kernel<T, D>, grid, (unsigned)p.splits, kTsThreads, 0, stream, p) ? ROCO_OK : ROCO_ERR_CUDA;
+  tree_simt_kernel<T, D><<<grid, kTsThreads, 0, stream>>>(p);
   if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
-  return p.splits > 1 ? launch_tree_join(p, kv_dtype, d, U, stream) : ROCO_OK;
+  return p.splits > 1 ? tree_join_t<T, D>(p, U, stream) : ROCO_OK;
+}
+
+roco_status launch_tree_attend_simt(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream) {
+  if (kv_dtype == ROCO_BF16)
+    return d == 128 ? tree_simt_t<__nv_bfloat16, 128>(p, U, stream) : tree_simt_t<__nv_bfloat16, 64>(p, U, stream);
+  return d == 128 ? tree_simt_t<float, 128>(p, U, stream) : tree_simt_t<float, 64>(p, U, stream);
 }
 
 }  // namespace roco

@@ -29,7 +29,6 @@ constexpr int kTtTile = 128;  // keys of a tile
 constexpr int kTtGroup = 128;            // threads of a consumer group
 constexpr int kTtBar = 1;     // named barriers of the consumer groups (kTtBar + group)
 constexpr int kTtBarQ = 3;    // and of all of them with the warp of the products
-constexpr int kTtMaxCluster = 8;
 constexpr float kTtMoveReference = 60.f;  // binary orders above the reference at which a row moves to a new one
 
 // W groups of four consumer warps, N query rows each, share the tiles of a CTA and the products over them, N W columns wide
@@ -93,19 +92,6 @@ __device__ __forceinline__ void prefetch_tensor_map(const CUtensorMap *map) {
 __device__ __forceinline__ uint32_t tt_pack(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t *>(&v);
-}
-
-__device__ __forceinline__ float ld_cluster_f32(uint32_t at) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ void ld_cluster_vec(uint32_t at, float (&v)[2]) {
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void ld_cluster_vec(uint32_t at, float (&v)[4]) {
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at) : "memory");
 }
 
 template <int D, int N, int W, int C>
@@ -486,7 +472,7 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
       const float ref = ns > 0 ? -nref[gt] : -INFINITY;
       alpha[gt] = p.splits > 1 ? sum : 1.f / sum;
       if (p.cluster) {
-        nref[gt] = -ref;
+        nref[gt] = ref;
       } else if (gt < rows) {
         if (p.splits > 1) {
           const size_t pt = ((size_t)u * p.splits + split) * p.rows + row0 + gt;
@@ -540,43 +526,9 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, Sh::kTmemCols);
   if (p.cluster) {
-    // Every CTA joins its share of the rows, a warp a row: with m the largest reference,
-    // o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
-    cluster_sync_all();
-    const int rows = min(kCols, n_nodes * p.group - cta_row0);
-    constexpr int kN = D / 32;
-    for (int row = split + p.splits * warp; row < rows; row += p.splits * (Sh::kThreads / 32)) {
-      const float *mine = floats + row / N * Sh::kGroupFloats + 4 * N + row % N;
-      float ref = -INFINITY, sum = 0.f;
-      if (lane < p.splits) {
-        ref = -ld_cluster_f32(map_to_rank(mine, lane));
-        sum = ld_cluster_f32(map_to_rank(mine + N, lane));
-      }
-      const float *o = reinterpret_cast<const float *>(pbuf) + row * D + lane * kN;
-      float v[kTtMaxCluster][kN], acc[kN];
-#pragma unroll
-      for (int r = 0; r < kTtMaxCluster; ++r) {
-#pragma unroll
-        for (int i = 0; i < kN; ++i) v[r][i] = 0.f;
-        if (r < p.splits) ld_cluster_vec(map_to_rank(o, r), v[r]);
-      }
-      const float m = warp_max(ref), f = exp2f(ref - m);  // (an empty part: 0)
-      const float l = warp_sum(f * sum), inv = 1.f / l;
-#pragma unroll
-      for (int i = 0; i < kN; ++i) acc[i] = 0.f;
-#pragma unroll
-      for (int r = 0; r < kTtMaxCluster; ++r) {
-        const float w = __shfl_sync(0xffffffffu, f, r);
-#pragma unroll
-        for (int i = 0; i < kN; ++i) acc[i] = fmaf(w, v[r][i], acc[i]);
-      }
-      const size_t to = (size_t)u * p.rows + cta_row0 + row;
-      uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + (to * D + lane * kN) * 2);
-#pragma unroll
-      for (int i = 0; i < kN; i += 2) dst[i / 2] = tt_pack(acc[i] * inv, acc[i + 1] * inv);
-      if (lane == 0 && p.lse) p.lse[to] = (m + log2f(l)) * kLn2;
-    }
-    cluster_sync_all();  // the others have read this CTA's results
+    tree_cluster_join<__nv_bfloat16, D>(p, u, cta_row0, min(kCols, n_nodes * p.group - cta_row0), split, warp, Sh::kThreads / 32, lane,
+                                        reinterpret_cast<const float *>(pbuf),
+                                        [&](int row) { return floats + row / N * Sh::kGroupFloats + 4 * N + row % N; }, N);
   }
 }
 
