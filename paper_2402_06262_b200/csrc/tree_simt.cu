@@ -36,6 +36,7 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
   if (drafts && tid < 32) tree_ancestors_warp(p, b, n_nodes, anc, up, rb == 0);
   const int grow = row0 + row;
   const bool valid = grow < n_nodes * p.group;
+  const bool busy = grow - (row & 1) < n_nodes * p.group;  // a row of this warp exists
   const T *Qu = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.rows * D;
   for (int w = tid; w < kTsRows * D / kEPC; w += kTsThreads) {
     const int rr = w / (D / kEPC), c = w % (D / kEPC);
@@ -91,44 +92,49 @@ __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams 
     __syncthreads();      // the tile before is used up (and, the first time, queries and ancestor sets are in place)
     stage(x);
     __syncthreads();
-    const unsigned long long sees = is_draft && valid ? anc[grow / p.group] : 0ull;
-    float z[4] = {0.f, 0.f, 0.f, 0.f};
+    unsigned long long sees = 0ull;
+    float alpha = 1.f;
+    if (busy) {
+      if (is_draft && valid) sees = anc[grow / p.group];
+      float z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int c = 0; c < D; c += 4) {
-      const float4 qv = *reinterpret_cast<const float4 *>(&sq[row * kPitch + c]);
+      for (int c = 0; c < D; c += 4) {
+        const float4 qv = *reinterpret_cast<const float4 *>(&sq[row * kPitch + c]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4 kv = *reinterpret_cast<const float4 *>(&skv[(part + 16 * k) * kPitch + c]);
+          z[k] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, z[k]))));
+        }
+      }
+      float top = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float4 kv = *reinterpret_cast<const float4 *>(&skv[(part + 16 * k) * kPitch + c]);
-        z[k] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, z[k]))));
+        const int j = part + 16 * k;
+        const bool seen = j < count && (!is_draft || ((sees >> j) & 1ull));
+        z[k] = seen ? z[k] * zscale : -INFINITY;
+        top = fmaxf(top, z[k]);
       }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float m_new = fmaxf(m, top);
+      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      alpha = exp2f(m - ref);  // 0 before the first seen key
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float e = exp2f(z[k] - ref);
+        sp[row][part + 16 * k] = e;
+        sum += e;
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l = fmaf(l, alpha, sum);
+      m = m_new;
     }
-    float top = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int j = part + 16 * k;
-      const bool seen = j < count && (!is_draft || ((sees >> j) & 1ull));
-      z[k] = seen ? z[k] * zscale : -INFINITY;
-      top = fmaxf(top, z[k]);
-    }
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float m_new = fmaxf(m, top);
-    const float ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = exp2f(m - ref);  // 0 before the first seen key
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float e = exp2f(z[k] - ref);
-      sp[row][part + 16 * k] = e;
-      sum += e;
-    }
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    l = fmaf(l, alpha, sum);
-    m = m_new;
     __syncthreads();  // the keys are used up, the probabilities in place
     stage(v);
     __syncthreads();
+    if (!busy) continue;
 #pragma unroll
     for (int c = 0; c < kVec; ++c) { acc[c].x *= alpha; acc[c].y *= alpha; acc[c].z *= alpha; acc[c].w *= alpha; }
     if (is_draft) {  // what a row does not see may be infinite or NaN
