@@ -82,6 +82,7 @@ roco_status launch_linear_step(const LinearParams &p, const int *active, int dty
 constexpr int kLpThreads = 256;
 constexpr int kLpChunk = 32;  // tokens of a chunk
 constexpr int kLpCols = 64;   // columns of the state per CTA
+constexpr int kLpSegments = 64;
 
 template <int D>
 struct LpSmem {
@@ -89,6 +90,7 @@ struct LpSmem {
   float v[kLpChunk][kLpCols], s[D][kLpCols];
   float p[kLpChunk][kLpChunk + 1];
   float pw[kLpChunk + 1];                        // g^n
+  float seg_w[kLpSegments];                      // what is left of the state behind segment m - 1 at this one's start
 };
 
 // In chunks of 32 tokens, with i, j counted inside the chunk and S the state before it:
@@ -120,13 +122,18 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
   const int first = linear_segment(n_chunks, p.segments, seg), last = linear_segment(n_chunks, p.segments, seg + 1);
   const double logd = (double)p.log_decay[u % p.G];
   if (tid <= kLpChunk) sm.pw[tid] = (float)decay_pow(logd, tid);
+  else if (!kStates && tid >= 64 && tid - 64 <= seg && tid < 64 + kLpSegments)
+    sm.seg_w[tid - 64] = (float)decay_pow(logd, (double)(first - linear_segment(n_chunks, p.segments, tid - 64)) * kLpChunk);
   const int sr0 = (tid >> 4) * kRows, sc = (tid & 15) * 4;  // this thread's rows and columns of the state
   float *S = p.state + (size_t)u * D * D + (size_t)sr0 * D + c0 + sc;
   float *part = p.parts + (size_t)u * p.segments * D * D + (size_t)sr0 * D + c0 + sc;
   float4 s[kRows];
 #pragma unroll
   for (int i = 0; i < kRows; ++i) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (!kStates) wait_for_launch_before();  // the segments' states
+  if (!kStates) {
+    __syncthreads();
+    wait_for_launch_before();  // the segments' states
+  }
   if (seg == 0) {
     const float *src = (p.segments == 1 || kStates) ? S : part;
 #pragma unroll
@@ -136,9 +143,9 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
       for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4 *>(part + (size_t)i * D) = s[i];
     }
   } else if (!kStates) {
+#pragma unroll 4
     for (int m = 1; m <= seg; ++m) {
-      const int t = first - linear_segment(n_chunks, p.segments, m);  // chunks between the end of segment m - 1 and here
-      const float w = (float)decay_pow(logd, (double)t * kLpChunk);
+      const float w = sm.seg_w[m];
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
         const float4 x = *reinterpret_cast<const float4 *>(part + (size_t)m * D * D + (size_t)i * D);
@@ -235,6 +242,7 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
       for (int h = 0; h < 2; ++h) { o[h].x *= w; o[h].y *= w; o[h].z *= w; o[h].w *= w; }
       __syncwarp();  // a row's scores come from eight lanes of the same warp
       const int upto = (row | 3) + 1;  // the warp's four rows end at most here
+#pragma unroll 4
       for (int j = 0; j < upto; ++j) {
         const float pj = sm.p[row][j];
 #pragma unroll
@@ -311,7 +319,7 @@ int linear_simt_segments(int U, int d, int Lmax, int sms) {
   long long n = 2LL * sms / ctas;
   const int most = Lmax / (2 * kLpChunk);
   if (n > most) n = most;
-  if (n > 64) n = 64;
+  if (n > kLpSegments) n = kLpSegments;
   return n < 2 ? 1 : (int)n;
 }
 
