@@ -79,16 +79,20 @@ roco_status launch_linear_step(const LinearParams &p, const int *active, int dty
 
 // ---------------------------------------------------------------- prompt pass
 
-constexpr int kLpThreads = 256;
+constexpr int kLpThreads = 128;
 constexpr int kLpChunk = 32;  // tokens of a chunk
 constexpr int kLpCols = 64;   // columns of the state per CTA
 constexpr int kLpSegments = 64;
+
+__device__ __forceinline__ void madd4(float4 &o, float w, const float4 &x) {
+  o.x = fmaf(w, x.x, o.x); o.y = fmaf(w, x.y, o.y); o.z = fmaf(w, x.z, o.z); o.w = fmaf(w, x.w, o.w);
+}
 
 template <int D>
 struct LpSmem {
   float q[kLpChunk][D + 4], k[kLpChunk][D + 4];  // pitch: eight rows read at once lie in different banks
   float v[kLpChunk][kLpCols], s[D][kLpCols];
-  float p[kLpChunk][kLpChunk + 1];
+  float p[kLpChunk][kLpChunk + 4];
   float pw[kLpChunk + 1];                        // g^n
   float seg_w[kLpSegments];                      // what is left of the state behind segment m - 1 at this one's start
 };
@@ -106,7 +110,7 @@ struct LpSmem {
 // launch starts segment i > 0 from  g^(t_i - t_1) slot_1 + sum_{m=1}^{i-1} g^(t_i - t_{m+1}) slot_{m+1}.
 template <typename T, int D, bool kStates>
 __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const LinearParams p) {
-  constexpr int kSlabs = D / kLpCols, kRows = D / 16, kEPC = Elem<T>::kPerChunk;
+  constexpr int kSlabs = D / kLpCols, kRows = D * 16 / kLpThreads, kEPC = Elem<T>::kPerChunk;
   extern __shared__ __align__(16) char lp_raw[];
   LpSmem<D> &sm = *reinterpret_cast<LpSmem<D> *>(lp_raw);
   const int tid = threadIdx.x;
@@ -122,7 +126,7 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
   const int first = linear_segment(n_chunks, p.segments, seg), last = linear_segment(n_chunks, p.segments, seg + 1);
   const double logd = (double)p.log_decay[u % p.G];
   if (tid <= kLpChunk) sm.pw[tid] = (float)decay_pow(logd, tid);
-  else if (!kStates && tid >= 64 && tid - 64 <= seg && tid < 64 + kLpSegments)
+  else if (!kStates && tid >= 64 && tid - 64 <= seg)
     sm.seg_w[tid - 64] = (float)decay_pow(logd, (double)(first - linear_segment(n_chunks, p.segments, tid - 64)) * kLpChunk);
   const int sr0 = (tid >> 4) * kRows, sc = (tid & 15) * 4;  // this thread's rows and columns of the state
   float *S = p.state + (size_t)u * D * D + (size_t)sr0 * D + c0 + sc;
@@ -157,7 +161,7 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
   const T *Q = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.Lmax * D, *K = reinterpret_cast<const T *>(p.K) + (size_t)u * p.Lmax * D;
   const T *V = reinterpret_cast<const T *>(p.V) + (size_t)u * p.Lmax * D + c0;
   T *O = reinterpret_cast<T *>(p.out) + (size_t)u * p.Lmax * D + c0;
-  const int row = tid >> 3, col = (tid & 7) * 4;  // this thread's token and columns (col, col + 32) of the output
+  const int row0 = (tid >> 4) * 4, col = sc;  // this thread's four tokens and four columns of the output
   const Decay2 g_chunk(decay_pow(logd, kLpChunk)), g_tail(decay_pow(logd, len - (n_chunks - 1) * kLpChunk));
   // A chunk's loads are issued while the one before is worked on.  Tokens behind the last are zeros: they add nothing to
   // the sums, and their own rows are not written.
@@ -211,55 +215,70 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
     }
     __syncthreads();
     if (!kStates) {
-      float z[4] = {0.f, 0.f, 0.f, 0.f};
-      float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+      // four tokens, four columns; and of the scores the four tokens' with keys tid & 15 and 16 further
+      float z[4][2];
+      float4 o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[i][0] = z[i][1] = 0.f;
+        o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
 #pragma unroll 2
       for (int x = 0; x < D; x += 4) {
-        const float4 q4 = *reinterpret_cast<const float4 *>(&sm.q[row][x]);
-        const float qs[4] = {q4.x, q4.y, q4.z, q4.w};
+        float4 q4[4], s4[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float4 k4 = *reinterpret_cast<const float4 *>(&sm.k[(tid & 7) + 8 * k][x]);
-          z[k] = fmaf(q4.x, k4.x, fmaf(q4.y, k4.y, fmaf(q4.z, k4.z, fmaf(q4.w, k4.w, z[k]))));
+        for (int i = 0; i < 4; ++i) {
+          q4[i] = *reinterpret_cast<const float4 *>(&sm.q[row0 + i][x]);
+          s4[i] = *reinterpret_cast<const float4 *>(&sm.s[x + i][col]);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float4 s4 = *reinterpret_cast<const float4 *>(&sm.s[x + e][col + 32 * h]);
-            o[h].x = fmaf(qs[e], s4.x, o[h].x); o[h].y = fmaf(qs[e], s4.y, o[h].y);
-            o[h].z = fmaf(qs[e], s4.z, o[h].z); o[h].w = fmaf(qs[e], s4.w, o[h].w);
-          }
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int j = (tid & 7) + 8 * k;
-        sm.p[row][j] = j <= row ? z[k] * sm.pw[row - j] : 0.f;
-      }
-      const float w = sm.pw[row + 1];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) { o[h].x *= w; o[h].y *= w; o[h].z *= w; o[h].w *= w; }
-      __syncwarp();  // a row's scores come from eight lanes of the same warp
-      const int upto = (row | 3) + 1;  // the warp's four rows end at most here
-#pragma unroll 4
-      for (int j = 0; j < upto; ++j) {
-        const float pj = sm.p[row][j];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float4 v4 = *reinterpret_cast<const float4 *>(&sm.v[j][col + 32 * h]);
-          o[h].x = fmaf(pj, v4.x, o[h].x); o[h].y = fmaf(pj, v4.y, o[h].y);
-          o[h].z = fmaf(pj, v4.z, o[h].z); o[h].w = fmaf(pj, v4.w, o[h].w);
+          const float4 k4 = *reinterpret_cast<const float4 *>(&sm.k[(tid & 15) + 16 * h][x]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            z[i][h] = fmaf(q4[i].x, k4.x, fmaf(q4[i].y, k4.y, fmaf(q4[i].z, k4.z, fmaf(q4[i].w, k4.w, z[i][h]))));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          madd4(o[i], q4[i].x, s4[0]);
+          madd4(o[i], q4[i].y, s4[1]);
+          madd4(o[i], q4[i].z, s4[2]);
+          madd4(o[i], q4[i].w, s4[3]);
         }
       }
-      if (row < nt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          T *dst = O + (size_t)(t0 + row) * D + col + 32 * h;
-          Elem<T>::store(dst, o[h].x * p.scale);
-          Elem<T>::store(dst + 1, o[h].y * p.scale);
-          Elem<T>::store(dst + 2, o[h].z * p.scale);
-          Elem<T>::store(dst + 3, o[h].w * p.scale);
+          const int j = (tid & 15) + 16 * h, row = row0 + i;
+          sm.p[row][j] = j <= row ? z[i][h] * sm.pw[row - j] : 0.f;
+        }
+        const float w = sm.pw[row0 + i + 1];
+        o[i].x *= w; o[i].y *= w; o[i].z *= w; o[i].w *= w;
+      }
+      __syncwarp();  // a row's scores come from sixteen lanes of the same warp
+#pragma unroll 1
+      for (int j = 0; j <= row0; j += 4) {
+        float4 v4[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v4[e] = *reinterpret_cast<const float4 *>(&sm.v[j + e][col]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 p4 = *reinterpret_cast<const float4 *>(&sm.p[row0 + i][j]);
+          madd4(o[i], p4.x, v4[0]);
+          madd4(o[i], p4.y, v4[1]);
+          madd4(o[i], p4.z, v4[2]);
+          madd4(o[i], p4.w, v4[3]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (row0 + i < nt) {
+          T *dst = O + (size_t)(t0 + row0 + i) * D + col;
+          Elem<T>::store(dst, o[i].x * p.scale);
+          Elem<T>::store(dst + 1, o[i].y * p.scale);
+          Elem<T>::store(dst + 2, o[i].z * p.scale);
+          Elem<T>::store(dst + 3, o[i].w * p.scale);
         }
       }
     }
