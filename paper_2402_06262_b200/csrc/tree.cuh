@@ -137,8 +137,9 @@ __device__ __forceinline__ void tree_cluster_join(const TreeParams &p, int u, in
     T *out = reinterpret_cast<T *>(p.out) + to * D + lane * kN;
 #pragma unroll
     for (int i = 0; i < kN; i += 2) {
-      if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162 *>(out + i) = __floats2bfloat162_rn(acc[i] * inv, acc[i + 1] * inv);
-      else *reinterpret_cast<float2 *>(out + i) = make_float2(acc[i] * inv, acc[i + 1] * inv);
+      const float a = acc[i] * inv, b = acc[i + 1] * inv;
+      if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162 *>(out + i) = __floats2bfloat162_rn(a, b);
+      else *reinterpret_cast<float2 *>(out + i) = make_float2(a, b);
     }
     if (lane == 0 && p.lse) p.lse[to] = (m + log2f(l)) * kLn2;
   }
@@ -158,7 +159,8 @@ struct CommitParams {
 };
 
 // Length of sequence b's accepted path: 0 unless path[0] hangs on the cached prefix and every next node on the one
-// before, which has to be an earlier one (any other parent hung on the prefix when the tree was attended).  Called by one whole warp; every lane gets the length and lane m < a the node path[m].
+// before, which has to be an earlier one (any other parent hung on the prefix when the tree was attended).  Called by one
+// whole warp; every lane gets the length and lane m < a the node path[m].
 __device__ __forceinline__ int commit_path(const CommitParams &p, int b, int lane, int &node, bool report) {
   int a = p.path_len[b];
   bool ok = a >= 0 && a <= p.A;

@@ -179,11 +179,12 @@ roco_status commit_insert_nt(const CommitParams &p, int U, cudaStream_t stream) 
 }
 
 // A unit is a chain of passes and loads: with few units more threads shorten the passes, with many it is the number of
-// units in flight that counts (8192 units x B 1024: 128 threads 60 us, 256 threads 105 us).
+// units in flight that counts.  Whole commits with 128, 256 and 512 threads: 8192 units x 1024 tokens 425, 450, 619 us; 1184 units
+// 82, 89, 113; 600 units 51, 48, 67; 32 units x 1024 18.0, 16.8, 16.8, x 2048 22, 20, 18, x 8192 40, 33, 27.
 template <typename T, int D>
 roco_status commit_insert_t(const CommitParams &p, int U, int sms, cudaStream_t stream) {
   if (U >= 8 * sms) return commit_insert_nt<T, D, 128>(p, U, stream);
-  return p.B <= 2048 ? commit_insert_nt<T, D, 256>(p, U, stream) : commit_insert_nt<T, D, 512>(p, U, stream);
+  return U > sms || p.B <= 1024 ? commit_insert_nt<T, D, 256>(p, U, stream) : commit_insert_nt<T, D, 512>(p, U, stream);
 }
 
 template <typename T, int D>

@@ -132,8 +132,8 @@ __device__ __forceinline__ bool exclude_highest(const uint32_t *vkey, float *mke
   return n >= 0;
 }
 
-// The kn slots of lowest_slots by a radix select on the keys, whatever the ties; unordered, to sc.ctl[24 ..] and sc.list_pos; false if
-// there are fewer.
+// The kn slots of lowest_slots by a radix select on the keys, whatever the ties; unordered, to sc.ctl[24 ..] and sc.list_pos;
+// false if there are fewer.
 template <int NT>
 __device__ __forceinline__ bool lowest_by_radix(const uint32_t *key, const int *pos, int live, int kn, CiScratch &sc) {
   const int tid = threadIdx.x;

@@ -12,6 +12,8 @@ constexpr int kTsKeys = 64;  // keys of a tile; the drafted nodes are one more t
 // drafted nodes), one pass with a running maximum and sum per row.  Sixteen threads share a row: each forms four of the
 // tile's 64 scores, then owns D / 16 of the row's output dimensions.  A key that a row does not see has probability
 // zero; a drafted one is left out of the sums too, so what lies in its value does not matter.
+// Bound by the latency of its two or three tiles where the cache is short (16 units x 1001 tokens x 64, 5 rows: 10.3 us), by
+// shared memory's ports in long ones (5 reads of 16 bytes for 16 products).
 template <typename T, int D>
 __global__ void __launch_bounds__(kTsThreads) tree_simt_kernel(const TreeParams p) {
   constexpr int kPitch = D + 4;  // float4 reads of 16 different rows hit different banks

@@ -14,8 +14,15 @@
 // out, so if one of their values is not finite their part of the output is formed on the CUDA cores instead, node by node
 // where a row sees the node: what lies on other branches cannot reach a row.
 //
-// What bounds it: the cache is read once; 64 KiB per tile of 128 tokens at d = 128 against about 700 cycles of
-// exponentials for N = 64.  Two CTAs per SM, so that one's prologue and epilogue run under the other's stream.
+// Few units: their tokens are divided among CTAs, which join their results as a cluster (tree_cluster_join), or in a second
+// launch where a cluster would not do.
+//
+// What bounds it.  The cache is read once.  Up to 32 rows two CTAs per SM, so that one's prologue and epilogue run under the
+// other's stream: 8192 units x 1024 tokens x 16 rows 680 us, 6.45 TB/s, the measured copy rate.  64 and 128 rows, one CTA: a
+// tile of 128 tokens at 128 rows costs its two groups about 3000 cycles (1050 of products, 770 of the exponential unit, the
+// rest instructions and what 8 warps cannot hide of their latencies; 16 warps came out the same) where its 64 KiB take 2850: 24
+// units x 8192 x 96 rows 33.5 us, of which 6 are the first tile's way here and 5 the join.  Small calls are latency: 32 units x
+// 1024 x 8 rows 9.0 us, of which about 2 are the launch, 2.5 the first tile's way, 2 the draft and 1.5 the join.
 #include <cuda.h>
 
 #include <type_traits>
@@ -526,9 +533,9 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, Sh::kTmemCols);
   if (p.cluster) {
-    tree_cluster_join<__nv_bfloat16, D>(p, u, cta_row0, min(kCols, n_nodes * p.group - cta_row0), split, warp, Sh::kThreads / 32, lane,
-                                        reinterpret_cast<const float *>(pbuf),
-                                        [&](int row) { return floats + row / N * Sh::kGroupFloats + 4 * N + row % N; }, N);
+    auto row_ref = [&](int row) { return floats + row / N * Sh::kGroupFloats + 4 * N + row % N; };
+    tree_cluster_join<__nv_bfloat16, D>(p, u, cta_row0, min(kCols, n_nodes * p.group - cta_row0), split, warp, Sh::kThreads / 32,
+                                        lane, reinterpret_cast<const float *>(pbuf), row_ref, N);
   }
 }
 
@@ -557,7 +564,10 @@ roco_status tree_tc_t(const TreeParams &p, int U, cudaStream_t stream) {
   static SmemLimit limit;
   if (!limit((const void *)kernel, Sh::kSmem)) return ROCO_ERR_CUDA;
   const unsigned blocks = (unsigned)U * (unsigned)((p.rows + N * W - 1) / (N * W)) * (unsigned)p.splits;
-  if (p.cluster) return launch_cluster(kernel, blocks, (unsigned)p.splits, Sh::kThreads, Sh::kSmem, stream, mk, mv, mn, mw, p) ? ROCO_OK : ROCO_ERR_CUDA;
+  if (p.cluster) {
+    const bool ok = launch_cluster(kernel, blocks, (unsigned)p.splits, Sh::kThreads, Sh::kSmem, stream, mk, mv, mn, mw, p);
+    return ok ? ROCO_OK : ROCO_ERR_CUDA;
+  }
   kernel<<<blocks, Sh::kThreads, Sh::kSmem, stream>>>(mk, mv, mn, mw, p);
   if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
   return p.splits > 1 ? launch_tree_join(p, ROCO_BF16, D, U, stream) : ROCO_OK;
