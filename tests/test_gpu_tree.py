@@ -202,3 +202,13 @@ def test_other_branches_may_hold_anything_however_many_rows(dtype, group, live, 
                                        low=dtype == "bf16")
         assert bool(((out[0, g, ::2].double().cpu() - o[::2]).abs() <= ob[::2]).all())
         assert bool(((lse[0, g, ::2].double().cpu() - l[::2]).abs() <= lb[::2]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,group", [(5, 1), (7, 3), (20, 2), (25, 5)])
+@pytest.mark.parametrize("ranks", [2, 3, 4, 5, 6, 7, 8])
+def test_every_number_of_ctas_that_share_a_unit(dtype, T, group, ranks):
+    """Two to eight ranges on either path, of a full cache, one that ends inside the first range (the others are empty) and
+    none."""
+    B = ranks * (256 if dtype == "bf16" else 128) - 3
+    check(make(40 + ranks, S=3, G=2, B=B, T=T, group=group, dtype=dtype, live=[B, 70, 0], nodes=[T, T - 1, T]))
