@@ -39,15 +39,18 @@ __device__ __forceinline__ int gather_candidates(const uint32_t *key, const int 
       int at = 0;
       if (lane == 0) at = atomicAdd(cnt, __popc(who));
       at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-      if (take && at < kCiShort) {
-        sc.cand[at] = j;
-        sc.cand_key[at] = (unsigned long long)k << 32 | (uint32_t)pos[j];
-      }
+      if (take && at < kCiShort) sc.cand[at] = j;
     }
   }
   named_bar_sync(kCiBar, NT);
   const int n = *cnt;
-  return n > kCiShort ? -1 : n;
+  if (n > kCiShort) return -1;
+  for (int c = threadIdx.x; c < n; c += NT) {  // (the positions, in global memory, all at once)
+    const int j = sc.cand[c];
+    sc.cand_key[c] = (unsigned long long)key[j] << 32 | (uint32_t)pos[j];
+  }
+  named_bar_sync(kCiBar, NT);
+  return n;
 }
 
 // How many of the n gathered come before (kLow) or behind this one in (key, position) order.
@@ -109,20 +112,16 @@ __device__ __forceinline__ bool exclude_highest(const uint32_t *vkey, float *mke
   }
   if (tid == 0) sc.ctl[20] = 0;
   named_bar_sync(kCiBar, NT);
-  if (tid < 32) {  // the x-th largest of them, bit by bit: the prefix grows by a one where enough values have it
-    uint32_t v[NT / 32], t = 0u;
-#pragma unroll
-    for (int i = 0; i < NT / 32; ++i) v[i] = 32 * i < groups ? sc.best[32 * i + tid] : 0u;
-#pragma unroll 1
-    for (int bit = 30; bit >= 0; --bit) {
-      const uint32_t cand = t | 1u << bit;
-      int have = 0;
-#pragma unroll
-      for (int i = 0; i < NT / 32; ++i)
-        if (32 * i < groups) have += __popc(__ballot_sync(0xffffffffu, v[i] >= cand));
-      if (have >= x) t = cand;
+  if (tid < groups) {  // the x-th largest of them: fewer than x are above it, x or more not below
+    const uint32_t mine = sc.best[tid];
+    int above = 0, below = 0;
+#pragma unroll 8
+    for (int i = 0; i < groups; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4 *>(&sc.best[i]);
+      above += (v.x > mine) + (v.y > mine) + (v.z > mine) + (v.w > mine);
+      below += (v.x < mine) + (v.y < mine) + (v.z < mine) + (v.w < mine);
     }
-    if (tid == 0) sc.threshold = t;
+    if (above < x && groups - below >= x) sc.threshold = mine;
   }
   named_bar_sync(kCiBar, NT);
   const int n = gather_candidates<NT, false>(vkey, pos, live, sc);
