@@ -179,8 +179,9 @@ roco_status commit_insert_nt(const CommitParams &p, int U, cudaStream_t stream) 
 }
 
 // A unit is a chain of passes and loads: with few units more threads shorten the passes, with many it is the number of
-// units in flight that counts.  Whole commits with 128, 256 and 512 threads: 8192 units x 1024 tokens 425, 450, 619 us; 1184 units
-// 82, 89, 113; 600 units 51, 48, 67; 32 units x 1024 18.0, 16.8, 16.8, x 2048 22, 20, 18, x 8192 40, 33, 27.
+// units in flight that counts.  Whole commits with 128, 256 and 512 threads: 8192 units x 1024 tokens 404, 430, 552 us; 1184 units
+// 80, 82, 100; 600 units 51, 47, 60; 300 units x 4096 77, 73, 79; 32 units x 1024 15.9, 15.0, 14.7, x 2048 19.1, 17.0, 15.7, x 8192
+// 35, 28, 23.
 template <typename T, int D>
 roco_status commit_insert_t(const CommitParams &p, int U, int sms, cudaStream_t stream) {
   if (U >= 8 * sms) return commit_insert_nt<T, D, 128>(p, U, stream);
