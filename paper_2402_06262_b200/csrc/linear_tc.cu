@@ -134,7 +134,6 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // uniform for the compiler too, and so is what follows
   const int segs = kStates ? p.segments - 1 : p.segments, seg = blockIdx.x % segs, u = blockIdx.x / segs;
   const int len = __shfl_sync(0xffffffffu, linear_len(p, u / p.G, tid == 0 && seg == 0 && (kStates || p.segments == 1)), 0);
-  if (kStates) launch_dependents();
   if (len == 0) {
     if (!kStates) wait_for_launch_before();
     return;
@@ -165,6 +164,10 @@ __global__ void __launch_bounds__(kLtThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_base;
+  // Not before this CTA has its tensor memory: the second launch's CTAs take all of an SM's too, and wait for this launch
+  // while they hold it.  One that came first would wait for a CTA that waits for its columns.  (At d = 64 the shared memory
+  // of both fits an SM.)
+  if (kStates) launch_dependents();
 
   // Keys of a piece of 32 tokens, times what is left of each token at the end of the chunk, as the sum of three bf16; by
   // eight warps: a lane quarter's 32 components each, 16 tokens each.  A register holds two neighbouring tokens.
