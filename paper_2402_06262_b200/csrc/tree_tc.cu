@@ -19,9 +19,9 @@
 //
 // What bounds it.  The cache is read once.  Up to 32 rows two CTAs per SM, so that one's prologue and epilogue run under the
 // other's stream: 8192 units x 1024 tokens x 16 rows 680 us, 6.45 TB/s, the measured copy rate.  64 and 128 rows, one CTA: a
-// tile of 128 tokens at 128 rows costs its two groups about 3000 cycles (1050 of products, 770 of the exponential unit, the
+// tile of 128 tokens at 128 rows costs its two groups about 3000 cycles (1050 of products, 1020 of the exponential unit, the
 // rest instructions and what 8 warps cannot hide of their latencies; 16 warps came out the same) where its 64 KiB take 2850: 24
-// units x 8192 x 96 rows 33.5 us, of which 6 are the first tile's way here and 5 the join.  Small calls are latency: 32 units x
+// units x 8192 x 96 rows 32.8 us, of which 6 are the first tile's way here and 5 the join.  Small calls are latency: 32 units x
 // 1024 x 8 rows 9.0 us, of which about 2 are the launch, 2.5 the first tile's way, 2 the draft and 1.5 the join.
 #include <cuda.h>
 
@@ -438,18 +438,15 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
         float f[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          // (two groups: of eight pairs two on the FMA pipe, the exponential unit being the limit otherwise)
-          const f32x2 e = W == 2 && ((x / 2 + i) & 7) < 2 ? exp2_poly2(d[x / 2 + i]) : exp2_mufu2(d[x / 2 + i]);
+          // (every one by the exponential unit, which keeps NaN and is good to 2^-22; a quarter by a polynomial on the FMA pipe
+          // was slower too: 1024 units x 1024 x 128 rows 158 us, now 153)
+          const f32x2 e = exp2_mufu2(d[x / 2 + i]);
           l[x / 2 + i] = add2(l[x / 2 + i], e);
           unpack2(e, f[2 * i], f[2 * i + 1]);
         }
-        if (is_draft) {  // (the polynomial ends at 2^-125, and a value that a row does not see may be as large as 2^127)
+        if (is_draft && by_hand && gt < kTreeMaxNodes) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] = (mine >> (x + i)) & 1ull ? f[i] : 0.f;
-          if (by_hand && gt < kTreeMaxNodes) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pd[gt * N + x + i] = f[i];
-          }
+          for (int i = 0; i < 8; ++i) pd[gt * N + x + i] = f[i];
         }
         *reinterpret_cast<uint4 *>(prow_p + (((pc0 + x / 8) ^ (prow & 7)) << 4)) =
             make_uint4(tt_pack(f[0], f[1]), tt_pack(f[2], f[3]), tt_pack(f[4], f[5]), tt_pack(f[6], f[7]));
