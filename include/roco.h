@@ -386,7 +386,8 @@ roco_status roco_decode_step_cluster(roco_cache *cache, const void *q, const voi
  *   workspace    >= roco_tree_attend_workspace_bytes(cache, T, group) device bytes (which may be 0: then NULL will do),
  *                256-byte aligned, of this call alone while it runs
  * What a node does not see has no influence on its row, whatever it holds: empty slots and nodes on other branches may
- * be infinite or NaN.  A node count outside [0, T] sets ROCO_DEV_BAD_TREE and counts as 0; a parent outside [-1, i) sets
+ * be infinite or NaN.  What it sees comes out as in the formula; finite values may be up to 2^80 in magnitude (sums of
+ * probabilities and values are formed before their division by the sum of the probabilities).  A node count outside [0, T] sets ROCO_DEV_BAD_TREE and counts as 0; a parent outside [-1, i) sets
  * it and counts as -1.
  * On the tensor cores for kv_dtype ROCO_BF16 and a positive scale, on the CUDA cores otherwise.
  */

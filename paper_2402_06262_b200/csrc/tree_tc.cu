@@ -6,10 +6,11 @@
 // One pass over the cache.  A thread owns one key of a tile: it forms p = 2^(z - m) for its N scores, keeps N partial sums
 // of its own in registers (joined over the lanes once, at the end) and writes the N probabilities as bf16, the second
 // product's operand.  The reference m of a row need not be its maximum: any score that the row's sum contains will do, so
-// it is that of the first cached key, and moves only when a score comes out more than 2^60 above it (fp32 and bf16 share
-// their exponents, so up to there neither sums nor probabilities lose anything; the sum holds a 1).  That costs one vote per
-// tile instead of a maximum over the lanes.  When it moves, to the tile's maximum, the row's column of O^T and its sums are
-// rescaled.
+// it is that of the first cached key, and moves only when a score comes out more than 32 binary orders above it (fp32 and bf16
+// share their exponents, so probabilities and sums above 1 lose nothing; the sum holds a 1).  The sum of a row's up to 8256 terms
+// p v is then below 2^(32 + 13.02) max |v|, inside fp32 for values up to 2^82.  (At 16 orders that would be 2^98, and the moves of
+// rows with a few dominant keys show: 24 units x 8192 x 96 rows 33.6 us instead of 32.0.)  It costs one vote per tile instead of
+// a maximum over the lanes.  When it moves, to the tile's maximum, the row's column of O^T and its sums are rescaled.
 // The drafted tokens are the last tile, masked by the rows' ancestor sets.  A product with zero keeps no NaN or infinity
 // out, so if one of their values is not finite their part of the output is formed on the CUDA cores instead, node by node
 // where a row sees the node: what lies on other branches cannot reach a row.
@@ -36,7 +37,7 @@ constexpr int kTtTile = 128;  // keys of a tile
 constexpr int kTtGroup = 128;            // threads of a consumer group
 constexpr int kTtBar = 1;     // named barriers of the consumer groups (kTtBar + group)
 constexpr int kTtBarQ = 3;    // and of all of them with the warp of the products
-constexpr float kTtMoveReference = 60.f;  // binary orders above the reference at which a row moves to a new one
+constexpr float kTtMoveReference = 32.f;  // binary orders above the reference at which a row moves to a new one
 
 // W groups of four consumer warps, N query rows each, share the tiles of a CTA and the products over them, N W columns wide
 // (a product reads its 4 KiB of keys or values per 16-step once, however many columns it has); C CTAs per SM.

@@ -1,5 +1,7 @@
-"""Attention of a tree of drafted tokens on values that a row does see: NaN and infinities have to come out, and a
-log-sum-exp is good to single precision in every row."""
+"""Attention of a tree of drafted tokens on values that a row does see: NaN and infinities have to come out, large finite
+values must not turn into them, and a log-sum-exp is good to single precision in every row."""
+import math
+
 import pytest
 import torch
 
@@ -96,6 +98,29 @@ def test_keys_of_score_minus_infinity_take_no_part(dtype, T, group, live):
     f = {n: c.t[n][0, 0].double() for n in ("Q", "K_new", "V_new")}
     o, l, ob, lb = ref.tree_attend(k, v, len(keep), f["Q"], f["K_new"], f["V_new"], c.t["parent"][0].tolist(), T, c.d ** -0.5,
                                    low=dtype == "bf16")
+    assert bool(((out[0, 0].double().cpu() - o).abs() <= ob).all()) and bool(((lse[0, 0].double().cpu() - l).abs() <= lb).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,group", ROWS)
+@pytest.mark.parametrize("live", [40, 300, 2000])
+@pytest.mark.parametrize("bits", [10, 31, 50, 90])
+def test_large_values(dtype, T, group, live, bits):
+    """Values up to 2^80 behind a first cached key whose score lies 10 to 90 binary orders below the others': the definition is
+    a mean of the values and stays finite.  (The second product's terms are far from the end of fp32 in the bound's
+    arithmetic too: it scales with the values.)"""
+    c = make(11 + T, S=1, G=1, B=2000, T=T, group=group, dtype=dtype, live=[live])
+    big = 2.0 ** 76
+    c.t["V"], c.t["V_new"] = c.t["V"] * big, c.t["V_new"] * big
+    assert float(c.t["V"][0, 0, :live].abs().max()) < 2.0 ** 80 and float(c.t["V_new"].abs().max()) < 2.0 ** 80
+    c.t["Q"][..., 5] = 4.0
+    c.t["K"][..., 5] = 0.0
+    c.t["K"][0, 0, 0, 5] = -bits * math.log(2) * math.sqrt(c.d) / 4
+    _, out, lse = run(c)
+    f = {n: c.t[n][0, 0].double() for n in ("K", "V", "Q", "K_new", "V_new")}
+    o, l, ob, lb = ref.tree_attend(f["K"], f["V"], live, f["Q"], f["K_new"], f["V_new"], c.t["parent"][0].tolist(), T, c.d ** -0.5,
+                                   low=dtype == "bf16")
+    assert bool(out[0, 0].isfinite().all())
     assert bool(((out[0, 0].double().cpu() - o).abs() <= ob).all()) and bool(((lse[0, 0].double().cpu() - l).abs() <= lb).all())
 
 
