@@ -26,6 +26,7 @@
 // 1024 x 8 rows 9.0 us, of which about 2 are the launch, 2.5 the first tile's way, 2 the draft and 1.5 the join.
 #include <cuda.h>
 
+#include <cfloat>
 #include <type_traits>
 
 #include "tc.cuh"
@@ -383,7 +384,8 @@ __global__ void __launch_bounds__((TtShape<D, N, W, C>::kThreads), C)
           const float top = fmaxf(fmaxf(red[gt], red[N + gt]), fmaxf(red[2 * N + gt], red[3 * N + gt]));
           const float old = t == 0 ? -INFINITY : -nref[gt];
           float ref = fmaxf(old, top);
-          if (ref == -INFINITY) ref = 0.f;  // a row that does not exist sees nothing
+          // nothing seen so far (every score is minus infinity, or the row does not exist): the first finite score moves it
+          if (ref == -INFINITY) ref = -FLT_MAX;
           alpha[gt] = t == 0 ? 0.f : exp2f(old - ref);
           nref[gt] = -ref;
         }

@@ -148,3 +148,22 @@ def test_the_log_sum_exp_is_good_to_single_precision(dtype, T, group):
     bound = 3 * u * x + 2.0 ** -22 + u + 4 * u * want + 2.0 ** -22 * want
     off = (lse[0].double().cpu() - want[:, None, None]).abs()
     assert bool((off <= bound[:, None, None]).all()), f"off by {float((off / bound[:, None, None]).max())} of its bound"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,group", ROWS)
+@pytest.mark.parametrize("B,live,far", [(300, 1, 1), (300, 200, 200), (700, 700, 300), (700, 700, 690), (8192, 8000, 5000)])
+def test_a_range_of_cached_keys_without_a_finite_score(dtype, T, group, B, live, far):
+    """The first `far` cached keys at scores below fp32's range (finite keys and queries), all others and the drafted ones 200
+    binary orders below zero: what is left is an ordinary softmax."""
+    c = make(15 + T, S=1, G=1, B=B, T=T, group=group, dtype=dtype, live=[live])
+    c.t["Q"][..., 3] = 200.0
+    for f in ("K", "K_new"):
+        c.t[f][..., 3] = -200 * math.log(2) * math.sqrt(c.d) / 200
+    c.t["K"][0, 0, :far, 3] = -3e38
+    _, out, lse = run(c)
+    k, v = c.t["K"][0, 0, far:live].double(), c.t["V"][0, 0, far:live].double()
+    f = {n: c.t[n][0, 0].double() for n in ("Q", "K_new", "V_new")}
+    o, l, ob, lb = ref.tree_attend(k, v, live - far, f["Q"], f["K_new"], f["V_new"], c.t["parent"][0].tolist(), T, c.d ** -0.5,
+                                   low=dtype == "bf16")
+    assert bool(((out[0, 0].double().cpu() - o).abs() <= ob).all()) and bool(((lse[0, 0].double().cpu() - l).abs() <= lb).all())
