@@ -1,0 +1,62 @@
+"""Commit of an accepted path: the eviction rule on exact ties at different counts."""
+import pytest
+import torch
+
+import paper_2402_06262_b200 as R
+from tree_cases import make
+
+pytestmark = pytest.mark.gpu
+
+
+def commit_without_mass(c, a, r, mode=R.ROCO_SCOPE_EXCLUDE_TOP_R):
+    """Commits nodes 0 .. a - 1 of a chain with a log-sum-exp at which every probability is exactly zero: Acc and Acc^square stay
+    as they are and Count grows by a."""
+    cache = c.cache()
+    q = c.dev("Q")
+    lse = torch.full(c.t["Q"].shape[:4], 1000.0, device="cuda")
+    ev, ep = (torch.zeros(c.S, c.G, a, dtype=torch.int32, device="cuda") for _ in range(2))
+    R.roco_tree_commit(cache, q, c.dev("K_new"), c.dev("V_new"), lse, c.dev("parent"),
+                       torch.arange(a, dtype=torch.int32, device="cuda").expand(c.S, a).contiguous(),
+                       torch.full((c.S,), a, dtype=torch.int32, device="cuda"), r, ev, evicted_pos=ep, scope_mode=mode)
+    assert R.roco_device_status(cache) == 0
+    return ep.sort(-1)[0].cpu()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,B", [(2, 400), (2, 1500), (1200, 160)])
+@pytest.mark.parametrize("a", [1, 3, 16])
+@pytest.mark.parametrize("den", [1, 3, 10, 49])
+def test_equal_means_at_different_counts_fall_to_the_lowest_position(dtype, G, B, a, den):
+    """Count = den m and Acc = m 2^-10, so every mean is 2^-10 / den, whatever the count, in fp32 or (3, 10, 49) not."""
+    c = make(21, S=1, G=G, B=B, d=64, T=16, dtype=dtype, shape="chain")
+    m = c.t["n"] + a                        # all different within a unit
+    c.t["n"] = den * m - a                  # Count becomes den m
+    c.t["s"] = m.float() * 2.0 ** -10
+    c.t["q"] = m.float() * 2.0 ** -19
+    got = commit_without_mass(c, a, 0)
+    assert torch.equal(got, c.t["pos"].sort(-1)[0][..., :a])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G,B", [(2, 400), (2, 1500), (1200, 160)])
+@pytest.mark.parametrize("a", [1, 3, 16])
+@pytest.mark.parametrize("r", [2, 60])
+@pytest.mark.parametrize("mode", [R.ROCO_SCOPE_EXCLUDE_TOP_R, R.ROCO_SCOPE_LOWEST_R])
+def test_equal_variances_at_different_counts_fall_to_the_lowest_position(dtype, G, B, a, r, mode):
+    """Acc^square = Count (c^2 + 2^-20) with the mean c = 2^-10 at the low positions and 2^-11 at the others: every variance is 2^-20
+    exactly, the scope is the lowest positions, and in it the lower mean leaves first, the lowest position of those."""
+    c = make(22, S=1, G=G, B=B, d=64, T=16, dtype=dtype, shape="chain")
+    n = (c.t["n"] + a).float()
+    order = c.t["pos"].argsort(-1).argsort(-1)          # 0: the lowest position
+    half = order >= B // 2
+    c.t["s"] = n * torch.where(half, 2.0 ** -11, 2.0 ** -10)
+    c.t["q"] = n * torch.where(half, 5 * 2.0 ** -22, 2.0 ** -19)
+    got = commit_without_mass(c, a, r, mode)
+    pos = c.t["pos"].sort(-1)[0]
+    left, want = list(range(B)), []
+    for _ in range(a):                                  # by rank of position
+        m = max(1, min(len(left), r if mode == R.ROCO_SCOPE_LOWEST_R else len(left) - r))
+        v = min(left[:m], key=lambda j: (j < B // 2, j))
+        want.append(v)
+        left.remove(v)
+    assert torch.equal(got, pos[..., sorted(want)])
