@@ -446,7 +446,8 @@ typedef struct {
  * Where the units are few the prompt is divided among several CTAs per unit, which meet in the workspace.
  *
  *   Q, K, V      [S][G][Lmax][d];  rows at lens[b] and behind may hold anything.  Rows before must be finite: a
- *                NaN or infinity there may reach every output row of its unit
+ *                NaN or infinity there may reach every output row of its unit.  A row does not depend on the rows behind
+ *                it; its products with the rows before it have to stay inside fp32's range
  *   lens         [S] int32 DEVICE array, 0 <= lens <= Lmax; any other value sets ROCO_DEV_BAD_LENS and counts as 0.
  *                lens 0 leaves a sequence's state as it is
  *   out          [S][G][Lmax][d]; rows at lens[b] and behind are left as they were; must not overlap Q, K or V

@@ -376,11 +376,11 @@ __global__ void __launch_bounds__(kLtThreads, 1)
                   pk[e >> 1] = lt_pack2(mul2(mul2(pack2(c4.x, c4.y), b2), pack2u(r[e], r[e + 1])));
                   pk[(e >> 1) + 1] = lt_pack2(mul2(mul2(pack2(c4.z, c4.w), b2), pack2u(r[e + 2], r[e + 3])));
                 }
-              } else {  // on it: the table's zeros are the mask
+              } else {  // on it: a later token's score is left out, not multiplied by zero (it may have left fp32's range)
                 tmem_ld_wait(r);
+                auto weighted = [&](int e) { return j0 + e <= i ? __uint_as_float(r[e]) * w[-e] : 0.f; };
 #pragma unroll
-                for (int e = 0; e < 32; e += 2)
-                  pk[e >> 1] = lt_pack(__uint_as_float(r[e]) * w[-e], __uint_as_float(r[e + 1]) * w[-e - 1]);
+                for (int e = 0; e < 32; e += 2) pk[e >> 1] = lt_pack(weighted(e), weighted(e + 1));
               }
             }
             tmem_st16(tl + kLtColS + (uint32_t)(half * 64 + cc * 16), pk);
