@@ -417,14 +417,23 @@ roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void 
  *   A            1 <= A <= ROCO_TREE_MAX_PATH, A <= T, r + A <= B; r >= 0 (ROCO_SCOPE_LOWEST_R: r >= 1)
  *   evicted_slot [S][G][A] freed slots in increasing order, padded with -1;   evicted_pos likewise, or NULL
  * A path_len outside [0, A] or a path that is not a chain of the tree from its root, every node behind its
- * parent, sets ROCO_DEV_BAD_TREE and counts
- * as a = 0.  K_new and V_new must not overlap the cache.
+ * parent, sets ROCO_DEV_BAD_TREE and counts as a = 0.  Where the sequences' trees have fewer than T nodes, the path's are among
+ * those that there are: this call cannot tell a padding row from a node, roco_tree_commit_nodes can.  K_new and V_new must
+ * not overlap the cache.
  */
 #define ROCO_TREE_MAX_PATH 16
 roco_status roco_tree_commit(roco_cache *cache, const void *Q, const void *K_new, const void *V_new, const float *lse,
                              const int32_t *parent, const int32_t *path, const int32_t *path_len, int T, int group,
                              int A, int r, int scope_mode, float scale, int32_t *evicted_slot, int32_t *evicted_pos,
                              void *stream);
+
+/* roco_tree_commit with the sequences' node counts as given to roco_tree_attend: a path through a node at nodes[b] or behind
+ * (whose rows and log-sum-exps hold anything), or a count outside [0, T], sets ROCO_DEV_BAD_TREE and counts as a = 0.
+ *   nodes        [S] int32 DEVICE array, or NULL: T everywhere                                                     */
+roco_status roco_tree_commit_nodes(roco_cache *cache, const void *Q, const void *K_new, const void *V_new,
+                                   const float *lse, const int32_t *parent, const int32_t *nodes, const int32_t *path,
+                                   const int32_t *path_len, int T, int group, int A, int r, int scope_mode, float scale,
+                                   int32_t *evicted_slot, int32_t *evicted_pos, void *stream);
 
 /*
  * Linear attention with a decay for each head (the paper has no counterpart): the other attention whose memory does not

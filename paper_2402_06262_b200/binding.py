@@ -31,7 +31,7 @@ EXPORTS = ("roco_version", "roco_status_string", "roco_prefill_workspace_bytes",
            "roco_decode_step_host_begin", "roco_decode_step_host_end", "roco_gqa_block_step",
            "roco_prefill_blockwise_gqa", "roco_prefill_with_output", "roco_decode_cluster_ranks",
            "roco_decode_step_cluster", "roco_decode_step_policy_ordered", "roco_decode_step_split_ordered",
-           "roco_tree_attend_workspace_bytes", "roco_tree_attend", "roco_tree_commit",
+           "roco_tree_attend_workspace_bytes", "roco_tree_attend", "roco_tree_commit", "roco_tree_commit_nodes",
            "roco_linear_prefill_workspace_bytes", "roco_linear_prefill", "roco_linear_step",
            "roco_linear_device_status")
 
@@ -164,6 +164,10 @@ def lib() -> C.CDLL:
         L.roco_tree_commit.argtypes = [C.POINTER(roco_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_float,
                                        C.c_void_p, C.c_void_p, C.c_void_p]
+        L.roco_tree_commit_nodes.restype = C.c_int
+        L.roco_tree_commit_nodes.argtypes = [C.POINTER(roco_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int,
+                                             C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]
         L.roco_linear_prefill_workspace_bytes.restype = C.c_size_t
         L.roco_linear_prefill_workspace_bytes.argtypes = [C.POINTER(roco_linear_state), C.c_int]
         L.roco_linear_prefill.restype = C.c_int
@@ -615,10 +619,11 @@ def roco_tree_attend(cache: Cache, Q, K_new, V_new, parent, attn_out, nodes=None
 
 
 def roco_tree_commit(cache: Cache, Q, K_new, V_new, lse, parent, path, path_len, r: int, evicted_slot, evicted_pos=None,
-                     scope_mode=ROCO_SCOPE_EXCLUDE_TOP_R, scale: Optional[float] = None):
+                     scope_mode=ROCO_SCOPE_EXCLUDE_TOP_R, scale: Optional[float] = None, nodes=None):
     """The accepted path of a draft tree enters the cache: statistics of its queries, evictions to the budget, insertion.
-    Q, K_new, V_new, parent as given to roco_tree_attend, lse what it returned; path [S][A] int32 node indices from the
-    root on, path_len [S] int32; evicted_slot, evicted_pos [S][G][A] int32."""
+    Q, K_new, V_new, parent, nodes as given to roco_tree_attend (without nodes a path through padding is not noticed), lse
+    what it returned; path [S][A] int32 node indices from the root on, path_len [S] int32; evicted_slot, evicted_pos
+    [S][G][A] int32."""
     what, dev = "roco_tree_commit", _device()
     T, group = _check_tree(what, cache, Q, K_new, V_new, dev)
     if not isinstance(path, torch.Tensor) or path.dim() != 2:
@@ -626,15 +631,17 @@ def roco_tree_commit(cache: Cache, Q, K_new, V_new, lse, parent, path, path_len,
     S, G, A = cache.S, cache.G, path.shape[1]
     _need(what, "lse", lse, Q.shape[:4], torch.float32, dev)
     _need(what, "parent", parent, (S, T), torch.int32, dev)
+    if nodes is not None:
+        _need(what, "nodes", nodes, (S,), torch.int32, dev)
     _need(what, "path", path, (S, A), torch.int32, dev)
     _need(what, "path_len", path_len, (S,), torch.int32, dev)
     _need(what, "evicted_slot", evicted_slot, (S, G, A), torch.int32, dev)
     if evicted_pos is not None:
         _need(what, "evicted_pos", evicted_pos, (S, G, A), torch.int32, dev)
     scale = cache.d ** -0.5 if scale is None else scale
-    rc = lib().roco_tree_commit(C.byref(cache.c), _at(Q), _at(K_new), _at(V_new), _at(lse), _at(parent), _at(path),
-                                _at(path_len), T, group, A, r, scope_mode, scale, _at(evicted_slot), _at(evicted_pos),
-                                _raw_stream(dev))
+    rc = lib().roco_tree_commit_nodes(C.byref(cache.c), _at(Q), _at(K_new), _at(V_new), _at(lse), _at(parent), _at(nodes),
+                                      _at(path), _at(path_len), T, group, A, r, scope_mode, scale, _at(evicted_slot),
+                                      _at(evicted_pos), _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
 

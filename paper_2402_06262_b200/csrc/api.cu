@@ -721,10 +721,10 @@ roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void 
   return launch_tree_attend_simt(p, cache->kv_dtype, cache->d, U, static_cast<cudaStream_t>(stream));
 }
 
-roco_status roco_tree_commit(roco_cache *cache, const void *Q, const void *K_new, const void *V_new, const float *lse,
-                             const int32_t *parent, const int32_t *path, const int32_t *path_len, int T, int group,
-                             int A, int r, int scope_mode, float scale, int32_t *evicted_slot, int32_t *evicted_pos,
-                             void *stream) {
+roco_status roco_tree_commit_nodes(roco_cache *cache, const void *Q, const void *K_new, const void *V_new,
+                                   const float *lse, const int32_t *parent, const int32_t *nodes, const int32_t *path,
+                                   const int32_t *path_len, int T, int group, int A, int r, int scope_mode, float scale,
+                                   int32_t *evicted_slot, int32_t *evicted_pos, void *stream) {
   NvtxRange range("roco_tree_commit");
   roco_status st = check_tree(cache, T, group);
   if (st != ROCO_OK) return st;
@@ -739,11 +739,19 @@ roco_status roco_tree_commit(roco_cache *cache, const void *Q, const void *K_new
   p.s = cache->s; p.q = cache->q; p.n = cache->n; p.pos = cache->pos; p.live = cache->live; p.t_next = cache->t_next;
   p.status = cache->status;
   p.Q = static_cast<const char *>(Q); p.k_new = static_cast<const char *>(K_new); p.v_new = static_cast<const char *>(V_new);
-  p.lse = lse; p.parent = parent; p.path = path; p.path_len = path_len;
+  p.lse = lse; p.parent = parent; p.nodes = nodes; p.path = path; p.path_len = path_len;
   p.ev_slot = evicted_slot; p.ev_pos = evicted_pos;
   p.B = cache->B; p.T = T; p.group = group; p.G = cache->G; p.A = A; p.r = r; p.scope_mode = scope_mode; p.scale = scale;
   return launch_tree_commit(p, cache->kv_dtype, cache->d, cache->S * cache->G, device_sms(),
                             static_cast<cudaStream_t>(stream));
+}
+
+roco_status roco_tree_commit(roco_cache *cache, const void *Q, const void *K_new, const void *V_new, const float *lse,
+                             const int32_t *parent, const int32_t *path, const int32_t *path_len, int T, int group,
+                             int A, int r, int scope_mode, float scale, int32_t *evicted_slot, int32_t *evicted_pos,
+                             void *stream) {
+  return roco_tree_commit_nodes(cache, Q, K_new, V_new, lse, parent, nullptr, path, path_len, T, group, A, r, scope_mode,
+                                scale, evicted_slot, evicted_pos, stream);
 }
 
 size_t roco_linear_prefill_workspace_bytes(const roco_linear_state *state, int Lmax) {

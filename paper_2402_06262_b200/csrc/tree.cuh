@@ -26,7 +26,8 @@ struct TreeParams {
 constexpr int kTreeMaxNodes = ROCO_TREE_MAX_NODES;
 
 // Nodes of sequence b; a count outside [0, T] is none.
-__device__ __forceinline__ int tree_nodes(const TreeParams &p, int b, bool report) {
+template <typename Params>
+__device__ __forceinline__ int tree_nodes(const Params &p, int b, bool report) {
   const int n = p.nodes ? p.nodes[b] : p.T;
   if (n >= 0 && n <= p.T) return n;
   if (report) atomicOr(p.status, ROCO_DEV_BAD_TREE);
@@ -152,17 +153,18 @@ struct CommitParams {
   int *n, *pos, *live, *t_next, *status;
   const char *Q, *k_new, *v_new;
   const float *lse;
-  const int *parent, *path, *path_len;
+  const int *parent, *nodes, *path, *path_len;  // nodes: NULL where every sequence has T
   int *ev_slot, *ev_pos;
   int B, T, group, G, A, r, scope_mode;
   float scale;
 };
 
-// Length of sequence b's accepted path: 0 unless path[0] hangs on the cached prefix and every next node on the one
-// before, which has to be an earlier one (any other parent hung on the prefix when the tree was attended).  Called by one
+// Length of sequence b's accepted path: 0 unless its nodes exist, path[0] hangs on the cached prefix and every next node on the
+// one before, which has to be an earlier one (any other parent hung on the prefix when the tree was attended).  Called by one
 // whole warp; every lane gets the length and lane m < a the node path[m].
 __device__ __forceinline__ int commit_path(const CommitParams &p, int b, int lane, int &node, bool report) {
   int a = p.path_len[b];
+  const int n_nodes = tree_nodes(p, b, report && lane == 0);
   bool ok = a >= 0 && a <= p.A;
   if (!ok) a = 0;
   node = lane < a ? p.path[(size_t)b * p.A + lane] : -1;
@@ -170,7 +172,7 @@ __device__ __forceinline__ int commit_path(const CommitParams &p, int b, int lan
   bool chain = true;
   if (lane < a) {
     const int from = lane ? before : -1;
-    chain = node > from && node < p.T && p.parent[(size_t)b * p.T + node] == from;
+    chain = node > from && node < n_nodes && p.parent[(size_t)b * p.T + node] == from;
   }
   ok = __all_sync(0xffffffffu, chain) && ok;
   if (!ok) {

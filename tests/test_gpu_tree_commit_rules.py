@@ -1,9 +1,9 @@
-"""Commit of an accepted path: the eviction rule on exact ties at different counts."""
+"""Commit of an accepted path: the eviction rule on exact ties at different counts and paths through padding."""
 import pytest
 import torch
 
 import paper_2402_06262_b200 as R
-from tree_cases import make
+from tree_cases import CACHE_FIELDS, make
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +60,33 @@ def test_equal_variances_at_different_counts_fall_to_the_lowest_position(dtype, 
         want.append(v)
         left.remove(v)
     assert torch.equal(got, pos[..., sorted(want)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_path_through_padding_is_refused(dtype):
+    """Sequences of 6, 3 and 0 drafted nodes whose padding continues the chain, and whose log-sum-exps behind the last node are
+    what happened to be there."""
+    c = make(23, S=3, G=2, B=60, T=6, dtype=dtype, shape="chain", nodes=[6, 3, 0])
+    cache, before = c.cache(), c.cache()
+    q = c.dev("Q")
+    nodes = torch.tensor(c.nodes, dtype=torch.int32, device="cuda")
+    lse = torch.zeros(q.shape[:4], device="cuda")
+    args = (q, c.dev("K_new"), c.dev("V_new"), c.dev("parent"))
+    R.roco_tree_attend(cache, *args, torch.zeros_like(q), nodes=nodes, lse_out=lse)
+    ev = torch.zeros(3, 2, 4, dtype=torch.int32, device="cuda")
+    path = torch.arange(4, dtype=torch.int32, device="cuda").expand(3, 4).contiguous()
+    R.roco_tree_commit(cache, *args[:3], lse, args[3], path, torch.tensor([4, 4, 1], dtype=torch.int32, device="cuda"), 5, ev,
+                       nodes=nodes)
+    assert R.roco_device_status(cache) == 8
+    for f in CACHE_FIELDS:
+        x, y = getattr(cache, f), getattr(before, f)
+        assert torch.equal(x[1:].view(torch.uint8), y[1:].view(torch.uint8)), f
+    assert bool((ev[0] >= 0).all()) and bool((ev[1:] == -1).all())
+    # the nodes that there are, and a node count that is none
+    for n, good in (([6, 3, 0], True), ([7, 3, 0], False), ([-1, 3, 0], False)):
+        cache = c.cache()
+        R.roco_tree_commit(cache, *args[:3], lse, args[3], path, torch.tensor([4, 3, 0], dtype=torch.int32, device="cuda"), 5, ev,
+                           nodes=torch.tensor(n, dtype=torch.int32, device="cuda"))
+        assert R.roco_device_status(cache) == (0 if good else 8)
+        assert (cache.t_next - before.t_next)[:, 0].tolist() == [4 if good else 0, 3, 0]
+        assert bool((ev[0] >= 0).all()) == good
