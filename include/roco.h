@@ -400,8 +400,7 @@ roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void 
 
 /*
  * The accepted path of a draft tree enters the cache.  For a sequence that accepted a nodes path[0..a-1] (path[0] a
- * child of the cached prefix, each next one a child of the one before), every unit of it does what a step of order
- * ROCO_ATTEND_FIRST does for one token:
+ * child of the cached prefix, each next one a child of the one before), in every unit of it:
  *   1. Statistics of Sec. 4.3 of the cached tokens j: Count += a, Acc += sum_i pbar_ij, Acc^square += sum_i pbar_ij^2 over
  *      the accepted queries i, where pbar is the mean over the group's heads of p_ij = exp(scale * Q_i.K_j - lse_i) and
  *      lse what roco_tree_attend returned for these Q, K_new, V_new, this scale and this cache.
@@ -410,7 +409,10 @@ roco_status roco_tree_attend(const roco_cache *cache, const void *Q, const void 
  *   3. The accepted tokens (positions t_next .. t_next + a - 1) take, in path order, the freed slots and then slots live,
  *      live + 1, ..., all in increasing slot order.  Accepted token m starts with the queries that saw it, its own and
  *      those behind it on the path: Count = a - m, Acc and Acc^square from their pbar_im.
- * a = 0 leaves a sequence's units as they are.
+ * a = 0 leaves a sequence's units as they are.  One token into a cache with room is a step of order ROCO_EVICT_FIRST (its query
+ * sees its own key and counts for it).  In a full cache that step evicts on the statistics before its attention, the commit on
+ * those behind it, since the tree was attended with every cached token in place.  It is not ROCO_ATTEND_FIRST, whose queries
+ * do not see their own tokens and whose tokens enter with empty statistics.
  *
  *   Q, K_new, V_new, parent, T, group   as given to roco_tree_attend;   lse [S][G][T][group] fp32
  *   path         [S][A] int32 DEVICE array of node indices;   path_len [S] int32 DEVICE array, 0..A

@@ -1,7 +1,9 @@
-"""Commit of an accepted path: the eviction rule on exact ties at different counts and paths through padding."""
+"""Commit of an accepted path: the eviction rule on exact ties at different counts, paths through padding, and what a commit of
+one token has in common with a decode step."""
 import pytest
 import torch
 
+import operator_reference as ref
 import paper_2402_06262_b200 as R
 from tree_cases import CACHE_FIELDS, make
 
@@ -90,3 +92,40 @@ def test_a_path_through_padding_is_refused(dtype):
         assert R.roco_device_status(cache) == (0 if good else 8)
         assert (cache.t_next - before.t_next)[:, 0].tolist() == [4 if good else 0, 3, 0]
         assert bool((ev[0] >= 0).all()) == good
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_with_room_a_commit_of_one_token_is_a_decode_step(dtype, d):
+    """Where nothing is evicted, a tree of one node that is attended and committed leaves what roco_decode_step leaves (EVICT_FIRST:
+    the query sees its own key): the same output, log-sum-exp and insertion, and statistics that differ by roundings."""
+    S, G, B = 2, 3, 200
+    c = make(24, S=S, G=G, B=B, T=1, d=d, dtype=dtype, live=[150, 199], junk=0.0)
+    tree, step = c.cache(), c.cache()
+    q, k, v = c.dev("Q"), c.dev("K_new"), c.dev("V_new")
+    out, lse = torch.zeros_like(q), torch.zeros(S, G, 1, 1, device="cuda")
+    R.roco_tree_attend(tree, q, k, v, c.dev("parent"), out, lse_out=lse)
+    one, zero = (f((S, 1), dtype=torch.int32, device="cuda") for f in (torch.ones, torch.zeros))
+    R.roco_tree_commit(tree, q, k, v, lse, c.dev("parent"), zero, one[:, 0].contiguous(), 20,
+                       torch.zeros(S, G, 1, dtype=torch.int32, device="cuda"))
+    out2 = torch.zeros(S, G, d, dtype=q.dtype, device="cuda")
+    R.roco_decode_step(step, q.reshape(S, G, d), k.reshape(S, G, d), v.reshape(S, G, d), 20, out2,
+                       torch.zeros(S, G, dtype=torch.int32, device="cuda"), step_order=R.ROCO_EVICT_FIRST)
+    for f in ("K", "V", "n", "pos", "live", "t_next"):
+        a, b = getattr(tree, f), getattr(step, f)
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), f
+    for b in range(S):
+        n = c.live[b] + 1
+        for g in range(G):
+            st = {f: c.t[f][b, g].clone().double() if f in ("K", "V", "s", "q") else c.t[f][b, g].clone() for f in CACHE_FIELDS}
+            st["live"], st["t_next"] = c.live[b], int(st["t_next"])
+            x = {f: c.t[f][b, g].double() for f in ("K", "V", "Q", "K_new", "V_new")}
+            o, l, ob, lb = ref.tree_attend(x["K"], x["V"], c.live[b], x["Q"], x["K_new"], x["V_new"], [-1], 1, d ** -0.5,
+                                           low=dtype == "bf16")
+            _, _, _, sb, qb = ref.tree_commit(st, x["Q"], x["K_new"], x["V_new"], l, [0], 20, False, d ** -0.5)
+            # the log-sum-exp that each took carries its own error into the probabilities (at most 1 each)
+            sb, qb = sb[:n] + 1.01 * float(lb), qb[:n] + 2.02 * float(lb)
+            for cache in (tree, step):
+                assert bool(((cache.s[b, g, :n].double().cpu() - st["s"][:n]).abs() <= sb).all())
+                assert bool(((cache.q[b, g, :n].double().cpu() - st["q"][:n]).abs() <= qb).all())
+            for y in (out[b, g, 0, 0], out2[b, g]):
+                assert bool(((y.double().cpu() - o[0, 0]).abs() <= ob[0, 0]).all())
