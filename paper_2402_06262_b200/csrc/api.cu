@@ -780,7 +780,7 @@ roco_status roco_linear_prefill(const roco_linear_state *state, const void *Q, c
   if ((long long)state->S * state->G * p.segments * (state->d / 64) > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
   if (state->dtype == ROCO_BF16)
     return launch_linear_prefill_tc(p, state->d, state->S * state->G, static_cast<cudaStream_t>(stream));
-  return launch_linear_prefill_simt(p, state->dtype, state->d, state->S * state->G, static_cast<cudaStream_t>(stream));
+  return launch_linear_prefill_simt(p, state->d, state->S * state->G, static_cast<cudaStream_t>(stream));
 }
 
 roco_status roco_linear_step(const roco_linear_state *state, const void *q, const void *k, const void *v,

@@ -150,14 +150,15 @@ __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddep
 // ---- attention of a tree of drafted tokens over the cache, commit of the accepted path (tree.cuh)
 struct TreeParams;
 struct CommitParams;
-// CUDA cores; p.splits > 1: partial results to p.part_o / p.part_ml and a second launch that joins them.
+// CUDA cores.  p.splits > 1: the CTAs that share a unit's tokens join their results as a cluster (p.cluster), or leave them in
+// p.part_o / p.part_ml for a second launch.
 int tree_simt_row_blocks(int rows);
 roco_status launch_tree_attend_simt(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
 // Tensor cores (bf16, positive scale); query rows of a CTA and CTAs per SM for that many rows of a unit.
 int tree_tc_rows(int rows);
 int tree_tc_ctas(int rows);
 roco_status launch_tree_attend_tc(const TreeParams &p, int d, int U, int sms, cudaStream_t stream);
-roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream);
+roco_status launch_tree_join_bf16(const TreeParams &p, int d, int U, cudaStream_t stream);  // that launch
 // Statistics of the accepted queries, then evictions and insertion (two launches).
 roco_status launch_commit_stats_tc(const CommitParams &p, int d, int U, int sms, cudaStream_t stream);  // bf16
 roco_status launch_tree_commit(const CommitParams &p, int kv_dtype, int d, int U, int sms, cudaStream_t stream);
@@ -165,10 +166,11 @@ roco_status launch_tree_commit(const CommitParams &p, int kv_dtype, int d, int U
 // ---- linear attention with a decay for each head (linear.cuh)
 struct LinearParams;
 roco_status launch_linear_step(const LinearParams &p, const int *active, int dtype, int d, int U, cudaStream_t stream);
-int linear_simt_segments(int U, int d, int Lmax, int sms);  // parts of the prompt that work side by side (p.segments)
-// Tensor cores (bf16).
+// Single precision, CUDA cores.  Segments: parts of the prompt that work side by side (p.segments).
+int linear_simt_segments(int U, int d, int Lmax, int sms);
+roco_status launch_linear_prefill_simt(const LinearParams &p, int d, int U, cudaStream_t stream);
+// bf16, tensor cores.
 int linear_tc_segments(int U, int Lmax, int sms);
 roco_status launch_linear_prefill_tc(const LinearParams &p, int d, int U, cudaStream_t stream);
-roco_status launch_linear_prefill_simt(const LinearParams &p, int dtype, int d, int U, cudaStream_t stream);
 
 }  // namespace roco

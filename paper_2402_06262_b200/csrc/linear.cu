@@ -1,5 +1,5 @@
-// Linear attention with a decay for each head on the CUDA cores: the single-token step (any dtype) and the prompt pass
-// for the dtypes and head dimensions that the tensor-core kernel does not take.
+// Linear attention with a decay for each head on the CUDA cores: the single-token step (any dtype) and the prompt pass in
+// single precision (bf16: linear_tc.cu).
 //
 //     state_t = g state_{t-1} + k_t v_t^T,     out_t = scale * q_t state_t
 //
@@ -110,9 +110,10 @@ struct LpSmem {
 // segment 0's (which starts from the unit's state) in slot 1, the others', started from zero, in the slot behind their
 // index; slot 0 takes a copy of the unit's state, which the second launch overwrites at a time of its own.  The second
 // launch starts segment i > 0 from  g^(t_i - t_1) slot_1 + sum_{m=1}^{i-1} g^(t_i - t_{m+1}) slot_{m+1}.
-template <typename T, int D, bool kStates>
+template <int D, bool kStates>
 __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const LinearParams p) {
-  constexpr int kSlabs = D / kLpCols, kRows = D * 16 / kLpThreads, kEPC = Elem<T>::kPerChunk;
+  constexpr int kSlabs = D / kLpCols, kRows = D * 16 / kLpThreads;
+  constexpr int kEPC = 4;  // elements of a 16-byte piece
   extern __shared__ __align__(16) char lp_raw[];
   LpSmem<D> &sm = *reinterpret_cast<LpSmem<D> *>(lp_raw);
   const int tid = threadIdx.x;
@@ -160,39 +161,34 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
       }
     }
   }
-  const T *Q = reinterpret_cast<const T *>(p.Q) + (size_t)u * p.Lmax * D, *K = reinterpret_cast<const T *>(p.K) + (size_t)u * p.Lmax * D;
-  const T *V = reinterpret_cast<const T *>(p.V) + (size_t)u * p.Lmax * D + c0;
-  T *O = reinterpret_cast<T *>(p.out) + (size_t)u * p.Lmax * D + c0;
+  const float *Q = reinterpret_cast<const float *>(p.Q) + (size_t)u * p.Lmax * D;
+  const float *K = reinterpret_cast<const float *>(p.K) + (size_t)u * p.Lmax * D;
+  const float *V = reinterpret_cast<const float *>(p.V) + (size_t)u * p.Lmax * D + c0;
+  float *O = reinterpret_cast<float *>(p.out) + (size_t)u * p.Lmax * D + c0;
   const int row0 = (tid >> 4) * 4, col = sc;  // this thread's four tokens and four columns of the output
   const Decay2 g_chunk(decay_pow(logd, kLpChunk)), g_tail(decay_pow(logd, len - (n_chunks - 1) * kLpChunk));
   // A chunk's loads are issued while the one before is worked on.  Tokens behind the last are zeros: they add nothing to
   // the sums, and their own rows are not written.
   constexpr int kPieces = kLpChunk * D / kEPC / kLpThreads, kVPieces = kLpChunk * kLpCols / kEPC / kLpThreads;
   static_assert(kPieces >= 1 && kVPieces >= 1, "a piece of 16 bytes per thread");
-  uint4 qv[kPieces], kv[kPieces], vv[kVPieces];
+  float4 qv[kPieces], kv[kPieces], vv[kVPieces];
   auto load = [&](int c) {
     const int t0 = c * kLpChunk;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int w = tid + i * kLpThreads, t = t0 + w / (D / kEPC), x = w % (D / kEPC) * kEPC;
-      qv[i] = kv[i] = make_uint4(0u, 0u, 0u, 0u);
+      qv[i] = kv[i] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (t < len) {
-        if (!kStates) qv[i] = *reinterpret_cast<const uint4 *>(Q + (size_t)t * D + x);
-        kv[i] = *reinterpret_cast<const uint4 *>(K + (size_t)t * D + x);
+        if (!kStates) qv[i] = *reinterpret_cast<const float4 *>(Q + (size_t)t * D + x);
+        kv[i] = *reinterpret_cast<const float4 *>(K + (size_t)t * D + x);
       }
     }
 #pragma unroll
     for (int i = 0; i < kVPieces; ++i) {
       const int w = tid + i * kLpThreads, t = t0 + w / (kLpCols / kEPC), x = w % (kLpCols / kEPC) * kEPC;
-      vv[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (t < len) vv[i] = *reinterpret_cast<const uint4 *>(V + (size_t)t * D + x);
+      vv[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (t < len) vv[i] = *reinterpret_cast<const float4 *>(V + (size_t)t * D + x);
     }
-  };
-  auto put = [&](float *dst, const uint4 &x) {
-    float f[kEPC];
-    Elem<T>::unpack(x, f);
-#pragma unroll
-    for (int e = 0; e < kEPC; e += 4) *reinterpret_cast<float4 *>(dst + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
   };
   if (first < last) load(first);
 #pragma unroll 1
@@ -202,13 +198,13 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int w = tid + i * kLpThreads, t = w / (D / kEPC), x = w % (D / kEPC) * kEPC;
-      if (!kStates) put(&sm.q[t][x], qv[i]);
-      put(&sm.k[t][x], kv[i]);
+      if (!kStates) *reinterpret_cast<float4 *>(&sm.q[t][x]) = qv[i];
+      *reinterpret_cast<float4 *>(&sm.k[t][x]) = kv[i];
     }
 #pragma unroll
     for (int i = 0; i < kVPieces; ++i) {
       const int w = tid + i * kLpThreads;
-      put(&sm.v[w / (kLpCols / kEPC)][w % (kLpCols / kEPC) * kEPC], vv[i]);
+      *reinterpret_cast<float4 *>(&sm.v[w / (kLpCols / kEPC)][w % (kLpCols / kEPC) * kEPC]) = vv[i];
     }
     if (c + 1 < last) load(c + 1);
     if (!kStates) {
@@ -276,11 +272,8 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (row0 + i < nt) {
-          T *dst = O + (size_t)(t0 + row0 + i) * D + col;
-          Elem<T>::store(dst, o[i].x * p.scale);
-          Elem<T>::store(dst + 1, o[i].y * p.scale);
-          Elem<T>::store(dst + 2, o[i].z * p.scale);
-          Elem<T>::store(dst + 3, o[i].w * p.scale);
+          *reinterpret_cast<float4 *>(O + (size_t)(t0 + row0 + i) * D + col) =
+              make_float4(o[i].x * p.scale, o[i].y * p.scale, o[i].z * p.scale, o[i].w * p.scale);
         }
       }
     }
@@ -317,12 +310,12 @@ __global__ void __launch_bounds__(kLpThreads) linear_prefill_simt_kernel(const L
   for (int i = 0; i < kRows; ++i) *reinterpret_cast<float4 *>(dst + (size_t)i * D) = s[i];
 }
 
-template <typename T, int D>
+template <int D>
 roco_status linear_prefill_simt_t(const LinearParams &p, int U, cudaStream_t stream) {
   constexpr int kSmem = (int)sizeof(LpSmem<D>);
   const unsigned slabs = (unsigned)U * (unsigned)(D / kLpCols);
-  auto states = linear_prefill_simt_kernel<T, D, true>;
-  auto whole = linear_prefill_simt_kernel<T, D, false>;
+  auto states = linear_prefill_simt_kernel<D, true>;
+  auto whole = linear_prefill_simt_kernel<D, false>;
   static SmemLimit limit_states, limit_whole;
   if (!limit_states((const void *)states, kSmem) || !limit_whole((const void *)whole, kSmem)) return ROCO_ERR_CUDA;
   if (p.segments > 1) states<<<slabs * (unsigned)(p.segments - 1), kLpThreads, kSmem, stream>>>(p);
@@ -344,10 +337,8 @@ int linear_simt_segments(int U, int d, int Lmax, int sms) {
   return n < 2 ? 1 : (int)n;
 }
 
-roco_status launch_linear_prefill_simt(const LinearParams &p, int dtype, int d, int U, cudaStream_t stream) {
-  if (dtype == ROCO_BF16)
-    return d == 128 ? linear_prefill_simt_t<__nv_bfloat16, 128>(p, U, stream) : linear_prefill_simt_t<__nv_bfloat16, 64>(p, U, stream);
-  return d == 128 ? linear_prefill_simt_t<float, 128>(p, U, stream) : linear_prefill_simt_t<float, 64>(p, U, stream);
+roco_status launch_linear_prefill_simt(const LinearParams &p, int d, int U, cudaStream_t stream) {
+  return d == 128 ? linear_prefill_simt_t<128>(p, U, stream) : linear_prefill_simt_t<64>(p, U, stream);
 }
 
 }  // namespace roco

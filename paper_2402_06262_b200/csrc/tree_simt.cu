@@ -297,10 +297,8 @@ roco_status tree_join_t(const TreeParams &p, int U, cudaStream_t stream) {
                                                                                                            : ROCO_ERR_CUDA;
 }
 
-roco_status launch_tree_join(const TreeParams &p, int kv_dtype, int d, int U, cudaStream_t stream) {
-  if (kv_dtype == ROCO_BF16)
-    return d == 128 ? tree_join_t<__nv_bfloat16, 128>(p, U, stream) : tree_join_t<__nv_bfloat16, 64>(p, U, stream);
-  return d == 128 ? tree_join_t<float, 128>(p, U, stream) : tree_join_t<float, 64>(p, U, stream);
+roco_status launch_tree_join_bf16(const TreeParams &p, int d, int U, cudaStream_t stream) {
+  return d == 128 ? tree_join_t<__nv_bfloat16, 128>(p, U, stream) : tree_join_t<__nv_bfloat16, 64>(p, U, stream);
 }
 
 // One row a thread up to sixteen rows (64 units x 2048 tokens x 16 rows 114 us, with four rows a thread 134; 8 rows 76 and 110), else

@@ -570,7 +570,7 @@ roco_status tree_tc_t(const TreeParams &p, int U, cudaStream_t stream) {
   }
   kernel<<<blocks, Sh::kThreads, Sh::kSmem, stream>>>(mk, mv, mn, mw, p);
   if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
-  return p.splits > 1 ? launch_tree_join(p, ROCO_BF16, D, U, stream) : ROCO_OK;
+  return p.splits > 1 ? launch_tree_join_bf16(p, D, U, stream) : ROCO_OK;
 }
 
 template <int D>
