@@ -5,6 +5,7 @@ import torch
 
 import operator_reference as ref
 import paper_2402_06262_b200 as R
+from test_gpu_tree_commit import check
 from tree_cases import CACHE_FIELDS, make
 
 pytestmark = pytest.mark.gpu
@@ -129,3 +130,13 @@ def test_with_room_a_commit_of_one_token_is_a_decode_step(dtype, d):
                 assert bool(((cache.q[b, g, :n].double().cpu() - st["q"][:n]).abs() <= qb).all())
             for y in (out[b, g, 0, 0], out2[b, g]):
                 assert bool(((y.double().cpu() - o[0, 0]).abs() <= ob[0, 0]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("G", [3, 200, 1300])
+@pytest.mark.parametrize("mode,r", [(R.ROCO_SCOPE_EXCLUDE_TOP_R, 2), (R.ROCO_SCOPE_EXCLUDE_TOP_R, 70), (R.ROCO_SCOPE_EXCLUDE_TOP_R, 200),
+                                    (R.ROCO_SCOPE_LOWEST_R, 30)])
+def test_every_number_of_threads_for_a_unit(dtype, G, mode, r):
+    """Few units, more than a B200 has SMs, more than eight to an SM; scopes that leave out two tokens, 70, most."""
+    c = make(25 + r, S=1, G=G, B=230, d=64, T=4, dtype=dtype, shape="chain", live=[229])
+    check(c, [[0, 1, 2, 3]], 4, r, mode)
