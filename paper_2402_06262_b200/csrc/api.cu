@@ -146,12 +146,13 @@ TreePlan tree_plan(const roco_cache *c, int T, int group, float scale) {
   if (want > most) want = most;
   if (want > 32) want = 32;
   // The CTAs of a range join their results through each other's shared memory where a cluster can hold them, which
-  // saves a launch and the partial results' way through L2 (32 units x 1024 tokens x 8 rows: 11.2 -> 9.4 us).  On the tensor cores,
-  // where the cache would be cut into more ranges than a cluster has CTAs, eight do too unless that leaves most SMs idle (8 units x 8192
-  // x 8 rows: 20.4 -> 17.9 us; 1 unit x 8192 x 32 rows would go from 20.0 to 21.6 us).  Clusters of CTAs that fill an SM each
-  // do not pack: 24 of six CTAs take two waves (35 -> 54 us), so those are four CTAs or few.
+  // saves a launch and the partial results' way through L2 (32 units x 1024 tokens x 8 rows: 11.2 -> 9.4 us).  On the tensor
+  // cores eight do too where the cache would be cut into more ranges than a cluster has CTAs (8 units x 8192 x 8 rows 20.4 -> 14.8 us,
+  // 1 unit 16.5 -> 14.3), but above 32 rows, where a range takes longer, only from three of them on (1 unit x 8192 x 96 rows would go
+  // from 21.7 to 22.2 us, 4 units go from 23.6 to 22.6).  Clusters of CTAs that fill an SM each do not pack: 24 of six CTAs take
+  // two waves (35 -> 54 us), so those are four CTAs or few.
   const long long ranks = want < 8 ? want : 8;
-  t.cluster = want > 1 && (want <= 8 || (t.tc && ctas >= 4)) && (per_sm > 1 || ranks <= 4 || ctas * ranks <= sms / 2);
+  t.cluster = want > 1 && (want <= 8 || (t.tc && (per_sm > 1 || ctas > 2))) && (per_sm > 1 || ranks <= 4 || ctas * ranks <= sms / 2);
   if (t.cluster) want = ranks;
   t.splits = want < 1 ? 1 : (int)want;
   const bool parts = t.splits > 1 && !t.cluster;
