@@ -374,8 +374,8 @@ roco_status roco_decode_step_cluster(roco_cache *cache, const void *q, const voi
  * continues the cached prefix.  Every query head of node i attends over the unit's cached tokens, node i's ancestors
  * and node i itself (Eq. 1 over that set):
  *     x_ij = scale * Q_i.k_j,   lse_i = log sum_j exp x_ij,   attn_out_i = sum_j exp(x_ij - lse_i) v_j
- * The cache and its statistics stay as they are: a verified path enters with roco_tree_commit.  One launch, two
- * where the cached tokens are divided among several CTAs (few units).
+ * The cache and its statistics stay as they are: a verified path enters with roco_tree_commit.  One launch; two where the
+ * cached tokens of few units are divided among more CTAs than join as a cluster.
  *
  *   Q            [S][G][T][group][d] (G counts key-value heads);  K_new, V_new [S][G][T][d]; cache->kv_dtype
  *   parent       [S][T] int32 DEVICE array

@@ -14,7 +14,7 @@ constexpr int kLsCols = 32;  // columns of the state per CTA: 128-byte rows
 
 // One CTA: 32 columns of a unit's state, eight threads (16 bytes each) across, sixteen rows at a time; every thread has
 // all of its D / 16 loads in flight before it uses the first.  Reads and writes the state once: bound by that traffic (8192
-// units x 128 x 128: 143 us, 6.6 TB/s; 32 units: 2.5 us, less than their launch).
+// units x 128 x 128: 143 us, 6.6 TB/s; 32 units: 2.8 us, less than their launch).
 template <typename T, int D>
 __global__ void __launch_bounds__(kLsThreads) linear_step_kernel(const LinearParams p, const int *active) {
   constexpr int kSlabs = D / kLsCols, kRows = D / 16;
@@ -104,7 +104,7 @@ struct LpSmem {
 // Three small matrix products per chunk in place of 32 dependent updates of the state.  A CTA has 64 columns of one
 // unit's state (registers; a copy in shared memory is the operand of the first product) and one segment of the prompt.
 // All powers are at most 1: nothing overflows however fast the head forgets.  A thread forms four tokens by four columns, eight
-// products per value read: shared memory's ports bound it (24 units x 777 tokens x 64: 26.8 us; one token by eight columns 40).
+// products per value read: shared memory's ports bound it (24 units x 777 tokens x 64: 28.7 us; one token by eight columns 40).
 //
 // Segments (few units): a first launch (kStates) runs every segment but the last and leaves its state in `parts`:
 // segment 0's (which starts from the unit's state) in slot 1, the others', started from zero, in the slot behind their

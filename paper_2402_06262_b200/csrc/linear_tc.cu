@@ -3,7 +3,7 @@
 // In chunks of C = 128 tokens, with i, j counted inside the chunk and S the fp32 state before it:
 //     out_i = scale * ( g^(i+1) q_i S + sum_{j <= i} g^(i-j) (q_i.k_j) v_j )
 //     S    <- g^C S + sum_j (g^(C-1-j) k_j)^T v_j
-// which is four products per chunk, issued by one thread, accumulators in tensor memory:
+// which is four products per chunk, issued by one elected lane of a converged warp, accumulators in tensor memory:
 //     S1 = Q K^T              both operands as TMA wrote them
 //     O  = Q bf16(S)          then, by the A warps, row i times scale g^(i+1)
 //     O += P V                P = S1 with the decays and the scale as bf16, from tensor memory
@@ -23,8 +23,8 @@
 // takes 48 products of 128 x 128 x 16, 3200 cycles at the tensor cores' rate (67 a product).  They follow one another without
 // a gap, at 127 cycles each: operands from shared memory (two per product for S1 and O, 8 KiB per 64 cycles, one for the
 // others) share its ports with the tiles that arrive and leave, and the chip is at its power limit (1.97 GHz falls to 1.4
-// within milliseconds, 1.0 kW).  1024 units x 8192 tokens: 2.15 ms, 770 Tflop/s and 4.1 TB/s at the same time, 0.63 of the
-// copy rate (1.83 ms before the clock falls).  Two terms per key instead of three would be 8 percent faster at five times
+// within milliseconds, 1.0 kW).  1024 units x 8192 tokens: 2.07 ms, 800 Tflop/s and 4.2 TB/s at the same time, 0.65 of the
+// copy rate (1.78 ms before the clock falls).  Two terms per key instead of three would be 8 percent faster at five times
 // the error of the state (2.4e-6).
 #include <cuda.h>
 

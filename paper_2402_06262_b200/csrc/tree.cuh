@@ -15,7 +15,7 @@ struct TreeParams {
   const int *parent, *nodes;
   char *out;
   float *lse;
-  float *part_o, *part_ml;  // splits > 1: [U][splits][rows][d] unnormalised outputs, [U][splits][rows][2] (max, sum)
+  float *part_o, *part_ml;  // splits > 1, no cluster: [U][splits][rows][d] unnormalised outputs, [U][splits][rows][2] (max, sum)
   int B, T, group, G;
   int rows;    // T * group query rows of a unit; row i is head i % group of node i / group
   int splits;  // CTAs that share a unit's cached tokens

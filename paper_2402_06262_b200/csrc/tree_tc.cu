@@ -19,11 +19,12 @@
 // launch where a cluster would not do.
 //
 // What bounds it.  The cache is read once.  Up to 32 rows two CTAs per SM, so that one's prologue and epilogue run under the
-// other's stream: 8192 units x 1024 tokens x 16 rows 680 us, 6.45 TB/s, the measured copy rate.  64 and 128 rows, one CTA: a
+// other's stream: 8192 units x 1024 tokens x 16 rows 676 us in a replayed
+// graph, 6.5 TB/s, the measured copy rate (687 us in single calls).  64 and 128 rows, one CTA: a
 // tile of 128 tokens at 128 rows costs its two groups about 3000 cycles (1050 of products, 1020 of the exponential unit, the
 // rest instructions and what 8 warps cannot hide of their latencies; 16 warps came out the same) where its 64 KiB take 2850: 24
-// units x 8192 x 96 rows 32.8 us, of which 6 are the first tile's way here and 5 the join.  Small calls are latency: 32 units x
-// 1024 x 8 rows 9.0 us, of which about 2 are the launch, 2.5 the first tile's way, 2 the draft and 1.5 the join.
+// units x 8192 x 96 rows (worked on as 128) 32.2 us, of which 6 are the first tile's way here and 5 the join.  Small calls are latency: 32 units x
+// 1024 x 8 rows 8.7 us, of which about 2 are the launch, 2.5 the first tile's way, 2 the draft and 1.5 the join.
 #include <cuda.h>
 
 #include <cfloat>
