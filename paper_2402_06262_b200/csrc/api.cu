@@ -138,11 +138,13 @@ TreePlan tree_plan(const roco_cache *c, int T, int group, float scale) {
   const long long U = (long long)c->S * c->G;
   t.tc = c->kv_dtype == ROCO_BF16 && scale > 0.f;
   const int row_blocks = t.tc ? (rows + tree_tc_rows(rows) - 1) / tree_tc_rows(rows) : tree_simt_row_blocks(rows);
-  // One wave of the CTAs that reside (CUDA cores: two per SM, by their registers), no range shorter than two tiles of 128
-  // keys (CUDA cores: 64).
-  const int per_sm = t.tc ? tree_tc_ctas(rows) : 2, sms = device_sms();
+  // Tensor cores: one wave, no range shorter than two 128-key tiles.  CUDA cores: four CTAs for every SM, rounded up, no range
+  // shorter than two 64-key tiles.  Two of the four reside (by their registers): ranges of half a wave leave less of the last
+  // wave idle, and clusters do not fill a wave to the last SM.  One wave instead is faster where it packs (64 units x 8192 x 24 rows
+  // 384 us, with this 452) and slower where it does not (37 units 375, with this 222; 149 units 1467 and 1128).
+  const int per_sm = t.tc ? tree_tc_ctas(rows) : 4, sms = device_sms();
   const long long ctas = U * row_blocks, slots = (long long)per_sm * sms;
-  long long want = slots / ctas, most = (c->B + (t.tc ? 255 : 127)) / (t.tc ? 256 : 128);
+  long long want = t.tc ? slots / ctas : (slots + ctas - 1) / ctas, most = (c->B + (t.tc ? 255 : 127)) / (t.tc ? 256 : 128);
   if (want > most) want = most;
   if (want > 32) want = 32;
   // The CTAs of a range join their results through each other's shared memory where a cluster can hold them, which

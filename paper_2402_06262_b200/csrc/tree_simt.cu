@@ -301,8 +301,8 @@ roco_status launch_tree_join_bf16(const TreeParams &p, int d, int U, cudaStream_
   return d == 128 ? tree_join_t<__nv_bfloat16, 128>(p, U, stream) : tree_join_t<__nv_bfloat16, 64>(p, U, stream);
 }
 
-// One row a thread up to sixteen rows (64 units x 2048 tokens x 16 rows 102 us, with four rows a thread 107; 8 rows 61 and 87), else
-// four (64 units x 8192 x 24 rows 384 us, with one 711; 4 units x 8192 x 512 rows 375 and 697).
+// One row a thread up to sixteen rows (64 units x 2048 tokens x 16 rows 114 us, with four rows a thread 134; 8 rows 76 and 110), else
+// four (64 units x 8192 x 24 rows 453 us, with one 666; 4 units x 8192 x 512 rows 444 and 754).
 int tree_simt_row_blocks(int rows) {
   constexpr int kRows = TsShape<64, 4>::kRows;
   return rows <= TsShape<64, 1>::kRows ? 1 : (rows + kRows - 1) / kRows;
