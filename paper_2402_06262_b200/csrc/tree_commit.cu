@@ -181,11 +181,11 @@ roco_status commit_insert_nt(const CommitParams &p, int U, cudaStream_t stream) 
 // A unit is a chain of passes and loads: with few units more threads shorten the passes, with many it is the number of
 // units in flight that counts.  Whole commits with 128, 256 and 512 threads: 8192 units x 1024 tokens 470, 499, 642 us (every unit
 // evicts five); 1184 units 80, 83, 101; 600 units 52, 47, 60; 300 units x 4096 80, 75, 80; 148 units x 1024 20.6, 18.6, 16.7; 32 units
-// x 512 12.5, 11.8, 11.3, x 1024 15.8, 14.1, 13.5, x 8192 41, 30, 23.
+// x 512 12.5, 11.8, 11.3, x 1024 15.8, 14.1, 13.5, x 8192 41, 30, 23; and x 256 tokens, d = 64, with 256 and 512 11.3, 11.9.
 template <typename T, int D>
 roco_status commit_insert_t(const CommitParams &p, int U, int sms, cudaStream_t stream) {
   if (U >= 8 * sms) return commit_insert_nt<T, D, 128>(p, U, stream);
-  return U > sms ? commit_insert_nt<T, D, 256>(p, U, stream) : commit_insert_nt<T, D, 512>(p, U, stream);
+  return U > sms || p.B < 512 ? commit_insert_nt<T, D, 256>(p, U, stream) : commit_insert_nt<T, D, 512>(p, U, stream);
 }
 
 template <typename T, int D>
