@@ -68,7 +68,9 @@ enum {
   ROCO_DEV_BAD_LIVE = 2,     /* live[u] outside [0, B]                            */
   ROCO_DEV_BAD_VICTIM = 4,   /* the selection produced no slot (NaN statistics)   */
   ROCO_DEV_BAD_TREE = 8,     /* a node count, parent or accepted path that is none */
-  ROCO_DEV_BAD_LENS = 16     /* a prompt length outside [0, Lmax]                 */
+  ROCO_DEV_BAD_LENS = 16,    /* a prompt length outside [0, Lmax]                 */
+  ROCO_DEV_BAD_PROBS = 32,   /* probabilities that are not finite, or all zero    */
+  ROCO_DEV_BAD_MAP = 64      /* a source sequence or a position axis that is none */
 };
 
 /* The budgeted cache of Sec. 3/4 for S sequences x G (= layers*heads) units each; U = S*G.
@@ -480,6 +482,118 @@ roco_status roco_linear_step(const roco_linear_state *state, const void *q, cons
 
 /* roco_device_status for the status word of a linear-attention state. */
 roco_status roco_linear_device_status(const roco_linear_state *state, void *stream, int32_t *flags_host);
+
+/*
+ * Which path of the drafted trees the target model accepts, and the token that follows it (speculative sampling; the paper
+ * has no counterpart): the decision between roco_tree_attend and roco_tree_commit, from given random numbers.  The tokens that
+ * come out are distributed as the target's own.
+ *
+ * A sequence's walk starts at the root and tries the children of the node it stands on in index order.  With p the target's
+ * and q the draft's probabilities behind that node, C = 0, R = 1, M = 1 at first, a child with token x is accepted if
+ *     u q(x) R < max(p(x) - C q(x), 0) M                                      (u: accept_u of the child)
+ * and becomes the node to stand on.  After a rejection what is left of p is max(p - C q, 0) with C increased by R / M (where
+ * M > 0); R is the sum of that over the vocabulary.  M stays 1 where siblings were drawn from q independently of each other;
+ * with `distinct` they were drawn without replacement, and M falls by q(x).  Without draft probabilities (the drafts are, say,
+ * the likeliest tokens) a child is accepted if u R < p(x), else p loses x and R is the sum of the rest.  A token that was
+ * rejected among its siblings already counts as having no probability (with `distinct` or without draft probabilities).
+ * Where no child is accepted, or the path has A nodes, next_token is the first v at which the sum over 0..v of what is left of
+ * p exceeds u' times the sum over all (u': sample_u); p itself where nothing is left.  All of this is in 64 bits.
+ *
+ *   target       [S][T] rows of V probabilities, of the token behind each node; element type `dtype`
+ *   draft        [S][T] rows of V probabilities that the children of each node were drawn from, or NULL.  Rows are given by
+ *                their strides, in elements (so they may lie in a wider matrix); within a row elements follow each other
+ *   target_prefix, draft_prefix   [S] rows of V, the same behind the cached prefix; the tree's roots (parent -1) are tried
+ *                against them.  target_prefix NULL: node 0 is the token that was sampled last and is accepted as it stands; it is
+ *                then the only root (other nodes with parent -1 are never accepted)
+ *   tokens, parent   [S][T] int32: a node's token, 0..V-1, and as in roco_tree_attend
+ *   nodes        [S] int32 or NULL, as in roco_tree_attend.  0: nothing is tried; without target_prefix next_token is then -1
+ *   accept_u     [S][T] fp32,  sample_u [S] fp32: independent and uniform in [0, 1)
+ *   A            1 <= A <= ROCO_TREE_MAX_PATH, A <= T
+ *   path         [S][A] accepted nodes from the root on, padded with -1;  path_len [S];  next_token [S];  all int32.  They are
+ *                what roco_tree_commit takes
+ *   status       [1] device status word.  ROCO_DEV_BAD_TREE: a node count outside [0, T] (counts as 0), a parent that is no earlier
+ *                node nor -1 or a token outside the vocabulary (that node is never accepted).  ROCO_DEV_BAD_PROBS: the next token
+ *                was to be taken from probabilities that are not finite or all zero (next_token is -1)
+ * Pointers are aligned to their elements; 16-byte aligned rows are read fastest.  1 <= T <= ROCO_TREE_MAX_NODES.  One launch.
+ */
+typedef struct {
+  int32_t dtype, S, T, V, A;
+  int32_t distinct; /* 0: siblings drawn independently; 1: without replacement */
+  const void *target, *draft, *target_prefix, *draft_prefix;
+  int64_t target_seq, target_row;   /* strides: from a sequence to the next, from a row to the next */
+  int64_t draft_seq, draft_row;
+  int64_t target_prefix_seq, draft_prefix_seq;
+  const int32_t *tokens, *parent, *nodes;
+  const float *accept_u, *sample_u;
+  int32_t *path, *path_len, *next_token, *status;
+} roco_verify;
+roco_status roco_tree_verify(const roco_verify *call, void *stream);
+
+/*
+ * Queries, keys and values of a layer out of its projections (the paper has no counterpart): the norm of each head's query and
+ * key, their rotation by the token's position, and the layout by unit that every other entry point takes, in one pass.
+ *     y = x / sqrt(mean(x^2) + eps) * weight          (over the d elements of a head; left out where the weight is NULL)
+ *     (a, b) -> (a cos t - b sin t, b cos t + a sin t)    for every pair i < rot/2 of the first rot elements,
+ *     t = freq[i] * (start + position on axis[i])
+ * Pairs are (i, i + rot/2) for ROCO_PAIR_HALVES, (2i, 2i + 1) for ROCO_PAIR_ADJACENT.  Values are laid out as they are.
+ * Arithmetic is fp32 with one rounding at the end; angles are reduced in 64 bits, so that far positions lose nothing.
+ */
+typedef enum { ROCO_PAIR_HALVES = 0, ROCO_PAIR_ADJACENT = 1 } roco_pairing;
+
+typedef struct {
+  int32_t d, rot;        /* head dimension, 64 or 128; rotated elements: a multiple of 16, 0 (none) to d */
+  int32_t pairing;       /* roco_pairing                                                                 */
+  int32_t axes;          /* numbers in a token's position, 1 to 4 (time, height, width, ...)             */
+  const float *freq;     /* [rot/2] radians per step                                                     */
+  const int32_t *axis;   /* [rot/2] the axis that turns each pair; NULL: axis 0                          */
+  const float *q_weight; /* [d], or NULL: queries are not normed                                         */
+  const float *k_weight; /* [d], or NULL: keys are not normed                                            */
+  float eps;
+  int32_t *status;       /* [1] device status word, zeroed by the caller                                 */
+} roco_rotary;
+
+/*
+ *   q, k, v      projections: [S][N][heads][d] with G * group heads of queries and G of keys and values; `dtype`; `strides` says
+ *                (in elements) how far apart sequences and tokens lie: {q sequence, q token, k sequence, k token, v sequence,
+ *                v token}, multiples of 16 bytes, so that all three may lie in the rows of one product.  k, v: or NULL
+ *   lens         [S] int32 DEVICE array, 0..N, or NULL: N everywhere.  Tokens at lens[b] and behind may hold anything and their
+ *                rows of Q, K, V are left as they were.  Any other value sets ROCO_DEV_BAD_LENS and counts as 0
+ *   start        DEVICE array of int32, one for each sequence start_stride elements apart (t_next of a cache: start_stride = G),
+ *                added to every position; NULL: 0
+ *   positions    [S][N][axes] int32 DEVICE array, or NULL: token n has position n on every axis
+ *   Q            [S][G][N][group][d];  K, V [S][G][N][d] (NULL where k, v are);  they overlap nothing else.  N = 1 is the
+ *                layout of the decode steps, N = T that of the trees, N = Lmax (group 1) that of the prompt passes
+ * An axis outside [0, axes) sets ROCO_DEV_BAD_MAP and counts as 0.  One launch.
+ */
+roco_status roco_norm_rotate(const roco_rotary *rotary, int dtype, int S, int N, int G, int group, const void *q,
+                             const void *k, const void *v, const int64_t *strides, const int32_t *lens,
+                             const int32_t *start, int start_stride, const int32_t *positions, void *Q, void *K, void *V,
+                             void *stream);
+
+/* roco_device_status for the status word of a rotary. */
+roco_status roco_rotary_device_status(const roco_rotary *rotary, void *stream, int32_t *flags_host);
+
+/*
+ * Sequences of a cache forked, reordered, compacted, freed (the paper has no counterpart): every sequence b of dst becomes a
+ * copy of sequence source[b] of src as it was before the call -- occupied slots with their statistics and positions, live and
+ * t_next.  ROCO_REORDER_KEEP leaves it as it is, ROCO_REORDER_FREE empties it (live = 0, t_next = 0, pos = -1).  Slots behind the
+ * occupied ones get pos = -1 and are otherwise left as they were.
+ *
+ *   src, dst     the same cache (in place: any map, cycles and forks among them; up to ROCO_REORDER_MAX_S sequences), or two that
+ *                share no memory, of equal dtype, G and d, with dst->B >= src->B
+ *   source       [dst->S] int32 DEVICE array.  A value that is neither a sequence of src nor one of the two below sets
+ *                ROCO_DEV_BAD_MAP in dst->status and counts as ROCO_REORDER_KEEP.  A unit of src whose live is outside [0, B] sets
+ *                ROCO_DEV_BAD_LIVE there and is not copied
+ * One launch; two in place.
+ */
+enum { ROCO_REORDER_KEEP = -1, ROCO_REORDER_FREE = -2 };
+#define ROCO_REORDER_MAX_S 256
+roco_status roco_cache_reorder(const roco_cache *src, roco_cache *dst, const int32_t *source, void *stream);
+
+/* The same for the states of linear attention (a freed sequence's states become zero); the log_decay of the two are not
+ * looked at.  One launch. */
+roco_status roco_linear_reorder(const roco_linear_state *src, const roco_linear_state *dst, const int32_t *source,
+                                void *stream);
 
 /*
  * Consistency of an importance score under a budget with its full-cache version (Sec. 4.3, preliminary

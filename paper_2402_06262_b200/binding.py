@@ -33,7 +33,10 @@ EXPORTS = ("roco_version", "roco_status_string", "roco_prefill_workspace_bytes",
            "roco_decode_step_cluster", "roco_decode_step_policy_ordered", "roco_decode_step_split_ordered",
            "roco_tree_attend_workspace_bytes", "roco_tree_attend", "roco_tree_commit", "roco_tree_commit_nodes",
            "roco_linear_prefill_workspace_bytes", "roco_linear_prefill", "roco_linear_step",
-           "roco_linear_device_status")
+           "roco_linear_device_status", "roco_tree_verify", "roco_norm_rotate", "roco_rotary_device_status",
+           "roco_cache_reorder", "roco_linear_reorder")
+ROCO_PAIR_HALVES, ROCO_PAIR_ADJACENT = 0, 1
+ROCO_REORDER_KEEP, ROCO_REORDER_FREE, REORDER_MAX_S = -1, -2, 256
 
 TREE_MAX_NODES, TREE_MAX_GROUP, TREE_MAX_PATH = 64, 16, 16
 
@@ -54,6 +57,21 @@ class roco_cache(C.Structure):
 class roco_linear_state(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("S", C.c_int32), ("G", C.c_int32), ("d", C.c_int32), ("state", C.c_void_p),
                 ("log_decay", C.c_void_p), ("status", C.c_void_p)]
+
+
+class roco_rotary(C.Structure):
+    _fields_ = [("d", C.c_int32), ("rot", C.c_int32), ("pairing", C.c_int32), ("axes", C.c_int32), ("freq", C.c_void_p),
+                ("axis", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float),
+                ("status", C.c_void_p)]
+
+
+class roco_verify(C.Structure):
+    _fields_ = ([(f, C.c_int32) for f in ("dtype", "S", "T", "V", "A", "distinct")] +
+                [(f, C.c_void_p) for f in ("target", "draft", "target_prefix", "draft_prefix")] +
+                [(f, C.c_int64) for f in ("target_seq", "target_row", "draft_seq", "draft_row", "target_prefix_seq",
+                                          "draft_prefix_seq")] +
+                [(f, C.c_void_p) for f in ("tokens", "parent", "nodes", "accept_u", "sample_u", "path", "path_len", "next_token",
+                                           "status")])
 
 
 _lib = None
@@ -178,6 +196,17 @@ def lib() -> C.CDLL:
                                        C.c_float, C.c_void_p, C.c_void_p]
         L.roco_linear_device_status.restype = C.c_int
         L.roco_linear_device_status.argtypes = [C.POINTER(roco_linear_state), C.c_void_p, C.c_void_p]
+        L.roco_tree_verify.restype = C.c_int
+        L.roco_tree_verify.argtypes = [C.POINTER(roco_verify), C.c_void_p]
+        L.roco_norm_rotate.restype = C.c_int
+        L.roco_norm_rotate.argtypes = ([C.POINTER(roco_rotary)] + [C.c_int] * 5 + [C.c_void_p] * 3 + [C.POINTER(C.c_int64 * 6)] +
+                                       [C.c_void_p] * 2 + [C.c_int] + [C.c_void_p] * 5)
+        L.roco_rotary_device_status.restype = C.c_int
+        L.roco_rotary_device_status.argtypes = [C.POINTER(roco_rotary), C.c_void_p, C.c_void_p]
+        L.roco_cache_reorder.restype = C.c_int
+        L.roco_cache_reorder.argtypes = [C.POINTER(roco_cache), C.POINTER(roco_cache), C.c_void_p, C.c_void_p]
+        L.roco_linear_reorder.restype = C.c_int
+        L.roco_linear_reorder.argtypes = [C.POINTER(roco_linear_state), C.POINTER(roco_linear_state), C.c_void_p, C.c_void_p]
         L.roco_device_status.restype = C.c_int
         L.roco_device_status.argtypes = [C.POINTER(roco_cache), C.c_void_p, C.c_void_p]
         _lib = L
@@ -305,6 +334,34 @@ class LinearState:
         self.state, self.log_decay, self.status, self.dtype = state, log_decay, status, dtype
         self.c = roco_linear_state(ROCO_F32 if dtype == torch.float32 else ROCO_BF16, self.S, self.G, self.d,
                                    state.data_ptr(), log_decay.data_ptr(), status.data_ptr())
+
+
+class Rotary:
+    """Norm and rotation of a layer's heads, plus the C struct over its tensors.  freq: radians per step of each pair, fp32 (None or
+    empty: no rotation), the first 2 * len(freq) elements of a head turn; axes: numbers in a token's position; axis: the axis that
+    turns each pair (int32, None: axis 0); q_weight, k_weight: [d] fp32 (None: no norm); status: [1] int32 (None: made here)."""
+
+    def __init__(self, d: int, freq, pairing: int = ROCO_PAIR_HALVES, axes: int = 1, axis=None, q_weight=None, k_weight=None,
+                 eps: float = 1e-6, status=None, device="cuda"):
+        as_type = lambda x, t: None if x is None else torch.as_tensor(x, dtype=t).to(device)  # noqa: E731
+        freq = as_type([] if freq is None else freq, torch.float32)
+        axis = as_type(axis, torch.int32)
+        q_weight, k_weight = as_type(q_weight, torch.float32), as_type(k_weight, torch.float32)
+        if status is None:
+            status = torch.zeros(1, dtype=torch.int32, device=device)
+        dev = _device()
+        if d not in (64, 128) or freq.dim() != 1 or 2 * freq.shape[0] > d or freq.shape[0] % 8 or not 1 <= axes <= 4:
+            raise RocoError(2, "Rotary: d is 64 or 128, freq has a multiple of 8 and at most d / 2 elements, axes is 1 to 4")
+        if pairing not in (ROCO_PAIR_HALVES, ROCO_PAIR_ADJACENT):
+            raise RocoError(1, "Rotary: pairing is ROCO_PAIR_HALVES or ROCO_PAIR_ADJACENT")
+        for name, t, shape, dtype in (("freq", freq, freq.shape, torch.float32), ("axis", axis, freq.shape, torch.int32),
+                                      ("q_weight", q_weight, (d,), torch.float32), ("k_weight", k_weight, (d,), torch.float32),
+                                      ("status", status, (1,), torch.int32)):
+            if t is not None:
+                _need("Rotary", name, t, shape, dtype, dev)
+        self.d, self.rot, self.axes, self.freq, self.axis, self.status = d, 2 * freq.shape[0], axes, freq, axis, status
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.c = roco_rotary(d, self.rot, pairing, axes, _at(freq), _at(axis), _at(q_weight), _at(k_weight), eps, _at(status))
 
 
 def roco_prefill_workspace_bytes(cache: Cache, Lmax: int) -> int:
@@ -695,3 +752,127 @@ def roco_linear_device_status(state: LinearState) -> int:
     if rc not in (ROCO_OK, 5):
         raise RocoError(rc, "roco_linear_device_status")
     return int(flags.value)
+
+
+def _need_rows(what: str, name: str, t, shape, dtype, dev: int):
+    """A tensor of this shape and type on the current device whose last dimension is dense; the others may have any strides."""
+    if (not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != dev
+            or (t.stride(-1) != 1 and t.shape[-1] > 1)):
+        raise RocoError(1, f"{what}: {name}: a {dtype} tensor of shape {list(shape)} with dense rows on the current CUDA device is "
+                           f"needed, got " + (f"{t.dtype} {list(t.shape)} with strides {list(t.stride())} on {t.device}"
+                                              if isinstance(t, torch.Tensor) else type(t).__name__))
+
+
+def roco_tree_verify(target, tokens, parent, accept_u, sample_u, path, path_len, next_token, status, nodes=None, draft=None,
+                     target_prefix=None, draft_prefix=None, distinct: bool = False):
+    """Which path of the drafted trees the target accepts, and the token behind it.  target, draft [S][T][V] probabilities behind
+    each node (fp32 or bf16, rows dense, other strides free; draft None: the drafts have no probabilities), target_prefix,
+    draft_prefix [S][V] those behind the cached prefix (None: node 0 was sampled last time), tokens, parent [S][T] int32, nodes [S]
+    int32 (None: T), accept_u [S][T] and sample_u [S] fp32 in [0, 1), distinct: siblings were drawn without replacement.  Written:
+    path [S][A] int32 (padded with -1), path_len, next_token [S] int32, status [1] int32."""
+    what, dev = "roco_tree_verify", _device()
+    if not isinstance(target, torch.Tensor) or target.dim() != 3 or target.dtype not in (torch.float32, torch.bfloat16):
+        raise RocoError(1, f"{what}: target is an fp32 or bf16 tensor [S][T][V]")
+    if not isinstance(path, torch.Tensor) or path.dim() != 2:
+        raise RocoError(1, f"{what}: path is [S][A]")
+    S, T, V = target.shape
+    dtype = target.dtype
+    _need_rows(what, "target", target, (S, T, V), dtype, dev)
+    if draft is not None:
+        _need_rows(what, "draft", draft, (S, T, V), dtype, dev)
+    for name, t in (("target_prefix", target_prefix), ("draft_prefix", draft_prefix)):
+        if t is not None:
+            _need_rows(what, name, t, (S, V), dtype, dev)
+    for name, t, shape, kind in (("tokens", tokens, (S, T), torch.int32), ("parent", parent, (S, T), torch.int32),
+                                 ("accept_u", accept_u, (S, T), torch.float32), ("sample_u", sample_u, (S,), torch.float32),
+                                 ("path", path, (S, path.shape[1]), torch.int32), ("path_len", path_len, (S,), torch.int32),
+                                 ("next_token", next_token, (S,), torch.int32), ("status", status, (1,), torch.int32)):
+        _need(what, name, t, shape, kind, dev)
+    if nodes is not None:
+        _need(what, "nodes", nodes, (S,), torch.int32, dev)
+    call = roco_verify(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, T, V, path.shape[1], int(bool(distinct)), _at(target),
+                       _at(draft), _at(target_prefix), _at(draft_prefix), target.stride(0), target.stride(1),
+                       0 if draft is None else draft.stride(0), 0 if draft is None else draft.stride(1),
+                       0 if target_prefix is None else target_prefix.stride(0), 0 if draft_prefix is None else draft_prefix.stride(0),
+                       _at(tokens), _at(parent), _at(nodes), _at(accept_u), _at(sample_u), _at(path), _at(path_len), _at(next_token),
+                       _at(status))
+    rc = lib().roco_tree_verify(C.byref(call), _raw_stream(dev))
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)
+
+
+def roco_norm_rotate(rotary: Rotary, q, k, v, Q, K, V, lens=None, start=None, positions=None):
+    """Norm, rotation and layout of a layer's projections.  q [S][N][G * group][d], k, v [S][N][G][d] (fp32 or bf16; heads dense,
+    strides of sequences and tokens free: the three may be views of one product's rows; k and K, v and V may be None); Q
+    [S][G][N][group][d], K, V [S][G][N][d]; lens [S] int32 (None: N); start [S] int32 with any stride, added to the positions (None: 0;
+    cache.t_next[:, 0]); positions [S][N][axes] int32 (None: 0, 1, 2, ... on every axis)."""
+    what, dev = "roco_norm_rotate", _device()
+    if not isinstance(Q, torch.Tensor) or Q.dim() != 5 or Q.dtype not in (torch.float32, torch.bfloat16):
+        raise RocoError(1, f"{what}: Q is an fp32 or bf16 tensor [S][G][N][group][d]")
+    S, G, N, group, d = Q.shape
+    if rotary.d != d:
+        raise RocoError(1, f"{what}: Q has heads of {d} elements, the rotary of {rotary.d}")
+    if rotary.freq.get_device() != dev:
+        raise RocoError(1, f"{what}: the rotary is not on the current CUDA device")
+    dtype = Q.dtype
+    _need(what, "Q", Q, (S, G, N, group, d), dtype, dev)
+    strides = []
+    for name, x, heads, out_name, out in (("q", q, G * group, "Q", Q), ("k", k, G, "K", K), ("v", v, G, "V", V)):
+        if x is None and out is None and name != "q":
+            strides += [0, 0]
+            continue
+        _need_rows(what, name, x, (S, N, heads, d), dtype, dev)
+        if heads > 1 and x.stride(2) != d:
+            raise RocoError(1, f"{what}: {name}: a token's heads lie {x.stride(2)} elements apart, not {d}")
+        if name != "q":
+            _need(what, out_name, out, (S, G, N, d), dtype, dev)
+        strides += [x.stride(0), x.stride(1)]
+    if lens is not None:
+        _need(what, "lens", lens, (S,), torch.int32, dev)
+    if start is not None and (not isinstance(start, torch.Tensor) or start.dtype is not torch.int32 or start.shape != (S,)
+                              or start.get_device() != dev):
+        raise RocoError(1, f"{what}: start: an int32 tensor of shape [{S}] on the current CUDA device is needed")
+    if positions is not None:
+        if rotary.axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 2:
+            positions = positions[..., None]
+        _need(what, "positions", positions, (S, N, rotary.axes), torch.int32, dev)
+    rc = lib().roco_norm_rotate(C.byref(rotary.c), ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, N, G, group, _at(q), _at(k),
+                                _at(v), C.byref((C.c_int64 * 6)(*strides)), _at(lens), _at(start),
+                                0 if start is None else start.stride(0), _at(positions), _at(Q), _at(K), _at(V), _raw_stream(dev))
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)
+
+
+def roco_rotary_device_status(rotary: Rotary) -> int:
+    flags = C.c_int32(0)
+    rc = lib().roco_rotary_device_status(C.byref(rotary.c), _stream(), C.byref(flags))
+    if rc not in (ROCO_OK, 5):
+        raise RocoError(rc, "roco_rotary_device_status")
+    return int(flags.value)
+
+
+def roco_cache_reorder(cache: Cache, source, dst: Optional[Cache] = None):
+    """Sequence b of dst (None: of the cache itself) becomes a copy of sequence source[b] of the cache as it was before the call;
+    ROCO_REORDER_KEEP: stays, ROCO_REORDER_FREE: is emptied.  source [dst.S] int32."""
+    what, dev = "roco_cache_reorder", _device()
+    dst = cache if dst is None else dst
+    for c in (cache, dst):
+        if c.K.get_device() != dev:
+            raise RocoError(1, f"{what}: the cache is not on the current CUDA device")
+    _need(what, "source", source, (dst.S,), torch.int32, dev)
+    rc = lib().roco_cache_reorder(C.byref(cache.c), C.byref(dst.c), _at(source), _raw_stream(dev))
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)
+
+
+def roco_linear_reorder(state: LinearState, source, dst: Optional[LinearState] = None):
+    """roco_cache_reorder for the states of linear attention (a freed sequence's become zero)."""
+    what, dev = "roco_linear_reorder", _device()
+    dst = state if dst is None else dst
+    for c in (state, dst):
+        if c.state.get_device() != dev:
+            raise RocoError(1, f"{what}: the state is not on the current CUDA device")
+    _need(what, "source", source, (dst.S,), torch.int32, dev)
+    rc = lib().roco_linear_reorder(C.byref(state.c), C.byref(dst.c), _at(source), _raw_stream(dev))
+    if rc != ROCO_OK:
+        raise RocoError(rc, what)

@@ -5,6 +5,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "heads.cuh"
 #include "launch.h"
 #include "linear.cuh"
 #include "tree.cuh"
@@ -40,6 +41,11 @@ roco_status check_scope(int r, int scope_mode, int B, bool decode) {
   if (scope_mode == ROCO_SCOPE_EXCLUDE_TOP_R) return (r >= 0 && (decode ? r < B : r <= B)) ? ROCO_OK : ROCO_ERR_INVALID_ARG;
   if (scope_mode == ROCO_SCOPE_LOWEST_R) return (r >= 1 && r <= B) ? ROCO_OK : ROCO_ERR_INVALID_ARG;
   return ROCO_ERR_INVALID_ARG;
+}
+
+bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
 }
 
 struct PrefillWs {
@@ -807,6 +813,126 @@ roco_status roco_linear_device_status(const roco_linear_state *state, void *stre
   if (cudaMemcpyAsync(flags_host, state->status, 4, cudaMemcpyDeviceToHost, cs) != cudaSuccess) return ROCO_ERR_CUDA;
   if (cudaStreamSynchronize(cs) != cudaSuccess) return ROCO_ERR_CUDA;
   return *flags_host ? ROCO_ERR_STATE : ROCO_OK;
+}
+
+roco_status roco_norm_rotate(const roco_rotary *rotary, int dtype, int S, int N, int G, int group, const void *q,
+                             const void *k, const void *v, const int64_t *strides, const int32_t *lens,
+                             const int32_t *start, int start_stride, const int32_t *positions, void *Q, void *K, void *V,
+                             void *stream) {
+  NvtxRange range("roco_norm_rotate");
+  if (!rotary || !rotary->status || !q || !Q || !strides || !k != !K || !v != !V) return ROCO_ERR_INVALID_ARG;
+  if (S < 1 || N < 1 || G < 1 || group < 1 || rotary->axes < 1 || rotary->rot < 0) return ROCO_ERR_INVALID_ARG;
+  if (rotary->rot > 0 && !rotary->freq) return ROCO_ERR_INVALID_ARG;
+  if (rotary->pairing != ROCO_PAIR_HALVES && rotary->pairing != ROCO_PAIR_ADJACENT) return ROCO_ERR_INVALID_ARG;
+  if (rotary->d != 64 && rotary->d != 128) return ROCO_ERR_UNSUPPORTED;
+  if (rotary->rot > rotary->d) return ROCO_ERR_INVALID_ARG;
+  if (rotary->rot % 16 || rotary->axes > 4 || group > ROCO_TREE_MAX_GROUP) return ROCO_ERR_UNSUPPORTED;
+  if (dtype != ROCO_F32 && dtype != ROCO_BF16) return ROCO_ERR_UNSUPPORTED;
+  if ((long long)S * G > 0x7fffffffLL / 64 || (long long)S * N > 0x7fffffffLL / 2) return ROCO_ERR_UNSUPPORTED;
+  const int e = dtype == ROCO_BF16 ? 2 : 4;
+  HeadsParams p;
+  const void *in[3] = {q, k, v};
+  void *out[3] = {Q, K, V};
+  for (int i = 0; i < 3; ++i) {
+    p.in[i] = static_cast<const char *>(in[i]);
+    p.out[i] = static_cast<char *>(out[i]);
+    p.seq[i] = p.row[i] = 0;
+    if (!in[i]) continue;
+    if (!aligned16(in[i]) || !aligned16(out[i])) return ROCO_ERR_INVALID_ARG;
+    // a stride that no index is multiplied with may be anything
+    if (S > 1) p.seq[i] = strides[2 * i] * e;
+    if (N > 1) p.row[i] = strides[2 * i + 1] * e;
+    if (p.seq[i] % 16 || p.row[i] % 16) return ROCO_ERR_INVALID_ARG;
+  }
+  p.lens = lens; p.start = start; p.positions = positions; p.start_stride = start_stride;
+  p.freq = rotary->freq; p.weight[0] = rotary->q_weight; p.weight[1] = rotary->k_weight; p.axis = rotary->axis;
+  p.status = rotary->status;
+  p.S = S; p.N = N; p.G = G; p.group = group; p.rot = rotary->rot; p.axes = rotary->axes; p.heads = 1; p.eps = rotary->eps;
+  return launch_norm_rotate(p, dtype, rotary->d, rotary->pairing, device_sms(), static_cast<cudaStream_t>(stream));
+}
+
+roco_status roco_rotary_device_status(const roco_rotary *rotary, void *stream, int32_t *flags_host) {
+  if (!rotary || !rotary->status || !flags_host) return ROCO_ERR_INVALID_ARG;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  if (cudaMemcpyAsync(flags_host, rotary->status, 4, cudaMemcpyDeviceToHost, cs) != cudaSuccess) return ROCO_ERR_CUDA;
+  if (cudaStreamSynchronize(cs) != cudaSuccess) return ROCO_ERR_CUDA;
+  return *flags_host ? ROCO_ERR_STATE : ROCO_OK;
+}
+
+roco_status roco_tree_verify(const roco_verify *call, void *stream) {
+  NvtxRange range("roco_tree_verify");
+  if (!call || !call->target || !call->tokens || !call->parent || !call->accept_u || !call->sample_u || !call->path ||
+      !call->path_len || !call->next_token || !call->status)
+    return ROCO_ERR_INVALID_ARG;
+  if (call->S < 1 || call->T < 1 || call->V < 1 || call->A < 1 || call->A > call->T) return ROCO_ERR_INVALID_ARG;
+  if (call->draft && call->target_prefix && !call->draft_prefix) return ROCO_ERR_INVALID_ARG;
+  if (call->distinct != 0 && call->distinct != 1) return ROCO_ERR_INVALID_ARG;
+  if (call->dtype != ROCO_F32 && call->dtype != ROCO_BF16) return ROCO_ERR_UNSUPPORTED;
+  if (call->T > ROCO_TREE_MAX_NODES || call->A > ROCO_TREE_MAX_PATH) return ROCO_ERR_UNSUPPORTED;
+  if (call->V > (1 << 30) || call->S > (1 << 24)) return ROCO_ERR_UNSUPPORTED;
+  const int e = call->dtype == ROCO_BF16 ? 2 : 4;
+  for (const void *x : {call->target, call->draft, call->target_prefix, call->draft_prefix})
+    if (reinterpret_cast<uintptr_t>(x) % e) return ROCO_ERR_INVALID_ARG;
+  VerifyParams p;
+  p.target = static_cast<const char *>(call->target); p.draft = static_cast<const char *>(call->draft);
+  p.target_prefix = static_cast<const char *>(call->target_prefix);
+  p.draft_prefix = static_cast<const char *>(call->draft_prefix);
+  p.target_seq = call->target_seq * e; p.target_row = call->target_row * e;
+  p.draft_seq = call->draft_seq * e; p.draft_row = call->draft_row * e;
+  p.target_prefix_seq = call->target_prefix_seq * e; p.draft_prefix_seq = call->draft_prefix_seq * e;
+  p.tokens = call->tokens; p.parent = call->parent; p.nodes = call->nodes;
+  p.accept_u = call->accept_u; p.sample_u = call->sample_u;
+  p.path = call->path; p.path_len = call->path_len; p.next_token = call->next_token; p.status = call->status;
+  p.T = call->T; p.V = call->V; p.A = call->A; p.distinct = call->distinct; p.ranks = 1;
+  return launch_tree_verify(p, call->dtype, call->S, device_sms(), static_cast<cudaStream_t>(stream));
+}
+
+roco_status roco_cache_reorder(const roco_cache *src, roco_cache *dst, const int32_t *source, void *stream) {
+  NvtxRange range("roco_cache_reorder");
+  roco_status st = check_cache(src);
+  if (st != ROCO_OK || (st = check_cache(dst)) != ROCO_OK) return st;
+  if (!source || src->kv_dtype != dst->kv_dtype || src->G != dst->G || src->d != dst->d || dst->B < src->B)
+    return ROCO_ERR_INVALID_ARG;
+  ReorderParams p;
+  p.in_place = src->K == dst->K;
+  if (p.in_place && (src->V != dst->V || src->s != dst->s || src->q != dst->q || src->n != dst->n || src->pos != dst->pos ||
+                     src->live != dst->live || src->t_next != dst->t_next || src->S != dst->S || src->B != dst->B))
+    return ROCO_ERR_INVALID_ARG;
+  if (p.in_place && src->S > ROCO_REORDER_MAX_S) return ROCO_ERR_UNSUPPORTED;
+  const int row = src->d * (src->kv_dtype == ROCO_BF16 ? 2 : 4);
+  const size_t src_bytes = (size_t)src->S * src->G * src->B * row, dst_bytes = (size_t)dst->S * dst->G * dst->B * row;
+  if (!p.in_place && (overlap(src->K, src_bytes, dst->K, dst_bytes) || overlap(src->V, src_bytes, dst->V, dst_bytes)))
+    return ROCO_ERR_INVALID_ARG;
+  p.src[0] = static_cast<const char *>(src->K); p.src[1] = static_cast<const char *>(src->V);
+  p.dst[0] = static_cast<char *>(dst->K); p.dst[1] = static_cast<char *>(dst->V);
+  p.src_unit = (long long)src->B * row; p.dst_unit = (long long)dst->B * row;
+  p.src_s = src->s; p.src_q = src->q; p.src_n = src->n; p.src_pos = src->pos; p.src_live = src->live; p.src_t_next = src->t_next;
+  p.dst_s = dst->s; p.dst_q = dst->q; p.dst_n = dst->n; p.dst_pos = dst->pos; p.dst_live = dst->live; p.dst_t_next = dst->t_next;
+  p.map = source; p.status = dst->status;
+  p.S_src = src->S; p.S_dst = dst->S; p.G = src->G; p.B_src = src->B; p.B_dst = dst->B;
+  p.row_shift = row == 128 ? 3 : row == 256 ? 4 : 5;
+  p.arrays = 2; p.parts = 1; p.room = 1;
+  return launch_reorder(p, device_sms(), static_cast<cudaStream_t>(stream));
+}
+
+roco_status roco_linear_reorder(const roco_linear_state *src, const roco_linear_state *dst, const int32_t *source,
+                                void *stream) {
+  NvtxRange range("roco_linear_reorder");
+  roco_status st = check_linear(src);
+  if (st != ROCO_OK || (st = check_linear(dst)) != ROCO_OK) return st;
+  if (!source || src->G != dst->G || src->d != dst->d) return ROCO_ERR_INVALID_ARG;
+  ReorderParams p = {};
+  p.in_place = src->state == dst->state;
+  const size_t unit = (size_t)src->d * src->d * 4;
+  if (p.in_place ? src->S != dst->S : overlap(src->state, src->S * src->G * unit, dst->state, dst->S * dst->G * unit))
+    return ROCO_ERR_INVALID_ARG;
+  if (p.in_place && src->S > ROCO_REORDER_MAX_S) return ROCO_ERR_UNSUPPORTED;
+  p.src[0] = reinterpret_cast<const char *>(src->state); p.dst[0] = reinterpret_cast<char *>(dst->state);
+  p.src_unit = p.dst_unit = (long long)unit;
+  p.map = source; p.status = dst->status;
+  p.S_src = src->S; p.S_dst = dst->S; p.G = src->G;
+  p.arrays = 1; p.parts = 1; p.room = 1;
+  return launch_reorder(p, device_sms(), static_cast<cudaStream_t>(stream));
 }
 
 roco_status roco_device_status(const roco_cache *cache, void *stream, int32_t *flags_host) {

@@ -1,0 +1,197 @@
+// Queries, keys and values of a layer out of its projections: norm of each head, rotation by position, layout by unit.
+//
+// A stream: every element is read once and written once, 2 d e bytes per head of a token, and that bounds it.  A row (the head
+// of one token) is held by d e / 32 lanes with two 16-byte pieces each.  For pairs (i, i + rot/2) the two pieces are the two
+// halves of the same pairs, so the rotation needs no exchange between lanes, and the norm a butterfly over 4 to 16 lanes.  A
+// thread keeps its place in the row and its token and goes through a range of heads: sines and cosines are formed once for all
+// of them, and four rows are in flight at a time.  Neighbouring rows of a CTA are neighbouring tokens, which follow one another in
+// the unit layout: what is read as rows of the projections leaves as blocks of 16 to 32 tokens per head.
+#include "heads.cuh"
+
+namespace roco {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kFlight = 4;  // rows of a thread in flight
+
+// position * freq in turns, without its whole turns: the product of two 24-bit numbers (a position has 32 bits at most) is
+// good to 2^-53 of itself in 64 bits, so a position of 2^31 is still off by less than 1e-6 of a turn.
+__device__ __forceinline__ void angle(double position, float freq, float &c, float &s) {
+  const double turns = position * ((double)freq * 0.15915494309189533577);
+  float half;
+  half = (float)(2.0 * (turns - rint(turns)));
+  sincospif(half, &s, &c);
+}
+
+__device__ __forceinline__ void rotate(float &a, float &b, float c, float s) {
+  const float x = a * c - b * s;
+  b = b * c + a * s;
+  a = x;
+}
+
+__device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&x);
+}
+__device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+  return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+}
+
+template <typename T, int D, bool kAdjacent>
+__global__ void __launch_bounds__(kThreads) norm_rotate_kernel(const HeadsParams p) {
+  constexpr int E = Elem<T>::kPerChunk, kLanes = D / E / 2, kRows = kThreads / kLanes;
+  const int lane = threadIdx.x % kLanes;
+  const unsigned token = blockIdx.x * kRows + threadIdx.x / kLanes;  // (there are fewer than 2^31)
+  int b = 0, n = 0;
+  bool on = token < (unsigned)p.S * (unsigned)p.N;
+  if (on) {
+    b = (int)(token / (unsigned)p.N);
+    n = (int)(token - (unsigned)b * (unsigned)p.N);
+    if (p.lens) {
+      int len = p.lens[b];
+      if (len < 0 || len > p.N) {
+        if (n == 0 && lane == 0 && blockIdx.y == 0) atomicOr(p.status, ROCO_DEV_BAD_LENS);
+        len = 0;
+      }
+      on = n < len;
+    }
+  }
+  if (!__syncthreads_or(on)) return;
+
+  // where the two pieces lie in the row, and what turns their pairs
+  const int half = p.rot / 2 / E;  // pieces in half of the rotated elements
+  int at[2];
+  bool turn[2];
+  if (kAdjacent) {
+    at[0] = lane;
+    at[1] = lane + kLanes;
+    turn[0] = at[0] * E < p.rot;
+    turn[1] = at[1] * E < p.rot;
+  } else {
+    turn[0] = turn[1] = lane < half;
+    at[0] = lane < half ? lane : 2 * half + 2 * (lane - half);
+    at[1] = lane < half ? lane + half : at[0] + 1;
+  }
+  float c[E], s[E];
+  if (on) {
+    const double start = p.start ? (double)p.start[(long long)b * p.start_stride] : 0.0;
+    const int *pos = p.positions ? p.positions + (long long)token * p.axes : nullptr;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      c[e] = 1.f;
+      s[e] = 0.f;
+      const int piece = kAdjacent ? 2 * e / E : 0;
+      if (!turn[piece]) continue;
+      const int pair = kAdjacent ? at[piece] * (E / 2) + e % (E / 2) : at[0] * E + e;
+      int axis = p.axis ? p.axis[pair] : 0;
+      if (axis < 0 || axis >= p.axes) {
+        if (token == 0 && blockIdx.y == 0) atomicOr(p.status, ROCO_DEV_BAD_MAP);
+        axis = 0;
+      }
+      angle(start + (double)(pos ? pos[axis] : n), p.freq[pair], c[e], s[e]);
+    }
+  }
+
+  const int q_heads = p.G * p.group;
+  int h = blockIdx.y * p.heads;
+  const int last = min(h + p.heads, q_heads + 2 * p.G);
+  while (h < last) {
+    const int kind = h < q_heads ? 0 : h < q_heads + p.G ? 1 : 2;
+    const int first = kind == 0 ? 0 : kind == 1 ? q_heads : q_heads + p.G;
+    const int end = min(last, kind == 0 ? q_heads : first + p.G);
+    const int per = kind == 0 ? p.group : 1;
+    if (!p.in[kind]) { h = end; continue; }
+    const char *in = p.in[kind] + b * p.seq[kind] + n * p.row[kind];
+    char *out = p.out[kind] + (((long long)b * p.G * p.N + n) * per) * (D * (int)sizeof(T));
+    const float *weight = kind < 2 ? p.weight[kind] : nullptr;
+    float w[2][E];
+    if (weight) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[i][e] = weight[at[i] * E + e];
+    }
+    for (; h < end; h += kFlight) {
+      uint4 raw[kFlight][2];
+#pragma unroll
+      for (int r = 0; r < kFlight; ++r)
+        if (on && h + r < end) {
+          const uint4 *src = reinterpret_cast<const uint4 *>(in + (long long)(h + r - first) * (D * (int)sizeof(T)));
+          raw[r][0] = src[at[0]];
+          raw[r][1] = src[at[1]];
+        }
+#pragma unroll
+      for (int r = 0; r < kFlight; ++r) {
+        if (h + r >= end) break;
+        if (kind < 2) {
+          float x[2][E];
+          Elem<T>::unpack(raw[r][0], x[0]);
+          Elem<T>::unpack(raw[r][1], x[1]);
+          if (weight) {
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum = fmaf(x[0][e], x[0][e], fmaf(x[1][e], x[1][e], sum));
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            const float norm = rsqrtf(sum * (1.f / D) + p.eps);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              x[0][e] = x[0][e] * norm * w[0][e];
+              x[1][e] = x[1][e] * norm * w[1][e];
+            }
+          }
+          if (kAdjacent) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+              if (turn[0]) rotate(x[0][e], x[0][e + 1], c[e / 2], s[e / 2]);
+              if (turn[1]) rotate(x[1][e], x[1][e + 1], c[E / 2 + e / 2], s[E / 2 + e / 2]);
+            }
+          } else if (turn[0]) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) rotate(x[0][e], x[1][e], c[e], s[e]);
+          }
+          raw[r][0] = pack(x[0]);
+          raw[r][1] = pack(x[1]);
+        }
+        if (on) {
+          const int head = h + r - first, g = head / per, j = head - g * per;
+          uint4 *dst = reinterpret_cast<uint4 *>(out + ((long long)g * p.N * per + j) * (D * (int)sizeof(T)));
+          dst[at[0]] = raw[r][0];
+          dst[at[1]] = raw[r][1];
+        }
+      }
+    }
+    h = end;
+  }
+}
+
+template <typename T, int D>
+roco_status launch_t(HeadsParams p, int pairing, int sms, cudaStream_t stream) {
+  constexpr int kRows = kThreads / (D / Elem<T>::kPerChunk / 2);
+  const long long tokens = (long long)p.S * p.N;
+  const long long tiles = (tokens + kRows - 1) / kRows;
+  const int all = p.G * (p.group + 2);
+  // Heads of a CTA: sixteen where there are tokens enough to fill the GPU several times over (eight CTAs per SM), fewer where not.
+  int heads = 16;
+  while (heads > 1 && tiles * ((all + heads - 1) / heads) < 4LL * 8 * sms) heads /= 2;
+  p.heads = heads;
+  const int parts = (all + heads - 1) / heads;
+  if (tokens > 0x7fffffffLL - kRows || parts > 65535) return ROCO_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)tiles, (unsigned)parts);
+  if (pairing == ROCO_PAIR_ADJACENT) norm_rotate_kernel<T, D, true><<<grid, kThreads, 0, stream>>>(p);
+  else norm_rotate_kernel<T, D, false><<<grid, kThreads, 0, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+}
+
+}  // namespace
+
+roco_status launch_norm_rotate(const HeadsParams &p, int dtype, int d, int pairing, int sms, cudaStream_t stream) {
+  if (dtype == ROCO_BF16)
+    return d == 128 ? launch_t<__nv_bfloat16, 128>(p, pairing, sms, stream) : launch_t<__nv_bfloat16, 64>(p, pairing, sms, stream);
+  return d == 128 ? launch_t<float, 128>(p, pairing, sms, stream) : launch_t<float, 64>(p, pairing, sms, stream);
+}
+
+}  // namespace roco

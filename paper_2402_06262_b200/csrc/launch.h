@@ -173,4 +173,12 @@ roco_status launch_linear_prefill_simt(const LinearParams &p, int d, int U, cuda
 int linear_tc_segments(int U, int Lmax, int sms);
 roco_status launch_linear_prefill_tc(const LinearParams &p, int d, int U, cudaStream_t stream);
 
+// ---- norm and rotation of a layer's heads, verification of drafted trees, reordering of sequences (heads.cuh)
+struct HeadsParams;
+struct VerifyParams;
+struct ReorderParams;
+roco_status launch_norm_rotate(const HeadsParams &p, int dtype, int d, int pairing, int sms, cudaStream_t stream);
+roco_status launch_tree_verify(const VerifyParams &p, int dtype, int S, int sms, cudaStream_t stream);
+roco_status launch_reorder(ReorderParams p, int sms, cudaStream_t stream);
+
 }  // namespace roco

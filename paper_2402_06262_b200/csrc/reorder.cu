@@ -1,0 +1,207 @@
+// Sequences of a cache or of linear states forked, reordered, compacted, freed.
+//
+// A copy, bound by the bytes that move: every source read once, every destination written once.  The work is cut by columns, 16 bytes
+// at one place of a unit, which a thread handles for all sequences: it fetches the column of every distinct source into its own part
+// of shared memory (asynchronous 16-byte copies), then writes it to every destination.  So a source that feeds many sequences is
+// read once, and in place any map is right (cycles, forks, chains): a column is written only after all of it has been read, and
+// nobody else touches it.  Threads share nothing but the map, so nobody waits for anybody.
+#include "heads.cuh"
+
+namespace roco {
+namespace {
+
+constexpr int kMost = ROCO_REORDER_MAX_S;  // destinations of a CTA
+
+struct Lists {
+  int map[kMost];        // validated: a source, KEEP or FREE
+  int first[kMost];      // the first destination with the same source
+  int slot_of[kMost];    // where that one's source is kept
+  int source[kMost];     // slot -> source sequence
+  int live[kMost];       // slot -> its occupied slots in this unit; -1: not copied
+  int to[kMost], from[kMost];  // copies: destination, slot
+  int empty[kMost];      // destinations that are freed
+  int n_slots, n_copies, n_empty, max_live;
+};
+
+__device__ __forceinline__ void fetch16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void fetch4(uint32_t dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// The source of destination b.
+__device__ __forceinline__ int source_of(const ReorderParams &p, int b, bool report) {
+  const int a = p.map[b];
+  if (a >= 0 ? a < p.S_src : a == ROCO_REORDER_KEEP || a == ROCO_REORDER_FREE) return a == b && p.in_place ? ROCO_REORDER_KEEP : a;
+  if (report) atomicOr(p.status, ROCO_DEV_BAD_MAP);
+  return ROCO_REORDER_KEEP;
+}
+
+__global__ void reorder_kernel(const ReorderParams p) {
+  extern __shared__ uint4 room[];
+  __shared__ Lists ls;
+  const int tid = threadIdx.x, threads = blockDim.x;
+  const int g = blockIdx.x / p.parts, part = blockIdx.x - g * p.parts;
+  const int b0 = blockIdx.y * kMost, nb = min(kMost, p.S_dst - b0);
+  const bool cache = p.arrays == 2;
+
+  for (int i = tid; i < nb; i += threads) ls.map[i] = source_of(p, b0 + i, blockIdx.x == 0);
+  if (tid == 0) ls.n_slots = ls.n_copies = ls.n_empty = ls.max_live = 0;
+  __syncthreads();
+  for (int i = tid; i < nb; i += threads) {
+    const int a = ls.map[i];
+    if (a == ROCO_REORDER_FREE) ls.empty[atomicAdd(&ls.n_empty, 1)] = b0 + i;
+    if (a < 0) continue;
+    int j = 0;
+    while (ls.map[j] != a) ++j;
+    ls.first[i] = j;
+    if (j != i) continue;
+    const int slot = atomicAdd(&ls.n_slots, 1);
+    int live = 0;
+    if (cache) {
+      live = p.src_live[(long long)a * p.G + g];
+      if (live < 0 || live > p.B_src) {
+        if (part == 0) atomicOr(p.status, ROCO_DEV_BAD_LIVE);
+        live = -1;
+      } else {
+        atomicMax(&ls.max_live, live);
+      }
+    }
+    ls.slot_of[i] = slot;
+    ls.source[slot] = a;
+    ls.live[slot] = live;
+  }
+  __syncthreads();
+  for (int i = tid; i < nb; i += threads) {
+    if (ls.map[i] < 0) continue;
+    const int slot = ls.slot_of[ls.first[i]];
+    if (cache && ls.live[slot] < 0) continue;
+    const int c = atomicAdd(&ls.n_copies, 1);
+    ls.to[c] = b0 + i;
+    ls.from[c] = slot;
+  }
+  __syncthreads();
+  launch_dependents();
+  const int n_slots = ls.n_slots, n_copies = ls.n_copies, n_empty = ls.n_empty;
+  const uint32_t mine = smem_u32(room + tid);
+  const uint32_t step = threads * 16;  // from one of a thread's 16-byte places to its next
+
+  // K and V, or the states: columns of 16 bytes
+  const int U = n_slots ? p.room / n_slots : 1;  // columns of a thread at a time
+  const long long chunks = cache ? (long long)ls.max_live << p.row_shift : p.src_unit / 16;
+  const long long per = (long long)threads * U;
+  const int tiles = (int)((chunks + per - 1) / per);
+  for (int t = part; t < p.arrays * tiles; t += p.parts) {
+    const int array = t >= tiles;
+    const long long c0 = (long long)(t - array * tiles) * per + tid;
+    const char *src = p.src[array] + (long long)g * p.src_unit;
+    char *dst = p.dst[array] + (long long)g * p.dst_unit;
+    const long long src_seq = p.src_unit * p.G, dst_seq = p.dst_unit * p.G;
+    for (int j = 0; j < n_slots; ++j) {
+      const long long end = cache ? (long long)ls.live[j] << p.row_shift : chunks;
+      const char *from = src + ls.source[j] * src_seq;
+      for (int u = 0; u < U; ++u) {
+        const long long c = c0 + (long long)u * threads;
+        if (c < end) fetch16(mine + (uint32_t)(j * U + u) * step, from + c * 16);
+      }
+    }
+    fetched();
+    for (int i = 0; i < n_copies; ++i) {
+      const int j = ls.from[i];
+      const long long end = cache ? (long long)ls.live[j] << p.row_shift : chunks;
+      char *to = dst + ls.to[i] * dst_seq;
+      for (int u = 0; u < U; ++u) {
+        const long long c = c0 + (long long)u * threads;
+        if (c < end) *reinterpret_cast<uint4 *>(to + c * 16) = room[(j * U + u) * threads + tid];
+      }
+    }
+  }
+  if (!cache) {
+    for (long long c = (long long)part * threads + tid; c < chunks; c += (long long)p.parts * threads)
+      for (int i = 0; i < n_empty; ++i)
+        *reinterpret_cast<uint4 *>(p.dst[0] + ((long long)ls.empty[i] * p.G + g) * p.dst_unit + c * 16) = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  if (!p.in_place && part == 0) {
+    for (int i = tid; i < n_copies; i += threads) {
+      const long long to = (long long)ls.to[i] * p.G + g;
+      p.dst_live[to] = ls.live[ls.from[i]];
+      p.dst_t_next[to] = p.src_t_next[(long long)ls.source[ls.from[i]] * p.G + g];
+    }
+    for (int i = tid; i < n_empty; i += threads) {
+      const long long to = (long long)ls.empty[i] * p.G + g;
+      p.dst_live[to] = p.dst_t_next[to] = 0;
+    }
+  }
+  // statistics and positions: the four numbers of a slot are a column
+  for (int k = part * threads + tid; k < p.B_dst; k += p.parts * threads) {
+    for (int j = 0; j < n_slots; ++j) {
+      if (k >= ls.live[j]) continue;
+      const long long at = ((long long)ls.source[j] * p.G + g) * p.B_src + k;
+      const uint32_t to = mine + (uint32_t)j * step;
+      fetch4(to, p.src_s + at);
+      fetch4(to + 4, p.src_q + at);
+      fetch4(to + 8, p.src_n + at);
+      fetch4(to + 12, p.src_pos + at);
+    }
+    fetched();
+    for (int i = 0; i < n_copies; ++i) {
+      const int j = ls.from[i];
+      const long long at = ((long long)ls.to[i] * p.G + g) * p.B_dst + k;
+      if (k < ls.live[j]) {
+        const uint4 x = room[j * threads + tid];
+        p.dst_s[at] = __uint_as_float(x.x);
+        p.dst_q[at] = __uint_as_float(x.y);
+        p.dst_n[at] = (int)x.z;
+        p.dst_pos[at] = (int)x.w;
+      } else {
+        p.dst_pos[at] = -1;
+      }
+    }
+    for (int i = 0; i < n_empty; ++i) p.dst_pos[((long long)ls.empty[i] * p.G + g) * p.B_dst + k] = -1;
+  }
+}
+
+// live and t_next of every unit in place, where every CTA of the kernel above reads them: they change behind it.
+__global__ void reorder_live_kernel(const ReorderParams p) {
+  const int g = blockIdx.x, b = threadIdx.x;
+  const int a = b < p.S_dst ? source_of(p, b, false) : ROCO_REORDER_KEEP;
+  wait_for_launch_before();
+  int live = 0, t_next = 0;
+  if (a >= 0) {
+    live = p.src_live[(long long)a * p.G + g];
+    t_next = p.src_t_next[(long long)a * p.G + g];
+  }
+  __syncthreads();
+  if (a == ROCO_REORDER_KEEP || live < 0 || live > p.B_src) return;
+  p.dst_live[(long long)b * p.G + g] = live;
+  p.dst_t_next[(long long)b * p.G + g] = t_next;
+}
+
+}  // namespace
+
+roco_status launch_reorder(ReorderParams p, int sms, cudaStream_t stream) {
+  const int most = p.S_dst < kMost ? p.S_dst : kMost;   // places a thread may need
+  // Threads so that a CTA's places take 64 KB at most (three CTAs per SM) down to one warp; at least eight places each, for the
+  // columns of few sources that are in flight together.
+  int threads = 256;
+  while (threads > 32 && threads * most * 16 > 65536) threads /= 2;
+  p.room = most < 8 ? 8 : most;
+  const int smem = threads * p.room * 16;
+  const long long chunks = p.arrays * (p.src_unit / 16);
+  long long parts = (chunks + 4LL * threads - 1) / (4LL * threads), most_parts = (16LL * sms + p.G - 1) / p.G;
+  if (parts > most_parts) parts = most_parts;
+  p.parts = parts < 1 ? 1 : (int)parts;
+  const unsigned blocks = (unsigned)((p.S_dst + kMost - 1) / kMost);
+  if (blocks > 65535 || (long long)p.G * p.parts > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
+  static SmemLimit limit;
+  if (!limit((const void *)reorder_kernel, 32 * kMost * 16)) return ROCO_ERR_CUDA;
+  reorder_kernel<<<dim3((unsigned)(p.G * p.parts), blocks), threads, smem, stream>>>(p);
+  if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
+  if (p.arrays == 1 || !p.in_place) return ROCO_OK;
+  return launch_overlapped(reorder_live_kernel, (unsigned)p.G, kMost, 0, stream, p) ? ROCO_OK : ROCO_ERR_CUDA;
+}
+
+}  // namespace roco
