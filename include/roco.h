@@ -553,9 +553,9 @@ typedef struct {
 } roco_rotary;
 
 /*
- *   q, k, v      projections: [S][N][heads][d] with G * group heads of queries and G of keys and values; `dtype`; `strides` says
- *                (in elements) how far apart sequences and tokens lie: {q sequence, q token, k sequence, k token, v sequence,
- *                v token}, multiples of 16 bytes, so that all three may lie in the rows of one product.  k, v: or NULL
+ *   q, k, v      projections: [S][N][heads][d] with G * group heads of queries and G of keys and values, `dtype`; a token's heads
+ *                follow each other, sequences and tokens lie `*_seq` and `*_row` elements apart (multiples of 16 bytes), so that
+ *                all three may lie in the rows of one product.  k, v: or NULL
  *   lens         [S] int32 DEVICE array, 0..N, or NULL: N everywhere.  Tokens at lens[b] and behind may hold anything and their
  *                rows of Q, K, V are left as they were.  Any other value sets ROCO_DEV_BAD_LENS and counts as 0
  *   start        DEVICE array of int32, one for each sequence start_stride elements apart (t_next of a cache: start_stride = G),
@@ -565,10 +565,15 @@ typedef struct {
  *                layout of the decode steps, N = T that of the trees, N = Lmax (group 1) that of the prompt passes
  * An axis outside [0, axes) sets ROCO_DEV_BAD_MAP and counts as 0.  One launch.
  */
-roco_status roco_norm_rotate(const roco_rotary *rotary, int dtype, int S, int N, int G, int group, const void *q,
-                             const void *k, const void *v, const int64_t *strides, const int32_t *lens,
-                             const int32_t *start, int start_stride, const int32_t *positions, void *Q, void *K, void *V,
-                             void *stream);
+typedef struct {
+  int32_t dtype, S, N, G, group;
+  int32_t start_stride;
+  const void *q, *k, *v;
+  int64_t q_seq, q_row, k_seq, k_row, v_seq, v_row;
+  const int32_t *lens, *start, *positions;
+  void *Q, *K, *V;
+} roco_heads;
+roco_status roco_norm_rotate(const roco_rotary *rotary, const roco_heads *call, void *stream);
 
 /* roco_device_status for the status word of a rotary. */
 roco_status roco_rotary_device_status(const roco_rotary *rotary, void *stream, int32_t *flags_host);

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -73,6 +74,18 @@ class roco_verify(C.Structure):
                 [(f, C.c_void_p) for f in ("tokens", "parent", "nodes", "accept_u", "sample_u", "path", "path_len", "next_token",
                                            "status")])
 
+
+class roco_heads(C.Structure):
+    _fields_ = ([(f, C.c_int32) for f in ("dtype", "S", "N", "G", "group", "start_stride")] +
+                [(f, C.c_void_p) for f in ("q", "k", "v")] +
+                [(f, C.c_int64) for f in ("q_seq", "q_row", "k_seq", "k_row", "v_seq", "v_row")] +
+                [(f, C.c_void_p) for f in ("lens", "start", "positions", "Q", "K", "V")])
+
+
+# The two structs above as bytes: filling a ctypes structure of thirty fields, or passing twenty arguments, takes longer than the
+# launch.  (NULL is 0 here.)
+_VERIFY, _HEADS = struct.Struct("@6i4P6q9P"), struct.Struct("@6i3P6q6P")
+assert _VERIFY.size == C.sizeof(roco_verify) and _HEADS.size == C.sizeof(roco_heads)
 
 _lib = None
 
@@ -197,10 +210,9 @@ def lib() -> C.CDLL:
         L.roco_linear_device_status.restype = C.c_int
         L.roco_linear_device_status.argtypes = [C.POINTER(roco_linear_state), C.c_void_p, C.c_void_p]
         L.roco_tree_verify.restype = C.c_int
-        L.roco_tree_verify.argtypes = [C.POINTER(roco_verify), C.c_void_p]
+        L.roco_tree_verify.argtypes = [C.c_char_p, C.c_void_p]            # a roco_verify as bytes
         L.roco_norm_rotate.restype = C.c_int
-        L.roco_norm_rotate.argtypes = ([C.POINTER(roco_rotary)] + [C.c_int] * 5 + [C.c_void_p] * 3 + [C.POINTER(C.c_int64 * 6)] +
-                                       [C.c_void_p] * 2 + [C.c_int] + [C.c_void_p] * 5)
+        L.roco_norm_rotate.argtypes = [C.POINTER(roco_rotary), C.c_char_p, C.c_void_p]   # a roco_heads as bytes
         L.roco_rotary_device_status.restype = C.c_int
         L.roco_rotary_device_status.argtypes = [C.POINTER(roco_rotary), C.c_void_p, C.c_void_p]
         L.roco_cache_reorder.restype = C.c_int
@@ -362,6 +374,7 @@ class Rotary:
         self.d, self.rot, self.axes, self.freq, self.axis, self.status = d, 2 * freq.shape[0], axes, freq, axis, status
         self.q_weight, self.k_weight = q_weight, k_weight
         self.c = roco_rotary(d, self.rot, pairing, axes, _at(freq), _at(axis), _at(q_weight), _at(k_weight), eps, _at(status))
+        self.ref = C.byref(self.c)
 
 
 def roco_prefill_workspace_bytes(cache: Cache, Lmax: int) -> int:
@@ -754,13 +767,20 @@ def roco_linear_device_status(state: LinearState) -> int:
     return int(flags.value)
 
 
+def _zero(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
 def _need_rows(what: str, name: str, t, shape, dtype, dev: int):
-    """A tensor of this shape and type on the current device whose last dimension is dense; the others may have any strides."""
-    if (not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != dev
-            or (t.stride(-1) != 1 and t.shape[-1] > 1)):
-        raise RocoError(1, f"{what}: {name}: a {dtype} tensor of shape {list(shape)} with dense rows on the current CUDA device is "
-                           f"needed, got " + (f"{t.dtype} {list(t.shape)} with strides {list(t.stride())} on {t.device}"
-                                              if isinstance(t, torch.Tensor) else type(t).__name__))
+    """A tensor of this shape and type on the current device whose last dimension is dense; the others may have any strides, which
+    are returned."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+        strides = t.stride()
+        if strides[-1] == 1 or shape[-1] == 1:
+            return strides
+    raise RocoError(1, f"{what}: {name}: a {dtype} tensor of shape {list(shape)} with dense rows on the current CUDA device is "
+                       f"needed, got " + (f"{t.dtype} {list(t.shape)} with strides {list(t.stride())} on {t.device}"
+                                          if isinstance(t, torch.Tensor) else type(t).__name__))
 
 
 def roco_tree_verify(target, tokens, parent, accept_u, sample_u, path, path_len, next_token, status, nodes=None, draft=None,
@@ -775,30 +795,38 @@ def roco_tree_verify(target, tokens, parent, accept_u, sample_u, path, path_len,
         raise RocoError(1, f"{what}: target is an fp32 or bf16 tensor [S][T][V]")
     if not isinstance(path, torch.Tensor) or path.dim() != 2:
         raise RocoError(1, f"{what}: path is [S][A]")
-    S, T, V = target.shape
-    dtype = target.dtype
-    _need_rows(what, "target", target, (S, T, V), dtype, dev)
-    if draft is not None:
-        _need_rows(what, "draft", draft, (S, T, V), dtype, dev)
-    for name, t in (("target_prefix", target_prefix), ("draft_prefix", draft_prefix)):
-        if t is not None:
-            _need_rows(what, name, t, (S, V), dtype, dev)
-    for name, t, shape, kind in (("tokens", tokens, (S, T), torch.int32), ("parent", parent, (S, T), torch.int32),
-                                 ("accept_u", accept_u, (S, T), torch.float32), ("sample_u", sample_u, (S,), torch.float32),
-                                 ("path", path, (S, path.shape[1]), torch.int32), ("path_len", path_len, (S,), torch.int32),
-                                 ("next_token", next_token, (S,), torch.int32), ("status", status, (1,), torch.int32)):
-        _need(what, name, t, shape, kind, dev)
+    shape, dtype, A = target.shape, target.dtype, path.shape[1]
+    S, T, V = shape
+    rows, each, i32 = (S, T), (S,), torch.int32
+    ts = _need_rows(what, "target", target, shape, dtype, dev)
+    ds = ts if draft is None else _need_rows(what, "draft", draft, shape, dtype, dev)
+    tp = 0 if target_prefix is None else _need_rows(what, "target_prefix", target_prefix, (S, V), dtype, dev)[0]
+    dp = 0 if draft_prefix is None else _need_rows(what, "draft_prefix", draft_prefix, (S, V), dtype, dev)[0]
+    _need(what, "tokens", tokens, rows, i32, dev)
+    _need(what, "parent", parent, rows, i32, dev)
+    _need(what, "accept_u", accept_u, rows, torch.float32, dev)
+    _need(what, "sample_u", sample_u, each, torch.float32, dev)
+    _need(what, "path", path, (S, A), i32, dev)
+    _need(what, "path_len", path_len, each, i32, dev)
+    _need(what, "next_token", next_token, each, i32, dev)
+    _need(what, "status", status, (1,), i32, dev)
     if nodes is not None:
-        _need(what, "nodes", nodes, (S,), torch.int32, dev)
-    call = roco_verify(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, T, V, path.shape[1], int(bool(distinct)), _at(target),
-                       _at(draft), _at(target_prefix), _at(draft_prefix), target.stride(0), target.stride(1),
-                       0 if draft is None else draft.stride(0), 0 if draft is None else draft.stride(1),
-                       0 if target_prefix is None else target_prefix.stride(0), 0 if draft_prefix is None else draft_prefix.stride(0),
-                       _at(tokens), _at(parent), _at(nodes), _at(accept_u), _at(sample_u), _at(path), _at(path_len), _at(next_token),
-                       _at(status))
-    rc = lib().roco_tree_verify(C.byref(call), _raw_stream(dev))
+        _need(what, "nodes", nodes, each, i32, dev)
+    call = _VERIFY.pack(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, T, V, A, 1 if distinct else 0, target.data_ptr(),
+                        _zero(draft), _zero(target_prefix), _zero(draft_prefix), ts[0], ts[1], ds[0], ds[1], tp, dp,
+                        tokens.data_ptr(), parent.data_ptr(), _zero(nodes), accept_u.data_ptr(), sample_u.data_ptr(),
+                        path.data_ptr(), path_len.data_ptr(), next_token.data_ptr(), status.data_ptr())
+    rc = lib().roco_tree_verify(call, _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
+
+
+def _need_heads(what: str, name: str, t, S: int, N: int, heads: int, d: int, dtype, dev: int):
+    """A projection [S][N][heads][d] whose heads follow each other; returns how far apart its sequences and tokens are."""
+    strides = _need_rows(what, name, t, (S, N, heads, d), dtype, dev)
+    if strides[2] != d and heads > 1:
+        raise RocoError(1, f"{what}: {name}: a token's heads lie {strides[2]} elements apart, not {d}")
+    return strides
 
 
 def roco_norm_rotate(rotary: Rotary, q, k, v, Q, K, V, lens=None, start=None, positions=None):
@@ -809,36 +837,37 @@ def roco_norm_rotate(rotary: Rotary, q, k, v, Q, K, V, lens=None, start=None, po
     what, dev = "roco_norm_rotate", _device()
     if not isinstance(Q, torch.Tensor) or Q.dim() != 5 or Q.dtype not in (torch.float32, torch.bfloat16):
         raise RocoError(1, f"{what}: Q is an fp32 or bf16 tensor [S][G][N][group][d]")
-    S, G, N, group, d = Q.shape
+    shape, dtype = Q.shape, Q.dtype
+    S, G, N, group, d = shape
     if rotary.d != d:
         raise RocoError(1, f"{what}: Q has heads of {d} elements, the rotary of {rotary.d}")
     if rotary.freq.get_device() != dev:
         raise RocoError(1, f"{what}: the rotary is not on the current CUDA device")
-    dtype = Q.dtype
-    _need(what, "Q", Q, (S, G, N, group, d), dtype, dev)
-    strides = []
-    for name, x, heads, out_name, out in (("q", q, G * group, "Q", Q), ("k", k, G, "K", K), ("v", v, G, "V", V)):
-        if x is None and out is None and name != "q":
-            strides += [0, 0]
-            continue
-        _need_rows(what, name, x, (S, N, heads, d), dtype, dev)
-        if heads > 1 and x.stride(2) != d:
-            raise RocoError(1, f"{what}: {name}: a token's heads lie {x.stride(2)} elements apart, not {d}")
-        if name != "q":
-            _need(what, out_name, out, (S, G, N, d), dtype, dev)
-        strides += [x.stride(0), x.stride(1)]
+    unit = (S, G, N, d)
+    _need(what, "Q", Q, shape, dtype, dev)
+    qs = _need_heads(what, "q", q, S, N, G * group, d, dtype, dev)
+    ks = vs = (0, 0)
+    if k is not None or K is not None:
+        ks = _need_heads(what, "k", k, S, N, G, d, dtype, dev)
+        _need(what, "K", K, unit, dtype, dev)
+    if v is not None or V is not None:
+        vs = _need_heads(what, "v", v, S, N, G, d, dtype, dev)
+        _need(what, "V", V, unit, dtype, dev)
     if lens is not None:
         _need(what, "lens", lens, (S,), torch.int32, dev)
-    if start is not None and (not isinstance(start, torch.Tensor) or start.dtype is not torch.int32 or start.shape != (S,)
-                              or start.get_device() != dev):
-        raise RocoError(1, f"{what}: start: an int32 tensor of shape [{S}] on the current CUDA device is needed")
+    apart = 0
+    if start is not None:
+        if (not isinstance(start, torch.Tensor) or start.dtype is not torch.int32 or start.shape != (S,) or start.get_device() != dev):
+            raise RocoError(1, f"{what}: start: an int32 tensor of shape [{S}] on the current CUDA device is needed")
+        apart = start.stride(0)
     if positions is not None:
         if rotary.axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 2:
             positions = positions[..., None]
         _need(what, "positions", positions, (S, N, rotary.axes), torch.int32, dev)
-    rc = lib().roco_norm_rotate(C.byref(rotary.c), ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, N, G, group, _at(q), _at(k),
-                                _at(v), C.byref((C.c_int64 * 6)(*strides)), _at(lens), _at(start),
-                                0 if start is None else start.stride(0), _at(positions), _at(Q), _at(K), _at(V), _raw_stream(dev))
+    call = _HEADS.pack(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, N, G, group, apart, q.data_ptr(), _zero(k), _zero(v),
+                       qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], _zero(lens), _zero(start), _zero(positions), Q.data_ptr(), _zero(K),
+                       _zero(V))
+    rc = lib().roco_norm_rotate(rotary.ref, call, _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
 

@@ -815,24 +815,24 @@ roco_status roco_linear_device_status(const roco_linear_state *state, void *stre
   return *flags_host ? ROCO_ERR_STATE : ROCO_OK;
 }
 
-roco_status roco_norm_rotate(const roco_rotary *rotary, int dtype, int S, int N, int G, int group, const void *q,
-                             const void *k, const void *v, const int64_t *strides, const int32_t *lens,
-                             const int32_t *start, int start_stride, const int32_t *positions, void *Q, void *K, void *V,
-                             void *stream) {
+roco_status roco_norm_rotate(const roco_rotary *rotary, const roco_heads *call, void *stream) {
   NvtxRange range("roco_norm_rotate");
-  if (!rotary || !rotary->status || !q || !Q || !strides || !k != !K || !v != !V) return ROCO_ERR_INVALID_ARG;
+  if (!rotary || !rotary->status || !call || !call->q || !call->Q || !call->k != !call->K || !call->v != !call->V)
+    return ROCO_ERR_INVALID_ARG;
+  const int S = call->S, N = call->N, G = call->G, group = call->group;
   if (S < 1 || N < 1 || G < 1 || group < 1 || rotary->axes < 1 || rotary->rot < 0) return ROCO_ERR_INVALID_ARG;
   if (rotary->rot > 0 && !rotary->freq) return ROCO_ERR_INVALID_ARG;
   if (rotary->pairing != ROCO_PAIR_HALVES && rotary->pairing != ROCO_PAIR_ADJACENT) return ROCO_ERR_INVALID_ARG;
   if (rotary->d != 64 && rotary->d != 128) return ROCO_ERR_UNSUPPORTED;
   if (rotary->rot > rotary->d) return ROCO_ERR_INVALID_ARG;
   if (rotary->rot % 16 || rotary->axes > 4 || group > ROCO_TREE_MAX_GROUP) return ROCO_ERR_UNSUPPORTED;
-  if (dtype != ROCO_F32 && dtype != ROCO_BF16) return ROCO_ERR_UNSUPPORTED;
+  if (call->dtype != ROCO_F32 && call->dtype != ROCO_BF16) return ROCO_ERR_UNSUPPORTED;
   if ((long long)S * G > 0x7fffffffLL / 64 || (long long)S * N > 0x7fffffffLL / 2) return ROCO_ERR_UNSUPPORTED;
-  const int e = dtype == ROCO_BF16 ? 2 : 4;
+  const int e = call->dtype == ROCO_BF16 ? 2 : 4;
   HeadsParams p;
-  const void *in[3] = {q, k, v};
-  void *out[3] = {Q, K, V};
+  const void *in[3] = {call->q, call->k, call->v};
+  void *out[3] = {call->Q, call->K, call->V};
+  const int64_t seq[3] = {call->q_seq, call->k_seq, call->v_seq}, row[3] = {call->q_row, call->k_row, call->v_row};
   for (int i = 0; i < 3; ++i) {
     p.in[i] = static_cast<const char *>(in[i]);
     p.out[i] = static_cast<char *>(out[i]);
@@ -840,15 +840,15 @@ roco_status roco_norm_rotate(const roco_rotary *rotary, int dtype, int S, int N,
     if (!in[i]) continue;
     if (!aligned16(in[i]) || !aligned16(out[i])) return ROCO_ERR_INVALID_ARG;
     // a stride that no index is multiplied with may be anything
-    if (S > 1) p.seq[i] = strides[2 * i] * e;
-    if (N > 1) p.row[i] = strides[2 * i + 1] * e;
+    if (S > 1) p.seq[i] = seq[i] * e;
+    if (N > 1) p.row[i] = row[i] * e;
     if (p.seq[i] % 16 || p.row[i] % 16) return ROCO_ERR_INVALID_ARG;
   }
-  p.lens = lens; p.start = start; p.positions = positions; p.start_stride = start_stride;
+  p.lens = call->lens; p.start = call->start; p.positions = call->positions; p.start_stride = call->start_stride;
   p.freq = rotary->freq; p.weight[0] = rotary->q_weight; p.weight[1] = rotary->k_weight; p.axis = rotary->axis;
   p.status = rotary->status;
   p.S = S; p.N = N; p.G = G; p.group = group; p.rot = rotary->rot; p.axes = rotary->axes; p.heads = 1; p.eps = rotary->eps;
-  return launch_norm_rotate(p, dtype, rotary->d, rotary->pairing, device_sms(), static_cast<cudaStream_t>(stream));
+  return launch_norm_rotate(p, call->dtype, rotary->d, rotary->pairing, device_sms(), static_cast<cudaStream_t>(stream));
 }
 
 roco_status roco_rotary_device_status(const roco_rotary *rotary, void *stream, int32_t *flags_host) {
@@ -883,7 +883,7 @@ roco_status roco_tree_verify(const roco_verify *call, void *stream) {
   p.tokens = call->tokens; p.parent = call->parent; p.nodes = call->nodes;
   p.accept_u = call->accept_u; p.sample_u = call->sample_u;
   p.path = call->path; p.path_len = call->path_len; p.next_token = call->next_token; p.status = call->status;
-  p.T = call->T; p.V = call->V; p.A = call->A; p.distinct = call->distinct; p.ranks = 1;
+  p.T = call->T; p.V = call->V; p.A = call->A; p.distinct = call->distinct; p.ranks = 1; p.rank_shift = 0;
   return launch_tree_verify(p, call->dtype, call->S, device_sms(), static_cast<cudaStream_t>(stream));
 }
 

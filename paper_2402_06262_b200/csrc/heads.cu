@@ -12,7 +12,7 @@ namespace roco {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kFlight = 4;  // rows of a thread in flight
+constexpr int kFlight = 4;  // rows of a thread that are fetched together
 
 // position * freq in turns, without its whole turns: the product of two 24-bit numbers (a position has 32 bits at most) is
 // good to 2^-53 of itself in 64 bits, so a position of 2^31 is still off by less than 1e-6 of a turn.
@@ -40,27 +40,32 @@ __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
   return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
 }
 
+// Heads h .. end - 1 of one kind (queries, keys, values) in a CTA's range.
+struct Run {
+  int kind, first, end;  // first: number of the kind's first head
+};
+__device__ __forceinline__ Run run_from(const HeadsParams &p, int h, int last) {
+  const int q_heads = p.G * p.group;
+  Run r;
+  r.kind = h < q_heads ? 0 : h < q_heads + p.G ? 1 : 2;
+  r.first = r.kind == 0 ? 0 : r.kind == 1 ? q_heads : q_heads + p.G;
+  r.end = min(last, r.kind == 0 ? q_heads : r.first + p.G);
+  return r;
+}
+
 template <typename T, int D, bool kAdjacent>
 __global__ void __launch_bounds__(kThreads) norm_rotate_kernel(const HeadsParams p) {
   constexpr int E = Elem<T>::kPerChunk, kLanes = D / E / 2, kRows = kThreads / kLanes;
+  constexpr int kRowBytes = D * (int)sizeof(T);
   const int lane = threadIdx.x % kLanes;
   const unsigned token = blockIdx.x * kRows + threadIdx.x / kLanes;  // (there are fewer than 2^31)
-  int b = 0, n = 0;
-  bool on = token < (unsigned)p.S * (unsigned)p.N;
-  if (on) {
+  int b = 0, n = 0, len = 0;
+  const bool real = token < (unsigned)p.S * (unsigned)p.N;
+  if (real) {
     b = (int)(token / (unsigned)p.N);
     n = (int)(token - (unsigned)b * (unsigned)p.N);
-    if (p.lens) {
-      int len = p.lens[b];
-      if (len < 0 || len > p.N) {
-        if (n == 0 && lane == 0 && blockIdx.y == 0) atomicOr(p.status, ROCO_DEV_BAD_LENS);
-        len = 0;
-      }
-      on = n < len;
-    }
+    len = p.lens ? p.lens[b] : p.N;
   }
-  if (!__syncthreads_or(on)) return;
-
   // where the two pieces lie in the row, and what turns their pairs
   const int half = p.rot / 2 / E;  // pieces in half of the rotated elements
   int at[2];
@@ -75,62 +80,78 @@ __global__ void __launch_bounds__(kThreads) norm_rotate_kernel(const HeadsParams
     at[0] = lane < half ? lane : 2 * half + 2 * (lane - half);
     at[1] = lane < half ? lane + half : at[0] + 1;
   }
-  float c[E], s[E];
-  if (on) {
-    const double start = p.start ? (double)p.start[(long long)b * p.start_stride] : 0.0;
-    const int *pos = p.positions ? p.positions + (long long)token * p.axes : nullptr;
+  float c[E], s[E];  // the frequencies at first
+  int steps[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      c[e] = 1.f;
-      s[e] = 0.f;
-      const int piece = kAdjacent ? 2 * e / E : 0;
-      if (!turn[piece]) continue;
-      const int pair = kAdjacent ? at[piece] * (E / 2) + e % (E / 2) : at[0] * E + e;
-      int axis = p.axis ? p.axis[pair] : 0;
-      if (axis < 0 || axis >= p.axes) {
-        if (token == 0 && blockIdx.y == 0) atomicOr(p.status, ROCO_DEV_BAD_MAP);
-        axis = 0;
-      }
-      angle(start + (double)(pos ? pos[axis] : n), p.freq[pair], c[e], s[e]);
+  for (int e = 0; e < E; ++e) {
+    const int piece = kAdjacent ? 2 * e / E : 0;
+    const int pair = kAdjacent ? at[piece] * (E / 2) + e % (E / 2) : at[0] * E + e;
+    c[e] = real && turn[piece] ? p.freq[pair] : 0.f;
+    int axis = real && turn[piece] && p.axis ? p.axis[pair] : 0;
+    if (axis < 0 || axis >= p.axes) {
+      if (token == 0 && blockIdx.y == 0) atomicOr(p.status, ROCO_DEV_BAD_MAP);
+      axis = 0;
     }
+    steps[e] = !real ? 0 : p.positions ? p.positions[(long long)token * p.axes + axis] : n;
   }
+  const double start = real && p.start ? (double)p.start[(long long)b * p.start_stride] : 0.0;
 
-  const int q_heads = p.G * p.group;
+  const int last = min((int)(blockIdx.y + 1) * p.heads, p.G * (p.group + 2));
   int h = blockIdx.y * p.heads;
-  const int last = min(h + p.heads, q_heads + 2 * p.G);
-  while (h < last) {
-    const int kind = h < q_heads ? 0 : h < q_heads + p.G ? 1 : 2;
-    const int first = kind == 0 ? 0 : kind == 1 ? q_heads : q_heads + p.G;
-    const int end = min(last, kind == 0 ? q_heads : first + p.G);
-    const int per = kind == 0 ? p.group : 1;
-    if (!p.in[kind]) { h = end; continue; }
-    const char *in = p.in[kind] + b * p.seq[kind] + n * p.row[kind];
-    char *out = p.out[kind] + (((long long)b * p.G * p.N + n) * per) * (D * (int)sizeof(T));
-    const float *weight = kind < 2 ? p.weight[kind] : nullptr;
-    float w[2][E];
+  Run run = run_from(p, h, last);
+  uint4 raw[kFlight][2];
+  auto fetch = [&](bool on) {
+    const char *in = p.in[run.kind] + b * p.seq[run.kind] + n * p.row[run.kind] + (long long)(h - run.first) * kRowBytes;
+    on = on && p.in[run.kind];
+#pragma unroll
+    for (int r = 0; r < kFlight; ++r)
+      if (on && h + r < run.end) {
+        const uint4 *src = reinterpret_cast<const uint4 *>(in + r * kRowBytes);
+        raw[r][0] = __ldg(src + at[0]);
+        raw[r][1] = __ldg(src + at[1]);
+      }
+  };
+  // Of a call that is a chain of latencies the first rows are under way before the length is here.
+  if (p.ahead) fetch(real);
+  float w[2][E];
+  auto fetch_weight = [&]() {
+    const float *weight = run.kind < 2 ? p.weight[run.kind] : nullptr;
     if (weight) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) w[i][e] = weight[at[i] * E + e];
+        for (int e = 0; e < E; ++e) w[i][e] = __ldg(weight + at[i] * E + e);
     }
-    for (; h < end; h += kFlight) {
-      uint4 raw[kFlight][2];
+    return weight != nullptr;
+  };
+  bool normed = fetch_weight();
+  if (len < 0 || len > p.N) {
+    if (n == 0 && lane == 0 && blockIdx.y == 0) atomicOr(p.status, ROCO_DEV_BAD_LENS);
+    len = 0;
+  }
+  const bool on = n < len;
+  if (!__syncthreads_or(on)) return;
 #pragma unroll
-      for (int r = 0; r < kFlight; ++r)
-        if (on && h + r < end) {
-          const uint4 *src = reinterpret_cast<const uint4 *>(in + (long long)(h + r - first) * (D * (int)sizeof(T)));
-          raw[r][0] = src[at[0]];
-          raw[r][1] = src[at[1]];
-        }
+  for (int e = 0; e < E; ++e) {
+    s[e] = 0.f;
+    if (turn[kAdjacent ? 2 * e / E : 0]) angle(start + (double)steps[e], c[e], c[e], s[e]);
+  }
+
+  bool here = p.ahead;
+  while (true) {
+    if (!here) fetch(on);
+    here = false;
+    const int per = run.kind == 0 ? p.group : 1;
+    char *out = p.out[run.kind] + (((long long)b * p.G * p.N + n) * per) * kRowBytes;
+    if (p.in[run.kind]) {
 #pragma unroll
       for (int r = 0; r < kFlight; ++r) {
-        if (h + r >= end) break;
-        if (kind < 2) {
+        if (h + r >= run.end) break;
+        if (run.kind < 2) {
           float x[2][E];
           Elem<T>::unpack(raw[r][0], x[0]);
           Elem<T>::unpack(raw[r][1], x[1]);
-          if (weight) {
+          if (normed) {
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) sum = fmaf(x[0][e], x[0][e], fmaf(x[1][e], x[1][e], sum));
@@ -157,14 +178,19 @@ __global__ void __launch_bounds__(kThreads) norm_rotate_kernel(const HeadsParams
           raw[r][1] = pack(x[1]);
         }
         if (on) {
-          const int head = h + r - first, g = head / per, j = head - g * per;
-          uint4 *dst = reinterpret_cast<uint4 *>(out + ((long long)g * p.N * per + j) * (D * (int)sizeof(T)));
+          const int head = h + r - run.first, g = head / per, j = head - g * per;
+          uint4 *dst = reinterpret_cast<uint4 *>(out + ((long long)g * p.N * per + j) * kRowBytes);
           dst[at[0]] = raw[r][0];
           dst[at[1]] = raw[r][1];
         }
       }
     }
-    h = end;
+    h = min(h + kFlight, run.end);
+    if (h >= last) break;
+    if (h == run.end) {
+      run = run_from(p, h, last);
+      normed = fetch_weight();
+    }
   }
 }
 
@@ -174,11 +200,15 @@ roco_status launch_t(HeadsParams p, int pairing, int sms, cudaStream_t stream) {
   const long long tokens = (long long)p.S * p.N;
   const long long tiles = (tokens + kRows - 1) / kRows;
   const int all = p.G * (p.group + 2);
-  // Heads of a CTA: sixteen where there are tokens enough to fill the GPU several times over (eight CTAs per SM), fewer where not.
-  int heads = 16;
-  while (heads > 1 && tiles * ((all + heads - 1) / heads) < 4LL * 8 * sms) heads /= 2;
-  p.heads = heads;
-  const int parts = (all + heads - 1) / heads;
+  // CTAs that share a tile of tokens: enough for four per SM, no more, since each forms the tile's sines and cosines anew (6002 tokens
+  // x 40 heads, fp32, d 64: 20.5 us; for 1 and 16 per SM 26.5 and 22.0).  Above 32 heads a CTA the last wave is the longer (32768
+  // tokens x 96 heads: 240 us, undivided 246; 16 heads 247).
+  long long parts = (4LL * sms + tiles - 1) / tiles;
+  if (parts > all) parts = all;
+  if (parts * 32 < all) parts = (all + 31) / 32;
+  p.heads = (all + (int)parts - 1) / (int)parts;
+  p.ahead = p.heads <= kFlight;
+  parts = (all + p.heads - 1) / p.heads;
   if (tokens > 0x7fffffffLL - kRows || parts > 65535) return ROCO_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)tiles, (unsigned)parts);
   if (pairing == ROCO_PAIR_ADJACENT) norm_rotate_kernel<T, D, true><<<grid, kThreads, 0, stream>>>(p);

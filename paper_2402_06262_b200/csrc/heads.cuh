@@ -18,6 +18,7 @@ struct HeadsParams {
   int *status;
   int S, N, G, group, rot, axes;
   int heads;                      // heads per CTA
+  bool ahead;                     // rows are fetched before the lengths are known
   float eps;
 };
 
@@ -27,7 +28,7 @@ struct VerifyParams {
   const int *tokens, *parent, *nodes;
   const float *accept_u, *sample_u;
   int *path, *path_len, *next_token, *status;
-  int T, V, A, distinct, ranks;   // ranks: CTAs that share a sequence
+  int T, V, A, distinct, ranks, rank_shift;  // ranks = 1 << rank_shift: CTAs that share a sequence
 };
 
 struct ReorderParams {

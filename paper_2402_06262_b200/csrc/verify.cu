@@ -14,21 +14,29 @@
 namespace roco {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxRanks = 8;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kResident = 3;  // (CTAs per SM)
+constexpr int kWarpShift = 3, kMaxRanks = 8, kRuns = kMaxRanks * kWarps, kPer = kRuns / 32;
+constexpr int kOneWarp = 256;  // chunks that one warp searches
+static_assert(kWarps == 1 << kWarpShift, "runs are divided by shifts");
 constexpr int kNodes = ROCO_TREE_MAX_NODES;
 static_assert(kNodes == 64, "a node's children are the bits of one 64-bit word");
 
 struct Smem {
   double p[kNodes], q[kNodes], u[kNodes];
   unsigned long long children[kNodes + 1];  // of the prefix, then of every node
-  double warp_sum[kWarps];
-  double rank_sum[2][kMaxRanks];            // written by all ranks, one set while the other may still be read
+  double sums[2][kRuns];                    // of every warp of every rank; one set while the other may still be read
+  double part[kWarps];
+  uint64_t bar[2];                          // completes when a set is here
+  unsigned first[2];                        // bits of the nodes that are accepted where no sibling was rejected before
   int token[kNodes];
   int gone[kNodes];                         // tokens rejected behind the node the walk stands on
-  int n_gone, path_len, path[ROCO_TREE_MAX_PATH];
-  int tip, more;                            // what the next pass is for
-  double C;
+  int path[ROCO_TREE_MAX_PATH];
+  // where the walk stands: node, nodes on the path, children of it that are not tried yet, tokens in gone
+  int tip, len, n_gone;
+  unsigned long long untried;
+  double C, R, M;
+  int more;                                 // R is to be summed before the walk goes on
+  int abort_flag;
 };
 
 __device__ __forceinline__ double warp_sum64(double v) {
@@ -46,6 +54,7 @@ struct Rows {
   int lead, V, chunks;
   bool q_like_p;    // the draft's row has the same alignment
 
+  __device__ Rows() {}
   __device__ Rows(const char *target, const char *draft, int v) : p(reinterpret_cast<const T *>(target)), q(reinterpret_cast<const T *>(draft)), V(v) {
     lead = (int)((reinterpret_cast<uintptr_t>(target) & 15u) / sizeof(T));
     chunks = (int)(((long long)V + lead + E - 1) / E);
@@ -57,27 +66,22 @@ struct Rows {
     for (int e = 0; e < E; ++e) f[e] = first + e >= 0 && first + e < V ? Elem<T>::load(row + first + e) : 0.f;
   }
 
-  // The probabilities of chunk i; elements outside the row are 0.
-  __device__ __forceinline__ void load(int i, float (&fp)[E], float (&fq)[E]) const {
+  // What is left of p in chunk i; 0 outside the row.  A NaN stays one.
+  __device__ __forceinline__ void left(int i, double C, const int *gone, int n_gone, double (&r)[E]) const {
     const int first = i * E - lead;
     const bool whole = first >= 0 && first + E <= V;
+    float fp[E], fq[E];
     if (whole) Elem<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(p + first)), fp);
     else some(p, first, fp);
     if (q) {
       if (whole && q_like_p) Elem<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(q + first)), fq);
       else some(q, first, fq);
     }
-  }
-
-  // What is left of p in them.  A NaN stays one.
-  __device__ __forceinline__ void left(int i, const float (&fp)[E], const float (&fq)[E], double C, const int *gone, int n_gone,
-                                       double (&r)[E]) const {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const double x = q ? (double)fp[e] - C * (double)fq[e] : (double)fp[e];
+      const double x = q ? fma(-C, (double)fq[e], (double)fp[e]) : (double)fp[e];
       r[e] = x <= 0.0 ? 0.0 : x;
     }
-    const int first = i * E - lead;
     for (int g = 0; g < n_gone; ++g) {
       const int e = gone[g] - first;
       if (e >= 0 && e < E) {
@@ -89,106 +93,227 @@ struct Rows {
   }
 };
 
-// Which of n runs holds the place `target` of the running sum that starts at `base`; the last one with any mass where roundings
-// leave the place behind the end.  base becomes the sum before the run; -1 where nothing has mass.
-__device__ __forceinline__ int pick_run(const double *sums, int n, double target, double &base) {
-  int at = -1;
-  double before = base, sum = base;
-  for (int i = 0; i < n; ++i) {
-    if (sums[i] > 0.0) {
-      at = i;
-      before = sum;
-      if (sum + sums[i] > target) break;
+// Conversions and comparisons in 64 bits are issued at an eighth to a quarter of the rate of its sums and products (16 and 21 of 62
+// per cycle and SM, measured), so where all numbers are positive and normal (bits from kLeastNormal on, kNormals of them) both are
+// done on the bits.
+constexpr uint32_t kLeastNormal = 0x00800000u, kNormals = 0x7f000000u;
+__device__ __forceinline__ double widen(float x) {
+  const uint32_t bits = __float_as_uint(x);
+  return __hiloint2double((int)((bits >> 3) + ((1023u - 127u) << 20)), (int)(bits << 29));
+}
+__device__ __forceinline__ double positive(double x) {  // max(x, 0) of a number
+  const int hi = __double2hiint(x), keep = ~(hi >> 31);
+  return __hiloint2double(hi & keep, __double2loint(x) & keep);
+}
+
+// A lane's part of the sum of what is left of p over chunks lo .. hi - 1 of a warp (chunks lane, lane + 32, ... of the run).  A row
+// is read at the pace of loads in flight, so kBatch chunks are fetched before any is worked on.
+template <typename T, bool kDraft>
+__device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end, double C) {
+  constexpr int E = Rows<T>::E, kBatch = 16 / E;
+  const uint4 *p = reinterpret_cast<const uint4 *>(rows.p - rows.lead), *q = reinterpret_cast<const uint4 *>(rows.q - rows.lead);
+  double sum = 0.0;
+  for (; i < end; i += 32 * kBatch) {
+    uint4 a[kBatch], b[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      a[k] = b[k] = make_uint4(0, 0, 0, 0);
+      if (i + 32 * k < end) {
+        a[k] = __ldg(p + i + 32 * k);
+        if (kDraft) b[k] = __ldg(q + i + 32 * k);
+      }
     }
-    sum += sums[i];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      float fp[E], fq[E];
+      Elem<T>::unpack(a[k], fp);
+      if (kDraft) Elem<T>::unpack(b[k], fq);
+      uint32_t most = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        most = max(most, __float_as_uint(fp[e]) - kLeastNormal);
+        if (kDraft) most = max(most, __float_as_uint(fq[e]) - kLeastNormal);
+      }
+      if (most < kNormals) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum += kDraft ? positive(fma(-C, widen(fq[e]), widen(fp[e]))) : widen(fp[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const double x = kDraft ? fma(-C, (double)fq[e], (double)fp[e]) : (double)fp[e];
+          sum += x <= 0.0 ? 0.0 : x;
+        }
+      }
+    }
   }
-  base = before;
+  return sum;
+}
+
+// One chunk's sum, whatever it holds and wherever it lies.
+template <typename T>
+__device__ __forceinline__ double sum_chunk(const Rows<T> &rows, int i, double C, const int *gone, int n_gone) {
+  double r[Rows<T>::E], sum = 0.0;
+  rows.left(i, C, gone, n_gone, r);
+#pragma unroll
+  for (int e = 0; e < Rows<T>::E; ++e) sum += r[e];
+  return sum;
+}
+
+template <typename T>
+__device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, double C, const int *gone, int n_gone) {
+  constexpr int E = Rows<T>::E;
+  const int lane = threadIdx.x & 31, full = (rows.V + rows.lead) / E;
+  int i = lo + lane;
+  double sum = 0.0;
+  bool plain = !rows.q || rows.q_like_p;
+  for (int g = 0; g < n_gone; ++g) {  // a rejected token in this run
+    const int at = gone[g] + rows.lead;
+    plain = plain && !(at >= lo * E && at < hi * E);
+  }
+  // the row's first and last chunk may reach beyond it
+  const bool head = plain && rows.lead && lo == 0 && hi > 0, tail = plain && full < rows.chunks && full >= lo && full < hi && (full > 0 || !head);
+  if (head && lane == 0) i += 32;
+  if (plain) sum = rows.q ? sum_whole<T, true>(rows, i, min(hi, full), C) : sum_whole<T, false>(rows, i, min(hi, full), C);
+  // what is left for one chunk at a time
+  int from = plain ? hi : lo + lane, step = 32;
+  if (lane == 0 && (head || tail)) {
+    from = head ? 0 : full;
+    step = head && tail ? full : hi;
+  }
+  for (; from < hi; from += step) sum += sum_chunk(rows, from, C, gone, n_gone);
+  return warp_sum64(sum);
+}
+
+// Which of n <= 32 runs (one per lane: its sum, from 0 on) holds the place `target` of the running sum that starts at `base`; the last
+// one with any mass where roundings leave the place behind the end.  base becomes the sum before it; -1 where nothing has mass.
+__device__ __forceinline__ int pick_run(double sum, double target, double &base) {
+  const int lane = threadIdx.x & 31;
+  double upto = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const double y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && base + upto > target);
+  const unsigned some = __ballot_sync(0xffffffffu, sum > 0.0);
+  if (!some) return -1;
+  const int at = over ? __ffs((int)over) - 1 : 31 - __clz((int)some);
+  const double before = __shfl_sync(0xffffffffu, upto, at > 0 ? at - 1 : 0);
+  if (at > 0) base += before;
   return at;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) tree_verify_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const VerifyParams p) {
   constexpr int E = Elem<T>::kPerChunk;
   __shared__ Smem sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int ranks = p.ranks, b = blockIdx.x / ranks, rank = blockIdx.x - b * ranks;
+  const int ranks = p.ranks, b = blockIdx.x >> p.rank_shift, rank = blockIdx.x & (ranks - 1);
   const bool rooted = p.target_prefix == nullptr;
   const char *target = p.target + b * p.target_seq;
   const char *draft = p.draft ? p.draft + b * p.draft_seq : nullptr;
   const char *target_prefix = rooted ? nullptr : p.target_prefix + b * p.target_prefix_seq;
   const char *draft_prefix = rooted || !draft ? nullptr : p.draft_prefix + b * p.draft_prefix_seq;
 
-  int nodes = p.nodes ? p.nodes[b] : p.T;
+  int nodes = p.nodes ? p.nodes[b] : p.T, up = -1, x = 0;
+  float u = 0.f;
+  if (tid < p.T) {
+    up = p.parent[b * p.T + tid];
+    x = p.tokens[b * p.T + tid];
+    u = p.accept_u[b * p.T + tid];
+  }
   if (nodes < 0 || nodes > p.T) {
     if (tid == 0 && rank == 0) atomicOr(p.status, ROCO_DEV_BAD_TREE);
     nodes = 0;
   }
   if (tid <= kNodes) sm.children[tid] = 0;
+  if (tid == 0) {
+    sm.abort_flag = 0;
+    mbar_init(&sm.bar[0], 1);
+    mbar_init(&sm.bar[1], 1);
+    mbar_init_fence();
+  }
   __syncthreads();
-  if (tid < nodes) {
-    const int up = p.parent[b * p.T + tid], x = p.tokens[b * p.T + tid];
-    const bool given = rooted && tid == 0;  // the token sampled last: nothing is looked up for it
-    const bool ok = up >= -1 && up < tid && (given || (x >= 0 && x < p.V));
-    if (!ok && rank == 0) atomicOr(p.status, ROCO_DEV_BAD_TREE);
-    if (ok && (given || up >= 0 || !rooted)) {
-      if (!given) {
-        const char *row = up < 0 ? target_prefix : target + up * p.target_row;
-        sm.p[tid] = Elem<T>::load(reinterpret_cast<const T *>(row) + x);
-        if (draft) {
-          row = up < 0 ? draft_prefix : draft + up * p.draft_row;
-          sm.q[tid] = Elem<T>::load(reinterpret_cast<const T *>(row) + x);
+  if (tid < kNodes) {
+    bool first = false;  // accepted if none of its siblings was rejected before it
+    if (tid < nodes) {
+      const bool given = rooted && tid == 0;  // the token sampled last: nothing is looked up for it
+      const bool ok = up >= -1 && up < tid && (given || (x >= 0 && x < p.V));
+      if (!ok && rank == 0) atomicOr(p.status, ROCO_DEV_BAD_TREE);
+      if (ok && (given || up >= 0 || !rooted)) {
+        if (!given) {
+          const char *row = up < 0 ? target_prefix : target + up * p.target_row;
+          const double px = Elem<T>::load(reinterpret_cast<const T *>(row) + x);
+          double qx = 1.0;
+          if (draft) {
+            row = up < 0 ? draft_prefix : draft + up * p.draft_row;
+            qx = Elem<T>::load(reinterpret_cast<const T *>(row) + x);
+          }
+          sm.p[tid] = px;
+          sm.q[tid] = qx;
+          sm.u[tid] = u;
+          first = u * qx < px;
         }
-        sm.u[tid] = p.accept_u[b * p.T + tid];
+        sm.token[tid] = x;
+        atomicOr(&sm.children[up + 1], 1ull << tid);
       }
-      sm.token[tid] = x;
-      atomicOr(&sm.children[up + 1], 1ull << tid);
     }
+    const unsigned accepted = __ballot_sync(0xffffffffu, first);
+    if (lane == 0) sm.first[warp] = accepted;
   }
   __syncthreads();
 
-  // The walk; thread 0 keeps it (every rank on its own, with the same numbers).
-  int tip = -1, len = 0, n_gone = 0;
-  double C = 0.0, R = 1.0, M = 1.0;
-  unsigned long long untried = sm.children[0];
-  if (rooted) {
-    if (!(untried & 1)) {  // no root: nothing to verify, nothing to draw from.  (Uniform, and before any exchange.)
-      if (rank == 0) {
-        if (tid < p.A) p.path[b * p.A + tid] = -1;
-        if (tid == 0) {
-          p.path_len[b] = 0;
-          p.next_token[b] = -1;
-        }
+  // The walk is thread 0's (every rank's on its own, with the same numbers).
+  if (rooted && !(sm.children[0] & 1)) {  // no root: nothing to verify, nothing to draw from (before any exchange)
+    if (rank == 0) {
+      if (tid < p.A) p.path[b * p.A + tid] = -1;
+      if (tid == 0) {
+        p.path_len[b] = 0;
+        p.next_token[b] = -1;
       }
-      return;
     }
-    if (tid == 0) sm.path[0] = 0;
-    tip = 0;
-    len = 1;
-    untried = sm.children[1];
+    return;
   }
-  // (a peer's shared memory may be written once the peer runs)
+  if (tid == 0) {
+    sm.path[0] = 0;
+    sm.tip = rooted ? 0 : -1;
+    sm.len = rooted ? 1 : 0;
+    sm.untried = sm.children[rooted ? 1 : 0];
+    sm.n_gone = 0;
+    sm.C = 0.0; sm.R = 1.0; sm.M = 1.0;
+  }
+  // (a peer's shared memory may be written once the peer runs and its barriers are ready)
   if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  bool met = ranks == 1;
   bool anew = false;   // nothing was left of p after the rejections: once more with p itself
-  double total = 0.0, base = 0.0;
-  int parity = 0;
+  double total = 0.0, base = 0.0, mine[kPer];
+  int pass = 0, out = 0, run = 0;   // out: tokens that are out of p
+  double c = 0.0;
+  Rows<T> rows;
+  int first = 0, end = 0;      // the chunks that hold the next token, once the sums are known
+  double place = 0.0;
   while (true) {
-    if (tid == 0 && !anew) {
-      bool rejected = false;
-      while (!rejected && len < p.A && untried) {
+    if (tid == 0 && !anew && end == 0) {
+      const unsigned long long firsts = sm.first[0] | (unsigned long long)sm.first[1] << 32;
+      unsigned long long untried = sm.untried;
+      int tip = sm.tip, len = sm.len, n_gone = sm.n_gone;
+      double C = sm.C, R = sm.R, M = sm.M;
+      bool more = false;
+      while (!more && len < p.A && untried) {
         const int i = __ffsll((long long)untried) - 1, x = sm.token[i];
         untried &= untried - 1;
-        const double u = sm.u[i];
         bool again = false;   // rejected already
         for (int g = 0; g < n_gone; ++g) again |= sm.gone[g] == x;
         bool yes;
         double q = 0.0;
-        if (draft) {
+        if (n_gone == 0) {
+          yes = firsts >> i & 1;
+          q = sm.q[i];
+        } else if (draft) {
           q = again && p.distinct ? 0.0 : sm.q[i];
-          const double x_left = sm.p[i] - C * sm.q[i];
-          yes = u * q * R < (x_left <= 0.0 ? 0.0 : x_left) * M;
+          const double left = sm.p[i] - C * sm.q[i];
+          yes = sm.u[i] * q * R < (left <= 0.0 ? 0.0 : left) * M;
         } else {
-          yes = u * R < (again ? 0.0 : sm.p[i]);
+          yes = sm.u[i] * R < (again ? 0.0 : sm.p[i]);
         }
         if (yes) {
           sm.path[len++] = i;
@@ -197,161 +322,135 @@ __global__ void __launch_bounds__(kThreads) tree_verify_kernel(const VerifyParam
           C = 0.0; R = 1.0; M = 1.0;
           n_gone = 0;
         } else {
-          rejected = true;
           sm.gone[n_gone++] = x;
-          if (draft && M > 0.0) C += R / M;
-          if (p.distinct) M -= q;
-        }
-      }
-      sm.tip = tip;
-      sm.C = C;
-      sm.n_gone = n_gone;
-      sm.path_len = len;
-      sm.more = rejected && len < p.A && untried;   // a sibling is left to try
-    }
-    __syncthreads();
-    const int at = sm.tip;
-    const double c = anew ? 0.0 : sm.C;
-    const int out = draft || anew ? 0 : sm.n_gone;
-    const Rows<T> rows(at < 0 ? target_prefix : target + at * p.target_row,
-                       c == 0.0 || !draft ? nullptr : at < 0 ? draft_prefix : draft + at * p.draft_row, p.V);
-    // runs of chunks: of this rank, of this warp in it
-    const int run = (rows.chunks + ranks * kWarps - 1) / (ranks * kWarps);
-    const int lo = min((rank * kWarps + warp) * run, rows.chunks), hi = min(lo + run, rows.chunks);
-    double sum = 0.0;
-#pragma unroll 4
-    for (int i = lo + lane; i < hi; i += 32) {
-      float fp[E], fq[E];
-      double r[E];
-      rows.load(i, fp, fq);
-      rows.left(i, fp, fq, c, sm.gone, out, r);
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum += r[e];
-    }
-    sum = warp_sum64(sum);
-    if (lane == 0) sm.warp_sum[warp] = sum;
-    __syncthreads();
-    double mine = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) mine += sm.warp_sum[w];
-    if (!met) {
-      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-      met = true;
-    }
-    if (ranks > 1) {
-      if (tid < ranks) {
-        const uint32_t dst = map_to_rank(&sm.rank_sum[parity][rank], tid);
-        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(dst), "d"(mine) : "memory");
-      }
-      cluster_sync_all();
-    } else {
-      if (tid == 0) sm.rank_sum[parity][0] = mine;
-      __syncthreads();
-    }
-    total = 0.0;
-    for (int k = 0; k < ranks; ++k) total += sm.rank_sum[parity][k];
-    R = total;
-    if (!anew && sm.more) {
-      parity ^= 1;
-      __syncthreads();   // (what thread 0 writes next has been read)
-      continue;
-    }
-    // the last pass, unless nothing is left
-    if (!(total > 0.0) && total == 0.0 && !anew && (sm.C != 0.0 || sm.n_gone > 0)) {
-      anew = true;
-      parity ^= 1;
-      __syncthreads();
-      continue;
-    }
-    if (rank == 0) {
-      if (tid < p.A) p.path[b * p.A + tid] = tid < sm.path_len ? sm.path[tid] : -1;
-      if (tid == 0) p.path_len[b] = sm.path_len;
-    }
-    if (!(total > 0.0) || isinf(total)) {   // no distribution to draw from
-      if (rank == 0 && tid == 0) {
-        p.next_token[b] = -1;
-        atomicOr(p.status, ROCO_DEV_BAD_PROBS);
-      }
-      return;
-    }
-    // the pick: rank, then warp, then chunk by chunk with one warp
-    const double place = (double)p.sample_u[b] * total;
-    base = 0.0;
-    if (pick_run(sm.rank_sum[parity], ranks, place, base) != rank) return;
-    const int w = pick_run(sm.warp_sum, kWarps, place, base);
-    int first = min((rank * kWarps + w) * run, rows.chunks), end = min(first + run, rows.chunks);
-    __syncthreads();   // (warp_sum has been read)
-    // A run of more than eight times 32 chunks is cut among the warps once more.
-    while (end - first > 256) {
-      const int sub = (end - first + kWarps - 1) / kWarps;
-      const int l = min(first + warp * sub, end), h = min(l + sub, end);
-      sum = 0.0;
-      for (int i = l + lane; i < h; i += 32) {
-        float fp[E], fq[E];
-        double r[E];
-        rows.load(i, fp, fq);
-        rows.left(i, fp, fq, c, sm.gone, out, r);
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum += r[e];
-      }
-      sum = warp_sum64(sum);
-      if (lane == 0) sm.warp_sum[warp] = sum;
-      __syncthreads();
-      const int k = pick_run(sm.warp_sum, kWarps, place, base);
-      first = min(first + k * sub, end);
-      end = min(first + sub, end);
-      __syncthreads();
-    }
-    if (warp != 0) return;
-    int answer = -1;
-    for (int i0 = first; i0 < end; i0 += 32) {
-      const int i = i0 + lane;
-      float fp[E], fq[E];
-      double r[E], own = 0.0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) r[e] = 0.0;
-      if (i < end) {
-        rows.load(i, fp, fq);
-        rows.left(i, fp, fq, c, sm.gone, out, r);
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) own += r[e];
-      double upto = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const double y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
-      }
-      const unsigned over = __ballot_sync(0xffffffffu, own > 0.0 && base + upto > place);
-      const unsigned some = __ballot_sync(0xffffffffu, own > 0.0);
-      const int who = over ? __ffs(over) - 1 : some ? 31 - __clz(some) : -1;
-      if (lane == who) {
-        double sums = base + (upto - own);
-        for (int e = 0; e < E; ++e) {
-          if (r[e] > 0.0) {
-            answer = i * E - rows.lead + e;
-            if (sums + r[e] > place) break;
+          if (draft) {
+            if (M > 0.0) C += M == 1.0 ? R : R / M;
+            if (p.distinct) M -= q;
+            more = untried != 0;
+          } else if (n_gone == 1) {
+            more = untried != 0;
+          } else if (!again && sm.p[i] > 0.0) {
+            R -= sm.p[i];   // (the first sum went without its token)
           }
-          sums += r[e];
         }
       }
-      const int found = __shfl_sync(0xffffffffu, answer, who < 0 ? 0 : who);
-      if (who >= 0) answer = found;
-      if (over) break;
-      base += __shfl_sync(0xffffffffu, upto, 31);
+      sm.untried = untried;
+      sm.tip = tip;
+      sm.len = len;
+      sm.n_gone = n_gone;
+      sm.C = C;
+      sm.R = R;
+      sm.M = M;
+      sm.more = more;
     }
-    if (lane == 0) p.next_token[b] = answer;
-    return;
+    __syncthreads();
+    int lo, hi;
+    if (end == 0) {
+      const int on = sm.tip;
+      c = anew ? 0.0 : sm.C;
+      out = draft || anew ? 0 : sm.n_gone;
+      rows = Rows<T>(on < 0 ? target_prefix : target + on * p.target_row,
+                     c == 0.0 || !draft ? nullptr : on < 0 ? draft_prefix : draft + on * p.draft_row, p.V);
+      // runs of chunks: of this rank, of this warp in it
+      run = (rows.chunks + (kWarps << p.rank_shift) - 1) >> (kWarpShift + p.rank_shift);
+      lo = min((rank * kWarps + warp) * run, rows.chunks);
+      hi = min(lo + run, rows.chunks);
+    } else {  // a long run is cut among the warps once more
+      run = (end - first + kWarps - 1) >> kWarpShift;
+      lo = min(first + warp * run, end);
+      hi = min(lo + run, end);
+    }
+    const double sum = sum_run(rows, lo, hi, c, sm.gone, out);
+    if (end != 0) {
+      if (lane == 0) sm.part[warp] = sum;
+      __syncthreads();
+      const int at = pick_run(lane < kWarps ? sm.part[lane] : 0.0, place, base);
+      first = min(first + at * run, end);
+      end = min(first + run, end);
+      if (end - first <= kOneWarp) break;
+      continue;
+    }
+    double *sums = sm.sums[pass & 1];
+    if (ranks > 1) {
+      // every warp sends its sum to every rank; the store and the signal that it is there travel together
+      if (pass == 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+      uint64_t *bar = &sm.bar[pass & 1];
+      if (tid == 0) mbar_expect_tx(bar, ranks * kWarps * 8);
+      if (lane < ranks)
+        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
+                         map_to_rank(&sums[rank * kWarps + warp], lane)),
+                     "l"(__double_as_longlong(sum)), "r"(map_to_rank(bar, lane))
+                     : "memory");
+      mbar_wait_compact(bar, (pass >> 1) & 1, &sm.abort_flag, p.status);
+    } else {
+      if (lane == 0) sums[warp] = sum;
+      __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) mine[k] = kPer * lane + k < ranks * kWarps ? sums[kPer * lane + k] : 0.0;
+    double some = mine[0];
+#pragma unroll
+    for (int k = 1; k < kPer; ++k) some += mine[k];
+    total = warp_sum64(some);
+    if (tid == 0) sm.R = total;
+    ++pass;
+    // on with the walk, or once more where nothing is left
+    const bool more = sm.more;
+    if (!anew && !more && total == 0.0 && (sm.C != 0.0 || sm.n_gone > 0)) anew = true;
+    else if (anew || !more) {
+      if (rank == 0) {
+        if (tid < p.A) p.path[b * p.A + tid] = tid < sm.len ? sm.path[tid] : -1;
+        if (tid == 0) p.path_len[b] = sm.len;
+      }
+      if (!(total > 0.0) || isinf(total)) {   // no distribution to draw from
+        if (rank == 0 && tid == 0) {
+          p.next_token[b] = -1;
+          atomicOr(p.status, ROCO_DEV_BAD_PROBS);
+        }
+        return;
+      }
+      // the pick descends the sums: a few warps, one of them, 32 chunks or a few times that, one chunk, one element
+      place = (double)p.sample_u[b] * total;
+      int at = pick_run(some, place, base);
+      double x = 0.0;
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        const double y = __shfl_sync(0xffffffffu, mine[k], at);
+        if (lane == k) x = y;
+      }
+      at = kPer * at + pick_run(x, place, base);
+      if (at / kWarps != rank) return;
+      first = min(at * run, rows.chunks);
+      end = min(first + run, rows.chunks);
+      if (end - first <= kOneWarp) break;
+    }
+    __syncthreads();   // (what is written next has been read)
   }
+  if (warp != 0) return;
+  while (end - first > 1) {
+    const int per = (end - first + 31) / 32, l = min(first + lane * per, end), h = min(l + per, end);
+    double part = 0.0;
+    for (int i = l; i < h; ++i) part += sum_chunk(rows, i, c, sm.gone, out);
+    first = min(first + pick_run(part, place, base) * per, end - 1);
+    end = min(first + per, end);
+  }
+  double r[E], element = 0.0;
+  rows.left(first, c, sm.gone, out, r);
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (lane == e) element = r[e];
+  const int e = pick_run(element, place, base);
+  if (lane == 0) p.next_token[b] = first * E - rows.lead + e;
 }
 
 template <typename T>
 roco_status launch_t(VerifyParams p, int S, int sms, cudaStream_t stream) {
-  // CTAs per sequence: as many as are resident together (two per SM), none with fewer than a chunk for every thread.
+  // CTAs per sequence: eight, or fewer where so many would be more than reside together; none with fewer chunks than threads.
   int ranks = 1;
   const long long chunks = (p.V + Elem<T>::kPerChunk - 1) / Elem<T>::kPerChunk;
-  while (ranks < kMaxRanks && 2LL * S * ranks <= 2LL * sms && chunks >= 2LL * ranks * kThreads) ranks *= 2;
+  while (ranks < kMaxRanks && 4LL * S * ranks < 3LL * kResident * sms && chunks >= 2LL * ranks * kThreads) ranks *= 2;
   p.ranks = ranks;
+  p.rank_shift = ranks == 1 ? 0 : ranks == 2 ? 1 : ranks == 4 ? 2 : 3;
   const bool ok = launch_cluster(tree_verify_kernel<T>, (unsigned)S * (unsigned)ranks, (unsigned)ranks, kThreads, 0, stream, p);
   return ok ? ROCO_OK : ROCO_ERR_CUDA;
 }

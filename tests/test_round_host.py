@@ -22,16 +22,18 @@ def rotary(**kw):
     return R.roco_rotary(*v.values())
 
 
-def rotate(r, dtype=R.ROCO_BF16, S=2, N=3, G=4, group=1, q=0x10000, k=0x20000, v=0x30000, strides=(512,) * 6, Q=0x40000, K=0x50000, V=0x60000):
-    return R.lib().roco_norm_rotate(r if r is None else C.byref(r), dtype, S, N, G, group, q, k, v,
-                                    None if strides is None else C.byref((C.c_int64 * 6)(*strides)), None, None, 0, None, Q, K, V, None)
+def rotate(r, **kw):
+    v = dict(dtype=R.ROCO_BF16, S=2, N=3, G=4, group=1, start_stride=0, q=0x10000, k=0x20000, v=0x30000, q_seq=512, q_row=512, k_seq=512,
+             k_row=512, v_seq=512, v_row=512, lens=None, start=None, positions=None, Q=0x40000, K=0x50000, V=0x60000)
+    v.update(kw)
+    return R.lib().roco_norm_rotate(r if r is None else C.byref(r), bytes(R.roco_heads(*v.values())), None)
 
 
 def test_norm_rotate_refuses_on_the_host():
     assert rotate(None) == INVALID and rotate(rotary(status=None)) == INVALID
-    for kw in (dict(q=None), dict(Q=None), dict(k=None), dict(K=None), dict(v=None), dict(V=None), dict(strides=None), dict(S=0),
-               dict(N=0), dict(G=0), dict(group=0), dict(q=0x10008), dict(Q=0x40008), dict(V=0x60004), dict(strides=(512, 4) + (512,) * 4),
-               dict(strides=(512, 512, 4, 512, 512, 512))):
+    assert R.lib().roco_norm_rotate(C.byref(rotary()), None, None) == INVALID
+    for kw in (dict(q=None), dict(Q=None), dict(k=None), dict(K=None), dict(v=None), dict(V=None), dict(S=0), dict(N=0), dict(G=0),
+               dict(group=0), dict(q=0x10008), dict(Q=0x40008), dict(V=0x60004), dict(q_row=4), dict(k_seq=4), dict(v_row=1)):
         assert rotate(rotary(), **kw) == INVALID, kw
     for kw in (dict(freq=None), dict(axes=0), dict(pairing=2), dict(rot=-16), dict(rot=144)):
         assert rotate(rotary(**kw)) == INVALID, kw
@@ -46,7 +48,7 @@ def verify(**kw):
              target_seq=400, target_row=100, draft_seq=400, draft_row=100, target_prefix_seq=100, draft_prefix_seq=100, tokens=0x5000,
              parent=0x6000, nodes=None, accept_u=0x7000, sample_u=0x8000, path=0x9000, path_len=0xa000, next_token=0xb000, status=0xc000)
     v.update(kw)
-    return R.lib().roco_tree_verify(C.byref(R.roco_verify(*v.values())), None)
+    return R.lib().roco_tree_verify(bytes(R.roco_verify(*v.values())), None)
 
 
 def test_tree_verify_refuses_on_the_host():
