@@ -1,10 +1,14 @@
 // Sequences of a cache or of linear states forked, reordered, compacted, freed.
 //
-// A copy, bound by the bytes that move: every source read once, every destination written once.  The work is cut by columns, 16 bytes
-// at one place of a unit, which a thread handles for all sequences: it fetches the column of every distinct source into its own part
-// of shared memory (asynchronous 16-byte copies), then writes it to every destination.  So a source that feeds many sequences is
-// read once, and in place any map is right (cycles, forks, chains): a column is written only after all of it has been read, and
-// nobody else touches it.  Threads share nothing but the map, so nobody waits for anybody.
+// A copy, bound by the bytes that move: every source read once, every destination written once.
+//
+// Into another cache a CTA copies a part of one unit, eight 16-byte pieces of a thread in flight; the destinations of one source are
+// neighbours in the grid, so that it is read from HBM once.
+//
+// In place the work is cut by columns, 16 bytes at one place of a unit, which a thread handles for all sequences: it fetches the
+// column of every distinct source into its own part of shared memory (asynchronous 16-byte copies), then writes it to every
+// destination.  So any map is right (cycles, forks, chains): a column is written only after all of it has been read, and nobody else
+// touches it.  Threads share nothing but the map, so nobody waits for anybody.
 #include "heads.cuh"
 
 namespace roco {
@@ -39,20 +43,74 @@ __device__ __forceinline__ int source_of(const ReorderParams &p, int b, bool rep
   return ROCO_REORDER_KEEP;
 }
 
+constexpr int kCopyThreads = 256, kCopyFlight = 8;
+
+// Part of one unit into another cache, or other states.
+__global__ void __launch_bounds__(kCopyThreads) reorder_copy_kernel(const ReorderParams p) {
+  const int b = blockIdx.x % p.S_dst, rest = blockIdx.x / p.S_dst, g = rest / p.parts, part = rest - g * p.parts;
+  const bool cache = p.arrays == 2;
+  const int a = source_of(p, b, rest == 0);
+  if (a == ROCO_REORDER_KEEP) return;
+  const long long to = (long long)b * p.G + g, from = (long long)a * p.G + g;
+  int live = 0;
+  if (cache && a >= 0) {
+    live = p.src_live[from];
+    if (live < 0 || live > p.B_src) {
+      if (part == 0 && threadIdx.x == 0) atomicOr(p.status, ROCO_DEV_BAD_LIVE);
+      return;
+    }
+  }
+  const int chunks = a < 0 && cache ? 0 : cache ? live << p.row_shift : (int)(p.src_unit / 16);
+  constexpr int kTile = kCopyThreads * kCopyFlight;
+  const int tiles = (chunks + kTile - 1) / kTile;
+  for (int t = part; t < p.arrays * tiles; t += p.parts) {
+    const int array = t >= tiles, c0 = (t - array * tiles) * kTile + threadIdx.x;
+    const uint4 *src = reinterpret_cast<const uint4 *>(p.src[array] + from * p.src_unit);
+    uint4 *dst = reinterpret_cast<uint4 *>(p.dst[array] + to * p.dst_unit);
+    uint4 x[kCopyFlight];
+#pragma unroll
+    for (int u = 0; u < kCopyFlight; ++u) {
+      const int c = c0 + u * kCopyThreads;
+      x[u] = make_uint4(0, 0, 0, 0);   // (what a freed sequence's states become)
+      if (a >= 0 && c < chunks) x[u] = __ldg(src + c);
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyFlight; ++u) {
+      const int c = c0 + u * kCopyThreads;
+      if (c < chunks) dst[c] = x[u];
+    }
+  }
+  if (!cache) return;
+  for (int k = part * kCopyThreads + threadIdx.x; k < p.B_dst; k += p.parts * kCopyThreads) {
+    const long long i = from * p.B_src + k, o = to * p.B_dst + k;
+    if (k < live) {
+      const float s = p.src_s[i], q = p.src_q[i];
+      const int n = p.src_n[i], pos = p.src_pos[i];
+      p.dst_s[o] = s; p.dst_q[o] = q; p.dst_n[o] = n; p.dst_pos[o] = pos;
+    } else {
+      p.dst_pos[o] = -1;
+    }
+  }
+  if (part == 0 && threadIdx.x == 0) {
+    p.dst_live[to] = live;
+    p.dst_t_next[to] = a < 0 ? 0 : p.src_t_next[from];
+  }
+}
+
 __global__ void reorder_kernel(const ReorderParams p) {
   extern __shared__ uint4 room[];
   __shared__ Lists ls;
   const int tid = threadIdx.x, threads = blockDim.x;
   const int g = blockIdx.x / p.parts, part = blockIdx.x - g * p.parts;
-  const int b0 = blockIdx.y * kMost, nb = min(kMost, p.S_dst - b0);
+  const int nb = p.S_dst;
   const bool cache = p.arrays == 2;
 
-  for (int i = tid; i < nb; i += threads) ls.map[i] = source_of(p, b0 + i, blockIdx.x == 0);
+  for (int i = tid; i < nb; i += threads) ls.map[i] = source_of(p, i, blockIdx.x == 0);
   if (tid == 0) ls.n_slots = ls.n_copies = ls.n_empty = ls.max_live = 0;
   __syncthreads();
   for (int i = tid; i < nb; i += threads) {
     const int a = ls.map[i];
-    if (a == ROCO_REORDER_FREE) ls.empty[atomicAdd(&ls.n_empty, 1)] = b0 + i;
+    if (a == ROCO_REORDER_FREE) ls.empty[atomicAdd(&ls.n_empty, 1)] = i;
     if (a < 0) continue;
     int j = 0;
     while (ls.map[j] != a) ++j;
@@ -79,7 +137,7 @@ __global__ void reorder_kernel(const ReorderParams p) {
     const int slot = ls.slot_of[ls.first[i]];
     if (cache && ls.live[slot] < 0) continue;
     const int c = atomicAdd(&ls.n_copies, 1);
-    ls.to[c] = b0 + i;
+    ls.to[c] = i;
     ls.from[c] = slot;
   }
   __syncthreads();
@@ -89,13 +147,45 @@ __global__ void reorder_kernel(const ReorderParams p) {
   const uint32_t step = threads * 16;  // from one of a thread's 16-byte places to its next
 
   // K and V, or the states: columns of 16 bytes
-  const int U = n_slots ? p.room / n_slots : 1;  // columns of a thread at a time
   const long long chunks = cache ? (long long)ls.max_live << p.row_shift : p.src_unit / 16;
+  // columns of a thread at a time: as many as there is room for, but no more than leave work for every CTA of the unit
+  const long long share = (chunks * p.arrays + (long long)p.parts * threads - 1) / ((long long)p.parts * threads);
+  const int U = n_slots ? (int)max(1LL, min((long long)(p.room / n_slots), share)) : 1;
   const long long per = (long long)threads * U;
-  const int tiles = (int)((chunks + per - 1) / per);
-  for (int t = part; t < p.arrays * tiles; t += p.parts) {
-    const int array = t >= tiles;
-    const long long c0 = (long long)(t - array * tiles) * per + tid;
+  const int tiles = (int)((chunks + per - 1) / per), stat_tiles = cache ? (p.B_dst + threads - 1) / threads : 0;
+  for (int t = part; t < stat_tiles + p.arrays * tiles; t += p.parts) {
+    if (t < stat_tiles) {
+      // statistics and positions: the four numbers of a slot are a column
+      const int k = t * threads + tid;
+      if (k >= p.B_dst) continue;
+      for (int j = 0; j < n_slots; ++j) {
+        if (k >= ls.live[j]) continue;
+        const long long at = ((long long)ls.source[j] * p.G + g) * p.B_src + k;
+        const uint32_t to = mine + (uint32_t)j * step;
+        fetch4(to, p.src_s + at);
+        fetch4(to + 4, p.src_q + at);
+        fetch4(to + 8, p.src_n + at);
+        fetch4(to + 12, p.src_pos + at);
+      }
+      fetched();
+      for (int i = 0; i < n_copies; ++i) {
+        const int j = ls.from[i];
+        const long long at = ((long long)ls.to[i] * p.G + g) * p.B_dst + k;
+        if (k < ls.live[j]) {
+          const uint4 x = room[j * threads + tid];
+          p.dst_s[at] = __uint_as_float(x.x);
+          p.dst_q[at] = __uint_as_float(x.y);
+          p.dst_n[at] = (int)x.z;
+          p.dst_pos[at] = (int)x.w;
+        } else {
+          p.dst_pos[at] = -1;
+        }
+      }
+      for (int i = 0; i < n_empty; ++i) p.dst_pos[((long long)ls.empty[i] * p.G + g) * p.B_dst + k] = -1;
+      continue;
+    }
+    const int array = t - stat_tiles >= tiles;
+    const long long c0 = (long long)(t - stat_tiles - array * tiles) * per + tid;
     const char *src = p.src[array] + (long long)g * p.src_unit;
     char *dst = p.dst[array] + (long long)g * p.dst_unit;
     const long long src_seq = p.src_unit * p.G, dst_seq = p.dst_unit * p.G;
@@ -122,45 +212,6 @@ __global__ void reorder_kernel(const ReorderParams p) {
     for (long long c = (long long)part * threads + tid; c < chunks; c += (long long)p.parts * threads)
       for (int i = 0; i < n_empty; ++i)
         *reinterpret_cast<uint4 *>(p.dst[0] + ((long long)ls.empty[i] * p.G + g) * p.dst_unit + c * 16) = make_uint4(0, 0, 0, 0);
-    return;
-  }
-  if (!p.in_place && part == 0) {
-    for (int i = tid; i < n_copies; i += threads) {
-      const long long to = (long long)ls.to[i] * p.G + g;
-      p.dst_live[to] = ls.live[ls.from[i]];
-      p.dst_t_next[to] = p.src_t_next[(long long)ls.source[ls.from[i]] * p.G + g];
-    }
-    for (int i = tid; i < n_empty; i += threads) {
-      const long long to = (long long)ls.empty[i] * p.G + g;
-      p.dst_live[to] = p.dst_t_next[to] = 0;
-    }
-  }
-  // statistics and positions: the four numbers of a slot are a column
-  for (int k = part * threads + tid; k < p.B_dst; k += p.parts * threads) {
-    for (int j = 0; j < n_slots; ++j) {
-      if (k >= ls.live[j]) continue;
-      const long long at = ((long long)ls.source[j] * p.G + g) * p.B_src + k;
-      const uint32_t to = mine + (uint32_t)j * step;
-      fetch4(to, p.src_s + at);
-      fetch4(to + 4, p.src_q + at);
-      fetch4(to + 8, p.src_n + at);
-      fetch4(to + 12, p.src_pos + at);
-    }
-    fetched();
-    for (int i = 0; i < n_copies; ++i) {
-      const int j = ls.from[i];
-      const long long at = ((long long)ls.to[i] * p.G + g) * p.B_dst + k;
-      if (k < ls.live[j]) {
-        const uint4 x = room[j * threads + tid];
-        p.dst_s[at] = __uint_as_float(x.x);
-        p.dst_q[at] = __uint_as_float(x.y);
-        p.dst_n[at] = (int)x.z;
-        p.dst_pos[at] = (int)x.w;
-      } else {
-        p.dst_pos[at] = -1;
-      }
-    }
-    for (int i = 0; i < n_empty; ++i) p.dst_pos[((long long)ls.empty[i] * p.G + g) * p.B_dst + k] = -1;
   }
 }
 
@@ -183,24 +234,30 @@ __global__ void reorder_live_kernel(const ReorderParams p) {
 }  // namespace
 
 roco_status launch_reorder(ReorderParams p, int sms, cudaStream_t stream) {
-  const int most = p.S_dst < kMost ? p.S_dst : kMost;   // places a thread may need
+  const long long chunks = p.arrays * (p.src_unit / 16);
+  if (!p.in_place) {
+    constexpr int kTile = kCopyThreads * kCopyFlight;
+    p.parts = (int)((chunks + kTile - 1) / kTile);
+    const long long ctas = (long long)p.S_dst * p.G * p.parts;
+    if (ctas > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
+    reorder_copy_kernel<<<(unsigned)ctas, kCopyThreads, 0, stream>>>(p);
+    return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
+  }
   // Threads so that a CTA's places take 64 KB at most (three CTAs per SM) down to one warp; at least eight places each, for the
   // columns of few sources that are in flight together.
   int threads = 256;
-  while (threads > 32 && threads * most * 16 > 65536) threads /= 2;
-  p.room = most < 8 ? 8 : most;
+  while (threads > 32 && threads * p.S_dst * 16 > 65536) threads /= 2;
+  p.room = p.S_dst < 8 ? 8 : p.S_dst;
   const int smem = threads * p.room * 16;
-  const long long chunks = p.arrays * (p.src_unit / 16);
-  long long parts = (chunks + 4LL * threads - 1) / (4LL * threads), most_parts = (16LL * sms + p.G - 1) / p.G;
-  if (parts > most_parts) parts = most_parts;
+  long long parts = (chunks + 2LL * threads - 1) / (2LL * threads), most = (64LL * sms + p.G - 1) / p.G;
+  if (parts > most) parts = most;
   p.parts = parts < 1 ? 1 : (int)parts;
-  const unsigned blocks = (unsigned)((p.S_dst + kMost - 1) / kMost);
-  if (blocks > 65535 || (long long)p.G * p.parts > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
+  if ((long long)p.G * p.parts > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
   static SmemLimit limit;
   if (!limit((const void *)reorder_kernel, 32 * kMost * 16)) return ROCO_ERR_CUDA;
-  reorder_kernel<<<dim3((unsigned)(p.G * p.parts), blocks), threads, smem, stream>>>(p);
+  reorder_kernel<<<(unsigned)(p.G * p.parts), threads, smem, stream>>>(p);
   if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
-  if (p.arrays == 1 || !p.in_place) return ROCO_OK;
+  if (p.arrays == 1) return ROCO_OK;
   return launch_overlapped(reorder_live_kernel, (unsigned)p.G, kMost, 0, stream, p) ? ROCO_OK : ROCO_ERR_CUDA;
 }
 
