@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kResident = 3;  // (CTAs per SM)
 constexpr int kWarpShift = 3, kMaxRanks = 8, kRuns = kMaxRanks * kWarps, kPer = kRuns / 32;
-constexpr int kOneWarp = 256;  // chunks that one warp searches
+constexpr int kLast = kThreads;  // chunks that are searched at once
 static_assert(kWarps == 1 << kWarpShift, "runs are divided by shifts");
 constexpr int kNodes = ROCO_TREE_MAX_NODES;
 static_assert(kNodes == 64, "a node's children are the bits of one 64-bit word");
@@ -29,12 +29,14 @@ struct Smem {
   uint64_t bar[2];                          // completes when a set is here
   unsigned first[2];                        // bits of the nodes that are accepted where no sibling was rejected before
   int token[kNodes];
-  int gone[kNodes];                         // tokens rejected behind the node the walk stands on
+  int gone[kNodes];                         // tokens rejected behind the node the walk stands on, each once
+  double gone_p[kNodes];                    // their probabilities
   int path[ROCO_TREE_MAX_PATH];
   // where the walk stands: node, nodes on the path, children of it that are not tried yet, tokens in gone
   int tip, len, n_gone;
   unsigned long long untried;
   double C, R, M;
+  double number;                            // sample_u
   int more;                                 // R is to be summed before the walk goes on
   int abort_flag;
 };
@@ -149,27 +151,14 @@ __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end,
   return sum;
 }
 
-// One chunk's sum, whatever it holds and wherever it lies.
-template <typename T>
-__device__ __forceinline__ double sum_chunk(const Rows<T> &rows, int i, double C, const int *gone, int n_gone) {
-  double r[Rows<T>::E], sum = 0.0;
-  rows.left(i, C, gone, n_gone, r);
-#pragma unroll
-  for (int e = 0; e < Rows<T>::E; ++e) sum += r[e];
-  return sum;
-}
-
+// What is left of p over chunks lo .. hi - 1 of a warp.
 template <typename T>
 __device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, double C, const int *gone, int n_gone) {
   constexpr int E = Rows<T>::E;
   const int lane = threadIdx.x & 31, full = (rows.V + rows.lead) / E;
   int i = lo + lane;
   double sum = 0.0;
-  bool plain = !rows.q || rows.q_like_p;
-  for (int g = 0; g < n_gone; ++g) {  // a rejected token in this run
-    const int at = gone[g] + rows.lead;
-    plain = plain && !(at >= lo * E && at < hi * E);
-  }
+  const bool plain = n_gone == 0 && (!rows.q || rows.q_like_p);
   // the row's first and last chunk may reach beyond it
   const bool head = plain && rows.lead && lo == 0 && hi > 0, tail = plain && full < rows.chunks && full >= lo && full < hi && (full > 0 || !head);
   if (head && lane == 0) i += 32;
@@ -180,20 +169,29 @@ __device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, d
     from = head ? 0 : full;
     step = head && tail ? full : hi;
   }
-  for (; from < hi; from += step) sum += sum_chunk(rows, from, C, gone, n_gone);
+  for (; from < hi; from += step) {
+    double r[E];
+    rows.left(from, C, gone, n_gone, r);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum += r[e];
+  }
   return warp_sum64(sum);
 }
 
-// Which of n <= 32 runs (one per lane: its sum, from 0 on) holds the place `target` of the running sum that starts at `base`; the last
-// one with any mass where roundings leave the place behind the end.  base becomes the sum before it; -1 where nothing has mass.
-__device__ __forceinline__ int pick_run(double sum, double target, double &base) {
+__device__ __forceinline__ double warp_scan64(double v) {
   const int lane = threadIdx.x & 31;
-  double upto = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const double y = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += y;
+    const double y = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += y;
   }
+  return v;
+}
+
+// Which of n <= 32 runs (one per lane: its sum, from 0 on, and the sum up to its end) holds the place `target` of the running sum that
+// starts at `base`; the last one with any mass where roundings leave the place behind the end.  base becomes the sum before it; -1
+// where nothing has mass.
+__device__ __forceinline__ int pick_run(double sum, double upto, double target, double &base) {
   const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && base + upto > target);
   const unsigned some = __ballot_sync(0xffffffffu, sum > 0.0);
   if (!some) return -1;
@@ -202,6 +200,7 @@ __device__ __forceinline__ int pick_run(double sum, double target, double &base)
   if (at > 0) base += before;
   return at;
 }
+__device__ __forceinline__ int pick_run(double sum, double target, double &base) { return pick_run(sum, warp_scan64(sum), target, base); }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const VerifyParams p) {
@@ -222,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
     x = p.tokens[b * p.T + tid];
     u = p.accept_u[b * p.T + tid];
   }
+  const float number = tid == 0 ? p.sample_u[b] : 0.f;
   if (nodes < 0 || nodes > p.T) {
     if (tid == 0 && rank == 0) atomicOr(p.status, ROCO_DEV_BAD_TREE);
     nodes = 0;
@@ -281,13 +281,16 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
     sm.untried = sm.children[rooted ? 1 : 0];
     sm.n_gone = 0;
     sm.C = 0.0; sm.R = 1.0; sm.M = 1.0;
+    sm.number = number;
+    sm.more = 0;
   }
   // (a peer's shared memory may be written once the peer runs and its barriers are ready)
   if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   bool anew = false;   // nothing was left of p after the rejections: once more with p itself
   double total = 0.0, base = 0.0, mine[kPer];
   int pass = 0, out = 0, run = 0;   // out: tokens that are out of p
-  double c = 0.0;
+  int all_of = -2;             // the node behind which `all` is this warp's sum over all of p
+  double c = 0.0, all = 0.0;
   Rows<T> rows;
   int first = 0, end = 0;      // the chunks that hold the next token, once the sums are known
   double place = 0.0;
@@ -297,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
       unsigned long long untried = sm.untried;
       int tip = sm.tip, len = sm.len, n_gone = sm.n_gone;
       double C = sm.C, R = sm.R, M = sm.M;
-      bool more = false;
+      bool more = false, summed = sm.more;   // R has been summed behind this node
       while (!more && len < p.A && untried) {
         const int i = __ffsll((long long)untried) - 1, x = sm.token[i];
         untried &= untried - 1;
@@ -321,16 +324,20 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
           untried = sm.children[i + 1];
           C = 0.0; R = 1.0; M = 1.0;
           n_gone = 0;
+          summed = false;
         } else {
-          sm.gone[n_gone++] = x;
+          if (!again) {
+            sm.gone_p[n_gone] = sm.p[i] > 0.0 ? sm.p[i] : 0.0;
+            sm.gone[n_gone++] = x;
+          }
           if (draft) {
             if (M > 0.0) C += M == 1.0 ? R : R / M;
             if (p.distinct) M -= q;
             more = untried != 0;
-          } else if (n_gone == 1) {
+          } else if (!summed) {
             more = untried != 0;
-          } else if (!again && sm.p[i] > 0.0) {
-            R -= sm.p[i];   // (the first sum went without its token)
+          } else if (!again) {
+            R -= sm.gone_p[n_gone - 1];
           }
         }
       }
@@ -360,14 +367,37 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
       lo = min(first + warp * run, end);
       hi = min(lo + run, end);
     }
-    const double sum = sum_run(rows, lo, hi, c, sm.gone, out);
+    // Tokens that are out are taken off a sum over all of p, which stands while the walk stays at its node; where next to nothing would
+    // be left of it, the sum is formed without them.
+    const bool from_all = !draft && end == 0 && !anew;
+    int here = 0;
+    double less = 0.0;
+    if (from_all) {
+      for (int g = 0; g < out; ++g) {
+        const int at = sm.gone[g] + rows.lead;
+        if (at >= lo * E && at < hi * E) {
+          ++here;
+          less += sm.gone_p[g];
+        }
+      }
+    }
+    const bool known = from_all && all_of == sm.tip;
+    double sum = known ? all : 0.0;
+    for (int exact = from_all ? 0 : 1; exact < 2; ++exact) {
+      if (exact || !known) sum = sum_run(rows, lo, hi, c, sm.gone, exact ? out : 0);
+      if (exact) break;
+      all = sum;
+      all_of = sm.tip;
+      sum -= less;
+      if (!here || sum > 1e-9 * all) break;
+    }
     if (end != 0) {
       if (lane == 0) sm.part[warp] = sum;
       __syncthreads();
       const int at = pick_run(lane < kWarps ? sm.part[lane] : 0.0, place, base);
       first = min(first + at * run, end);
       end = min(first + run, end);
-      if (end - first <= kOneWarp) break;
+      if (end - first <= kLast) break;
       continue;
     }
     double *sums = sm.sums[pass & 1];
@@ -391,7 +421,8 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
     double some = mine[0];
 #pragma unroll
     for (int k = 1; k < kPer; ++k) some += mine[k];
-    total = warp_sum64(some);
+    const double upto = warp_scan64(some);
+    total = __shfl_sync(0xffffffffu, upto, 31);
     if (tid == 0) sm.R = total;
     ++pass;
     // on with the walk, or once more where nothing is left
@@ -409,38 +440,54 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
         }
         return;
       }
-      // the pick descends the sums: a few warps, one of them, 32 chunks or a few times that, one chunk, one element
-      place = (double)p.sample_u[b] * total;
-      int at = pick_run(some, place, base);
-      double x = 0.0;
+      // the pick descends the sums: a few warps, one of them, chunks of its run, one chunk, one element
+      place = sm.number * total;
+      const int lane_at = pick_run(some, upto, place, base);
+      int k_at = 0;   // (the lane's first run with mass that reaches the place, else its last with mass)
+      double before = 0.0, sofar = 0.0;
+      bool found = false;
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
-        const double y = __shfl_sync(0xffffffffu, mine[k], at);
-        if (lane == k) x = y;
+        if (!found && mine[k] > 0.0) {
+          k_at = k;
+          before = sofar;
+          found = base + (sofar + mine[k]) > place;
+        }
+        sofar += mine[k];
       }
-      at = kPer * at + pick_run(x, place, base);
+      const int at = __shfl_sync(0xffffffffu, kPer * lane + k_at, lane_at);
+      base += __shfl_sync(0xffffffffu, before, lane_at);
       if (at / kWarps != rank) return;
       first = min(at * run, rows.chunks);
       end = min(first + run, rows.chunks);
-      if (end - first <= kOneWarp) break;
+      if (end - first <= kLast) break;
     }
     __syncthreads();   // (what is written next has been read)
   }
-  if (warp != 0) return;
-  while (end - first > 1) {
-    const int per = (end - first + 31) / 32, l = min(first + lane * per, end), h = min(l + per, end);
-    double part = 0.0;
-    for (int i = l; i < h; ++i) part += sum_chunk(rows, i, c, sm.gone, out);
-    first = min(first + pick_run(part, place, base) * per, end - 1);
-    end = min(first + per, end);
-  }
-  double r[E], element = 0.0;
-  rows.left(first, c, sm.gone, out, r);
+  // a chunk per thread
+  double r[E], own = 0.0;
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (lane == e) element = r[e];
-  const int e = pick_run(element, place, base);
-  if (lane == 0) p.next_token[b] = first * E - rows.lead + e;
+  for (int e = 0; e < E; ++e) r[e] = 0.0;
+  if (first + tid < end) rows.left(first + tid, c, sm.gone, out, r);
+#pragma unroll
+  for (int e = 0; e < E; ++e) own += r[e];
+  const double upto = warp_scan64(own);
+  __syncthreads();   // (part has been read)
+  if (lane == 31) sm.part[warp] = upto;
+  __syncthreads();
+  if (pick_run(lane < kWarps ? sm.part[lane] : 0.0, place, base) != warp) return;
+  if (pick_run(own, upto, place, base) != lane) return;
+  int token = 0;   // the first element with mass that reaches the place, else the last with mass
+  bool found = false;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (!found && r[e] > 0.0) {
+      token = (first + tid) * E - rows.lead + e;
+      found = base + r[e] > place;
+      base += r[e];
+    }
+  }
+  p.next_token[b] = token;
 }
 
 template <typename T>
