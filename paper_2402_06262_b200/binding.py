@@ -87,6 +87,7 @@ class roco_heads(C.Structure):
 _VERIFY, _HEADS = struct.Struct("@6i4P6q9P"), struct.Struct("@6i3P6q6P")
 assert _VERIFY.size == C.sizeof(roco_verify) and _HEADS.size == C.sizeof(roco_heads)
 
+_Tensor = torch.Tensor
 _lib = None
 
 
@@ -247,8 +248,7 @@ def _device() -> int:
 def _need(what: str, name: str, t, shape, dtype, dev: int):
     """The argument checks that the C entry points cannot make: a tensor of this shape and type, contiguous, on the
     current device."""
-    if (not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != dev
-            or not t.is_contiguous()):
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous()):
         raise RocoError(1, f"{what}: {name}: a contiguous {dtype} tensor of shape {list(shape)} on the current CUDA device is "
                            f"needed, got " + (f"{t.dtype} {list(t.shape)} on {t.device}" if isinstance(t, torch.Tensor)
                                               else type(t).__name__))
@@ -774,7 +774,7 @@ def _zero(t: Optional[torch.Tensor]) -> int:
 def _need_rows(what: str, name: str, t, shape, dtype, dev: int):
     """A tensor of this shape and type on the current device whose last dimension is dense; the others may have any strides, which
     are returned."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == dev:
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev and t.shape == shape:
         strides = t.stride()
         if strides[-1] == 1 or shape[-1] == 1:
             return strides
@@ -814,7 +814,7 @@ def roco_tree_verify(target, tokens, parent, accept_u, sample_u, path, path_len,
         _need(what, "nodes", nodes, each, i32, dev)
     call = _VERIFY.pack(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, T, V, A, 1 if distinct else 0, target.data_ptr(),
                         _zero(draft), _zero(target_prefix), _zero(draft_prefix), ts[0], ts[1], ds[0], ds[1], tp, dp,
-                        tokens.data_ptr(), parent.data_ptr(), _zero(nodes), accept_u.data_ptr(), sample_u.data_ptr(),
+                        tokens.data_ptr(), parent.data_ptr(), 0 if nodes is None else nodes.data_ptr(), accept_u.data_ptr(), sample_u.data_ptr(),
                         path.data_ptr(), path_len.data_ptr(), next_token.data_ptr(), status.data_ptr())
     rc = lib().roco_tree_verify(call, _raw_stream(dev))
     if rc != ROCO_OK:

@@ -17,13 +17,13 @@ namespace {
 constexpr int kMost = ROCO_REORDER_MAX_S;  // destinations of a CTA
 
 struct Lists {
-  int map[kMost];        // validated: a source, KEEP or FREE
-  int first[kMost];      // the first destination with the same source
-  int slot_of[kMost];    // where that one's source is kept
-  int source[kMost];     // slot -> source sequence
-  int live[kMost];       // slot -> its occupied slots in this unit; -1: not copied
+  int map[kMost];              // a destination's source, KEEP or FREE
+  int occupied[kMost];         // occupied slots of every sequence in this unit
+  int slot_of[kMost];          // source sequence -> the slot that it is kept in, -1: none yet
+  int source[kMost];           // slot -> source sequence
+  int live[kMost];             // slot -> its occupied slots in this unit; -1: not copied
   int to[kMost], from[kMost];  // copies: destination, slot
-  int empty[kMost];      // destinations that are freed
+  int empty[kMost];            // destinations that are freed
   int n_slots, n_copies, n_empty, max_live;
 };
 
@@ -101,40 +101,39 @@ __global__ void reorder_kernel(const ReorderParams p) {
   extern __shared__ uint4 room[];
   __shared__ Lists ls;
   const int tid = threadIdx.x, threads = blockDim.x;
-  const int g = blockIdx.x / p.parts, part = blockIdx.x - g * p.parts;
-  const int nb = p.S_dst;
+  const int g = blockIdx.x / p.parts, part = blockIdx.x - g * p.parts, S = p.S_dst;
   const bool cache = p.arrays == 2;
 
-  for (int i = tid; i < nb; i += threads) ls.map[i] = source_of(p, i, blockIdx.x == 0);
+  // which sources there are, and who gets them (up to kMost / threads sequences a thread)
+  for (int i = tid; i < S; i += threads) {
+    ls.slot_of[i] = -1;
+    ls.occupied[i] = cache ? p.src_live[(long long)i * p.G + g] : 0;
+    ls.map[i] = source_of(p, i, blockIdx.x == 0);
+  }
   if (tid == 0) ls.n_slots = ls.n_copies = ls.n_empty = ls.max_live = 0;
   __syncthreads();
-  for (int i = tid; i < nb; i += threads) {
+  for (int i = tid; i < S; i += threads) {
     const int a = ls.map[i];
     if (a == ROCO_REORDER_FREE) ls.empty[atomicAdd(&ls.n_empty, 1)] = i;
     if (a < 0) continue;
-    int j = 0;
-    while (ls.map[j] != a) ++j;
-    ls.first[i] = j;
-    if (j != i) continue;
-    const int slot = atomicAdd(&ls.n_slots, 1);
-    int live = 0;
-    if (cache) {
-      live = p.src_live[(long long)a * p.G + g];
-      if (live < 0 || live > p.B_src) {
+    if (atomicCAS(&ls.slot_of[a], -1, kMost) == -1) {   // the first to ask for it
+      const int slot = atomicAdd(&ls.n_slots, 1);
+      int live = ls.occupied[a];
+      if (cache && (live < 0 || live > p.B_src)) {
         if (part == 0) atomicOr(p.status, ROCO_DEV_BAD_LIVE);
         live = -1;
-      } else {
-        atomicMax(&ls.max_live, live);
       }
+      atomicMax(&ls.max_live, live);
+      ls.source[slot] = a;
+      ls.live[slot] = live;
+      ls.slot_of[a] = slot;
     }
-    ls.slot_of[i] = slot;
-    ls.source[slot] = a;
-    ls.live[slot] = live;
   }
   __syncthreads();
-  for (int i = tid; i < nb; i += threads) {
-    if (ls.map[i] < 0) continue;
-    const int slot = ls.slot_of[ls.first[i]];
+  for (int i = tid; i < S; i += threads) {
+    const int a = ls.map[i];
+    if (a < 0) continue;
+    const int slot = ls.slot_of[a];
     if (cache && ls.live[slot] < 0) continue;
     const int c = atomicAdd(&ls.n_copies, 1);
     ls.to[c] = i;
@@ -147,12 +146,11 @@ __global__ void reorder_kernel(const ReorderParams p) {
   const uint32_t step = threads * 16;  // from one of a thread's 16-byte places to its next
 
   // K and V, or the states: columns of 16 bytes
-  const long long chunks = cache ? (long long)ls.max_live << p.row_shift : p.src_unit / 16;
+  const int chunks = cache ? ls.max_live << p.row_shift : (int)(p.src_unit / 16);
   // columns of a thread at a time: as many as there is room for, but no more than leave work for every CTA of the unit
-  const long long share = (chunks * p.arrays + (long long)p.parts * threads - 1) / ((long long)p.parts * threads);
-  const int U = n_slots ? (int)max(1LL, min((long long)(p.room / n_slots), share)) : 1;
-  const long long per = (long long)threads * U;
-  const int tiles = (int)((chunks + per - 1) / per), stat_tiles = cache ? (p.B_dst + threads - 1) / threads : 0;
+  const int lanes = p.parts * threads, share = (chunks * p.arrays + lanes - 1) / lanes;
+  const int U = n_slots ? max(1, min(p.room / n_slots, share)) : 1;
+  const int per = threads * U, tiles = (chunks + per - 1) / per, stat_tiles = cache ? (p.B_dst + threads - 1) / threads : 0;
   for (int t = part; t < stat_tiles + p.arrays * tiles; t += p.parts) {
     if (t < stat_tiles) {
       // statistics and positions: the four numbers of a slot are a column
@@ -185,33 +183,33 @@ __global__ void reorder_kernel(const ReorderParams p) {
       continue;
     }
     const int array = t - stat_tiles >= tiles;
-    const long long c0 = (long long)(t - stat_tiles - array * tiles) * per + tid;
+    const int c0 = (t - stat_tiles - array * tiles) * per + tid;
     const char *src = p.src[array] + (long long)g * p.src_unit;
     char *dst = p.dst[array] + (long long)g * p.dst_unit;
     const long long src_seq = p.src_unit * p.G, dst_seq = p.dst_unit * p.G;
     for (int j = 0; j < n_slots; ++j) {
-      const long long end = cache ? (long long)ls.live[j] << p.row_shift : chunks;
+      const int end = cache ? ls.live[j] << p.row_shift : chunks;
       const char *from = src + ls.source[j] * src_seq;
       for (int u = 0; u < U; ++u) {
-        const long long c = c0 + (long long)u * threads;
-        if (c < end) fetch16(mine + (uint32_t)(j * U + u) * step, from + c * 16);
+        const int c = c0 + u * threads;
+        if (c < end) fetch16(mine + (uint32_t)(j * U + u) * step, from + c * 16LL);
       }
     }
     fetched();
     for (int i = 0; i < n_copies; ++i) {
       const int j = ls.from[i];
-      const long long end = cache ? (long long)ls.live[j] << p.row_shift : chunks;
+      const int end = cache ? ls.live[j] << p.row_shift : chunks;
       char *to = dst + ls.to[i] * dst_seq;
       for (int u = 0; u < U; ++u) {
-        const long long c = c0 + (long long)u * threads;
-        if (c < end) *reinterpret_cast<uint4 *>(to + c * 16) = room[(j * U + u) * threads + tid];
+        const int c = c0 + u * threads;
+        if (c < end) *reinterpret_cast<uint4 *>(to + c * 16LL) = room[(j * U + u) * threads + tid];
       }
     }
   }
   if (!cache) {
-    for (long long c = (long long)part * threads + tid; c < chunks; c += (long long)p.parts * threads)
+    for (int c = part * threads + tid; c < chunks; c += lanes)
       for (int i = 0; i < n_empty; ++i)
-        *reinterpret_cast<uint4 *>(p.dst[0] + ((long long)ls.empty[i] * p.G + g) * p.dst_unit + c * 16) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(p.dst[0] + ((long long)ls.empty[i] * p.G + g) * p.dst_unit + c * 16LL) = make_uint4(0, 0, 0, 0);
   }
 }
 
