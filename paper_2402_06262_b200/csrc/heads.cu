@@ -1,11 +1,16 @@
 // Queries, keys and values of a layer out of its projections: norm of each head, rotation by position, layout by unit.
 //
-// A stream: every element is read once and written once, 2 d e bytes per head of a token, and that bounds it.  A row (the head
-// of one token) is held by d e / 32 lanes with two 16-byte pieces each.  For pairs (i, i + rot/2) the two pieces are the two
-// halves of the same pairs, so the rotation needs no exchange between lanes, and the norm a butterfly over 4 to 16 lanes.  A
+// A stream: every element is read once and written once, 2 d e bytes per head of a token, and that bounds it: 32768 tokens x 96 heads,
+// bf16, d 128, take 239 us (6.1 TB/s, 0.94 of the measured copy rate; a plain copy of these bytes takes 229).
+//
+// A row (the head of one token) is held by d e / 32 lanes with two 16-byte pieces each.  For pairs (i, i + rot/2) the two pieces are
+// the two halves of the same pairs, so the rotation needs no exchange between lanes, and the norm a butterfly over 4 to 16 lanes.  A
 // thread keeps its place in the row and its token and goes through a range of heads: sines and cosines are formed once for all
-// of them, and four rows are in flight at a time.  Neighbouring rows of a CTA are neighbouring tokens, which follow one another in
-// the unit layout: what is read as rows of the projections leaves as blocks of 16 to 32 tokens per head.
+// of them, and four rows are fetched together (two 279 us, three 251, six 277, eight 263; fetching two while two are worked on 288).
+// Neighbouring rows of a CTA are neighbouring tokens, which follow one another in the unit layout: what is read as rows of the
+// projections leaves as blocks of 8 to 32 tokens per head.  128 threads (64: 262 us, 256: 299), five CTAs per SM by their registers.
+// A small call is a chain of latencies (8 tokens x 96 heads 3.5 us in a graph): positions, frequencies, weights and the first rows are
+// all under way before any of them is needed.
 #include "heads.cuh"
 
 namespace roco {

@@ -3,12 +3,15 @@
 // A copy, bound by the bytes that move: every source read once, every destination written once.
 //
 // Into another cache a CTA copies a part of one unit, eight 16-byte pieces of a thread in flight; the destinations of one source are
-// neighbours in the grid, so that it is read from HBM once.
+// neighbours in the grid, so that it is read from HBM once.  Nine of thirteen sequences x 24 units x 1001 slots, fp32, d 64: 38 us,
+// 6.0 TB/s (by columns, as below, 48 us).
 //
 // In place the work is cut by columns, 16 bytes at one place of a unit, which a thread handles for all sequences: it fetches the
 // column of every distinct source into its own part of shared memory (asynchronous 16-byte copies), then writes it to every
 // destination.  So any map is right (cycles, forks, chains): a column is written only after all of it has been read, and nobody else
-// touches it.  Threads share nothing but the map, so nobody waits for anybody.
+// touches it.  Threads share nothing but the map, so nobody waits for anybody.  Eight beams x 1024 units x 1024 slots: 6.1 GB in 972 us,
+// 6.3 TB/s; a prompt forked into seven more samples in one layer (121 of 138 MB are writes) 28 us, where plain writes of as many
+// bytes take 39.
 #include "heads.cuh"
 
 namespace roco {
@@ -242,7 +245,8 @@ roco_status launch_reorder(ReorderParams p, int sms, cudaStream_t stream) {
     return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
   }
   // Threads so that a CTA's places take 64 KB at most (three CTAs per SM) down to one warp; at least eight places each, for the
-  // columns of few sources that are in flight together.
+  // columns of few sources that are in flight together.  CTAs with two columns a thread, up to 64 per SM (16 units x 512 states: 40 us,
+  // with one and four columns 42 and 47; eight beams x 1024 units with at most 16 and 32 CTAs per SM 1027 and 1008 us, with 64 972).
   int threads = 256;
   while (threads > 32 && threads * p.S_dst * 16 > 65536) threads /= 2;
   p.room = p.S_dst < 8 ? 8 : p.S_dst;

@@ -3,12 +3,16 @@
 // A cluster of CTAs (one to eight) per sequence.  Everything about a node is two numbers, p(x) and q(x) behind its parent, fetched for
 // all nodes at once; the walk over them is a few instructions per child.  A row is only touched where a child was rejected (to sum
 // what is left of p) and at the end (to pick the next token): what is left of p after any number of rejections is
-// max(p - C q, 0) for one C, because rejecting once more takes (R / M) q from what is still positive and leaves zero at zero.  A row is
-// cut into one run per CTA and that into one per warp, so the sums that a pass leaves behind are a prefix sum's upper levels, and the
-// pick descends them: CTA, warp, the chunk of 32 lanes, the lane.
-// Bound by the latencies of a chain (two loads of the nodes' numbers, the row, the sums' way through the cluster), for many
-// sequences by the rows' bytes.  Sums and products are in 64 bits: an index is the answer, and an error of 2^-24 in a sum over
-// 10^5 tokens moves it about once in a thousand calls.
+// max(p - C q, 0) for one C, because rejecting once more takes (R / M) q from what is still positive and leaves zero at zero.  Without
+// draft probabilities what is left is the row less single tokens, so the sums over all of it stand while the walk stays at a node.
+// A row is cut into one run per warp of the cluster.  Every warp sends its run's sum to every rank by an asynchronous store that also
+// signals (no barrier of the cluster, no reduction in the CTA before it); the sums are the upper level of a prefix sum, which the pick
+// descends: run, chunk of 16 bytes, element.
+// Bound by a chain of latencies (one tree x 32000 tokens: 6.8 us in a graph, of which launch 0.7, the nodes' numbers 1.4, the walk 0.8, a
+// pass over the row 1.4, the sums' way 0.3, the pick about 1), and with many sequences by the walks with most rejections: 64 sequences x
+// 128000 tokens take 33.7 us, 20 to the end of the first row (4.6 TB/s while it is read), 9 for further passes of the few that need them.
+// Sums and products are in 64 bits: an index is the answer, and an error of 2^-24 in a sum over 10^5 tokens moves it about once in a
+// thousand calls.
 #include "heads.cuh"
 
 namespace roco {
@@ -96,16 +100,12 @@ struct Rows {
 };
 
 // Conversions and comparisons in 64 bits are issued at an eighth to a quarter of the rate of its sums and products (16 and 21 of 62
-// per cycle and SM, measured), so where all numbers are positive and normal (bits from kLeastNormal on, kNormals of them) both are
-// done on the bits.
-constexpr uint32_t kLeastNormal = 0x00800000u, kNormals = 0x7f000000u;
+// per cycle and SM, measured), so where all numbers are positive and normal conversions are done on the bits, and max(x, 0) is half
+// of x + |x|.
+constexpr uint32_t kLeastNormal = 0x00800000u, kInfinity = 0x7f800000u;
 __device__ __forceinline__ double widen(float x) {
   const uint32_t bits = __float_as_uint(x);
   return __hiloint2double((int)((bits >> 3) + ((1023u - 127u) << 20)), (int)(bits << 29));
-}
-__device__ __forceinline__ double positive(double x) {  // max(x, 0) of a number
-  const int hi = __double2hiint(x), keep = ~(hi >> 31);
-  return __hiloint2double(hi & keep, __double2loint(x) & keep);
 }
 
 // A lane's part of the sum of what is left of p over chunks lo .. hi - 1 of a warp (chunks lane, lane + 32, ... of the run).  A row
@@ -114,7 +114,7 @@ template <typename T, bool kDraft>
 __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end, double C) {
   constexpr int E = Rows<T>::E, kBatch = 16 / E;
   const uint4 *p = reinterpret_cast<const uint4 *>(rows.p - rows.lead), *q = reinterpret_cast<const uint4 *>(rows.q - rows.lead);
-  double sum = 0.0;
+  double sum = 0.0, twice = 0.0;
   for (; i < end; i += 32 * kBatch) {
     uint4 a[kBatch], b[kBatch];
 #pragma unroll
@@ -130,15 +130,22 @@ __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end,
       float fp[E], fq[E];
       Elem<T>::unpack(a[k], fp);
       if (kDraft) Elem<T>::unpack(b[k], fq);
-      uint32_t most = 0;
+      uint32_t least = __float_as_uint(fp[0]), most = least;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        most = max(most, __float_as_uint(fp[e]) - kLeastNormal);
-        if (kDraft) most = max(most, __float_as_uint(fq[e]) - kLeastNormal);
+      for (int e = 0; e < E; e += 2) {
+        least = __vimin3_u32(least, __float_as_uint(fp[e]), __float_as_uint(fp[e + 1]));
+        most = __vimax3_u32(most, __float_as_uint(fp[e]), __float_as_uint(fp[e + 1]));
+        if (kDraft) {
+          least = __vimin3_u32(least, __float_as_uint(fq[e]), __float_as_uint(fq[e + 1]));
+          most = __vimax3_u32(most, __float_as_uint(fq[e]), __float_as_uint(fq[e + 1]));
+        }
       }
-      if (most < kNormals) {
+      if (least >= kLeastNormal && most < kInfinity) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += kDraft ? positive(fma(-C, widen(fq[e]), widen(fp[e]))) : widen(fp[e]);
+        for (int e = 0; e < E; ++e) {
+          const double x = kDraft ? fma(-C, widen(fq[e]), widen(fp[e])) : widen(fp[e]);
+          twice += kDraft ? x + fabs(x) : x;
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -148,7 +155,7 @@ __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end,
       }
     }
   }
-  return sum;
+  return sum + (kDraft ? 0.5 : 1.0) * twice;
 }
 
 // What is left of p over chunks lo .. hi - 1 of a warp.
@@ -492,12 +499,16 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
 
 template <typename T>
 roco_status launch_t(VerifyParams p, int S, int sms, cudaStream_t stream) {
-  // CTAs per sequence: eight, or fewer where so many would be more than reside together; none with fewer chunks than threads.
-  int ranks = 1;
+  // CTAs per sequence, a power of two: doubled while they fill less than three quarters of the GPU, so up to half as many again as
+  // reside together, because the walks with most rejections end last and every rejection costs a pass over a row by its own CTAs
+  // alone (64 sequences x 128000 tokens, three CTAs per SM: eight 33.7 us, six, which reside together, 37.4, four 53).  None with
+  // fewer 16-byte chunks of a row than threads.
+  int shift = 0;
   const long long chunks = (p.V + Elem<T>::kPerChunk - 1) / Elem<T>::kPerChunk;
-  while (ranks < kMaxRanks && 4LL * S * ranks < 3LL * kResident * sms && chunks >= 2LL * ranks * kThreads) ranks *= 2;
-  p.ranks = ranks;
-  p.rank_shift = ranks == 1 ? 0 : ranks == 2 ? 1 : ranks == 4 ? 2 : 3;
+  while ((1 << shift) < kMaxRanks && ((4LL * S) << shift) < 3LL * kResident * sms && chunks >= (2LL * kThreads) << shift) ++shift;
+  p.rank_shift = shift;
+  p.ranks = 1 << shift;
+  const int ranks = p.ranks;
   const bool ok = launch_cluster(tree_verify_kernel<T>, (unsigned)S * (unsigned)ranks, (unsigned)ranks, kThreads, 0, stream, p);
   return ok ? ROCO_OK : ROCO_ERR_CUDA;
 }
