@@ -563,6 +563,7 @@ typedef struct {
  *   positions    [S][N][axes] int32 DEVICE array, or NULL: token n has position n on every axis
  *   Q            [S][G][N][group][d];  K, V [S][G][N][d] (NULL where k, v are);  they overlap nothing else.  N = 1 is the
  *                layout of the decode steps, N = T that of the trees, N = Lmax (group 1) that of the prompt passes
+ *   limits       1 <= group <= ROCO_TREE_MAX_GROUP, S * N < 2^30
  * An axis outside [0, axes) sets ROCO_DEV_BAD_MAP and counts as 0.  One launch.
  */
 typedef struct {

@@ -8,9 +8,9 @@
 // A row is cut into one run per warp of the cluster.  Every warp sends its run's sum to every rank by an asynchronous store that also
 // signals (no barrier of the cluster, no reduction in the CTA before it); the sums are the upper level of a prefix sum, which the pick
 // descends: run, chunk of 16 bytes, element.
-// Bound by a chain of latencies (one tree x 32000 tokens: 6.8 us in a graph, of which launch 0.7, the nodes' numbers 1.4, the walk 0.8, a
+// Bound by a chain of latencies (one tree x 32000 tokens: 6.9 us in a graph, of which launch 0.7, the nodes' numbers 1.4, the walk 0.8, a
 // pass over the row 1.4, the sums' way 0.3, the pick about 1), and with many sequences by the walks with most rejections: 64 sequences x
-// 128000 tokens take 33.7 us, 20 to the end of the first row (4.6 TB/s while it is read), 9 for further passes of the few that need them.
+// 128000 tokens take 34 us, 20 to the end of the first row (4.6 TB/s while it is read), 9 for further passes of the few that need them.
 // Sums and products are in 64 bits: an index is the answer, and an error of 2^-24 in a sum over 10^5 tokens moves it about once in a
 // thousand calls.
 #include "heads.cuh"
@@ -436,6 +436,9 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
     const bool more = sm.more;
     if (!anew && !more && total == 0.0 && (sm.C != 0.0 || sm.n_gone > 0)) anew = true;
     else if (anew || !more) {
+      // the last exchange; nobody leaves before everybody has it
+      __syncwarp();
+      if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
       if (rank == 0) {
         if (tid < p.A) p.path[b * p.A + tid] = tid < sm.len ? sm.path[tid] : -1;
         if (tid == 0) p.path_len[b] = sm.len;
@@ -445,6 +448,8 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
           p.next_token[b] = -1;
           atomicOr(p.status, ROCO_DEV_BAD_PROBS);
         }
+        __syncwarp();
+        if (ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         return;
       }
       // the pick descends the sums: a few warps, one of them, chunks of its run, one chunk, one element
@@ -464,7 +469,10 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
       }
       const int at = __shfl_sync(0xffffffffu, kPer * lane + k_at, lane_at);
       base += __shfl_sync(0xffffffffu, before, lane_at);
-      if (at / kWarps != rank) return;
+      if (at / kWarps != rank) {
+        if (ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        return;
+      }
       first = min(at * run, rows.chunks);
       end = min(first + run, rows.chunks);
       if (end - first <= kLast) break;
@@ -481,6 +489,8 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
   const double upto = warp_scan64(own);
   __syncthreads();   // (part has been read)
   if (lane == 31) sm.part[warp] = upto;
+  __syncwarp();
+  if (ranks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   __syncthreads();
   if (pick_run(lane < kWarps ? sm.part[lane] : 0.0, place, base) != warp) return;
   if (pick_run(own, upto, place, base) != lane) return;
@@ -501,7 +511,7 @@ template <typename T>
 roco_status launch_t(VerifyParams p, int S, int sms, cudaStream_t stream) {
   // CTAs per sequence, a power of two: doubled while they fill less than three quarters of the GPU, so up to half as many again as
   // reside together, because the walks with most rejections end last and every rejection costs a pass over a row by its own CTAs
-  // alone (64 sequences x 128000 tokens, three CTAs per SM: eight 33.7 us, six, which reside together, 37.4, four 53).  None with
+  // alone (64 sequences x 128000 tokens, three CTAs per SM: eight 34 us, six, which reside together, 37.4, four 53).  None with
   // fewer 16-byte chunks of a row than threads.
   int shift = 0;
   const long long chunks = (p.V + Elem<T>::kPerChunk - 1) / Elem<T>::kPerChunk;
