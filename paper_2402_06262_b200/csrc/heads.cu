@@ -205,16 +205,28 @@ roco_status launch_t(HeadsParams p, int pairing, int sms, cudaStream_t stream) {
   const long long tokens = (long long)p.S * p.N;
   const long long tiles = (tokens + kRows - 1) / kRows;
   const int all = p.G * (p.group + 2);
-  // CTAs that share a tile of tokens: enough for four per SM, no more, since each forms the tile's sines and cosines anew (6002 tokens
-  // x 40 heads, fp32, d 64: 20.5 us; for 1 and 16 per SM 26.5 and 22.0).  Above 32 heads a CTA the last wave is the longer (32768
-  // tokens x 96 heads: 240 us, undivided 246; 16 heads 247).
-  long long parts = (4LL * sms + tiles - 1) / tiles;
-  if (parts > all) parts = all;
-  if (parts * 32 < all) parts = (all + 31) / 32;
-  p.heads = (all + (int)parts - 1) / (int)parts;
+  // CTAs that share a tile of tokens: a head each where all of them reside together.  Else, as each forms the tile's sines and cosines
+  // anew, which costs as much as kSetup heads, and of more than one wave the last is half full on average, the time is about
+  // (waves + 1/2) (heads per CTA + kSetup) (1180 tokens x 400 heads: ten CTAs, one wave, 44 us; 6, 13 and 30 take 56, 54 and 47; 32768 tokens
+  // x 96 heads: three 239 us, one and six 246; 6002 x 40 heads, fp32, d 64: two 20.5 us, one and seven 26.5 and 22).
+  constexpr double kSetup = 3.0, kResident = sizeof(T) == 2 ? 5.0 : 6.0;   // (CTAs per SM, by their registers)
+  const double slots = kResident * sms;
+  int parts = all;
+  if ((double)tiles * all > slots) {
+    double best = 0.0;
+    for (int n = 1; n <= all && n <= 128; ++n) {
+      const double waves = (double)tiles * n / slots;
+      const double cost = (waves > 1.0 ? waves + 0.5 : 1.0) * ((all + n - 1) / n + kSetup);
+      if (n == 1 || cost < best) {
+        best = cost;
+        parts = n;
+      }
+    }
+  }
+  p.heads = (all + parts - 1) / parts;
   p.ahead = p.heads <= kFlight;
   parts = (all + p.heads - 1) / p.heads;
-  if (tokens > 0x7fffffffLL - kRows || parts > 65535) return ROCO_ERR_UNSUPPORTED;
+  if (tokens > 0x7fffffffLL - kRows) return ROCO_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)tiles, (unsigned)parts);
   if (pairing == ROCO_PAIR_ADJACENT) norm_rotate_kernel<T, D, true><<<grid, kThreads, 0, stream>>>(p);
   else norm_rotate_kernel<T, D, false><<<grid, kThreads, 0, stream>>>(p);

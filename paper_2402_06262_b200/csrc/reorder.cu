@@ -23,9 +23,12 @@ struct Lists {
   int map[kMost];              // a destination's source, KEEP or FREE
   int occupied[kMost];         // occupied slots of every sequence in this unit
   int slot_of[kMost];          // source sequence -> the slot that it is kept in, -1: none yet
-  int source[kMost];           // slot -> source sequence
   int live[kMost];             // slot -> its occupied slots in this unit; -1: not copied
-  int to[kMost], from[kMost];  // copies: destination, slot
+  struct Place {
+    long long unit;            // number of the unit
+    int end, slot;             // its 16-byte chunks that move; the slot that they are kept in
+  };
+  Place from[kMost], to[kMost];  // of every slot; of every copy
   int empty[kMost];            // destinations that are freed
   int n_slots, n_copies, n_empty, max_live;
 };
@@ -127,8 +130,8 @@ __global__ void reorder_kernel(const ReorderParams p) {
         live = -1;
       }
       atomicMax(&ls.max_live, live);
-      ls.source[slot] = a;
       ls.live[slot] = live;
+      ls.from[slot] = {(long long)a * p.G + g, cache ? max(live, 0) << p.row_shift : (int)(p.src_unit / 16), slot};
       ls.slot_of[a] = slot;
     }
   }
@@ -138,9 +141,7 @@ __global__ void reorder_kernel(const ReorderParams p) {
     if (a < 0) continue;
     const int slot = ls.slot_of[a];
     if (cache && ls.live[slot] < 0) continue;
-    const int c = atomicAdd(&ls.n_copies, 1);
-    ls.to[c] = i;
-    ls.from[c] = slot;
+    ls.to[atomicAdd(&ls.n_copies, 1)] = {(long long)i * p.G + g, ls.from[slot].end, slot};
   }
   __syncthreads();
   launch_dependents();
@@ -161,7 +162,7 @@ __global__ void reorder_kernel(const ReorderParams p) {
       if (k >= p.B_dst) continue;
       for (int j = 0; j < n_slots; ++j) {
         if (k >= ls.live[j]) continue;
-        const long long at = ((long long)ls.source[j] * p.G + g) * p.B_src + k;
+        const long long at = ls.from[j].unit * p.B_src + k;
         const uint32_t to = mine + (uint32_t)j * step;
         fetch4(to, p.src_s + at);
         fetch4(to + 4, p.src_q + at);
@@ -170,8 +171,8 @@ __global__ void reorder_kernel(const ReorderParams p) {
       }
       fetched();
       for (int i = 0; i < n_copies; ++i) {
-        const int j = ls.from[i];
-        const long long at = ((long long)ls.to[i] * p.G + g) * p.B_dst + k;
+        const int j = ls.to[i].slot;
+        const long long at = ls.to[i].unit * p.B_dst + k;
         if (k < ls.live[j]) {
           const uint4 x = room[j * threads + tid];
           p.dst_s[at] = __uint_as_float(x.x);
@@ -187,25 +188,23 @@ __global__ void reorder_kernel(const ReorderParams p) {
     }
     const int array = t - stat_tiles >= tiles;
     const int c0 = (t - stat_tiles - array * tiles) * per + tid;
-    const char *src = p.src[array] + (long long)g * p.src_unit;
-    char *dst = p.dst[array] + (long long)g * p.dst_unit;
-    const long long src_seq = p.src_unit * p.G, dst_seq = p.dst_unit * p.G;
-    for (int j = 0; j < n_slots; ++j) {
-      const int end = cache ? ls.live[j] << p.row_shift : chunks;
-      const char *from = src + ls.source[j] * src_seq;
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * threads;
-        if (c < end) fetch16(mine + (uint32_t)(j * U + u) * step, from + c * 16LL);
+    const char *src = p.src[array] + c0 * 16LL;
+    char *dst = p.dst[array] + c0 * 16LL;
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * threads;
+#pragma unroll 4
+      for (int j = 0; j < n_slots; ++j) {
+        const Lists::Place f = ls.from[j];
+        if (c < f.end) fetch16(mine + (uint32_t)(j * U + u) * step, src + f.unit * p.src_unit + u * step);
       }
     }
     fetched();
-    for (int i = 0; i < n_copies; ++i) {
-      const int j = ls.from[i];
-      const int end = cache ? ls.live[j] << p.row_shift : chunks;
-      char *to = dst + ls.to[i] * dst_seq;
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * threads;
-        if (c < end) *reinterpret_cast<uint4 *>(to + c * 16LL) = room[(j * U + u) * threads + tid];
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * threads;
+#pragma unroll 4
+      for (int i = 0; i < n_copies; ++i) {
+        const Lists::Place t = ls.to[i];
+        if (c < t.end) *reinterpret_cast<uint4 *>(dst + t.unit * p.dst_unit + u * step) = room[(t.slot * U + u) * threads + tid];
       }
     }
   }
