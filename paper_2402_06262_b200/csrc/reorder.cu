@@ -17,21 +17,14 @@
 namespace roco {
 namespace {
 
-constexpr int kMost = ROCO_REORDER_MAX_S;  // destinations of a CTA
+constexpr int kMost = ROCO_REORDER_MAX_S;  // sequences of an in-place call
 
-struct Lists {
-  int map[kMost];              // a destination's source, KEEP or FREE
-  int occupied[kMost];         // occupied slots of every sequence in this unit
-  int slot_of[kMost];          // source sequence -> the slot that it is kept in, -1: none yet
-  int live[kMost];             // slot -> its occupied slots in this unit; -1: not copied
-  struct Place {
-    long long unit;            // number of the unit
-    int end, slot;             // its 16-byte chunks that move; the slot that they are kept in
-  };
-  Place from[kMost], to[kMost];  // of every slot; of every copy
-  int empty[kMost];            // destinations that are freed
-  int n_slots, n_copies, n_empty, max_live;
+// A column that moves: number of the unit, its 16-byte chunks that move, the slot of a thread's room that they are kept in.
+struct Place {
+  long long unit;
+  int end, slot;
 };
+constexpr int kListBytes = 2 * sizeof(Place) + 5 * sizeof(int);
 
 __device__ __forceinline__ void fetch16(uint32_t dst, const void *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -105,52 +98,59 @@ __global__ void __launch_bounds__(kCopyThreads) reorder_copy_kernel(const Reorde
 
 __global__ void reorder_kernel(const ReorderParams p) {
   extern __shared__ uint4 room[];
-  __shared__ Lists ls;
+  __shared__ int n_slots_, n_copies_, n_empty_, max_live;
   const int tid = threadIdx.x, threads = blockDim.x;
   const int g = blockIdx.x / p.parts, part = blockIdx.x - g * p.parts, S = p.S_dst;
   const bool cache = p.arrays == 2;
+  // behind the threads' room (kListBytes for every sequence)
+  Place *const from = reinterpret_cast<Place *>(room + threads * p.room), *const to = from + S;  // of every slot; of every copy
+  int *const map = reinterpret_cast<int *>(to + S);   // a destination's source, KEEP or FREE
+  int *const occupied = map + S;                      // occupied slots of every sequence in this unit
+  int *const slot_of = occupied + S;                  // source sequence -> its slot, -1: none yet
+  int *const live_of = slot_of + S;                   // slot -> its occupied slots in this unit; -1: not copied
+  int *const empty = live_of + S;                     // destinations that are freed
 
   // which sources there are, and who gets them (up to kMost / threads sequences a thread)
   for (int i = tid; i < S; i += threads) {
-    ls.slot_of[i] = -1;
-    ls.occupied[i] = cache ? p.src_live[(long long)i * p.G + g] : 0;
-    ls.map[i] = source_of(p, i, blockIdx.x == 0);
+    slot_of[i] = -1;
+    occupied[i] = cache ? p.src_live[(long long)i * p.G + g] : 0;
+    map[i] = source_of(p, i, blockIdx.x == 0);
   }
-  if (tid == 0) ls.n_slots = ls.n_copies = ls.n_empty = ls.max_live = 0;
+  if (tid == 0) n_slots_ = n_copies_ = n_empty_ = max_live = 0;
   __syncthreads();
   for (int i = tid; i < S; i += threads) {
-    const int a = ls.map[i];
-    if (a == ROCO_REORDER_FREE) ls.empty[atomicAdd(&ls.n_empty, 1)] = i;
+    const int a = map[i];
+    if (a == ROCO_REORDER_FREE) empty[atomicAdd(&n_empty_, 1)] = i;
     if (a < 0) continue;
-    if (atomicCAS(&ls.slot_of[a], -1, kMost) == -1) {   // the first to ask for it
-      const int slot = atomicAdd(&ls.n_slots, 1);
-      int live = ls.occupied[a];
+    if (atomicCAS(&slot_of[a], -1, kMost) == -1) {   // the first to ask for it
+      const int slot = atomicAdd(&n_slots_, 1);
+      int live = occupied[a];
       if (cache && (live < 0 || live > p.B_src)) {
         if (part == 0) atomicOr(p.status, ROCO_DEV_BAD_LIVE);
         live = -1;
       }
-      atomicMax(&ls.max_live, live);
-      ls.live[slot] = live;
-      ls.from[slot] = {(long long)a * p.G + g, cache ? max(live, 0) << p.row_shift : (int)(p.src_unit / 16), slot};
-      ls.slot_of[a] = slot;
+      atomicMax(&max_live, live);
+      live_of[slot] = live;
+      from[slot] = {(long long)a * p.G + g, cache ? max(live, 0) << p.row_shift : (int)(p.src_unit / 16), slot};
+      slot_of[a] = slot;
     }
   }
   __syncthreads();
   for (int i = tid; i < S; i += threads) {
-    const int a = ls.map[i];
+    const int a = map[i];
     if (a < 0) continue;
-    const int slot = ls.slot_of[a];
-    if (cache && ls.live[slot] < 0) continue;
-    ls.to[atomicAdd(&ls.n_copies, 1)] = {(long long)i * p.G + g, ls.from[slot].end, slot};
+    const int slot = slot_of[a];
+    if (cache && live_of[slot] < 0) continue;
+    to[atomicAdd(&n_copies_, 1)] = {(long long)i * p.G + g, from[slot].end, slot};
   }
   __syncthreads();
   launch_dependents();
-  const int n_slots = ls.n_slots, n_copies = ls.n_copies, n_empty = ls.n_empty;
+  const int n_slots = n_slots_, n_copies = n_copies_, n_empty = n_empty_;
   const uint32_t mine = smem_u32(room + tid);
   const uint32_t step = threads * 16;  // from one of a thread's 16-byte places to its next
 
   // K and V, or the states: columns of 16 bytes
-  const int chunks = cache ? ls.max_live << p.row_shift : (int)(p.src_unit / 16);
+  const int chunks = cache ? max_live << p.row_shift : (int)(p.src_unit / 16);
   // columns of a thread at a time: as many as there is room for, but no more than leave work for every CTA of the unit
   const int lanes = p.parts * threads, share = (chunks * p.arrays + lanes - 1) / lanes;
   const int U = n_slots ? max(1, min(p.room / n_slots, share)) : 1;
@@ -161,8 +161,8 @@ __global__ void reorder_kernel(const ReorderParams p) {
       const int k = t * threads + tid;
       if (k >= p.B_dst) continue;
       for (int j = 0; j < n_slots; ++j) {
-        if (k >= ls.live[j]) continue;
-        const long long at = ls.from[j].unit * p.B_src + k;
+        if (k >= live_of[j]) continue;
+        const long long at = from[j].unit * p.B_src + k;
         const uint32_t to = mine + (uint32_t)j * step;
         fetch4(to, p.src_s + at);
         fetch4(to + 4, p.src_q + at);
@@ -171,9 +171,9 @@ __global__ void reorder_kernel(const ReorderParams p) {
       }
       fetched();
       for (int i = 0; i < n_copies; ++i) {
-        const int j = ls.to[i].slot;
-        const long long at = ls.to[i].unit * p.B_dst + k;
-        if (k < ls.live[j]) {
+        const int j = to[i].slot;
+        const long long at = to[i].unit * p.B_dst + k;
+        if (k < live_of[j]) {
           const uint4 x = room[j * threads + tid];
           p.dst_s[at] = __uint_as_float(x.x);
           p.dst_q[at] = __uint_as_float(x.y);
@@ -183,7 +183,7 @@ __global__ void reorder_kernel(const ReorderParams p) {
           p.dst_pos[at] = -1;
         }
       }
-      for (int i = 0; i < n_empty; ++i) p.dst_pos[((long long)ls.empty[i] * p.G + g) * p.B_dst + k] = -1;
+      for (int i = 0; i < n_empty; ++i) p.dst_pos[((long long)empty[i] * p.G + g) * p.B_dst + k] = -1;
       continue;
     }
     const int array = t - stat_tiles >= tiles;
@@ -194,7 +194,7 @@ __global__ void reorder_kernel(const ReorderParams p) {
       const int c = c0 + u * threads;
 #pragma unroll 4
       for (int j = 0; j < n_slots; ++j) {
-        const Lists::Place f = ls.from[j];
+        const Place f = from[j];
         if (c < f.end) fetch16(mine + (uint32_t)(j * U + u) * step, src + f.unit * p.src_unit + u * step);
       }
     }
@@ -203,7 +203,7 @@ __global__ void reorder_kernel(const ReorderParams p) {
       const int c = c0 + u * threads;
 #pragma unroll 4
       for (int i = 0; i < n_copies; ++i) {
-        const Lists::Place t = ls.to[i];
+        const Place t = to[i];
         if (c < t.end) *reinterpret_cast<uint4 *>(dst + t.unit * p.dst_unit + u * step) = room[(t.slot * U + u) * threads + tid];
       }
     }
@@ -211,7 +211,7 @@ __global__ void reorder_kernel(const ReorderParams p) {
   if (!cache) {
     for (int c = part * threads + tid; c < chunks; c += lanes)
       for (int i = 0; i < n_empty; ++i)
-        *reinterpret_cast<uint4 *>(p.dst[0] + ((long long)ls.empty[i] * p.G + g) * p.dst_unit + c * 16LL) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(p.dst[0] + ((long long)empty[i] * p.G + g) * p.dst_unit + c * 16LL) = make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -243,19 +243,21 @@ roco_status launch_reorder(ReorderParams p, int sms, cudaStream_t stream) {
     reorder_copy_kernel<<<(unsigned)ctas, kCopyThreads, 0, stream>>>(p);
     return cudaGetLastError() == cudaSuccess ? ROCO_OK : ROCO_ERR_CUDA;
   }
-  // Threads so that a CTA's places take 64 KB at most (three CTAs per SM) down to one warp; at least eight places each, for the
-  // columns of few sources that are in flight together.  CTAs with two columns a thread, up to 64 per SM (16 units x 512 states: 40 us,
-  // with one and four columns 42 and 47; eight beams x 1024 units with at most 16 and 32 CTAs per SM 1027 and 1008 us, with 64 972).
+  // Threads so that a CTA's places take 48 KB at most (four CTAs per SM) down to one warp; at least eight places each, for the
+  // columns of few sources that are in flight together (16 beams x 512 states 37 us, with 64 KB 39; 54 sequences forked from one x 40 units x 1016
+  // 199 and 215, 52 beams x 10 units x 3223, d 64, 128 and 120).  CTAs with two columns a thread, up to 64 per SM (16 beams x 512 states with
+  // one and four columns 42 and 47 us where this took 40; eight beams x 1024 units with at most 16 and 32 CTAs per SM 1027 and 1008
+  // us, with 64 972).
   int threads = 256;
-  while (threads > 32 && threads * p.S_dst * 16 > 65536) threads /= 2;
+  while (threads > 32 && threads * p.S_dst * 16 > 49152) threads /= 2;
   p.room = p.S_dst < 8 ? 8 : p.S_dst;
-  const int smem = threads * p.room * 16;
+  const int smem = threads * p.room * 16 + p.S_dst * kListBytes;
   long long parts = (chunks + 2LL * threads - 1) / (2LL * threads), most = (64LL * sms + p.G - 1) / p.G;
   if (parts > most) parts = most;
   p.parts = parts < 1 ? 1 : (int)parts;
   if ((long long)p.G * p.parts > 0x7fffffffLL) return ROCO_ERR_UNSUPPORTED;
   static SmemLimit limit;
-  if (!limit((const void *)reorder_kernel, 32 * kMost * 16)) return ROCO_ERR_CUDA;
+  if (!limit((const void *)reorder_kernel, 32 * kMost * 16 + kMost * kListBytes)) return ROCO_ERR_CUDA;
   reorder_kernel<<<(unsigned)(p.G * p.parts), threads, smem, stream>>>(p);
   if (cudaGetLastError() != cudaSuccess) return ROCO_ERR_CUDA;
   if (p.arrays == 1) return ROCO_OK;
