@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2402_06262_b200 as R
-import round_reference as ref
+import decoding_reference as ref
 from paper_2402_06262_b200 import binding
 from test_abi_cpu import fake_cache
 from test_operators_host import linear_state

@@ -5,7 +5,7 @@ import torch
 
 import operator_reference as ops
 import paper_2402_06262_b200 as R
-import round_reference as ref
+import decoding_reference as ref
 from tree_cases import CACHE_FIELDS
 
 pytestmark = pytest.mark.gpu

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2402_06262_b200 as R
-import round_reference as ref
+import decoding_reference as ref
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -101,7 +101,7 @@ def test_more_heads_than_one_cta_takes_and_more_tokens_than_a_tile():
     run(12, S=1, N=2, G=40, group=8, d=128, adjacent=True, dtype="f32")
 
 
-def test_many_tokens_take_sixteen_heads_at_a_time():
+def test_heads_per_cta_change_no_bit():
     """The number of heads that a thread goes through depends on the number of tokens and changes no bit: a call that fills the GPU
     gives what calls of a few sequences each give."""
     S, N, G, group, d = 16, 513, 10, 2, 128

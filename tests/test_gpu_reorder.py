@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2402_06262_b200 as R
-import round_reference as ref
+import decoding_reference as ref
 
 pytestmark = pytest.mark.gpu
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
