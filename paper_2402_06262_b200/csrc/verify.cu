@@ -8,9 +8,10 @@
 // A row is cut into one run per warp of the cluster.  Every warp sends its run's sum to every rank by an asynchronous store that also
 // signals (no barrier of the cluster, no reduction in the CTA before it); the sums are the upper level of a prefix sum, which the pick
 // descends: run, chunk of 16 bytes, element.
-// Bound by a chain of latencies (one tree x 32000 tokens: 6.9 us in a graph, of which launch 0.7, the nodes' numbers 1.4, the walk 0.8, a
+// Bound by a chain of latencies (one tree x 32000 tokens: 7 us in a graph, of which launch 0.7, the nodes' numbers 1.4, the walk 0.8, a
 // pass over the row 1.4, the sums' way 0.3, the pick about 1), and with many sequences by the walks with most rejections: 64 sequences x
-// 128000 tokens take 34 us, 20 to the end of the first row (4.6 TB/s while it is read), 9 for further passes of the few that need them.
+// 128000 tokens take 32.8 us: the first row ends at 11 to 13, every further pass takes 3 to 4 (with three CTAs per SM a quarter of the
+// clusters found no room at first and started when others ended).
 // Sums and products are in 64 bits: an index is the answer, and an error of 2^-24 in a sum over 10^5 tokens moves it about once in a
 // thousand calls.
 #include "heads.cuh"
@@ -18,7 +19,10 @@
 namespace roco {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kResident = 3;  // (CTAs per SM)
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+template <typename T>
+constexpr int kResident = sizeof(T) == 4 ? 4 : 3;  // CTAs per SM: as many as their registers allow
+constexpr int kDepth = 4, kRingBytes = kDepth * 2 * kThreads * 16;  // chunks of a thread under way
 constexpr int kWarpShift = 3, kMaxRanks = 8, kRuns = kMaxRanks * kWarps, kPer = kRuns / 32;
 constexpr int kLast = kThreads;  // chunks that are searched at once
 static_assert(kWarps == 1 << kWarpShift, "runs are divided by shifts");
@@ -108,50 +112,58 @@ __device__ __forceinline__ double widen(float x) {
   return __hiloint2double((int)((bits >> 3) + ((1023u - 127u) << 20)), (int)(bits << 29));
 }
 
-// A lane's part of the sum of what is left of p over chunks lo .. hi - 1 of a warp (chunks lane, lane + 32, ... of the run).  A row
-// is read at the pace of loads in flight, so kBatch chunks are fetched before any is worked on.
+// A lane's part of the sum of what is left of p over whole chunks i, i + 32, ... before `end`.  A row is read at the pace of loads in
+// flight, so the thread keeps kDepth of them under way into places of its own in shared memory (`ring`: the address of its first; through
+// registers, four at a time, 34.1 us where this takes 32.8, and fewer CTAs per SM).  One chunk is worked on at a time: two cost more
+// registers than they hide (37 us).
 template <typename T, bool kDraft>
-__device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end, double C) {
-  constexpr int E = Rows<T>::E, kBatch = 16 / E;
-  const uint4 *p = reinterpret_cast<const uint4 *>(rows.p - rows.lead), *q = reinterpret_cast<const uint4 *>(rows.q - rows.lead);
+__device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end, double C, const uint4 *ring) {
+  constexpr int E = Rows<T>::E;
+  const uint4 *p = reinterpret_cast<const uint4 *>(rows.p - rows.lead) + i, *q = reinterpret_cast<const uint4 *>(rows.q - rows.lead) + i;
+  const uint32_t at = smem_u32(ring);
+  auto fetch = [&](int slot, int ahead) {
+    if (i + ahead < end) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + slot * (2 * kThreads * 16)), "l"(p + ahead) : "memory");
+      if (kDraft)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + slot * (2 * kThreads * 16) + kThreads * 16), "l"(q + ahead) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
   double sum = 0.0, twice = 0.0;
-  for (; i < end; i += 32 * kBatch) {
-    uint4 a[kBatch], b[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      a[k] = b[k] = make_uint4(0, 0, 0, 0);
-      if (i + 32 * k < end) {
-        a[k] = __ldg(p + i + 32 * k);
-        if (kDraft) b[k] = __ldg(q + i + 32 * k);
+  for (int s = 0; s < kDepth; ++s) fetch(s, 32 * s);
+  for (int n = 0; i < end; n = (n + 1) % kDepth) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    const uint4 a = ring[n * (2 * kThreads)];
+    const uint4 b = kDraft ? ring[n * (2 * kThreads) + kThreads] : a;
+    fetch(n, 32 * kDepth);
+    i += 32;
+    p += 32;
+    q += 32;
+    float fp[E], fq[E];
+    Elem<T>::unpack(a, fp);
+    if (kDraft) Elem<T>::unpack(b, fq);
+    uint32_t least = __float_as_uint(fp[0]), most = least;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      least = __vimin3_u32(least, __float_as_uint(fp[e]), __float_as_uint(fp[e + 1]));
+      most = __vimax3_u32(most, __float_as_uint(fp[e]), __float_as_uint(fp[e + 1]));
+      if (kDraft) {
+        least = __vimin3_u32(least, __float_as_uint(fq[e]), __float_as_uint(fq[e + 1]));
+        most = __vimax3_u32(most, __float_as_uint(fq[e]), __float_as_uint(fq[e + 1]));
       }
     }
+    if (least >= kLeastNormal && most < kInfinity) {
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      float fp[E], fq[E];
-      Elem<T>::unpack(a[k], fp);
-      if (kDraft) Elem<T>::unpack(b[k], fq);
-      uint32_t least = __float_as_uint(fp[0]), most = least;
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        least = __vimin3_u32(least, __float_as_uint(fp[e]), __float_as_uint(fp[e + 1]));
-        most = __vimax3_u32(most, __float_as_uint(fp[e]), __float_as_uint(fp[e + 1]));
-        if (kDraft) {
-          least = __vimin3_u32(least, __float_as_uint(fq[e]), __float_as_uint(fq[e + 1]));
-          most = __vimax3_u32(most, __float_as_uint(fq[e]), __float_as_uint(fq[e + 1]));
-        }
+      for (int e = 0; e < E; ++e) {
+        const double x = kDraft ? fma(-C, widen(fq[e]), widen(fp[e])) : widen(fp[e]);
+        twice += kDraft ? x + fabs(x) : x;
       }
-      if (least >= kLeastNormal && most < kInfinity) {
+    } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const double x = kDraft ? fma(-C, widen(fq[e]), widen(fp[e])) : widen(fp[e]);
-          twice += kDraft ? x + fabs(x) : x;
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const double x = kDraft ? fma(-C, (double)fq[e], (double)fp[e]) : (double)fp[e];
-          sum += x <= 0.0 ? 0.0 : x;
-        }
+      for (int e = 0; e < E; ++e) {
+        const double x = kDraft ? fma(-C, (double)fq[e], (double)fp[e]) : (double)fp[e];
+        sum += x <= 0.0 ? 0.0 : x;
       }
     }
   }
@@ -160,7 +172,7 @@ __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end,
 
 // What is left of p over chunks lo .. hi - 1 of a warp.
 template <typename T>
-__device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, double C, const int *gone, int n_gone) {
+__device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, double C, const int *gone, int n_gone, const uint4 *ring) {
   constexpr int E = Rows<T>::E;
   const int lane = threadIdx.x & 31, full = (rows.V + rows.lead) / E;
   int i = lo + lane;
@@ -169,7 +181,7 @@ __device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, d
   // the row's first and last chunk may reach beyond it
   const bool head = plain && rows.lead && lo == 0 && hi > 0, tail = plain && full < rows.chunks && full >= lo && full < hi && (full > 0 || !head);
   if (head && lane == 0) i += 32;
-  if (plain) sum = rows.q ? sum_whole<T, true>(rows, i, min(hi, full), C) : sum_whole<T, false>(rows, i, min(hi, full), C);
+  if (plain) sum = rows.q ? sum_whole<T, true>(rows, i, min(hi, full), C, ring) : sum_whole<T, false>(rows, i, min(hi, full), C, ring);
   // what is left for one chunk at a time
   int from = plain ? hi : lo + lane, step = 32;
   if (lane == 0 && (head || tail)) {
@@ -210,8 +222,9 @@ __device__ __forceinline__ int pick_run(double sum, double upto, double target, 
 __device__ __forceinline__ int pick_run(double sum, double target, double &base) { return pick_run(sum, warp_scan64(sum), target, base); }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(const VerifyParams p) {
   constexpr int E = Elem<T>::kPerChunk;
+  extern __shared__ uint4 ring[];   // kDepth times a chunk of p and one of q for every thread
   __shared__ Smem sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ranks = p.ranks, b = blockIdx.x >> p.rank_shift, rank = blockIdx.x & (ranks - 1);
@@ -391,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, kResident) tree_verify_kernel(const 
     const bool known = from_all && all_of == sm.tip;
     double sum = known ? all : 0.0;
     for (int exact = from_all ? 0 : 1; exact < 2; ++exact) {
-      if (exact || !known) sum = sum_run(rows, lo, hi, c, sm.gone, exact ? out : 0);
+      if (exact || !known) sum = sum_run(rows, lo, hi, c, sm.gone, exact ? out : 0, ring + tid);
       if (exact) break;
       all = sum;
       all_of = sm.tip;
@@ -511,15 +524,17 @@ template <typename T>
 roco_status launch_t(VerifyParams p, int S, int sms, cudaStream_t stream) {
   // CTAs per sequence, a power of two: doubled while they fill less than three quarters of the GPU, so up to half as many again as
   // reside together, because the walks with most rejections end last and every rejection costs a pass over a row by its own CTAs
-  // alone (64 sequences x 128000 tokens, three CTAs per SM: eight 34 us, six, which reside together, 37.4, four 53).  None with
-  // fewer 16-byte chunks of a row than threads.
+  // alone (64 sequences x 128000 tokens, fp32: eight 32.8 us; with three CTAs per SM eight took 34, six, which reside together, 37, four 53).
+  // None with fewer 16-byte chunks of a row than threads.
   int shift = 0;
   const long long chunks = (p.V + Elem<T>::kPerChunk - 1) / Elem<T>::kPerChunk;
-  while ((1 << shift) < kMaxRanks && ((4LL * S) << shift) < 3LL * kResident * sms && chunks >= (2LL * kThreads) << shift) ++shift;
+  while ((1 << shift) < kMaxRanks && ((4LL * S) << shift) < 3LL * kResident<T> * sms && chunks >= (2LL * kThreads) << shift) ++shift;
   p.rank_shift = shift;
   p.ranks = 1 << shift;
   const int ranks = p.ranks;
-  const bool ok = launch_cluster(tree_verify_kernel<T>, (unsigned)S * (unsigned)ranks, (unsigned)ranks, kThreads, 0, stream, p);
+  static SmemLimit limit;
+  if (!limit((const void *)tree_verify_kernel<T>, kRingBytes)) return ROCO_ERR_CUDA;
+  const bool ok = launch_cluster(tree_verify_kernel<T>, (unsigned)S * (unsigned)ranks, (unsigned)ranks, kThreads, kRingBytes, stream, p);
   return ok ? ROCO_OK : ROCO_ERR_CUDA;
 }
 
