@@ -153,3 +153,20 @@ def test_another_stream_and_a_captured_call():
     for _ in range(2):
         t = ref.reorder_cache(t, t, seq)
     same(c, t)
+
+
+def test_two_calls_at_once():
+    sides = torch.cuda.Stream(), torch.cuda.Stream()
+    ts = [fields(30 + i, 8, 16, 300, 128, "bf16") for i in range(2)]
+    caches, maps = [wrap(t) for t in ts], [random_map(3 + i, 8, 8) for i in range(2)]
+    sources = [ints(m) for m in maps]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, s, side in zip(caches, sources, sides):
+            with torch.cuda.stream(side):
+                R.roco_cache_reorder(c, s)
+    torch.cuda.synchronize()
+    for t, c, m in zip(ts, caches, maps):
+        for _ in range(3):
+            t = ref.reorder_cache(t, t, m)
+        same(c, t)

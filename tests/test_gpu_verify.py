@@ -336,3 +336,52 @@ def test_another_stream_a_captured_call_and_two_at_once():
     launch(first)
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(first, held)) and int(status) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("drafts", ["drawn", "distinct", "fixed"])
+def test_rows_cut_to_their_likeliest_tokens(dtype, drafts):
+    """Most probabilities are exactly zero, as after a cut to the likeliest tokens, in the target and (elsewhere) in the draft."""
+    for V in (40, 5003, 40000):
+        c = make(23 + V, 20, 6, V, drafts, True, dtype, near=1.5)
+        for name, keep in (("target", 0.02), ("target_prefix", 0.02), ("draft", 0.05), ("draft_prefix", 0.05)):
+            if c[name] is None:
+                continue
+            x = c[name].double()
+            border = x.quantile(1 - keep, dim=-1, keepdim=True) if V < 10000 else x.topk(int(keep * V), -1).values[..., -1:]
+            x = torch.where(x >= border, x, 0)
+            c[name] = (x / x.sum(-1, keepdim=True)).to(DT[dtype])
+        check(c, 6)
+
+
+@pytest.mark.parametrize("drafts", ["drawn", "fixed"])
+def test_probabilities_below_the_normal_numbers(drafts):
+    """A token of probability 2^-140 is one that can be drawn: by u' = 0 it is the first, and it is accepted by u = 0."""
+    c = make(24, 4, 1, 5000, drafts, True)
+    tiny = 2.0 ** -140
+    c["target_prefix"][:, :7], c["target"][:, :, :7] = 0, 0
+    c["target_prefix"][:, 3], c["target"][:, :, 3] = tiny, tiny
+    c["tokens"][:2], c["tokens"][2:] = 3, 5
+    c["accept_u"][:], c["sample_u"][:] = 0, 0
+    path, n, nxt = check(c, 1)
+    assert n.tolist() == [1, 1, 0, 0] and (nxt[:2] == 3).all()
+    if drafts == "fixed":
+        assert (nxt[2:] == 3).all()
+    else:
+        c["draft_prefix"][:, 3] = 0
+        path, n, nxt = check(c, 1)
+        assert n.tolist() == [1, 1, 0, 0] and (nxt[2:] == 3).all()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_drafts_that_are_no_probabilities(bad):
+    """A draft's row with a NaN leaves nothing to draw from where a child was rejected against it; an infinity there takes all of its
+    token; where the child was accepted the row is not looked at."""
+    c = make(25, 2, 1, 3000, "drawn", True)
+    c["draft_prefix"][:, 1234] = bad
+    c["tokens"][:] = 77
+    c["target_prefix"][0, 77], c["target_prefix"][1, 77] = 0.5, 0
+    c["draft_prefix"][:, 77] = 0.25
+    path, n, nxt = call(c, 1, status=BAD_PROBS if math.isnan(bad) else 0)
+    assert n.tolist() == [1, 0] and int(nxt[0]) >= 0
+    assert int(nxt[1]) == -1 if math.isnan(bad) else int(nxt[1]) not in (-1, 77, 1234)
