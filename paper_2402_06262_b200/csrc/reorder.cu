@@ -8,10 +8,10 @@
 //
 // In place the work is cut by columns, 16 bytes at one place of a unit, which a thread handles for all sequences: it fetches the
 // column of every distinct source into its own part of shared memory (asynchronous 16-byte copies), then writes it to every
-// destination.  So any map is right (cycles, forks, chains): a column is written only after all of it has been read, and nobody else
-// touches it.  Threads share nothing but the map, so nobody waits for anybody.  Eight beams x 1024 units x 1024 slots: 6.1 GB in 972 us,
-// 6.3 TB/s; a prompt forked into seven more samples in one layer (121 of 138 MB are writes) 28 us, where plain writes of as many
-// bytes take 39.
+// destination, zeros of freed states among them.  So any map is right (cycles, forks, chains, freed sources): a column is written
+// only after all of it has been read, and nobody else touches it.  Threads share nothing but the map, so nobody waits for anybody.
+// Eight beams x 1024 units x 1024 slots: 6.1 GB in 972 us, 6.3 TB/s; a prompt forked into seven more samples in one layer (121 of
+// 138 MB are writes) 28 us, where plain writes of as many bytes take 39.
 #include "heads.cuh"
 
 namespace roco {
@@ -206,12 +206,11 @@ __global__ void reorder_kernel(const ReorderParams p) {
         const Place t = to[i];
         if (c < t.end) *reinterpret_cast<uint4 *>(dst + t.unit * p.dst_unit + u * step) = room[(t.slot * U + u) * threads + tid];
       }
+      // a freed sequence's states become zero here too: it may be the source of others, whose column this thread has fetched
+      if (!cache && c < chunks)
+        for (int i = 0; i < n_empty; ++i)
+          *reinterpret_cast<uint4 *>(dst + ((long long)empty[i] * p.G + g) * p.dst_unit + u * step) = make_uint4(0, 0, 0, 0);
     }
-  }
-  if (!cache) {
-    for (int c = part * threads + tid; c < chunks; c += lanes)
-      for (int i = 0; i < n_empty; ++i)
-        *reinterpret_cast<uint4 *>(p.dst[0] + ((long long)empty[i] * p.G + g) * p.dst_unit + c * 16LL) = make_uint4(0, 0, 0, 0);
   }
 }
 
