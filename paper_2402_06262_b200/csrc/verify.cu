@@ -304,7 +304,8 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
     sm.number = number;
     sm.more = 0;
   }
-  // (a peer's shared memory may be written once the peer runs and its barriers are ready)
+  // (a peer's shared memory may be written once the peer runs and its barriers are ready; an aligned barrier wants the whole warp)
+  __syncwarp();
   if (ranks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   bool anew = false;   // nothing was left of p after the rejections: once more with p itself
   double total = 0.0, base = 0.0, mine[kPer];
@@ -423,6 +424,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
     double *sums = sm.sums[pass & 1];
     if (ranks > 1) {
       // every warp sends its sum to every rank; the store and the signal that it is there travel together
+      __syncwarp();
       if (pass == 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
       uint64_t *bar = &sm.bar[pass & 1];
       if (tid == 0) mbar_expect_tx(bar, ranks * kWarps * 8);
