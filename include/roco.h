@@ -586,7 +586,7 @@ roco_status roco_rotary_device_status(const roco_rotary *rotary, void *stream, i
  * occupied ones get pos = -1 and are otherwise left as they were.
  *
  *   src, dst     the same cache (in place: any map, cycles and forks among them; up to ROCO_REORDER_MAX_S sequences), or two that
- *                share no memory, of equal dtype, G and d, with dst->B >= src->B
+ *                share no memory but perhaps the status word, of equal dtype, G and d, with dst->B >= src->B
  *   source       [dst->S] int32 DEVICE array.  A value that is neither a sequence of src nor one of the two below sets
  *                ROCO_DEV_BAD_MAP in dst->status and counts as ROCO_REORDER_KEEP.  A unit of src whose live is outside [0, B] sets
  *                ROCO_DEV_BAD_LIVE there and is not copied

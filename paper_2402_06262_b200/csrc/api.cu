@@ -48,6 +48,25 @@ bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
   return x < y + b_bytes && y < x + a_bytes;
 }
 
+// Whether any of the eight arrays of a overlaps any of b's.
+bool share_memory(const roco_cache *a, const roco_cache *b) {
+  const void *at[2][8];
+  size_t bytes[2][8];
+  for (int i = 0; i < 2; ++i) {
+    const roco_cache *c = i ? b : a;
+    const size_t units = (size_t)c->S * c->G, slots = units * c->B, rows = slots * c->d * (c->kv_dtype == ROCO_BF16 ? 2 : 4);
+    const void *arrays[8] = {c->K, c->V, c->s, c->q, c->n, c->pos, c->live, c->t_next};
+    for (int k = 0; k < 8; ++k) {
+      at[i][k] = arrays[k];
+      bytes[i][k] = k < 2 ? rows : 4 * (k < 6 ? slots : units);
+    }
+  }
+  for (int k = 0; k < 8; ++k)
+    for (int j = 0; j < 8; ++j)
+      if (overlap(at[0][k], bytes[0][k], at[1][j], bytes[1][j])) return true;
+  return false;
+}
+
 struct PrefillWs {
   size_t lens_off, lse_off, s_off, q_off, dst_off, total;
 };
@@ -900,9 +919,7 @@ roco_status roco_cache_reorder(const roco_cache *src, roco_cache *dst, const int
     return ROCO_ERR_INVALID_ARG;
   if (p.in_place && src->S > ROCO_REORDER_MAX_S) return ROCO_ERR_UNSUPPORTED;
   const int row = src->d * (src->kv_dtype == ROCO_BF16 ? 2 : 4);
-  const size_t src_bytes = (size_t)src->S * src->G * src->B * row, dst_bytes = (size_t)dst->S * dst->G * dst->B * row;
-  if (!p.in_place && (overlap(src->K, src_bytes, dst->K, dst_bytes) || overlap(src->V, src_bytes, dst->V, dst_bytes)))
-    return ROCO_ERR_INVALID_ARG;
+  if (!p.in_place && share_memory(src, dst)) return ROCO_ERR_INVALID_ARG;
   p.src[0] = static_cast<const char *>(src->K); p.src[1] = static_cast<const char *>(src->V);
   p.dst[0] = static_cast<char *>(dst->K); p.dst[1] = static_cast<char *>(dst->V);
   p.src_unit = (long long)src->B * row; p.dst_unit = (long long)dst->B * row;
