@@ -26,6 +26,8 @@ constexpr int kDepth = 4, kRingBytes = kDepth * 2 * kThreads * 16;  // chunks of
 constexpr int kWarpShift = 3, kMaxRanks = 8, kRuns = kMaxRanks * kWarps, kPer = kRuns / 32;
 constexpr int kLast = kThreads;  // chunks that are searched at once
 static_assert(kWarps == 1 << kWarpShift, "runs are divided by shifts");
+// Of a sum less some of its terms at least this much has to be left, or it is formed again without them: no more than ten bits are lost.
+constexpr double kLeast = 1.0 / 1024;
 constexpr int kNodes = ROCO_TREE_MAX_NODES;
 static_assert(kNodes == 64, "a node's children are the bits of one 64-bit word");
 
@@ -322,6 +324,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
       int tip = sm.tip, len = sm.len, n_gone = sm.n_gone;
       double C = sm.C, R = sm.R, M = sm.M;
       bool more = false, summed = sm.more;   // R has been summed behind this node
+      const double least = kLeast * R;
       while (!more && len < p.A && untried) {
         const int i = __ffsll((long long)untried) - 1, x = sm.token[i];
         untried &= untried - 1;
@@ -359,6 +362,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
             more = untried != 0;
           } else if (!again) {
             R -= sm.gone_p[n_gone - 1];
+            more = untried != 0 && R < least;
           }
         }
       }
@@ -388,8 +392,8 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
       lo = min(first + warp * run, end);
       hi = min(lo + run, end);
     }
-    // Tokens that are out are taken off a sum over all of p, which stands while the walk stays at its node; where next to nothing would
-    // be left of it, the sum is formed without them.
+    // Tokens that are out are taken off a sum over all of p, which stands while the walk stays at its node; where too little would be
+    // left of it, the sum is formed without them.
     const bool from_all = !draft && end == 0 && !anew;
     int here = 0;
     double less = 0.0;
@@ -410,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
       all = sum;
       all_of = sm.tip;
       sum -= less;
-      if (!here || sum > 1e-9 * all) break;
+      if (!here || sum > kLeast * all) break;
     }
     if (end != 0) {
       if (lane == 0) sm.part[warp] = sum;
