@@ -486,18 +486,23 @@ roco_status roco_linear_device_status(const roco_linear_state *state, void *stre
 /*
  * Which path of the drafted trees the target model accepts, and the token that follows it (speculative sampling; the paper
  * has no counterpart): the decision between roco_tree_attend and roco_tree_commit, from given random numbers.  The tokens that
- * come out are distributed as the target's own.
+ * come out are distributed as the target's own, as far as the rows sum to one (below).
  *
  * A sequence's walk starts at the root and tries the children of the node it stands on in index order.  With p the target's
  * and q the draft's probabilities behind that node, C = 0, R = 1, M = 1 at first, a child with token x is accepted if
  *     u q(x) R < max(p(x) - C q(x), 0) M                                      (u: accept_u of the child)
  * and becomes the node to stand on.  After a rejection what is left of p is max(p - C q, 0) with C increased by R / M (where
  * M > 0); R is the sum of that over the vocabulary.  M stays 1 where siblings were drawn from q independently of each other;
- * with `distinct` they were drawn without replacement, and M falls by q(x).  Without draft probabilities (the drafts are, say,
- * the likeliest tokens) a child is accepted if u R < p(x), else p loses x and R is the sum of the rest.  A token that was
- * rejected among its siblings already counts as having no probability (with `distinct` or without draft probabilities).
+ * with `distinct` they were drawn without replacement, and M falls by q(x); where that leaves less than 3/16, M becomes the sum of
+ * q over the tokens that were not rejected.  Without draft probabilities (the drafts are, say, the likeliest tokens) a child is
+ * accepted if u R < p(x), else p loses x and R is the sum of the rest.  A token that was rejected among its siblings already counts
+ * as having no probability (with `distinct` or without draft probabilities).
  * Where no child is accepted, or the path has A nodes, next_token is the first v at which the sum over 0..v of what is left of
  * p exceeds u' times the sum over all (u': sample_u); p itself where nothing is left.  All of this is in 64 bits.
+ *
+ * What is trusted: that p and q sum to one in the first test at a node, and q later on while M is 3/16 or more; R and lesser M are
+ * sums.  Rows rounded to bf16 miss one by up to 2^-8, usually about 2^-10, and the distribution of a token then misses the target's by
+ * about as much (at most 0.003 in total variation, enumerated over peaked rows of few tokens); fp32 rows by about 10^-7.
  *
  *   target       [S][T] rows of V probabilities, of the token behind each node; element type `dtype`
  *   draft        [S][T] rows of V probabilities that the children of each node were drawn from, or NULL.  Rows are given by

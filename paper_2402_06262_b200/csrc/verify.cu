@@ -28,19 +28,27 @@ constexpr int kLast = kThreads;  // chunks that are searched at once
 static_assert(kWarps == 1 << kWarpShift, "runs are divided by shifts");
 // Of a sum less some of its terms at least this much has to be left, or it is formed again without them: no more than ten bits are lost.
 constexpr double kLeast = 1.0 / 1024;
+// Where drafts are drawn without replacement and less than this is left of the draft, its mass is summed.  One less the rejected is off
+// by as much as the row's sum is off one (up to 2^-8 in bf16), which is all that matters once little is left.  Exact distributions of the
+// first token over bf16 rows of five and six tokens, two and three siblings, from flat drafts to a token of 0.999: at most 0.003 in
+// total variation from the target's (never summed 0.19, from 1/8 on 0.008, from 1/4 on 0.0028, always 0.0024, which is what the rows' sums
+// cost in the first test).
+constexpr double kLittle = 3.0 / 16;
 constexpr int kNodes = ROCO_TREE_MAX_NODES;
 static_assert(kNodes == 64, "a node's children are the bits of one 64-bit word");
 
+template <bool kDistinct>
 struct Smem {
-  double p[kNodes], q[kNodes], u[kNodes];
+  float p[kNodes], q[kNodes], u[kNodes];
   unsigned long long children[kNodes + 1];  // of the prefix, then of every node
   double sums[2][kRuns];                    // of every warp of every rank; one set while the other may still be read
+  double masses[2][kDistinct ? kRuns : 1];  // the same of the draft's tokens that are not rejected, where that is wanted
   double part[kWarps];
   uint64_t bar[2];                          // completes when a set is here
   unsigned first[2];                        // bits of the nodes that are accepted where no sibling was rejected before
   int token[kNodes];
   int gone[kNodes];                         // tokens rejected behind the node the walk stands on, each once
-  double gone_p[kNodes];                    // their probabilities
+  float gone_p[kNodes];                     // their probabilities
   int path[ROCO_TREE_MAX_PATH];
   // where the walk stands: node, nodes on the path, children of it that are not tried yet, tokens in gone
   int tip, len, n_gone;
@@ -48,6 +56,7 @@ struct Smem {
   double C, R, M;
   double number;                            // sample_u
   int more;                                 // R is to be summed before the walk goes on
+  int weigh;                                // and M, from the draft's row
   int abort_flag;
 };
 
@@ -71,6 +80,22 @@ struct Rows {
     lead = (int)((reinterpret_cast<uintptr_t>(target) & 15u) / sizeof(T));
     chunks = (int)(((long long)V + lead + E - 1) / E);
     q_like_p = ((reinterpret_cast<uintptr_t>(target) ^ reinterpret_cast<uintptr_t>(draft)) & 15u) == 0;
+  }
+
+  // The draft's probabilities in chunk i but for the tokens in gone; 0 outside the row.
+  __device__ __forceinline__ double mass(int i, const int *gone, int n_gone) const {
+    const int first = i * E - lead;
+    float f[E];
+    if (q_like_p && first >= 0 && first + E <= V) Elem<T>::unpack(__ldg(reinterpret_cast<const uint4 *>(q + first)), f);
+    else some(q, first, f);
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      for (int g = 0; g < n_gone; ++g)
+        if (gone[g] == first + e) f[e] = 0.f;
+      sum += f[e] <= 0.f ? 0.0 : (double)f[e];
+    }
+    return sum;
   }
 
   __device__ __forceinline__ void some(const T *row, int first, float (&f)[E]) const {
@@ -118,8 +143,8 @@ __device__ __forceinline__ double widen(float x) {
 // flight, so the thread keeps kDepth of them under way into places of its own in shared memory (`ring`: the address of its first; through
 // registers, four at a time, 34.1 us where this takes 32.8, and fewer CTAs per SM).  One chunk is worked on at a time: two cost more
 // registers than they hide (37 us).
-template <typename T, bool kDraft>
-__device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end, double C, const uint4 *ring) {
+template <typename T, bool kDraft, bool kMass>
+__device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end, double C, const uint4 *ring, double &mass) {
   constexpr int E = Rows<T>::E;
   const uint4 *p = reinterpret_cast<const uint4 *>(rows.p - rows.lead) + i, *q = reinterpret_cast<const uint4 *>(rows.q - rows.lead) + i;
   const uint32_t at = smem_u32(ring);
@@ -131,7 +156,7 @@ __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end,
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  double sum = 0.0, twice = 0.0;
+  double twice = 0.0;
 #pragma unroll
   for (int s = 0; s < kDepth; ++s) fetch(s, 32 * s);
   for (int n = 0; i < end; n = (n + 1) % kDepth) {
@@ -160,30 +185,37 @@ __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end,
       for (int e = 0; e < E; ++e) {
         const double x = kDraft ? fma(-C, widen(fq[e]), widen(fp[e])) : widen(fp[e]);
         twice += kDraft ? x + fabs(x) : x;
+        if (kMass) mass += widen(fq[e]);
       }
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const double x = kDraft ? fma(-C, (double)fq[e], (double)fp[e]) : (double)fp[e];
-        sum += x <= 0.0 ? 0.0 : x;
+        twice += x <= 0.0 ? 0.0 : kDraft ? x + x : x;
+        if (kMass) mass += fq[e] <= 0.f ? 0.0 : (double)fq[e];
       }
     }
   }
-  return sum + (kDraft ? 0.5 : 1.0) * twice;
+  return (kDraft ? 0.5 : 1.0) * twice;
 }
 
-// What is left of p over chunks lo .. hi - 1 of a warp.
+// What is left of p over chunks lo .. hi - 1 of a warp; where it is wanted, the draft's mass there as well.
 template <typename T>
-__device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, double C, const int *gone, int n_gone, const uint4 *ring) {
+__device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, double C, const int *gone, int n_gone, const uint4 *ring,
+                                          bool weigh, double &mass) {
   constexpr int E = Rows<T>::E;
   const int lane = threadIdx.x & 31, full = (rows.V + rows.lead) / E;
   int i = lo + lane;
-  double sum = 0.0;
+  double sum = 0.0, held = 0.0;
   const bool plain = n_gone == 0 && (!rows.q || rows.q_like_p);
   // the row's first and last chunk may reach beyond it
   const bool head = plain && rows.lead && lo == 0 && hi > 0, tail = plain && full < rows.chunks && full >= lo && full < hi && (full > 0 || !head);
   if (head && lane == 0) i += 32;
-  if (plain) sum = rows.q ? sum_whole<T, true>(rows, i, min(hi, full), C, ring) : sum_whole<T, false>(rows, i, min(hi, full), C, ring);
+  if (plain) {
+    if (weigh) sum = sum_whole<T, true, true>(rows, i, min(hi, full), C, ring, held);
+    else if (rows.q) sum = sum_whole<T, true, false>(rows, i, min(hi, full), C, ring, held);
+    else sum = sum_whole<T, false, false>(rows, i, min(hi, full), C, ring, held);
+  }
   // what is left for one chunk at a time
   int from = plain ? hi : lo + lane, step = 32;
   if (lane == 0 && (head || tail)) {
@@ -195,8 +227,35 @@ __device__ __forceinline__ double sum_run(const Rows<T> &rows, int lo, int hi, d
     rows.left(from, C, gone, n_gone, r);
 #pragma unroll
     for (int e = 0; e < E; ++e) sum += r[e];
+    if (weigh) held += rows.mass(from, gone, 0);
   }
+  if (weigh) mass = warp_sum64(held);
   return warp_sum64(sum);
+}
+
+// The draft's mass over chunks lo .. hi - 1 of a warp without the rejected tokens, from `all` of it there.
+template <typename T>
+__device__ __forceinline__ double mass_left(const Rows<T> &rows, int lo, int hi, double all, const int *gone, int n_gone) {
+  constexpr int E = Rows<T>::E;
+  double less = 0.0;
+  bool here = false;
+  for (int g = 0; g < n_gone; ++g) {
+    const int at = gone[g] + rows.lead;
+    if (at < lo * E || at >= hi * E) continue;
+    here = true;
+    less += fmaxf(Elem<T>::load(rows.q + gone[g]), 0.f);
+  }
+  if (!here || all - less > kLeast * all) return all - less;
+  double sum = 0.0;
+  for (int i = lo + (threadIdx.x & 31); i < hi; i += 32) sum += rows.mass(i, gone, n_gone);
+  return warp_sum64(sum);
+}
+
+// A number into another CTA's shared memory (or the own), and the signal that it is there.
+__device__ __forceinline__ void send(uint32_t to, double x, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(to), "l"(__double_as_longlong(x)),
+               "r"(bar)
+               : "memory");
 }
 
 __device__ __forceinline__ double warp_scan64(double v) {
@@ -223,11 +282,13 @@ __device__ __forceinline__ int pick_run(double sum, double upto, double target, 
 }
 __device__ __forceinline__ int pick_run(double sum, double target, double &base) { return pick_run(sum, warp_scan64(sum), target, base); }
 
-template <typename T>
+// kDistinct: there is a draft, drawn from without replacement.
+template <typename T, bool kDistinct>
 __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(const VerifyParams p) {
   constexpr int E = Elem<T>::kPerChunk;
-  extern __shared__ uint4 ring[];   // kDepth times a chunk of p and one of q for every thread
-  __shared__ Smem sm;
+  // kDepth times a chunk of p and one of q for every thread (16 bytes off a 32-byte boundary a batch takes 8 % longer)
+  extern __shared__ __align__(128) uint4 ring[];
+  __shared__ Smem<kDistinct> sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ranks = p.ranks, b = blockIdx.x >> p.rank_shift, rank = blockIdx.x & (ranks - 1);
   const bool rooted = p.target_prefix == nullptr;
@@ -265,8 +326,8 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
       if (ok && (given || up >= 0 || !rooted)) {
         if (!given) {
           const char *row = up < 0 ? target_prefix : target + up * p.target_row;
-          const double px = Elem<T>::load(reinterpret_cast<const T *>(row) + x);
-          double qx = 1.0;
+          const float px = Elem<T>::load(reinterpret_cast<const T *>(row) + x);
+          float qx = 1.f;
           if (draft) {
             row = up < 0 ? draft_prefix : draft + up * p.draft_row;
             qx = Elem<T>::load(reinterpret_cast<const T *>(row) + x);
@@ -274,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
           sm.p[tid] = px;
           sm.q[tid] = qx;
           sm.u[tid] = u;
-          first = u * qx < px;
+          first = (double)u * qx < px;
         }
         sm.token[tid] = x;
         atomicOr(&sm.children[up + 1], 1ull << tid);
@@ -305,6 +366,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
     sm.C = 0.0; sm.R = 1.0; sm.M = 1.0;
     sm.number = number;
     sm.more = 0;
+    sm.weigh = 0;
   }
   // (a peer's shared memory may be written once the peer runs and its barriers are ready; an aligned barrier wants the whole warp)
   __syncwarp();
@@ -335,8 +397,8 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
         if (n_gone == 0) {
           yes = firsts >> i & 1;
           q = sm.q[i];
-        } else if (draft) {
-          q = again && p.distinct ? 0.0 : sm.q[i];
+        } else if (kDistinct || draft) {
+          q = again && kDistinct ? 0.0 : sm.q[i];
           const double left = sm.p[i] - C * sm.q[i];
           yes = sm.u[i] * q * R < (left <= 0.0 ? 0.0 : left) * M;
         } else {
@@ -354,9 +416,9 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
             sm.gone_p[n_gone] = sm.p[i] > 0.0 ? sm.p[i] : 0.0;
             sm.gone[n_gone++] = x;
           }
-          if (draft) {
+          if (kDistinct || draft) {
             if (M > 0.0) C += M == 1.0 ? R : R / M;
-            if (p.distinct) M -= q;
+            if (kDistinct) M -= q;
             more = untried != 0;
           } else if (!summed) {
             more = untried != 0;
@@ -374,15 +436,17 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
       sm.R = R;
       sm.M = M;
       sm.more = more;
+      if (kDistinct) sm.weigh = more && M < kLittle;
     }
     __syncthreads();
     int lo, hi;
+    const bool weigh = kDistinct && end == 0 && !anew && sm.weigh;
     if (end == 0) {
       const int on = sm.tip;
       c = anew ? 0.0 : sm.C;
-      out = draft || anew ? 0 : sm.n_gone;
+      out = kDistinct || draft || anew ? 0 : sm.n_gone;
       rows = Rows<T>(on < 0 ? target_prefix : target + on * p.target_row,
-                     c == 0.0 || !draft ? nullptr : on < 0 ? draft_prefix : draft + on * p.draft_row, p.V);
+                     !draft || (c == 0.0 && !weigh) ? nullptr : on < 0 ? draft_prefix : draft + on * p.draft_row, p.V);
       // runs of chunks: of this rank, of this warp in it
       run = (rows.chunks + (kWarps << p.rank_shift) - 1) >> (kWarpShift + p.rank_shift);
       lo = min((rank * kWarps + warp) * run, rows.chunks);
@@ -394,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
     }
     // Tokens that are out are taken off a sum over all of p, which stands while the walk stays at its node; where too little would be
     // left of it, the sum is formed without them.
-    const bool from_all = !draft && end == 0 && !anew;
+    const bool from_all = !kDistinct && !draft && end == 0 && !anew;
     int here = 0;
     double less = 0.0;
     if (from_all) {
@@ -407,15 +471,16 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
       }
     }
     const bool known = from_all && all_of == sm.tip;
-    double sum = known ? all : 0.0;
+    double sum = known ? all : 0.0, mass = 0.0;
     for (int exact = from_all ? 0 : 1; exact < 2; ++exact) {
-      if (exact || !known) sum = sum_run(rows, lo, hi, c, sm.gone, exact ? out : 0, ring + tid);
+      if (exact || !known) sum = sum_run(rows, lo, hi, c, sm.gone, exact ? out : 0, ring + tid, weigh, mass);
       if (exact) break;
       all = sum;
       all_of = sm.tip;
       sum -= less;
       if (!here || sum > kLeast * all) break;
     }
+    if (weigh) mass = mass_left(rows, lo, hi, mass, sm.gone, sm.n_gone);
     if (end != 0) {
       if (lane == 0) sm.part[warp] = sum;
       __syncthreads();
@@ -425,21 +490,23 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
       if (end - first <= kLast) break;
       continue;
     }
-    double *sums = sm.sums[pass & 1];
+    double *sums = sm.sums[pass & 1], *masses = sm.masses[pass & 1];
     if (ranks > 1) {
       // every warp sends its sum to every rank; the store and the signal that it is there travel together
       __syncwarp();
       if (pass == 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
       uint64_t *bar = &sm.bar[pass & 1];
-      if (tid == 0) mbar_expect_tx(bar, ranks * kWarps * 8);
-      if (lane < ranks)
-        asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
-                         map_to_rank(&sums[rank * kWarps + warp], lane)),
-                     "l"(__double_as_longlong(sum)), "r"(map_to_rank(bar, lane))
-                     : "memory");
+      if (tid == 0) mbar_expect_tx(bar, ranks * kWarps * (weigh ? 16 : 8));
+      if (lane < ranks) {
+        send(map_to_rank(&sums[rank * kWarps + warp], lane), sum, map_to_rank(bar, lane));
+        if (weigh) send(map_to_rank(&masses[rank * kWarps + warp], lane), mass, map_to_rank(bar, lane));
+      }
       mbar_wait_compact(bar, (pass >> 1) & 1, &sm.abort_flag, p.status);
     } else {
-      if (lane == 0) sums[warp] = sum;
+      if (lane == 0) {
+        sums[warp] = sum;
+        if (kDistinct) masses[warp] = mass;
+      }
       __syncthreads();
     }
 #pragma unroll
@@ -450,6 +517,13 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
     const double upto = warp_scan64(some);
     total = __shfl_sync(0xffffffffu, upto, 31);
     if (tid == 0) sm.R = total;
+    if (weigh && warp == 0) {
+      double m = 0.0;
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) m += kPer * lane + k < ranks * kWarps ? masses[kPer * lane + k] : 0.0;
+      m = warp_sum64(m);
+      if (lane == 0 && isfinite(m)) sm.M = m;
+    }
     ++pass;
     // on with the walk, or once more where nothing is left
     const bool more = sm.more;
@@ -526,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, kResident<T>) tree_verify_kernel(con
   p.next_token[b] = token;
 }
 
-template <typename T>
+template <typename T, bool kDistinct>
 roco_status launch_t(VerifyParams p, int S, int sms, cudaStream_t stream) {
   // CTAs per sequence, a power of two: doubled while they fill less than three quarters of the GPU, so up to half as many again as
   // reside together, because the walks with most rejections end last and every rejection costs a pass over a row by its own CTAs
@@ -539,15 +613,18 @@ roco_status launch_t(VerifyParams p, int S, int sms, cudaStream_t stream) {
   p.ranks = 1 << shift;
   const int ranks = p.ranks;
   static SmemLimit limit;
-  if (!limit((const void *)tree_verify_kernel<T>, kRingBytes)) return ROCO_ERR_CUDA;
-  const bool ok = launch_cluster(tree_verify_kernel<T>, (unsigned)S * (unsigned)ranks, (unsigned)ranks, kThreads, kRingBytes, stream, p);
+  const auto kernel = tree_verify_kernel<T, kDistinct>;
+  if (!limit((const void *)kernel, kRingBytes)) return ROCO_ERR_CUDA;
+  const bool ok = launch_cluster(kernel, (unsigned)S * (unsigned)ranks, (unsigned)ranks, kThreads, kRingBytes, stream, p);
   return ok ? ROCO_OK : ROCO_ERR_CUDA;
 }
 
 }  // namespace
 
 roco_status launch_tree_verify(const VerifyParams &p, int dtype, int S, int sms, cudaStream_t stream) {
-  return dtype == ROCO_BF16 ? launch_t<__nv_bfloat16>(p, S, sms, stream) : launch_t<float>(p, S, sms, stream);
+  if (p.draft && p.distinct)
+    return dtype == ROCO_BF16 ? launch_t<__nv_bfloat16, true>(p, S, sms, stream) : launch_t<float, true>(p, S, sms, stream);
+  return dtype == ROCO_BF16 ? launch_t<__nv_bfloat16, false>(p, S, sms, stream) : launch_t<float, false>(p, S, sms, stream);
 }
 
 }  // namespace roco
