@@ -812,10 +812,13 @@ def roco_tree_verify(target, tokens, parent, accept_u, sample_u, path, path_len,
     _need(what, "status", status, (1,), i32, dev)
     if nodes is not None:
         _need(what, "nodes", nodes, each, i32, dev)
-    call = _VERIFY.pack(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, T, V, A, 1 if distinct else 0, target.data_ptr(),
-                        _zero(draft), _zero(target_prefix), _zero(draft_prefix), ts[0], ts[1], ds[0], ds[1], tp, dp,
-                        tokens.data_ptr(), parent.data_ptr(), 0 if nodes is None else nodes.data_ptr(), accept_u.data_ptr(), sample_u.data_ptr(),
-                        path.data_ptr(), path_len.data_ptr(), next_token.data_ptr(), status.data_ptr())
+    try:
+        call = _VERIFY.pack(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, T, V, A, 1 if distinct else 0, target.data_ptr(),
+                            _zero(draft), _zero(target_prefix), _zero(draft_prefix), ts[0], ts[1], ds[0], ds[1], tp, dp,
+                            tokens.data_ptr(), parent.data_ptr(), 0 if nodes is None else nodes.data_ptr(), accept_u.data_ptr(),
+                            sample_u.data_ptr(), path.data_ptr(), path_len.data_ptr(), next_token.data_ptr(), status.data_ptr())
+    except struct.error as e:
+        raise RocoError(2, f"{what}: a size beyond 32 bits") from e
     rc = lib().roco_tree_verify(call, _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
@@ -859,14 +862,17 @@ def roco_norm_rotate(rotary: Rotary, q, k, v, Q, K, V, lens=None, start=None, po
     if start is not None:
         if (not isinstance(start, torch.Tensor) or start.dtype is not torch.int32 or start.shape != (S,) or start.get_device() != dev):
             raise RocoError(1, f"{what}: start: an int32 tensor of shape [{S}] on the current CUDA device is needed")
-        apart = start.stride(0)
+        apart = start.stride(0) if S > 1 else 0   # (what no index is multiplied with may be anything)
     if positions is not None:
         if rotary.axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 2:
             positions = positions[..., None]
         _need(what, "positions", positions, (S, N, rotary.axes), torch.int32, dev)
-    call = _HEADS.pack(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, N, G, group, apart, q.data_ptr(), _zero(k), _zero(v),
-                       qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], _zero(lens), _zero(start), _zero(positions), Q.data_ptr(), _zero(K),
-                       _zero(V))
+    try:
+        call = _HEADS.pack(ROCO_F32 if dtype is torch.float32 else ROCO_BF16, S, N, G, group, apart, q.data_ptr(), _zero(k), _zero(v),
+                           qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], _zero(lens), _zero(start), _zero(positions), Q.data_ptr(),
+                           _zero(K), _zero(V))
+    except struct.error as e:
+        raise RocoError(2, f"{what}: a size, or the stride of start, beyond 32 bits") from e
     rc = lib().roco_norm_rotate(rotary.ref, call, _raw_stream(dev))
     if rc != ROCO_OK:
         raise RocoError(rc, what)
