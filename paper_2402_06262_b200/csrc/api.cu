@@ -5,7 +5,7 @@
 #include <mutex>
 
 #include "common.cuh"
-#include "heads.cuh"
+#include "decoding.cuh"
 #include "launch.h"
 #include "linear.cuh"
 #include "tree.cuh"

@@ -11,7 +11,7 @@
 // projections leaves as blocks of 8 to 32 tokens per head.  128 threads (64: 262 us, 256: 299), five CTAs per SM by their registers.
 // A small call is a chain of latencies (8 tokens x 96 heads 3.5 us in a graph): positions, frequencies, weights and the first rows are
 // all under way before any of them is needed.
-#include "heads.cuh"
+#include "decoding.cuh"
 
 namespace roco {
 namespace {

@@ -173,7 +173,7 @@ roco_status launch_linear_prefill_simt(const LinearParams &p, int d, int U, cuda
 int linear_tc_segments(int U, int Lmax, int sms);
 roco_status launch_linear_prefill_tc(const LinearParams &p, int d, int U, cudaStream_t stream);
 
-// ---- norm and rotation of a layer's heads, verification of drafted trees, reordering of sequences (heads.cuh)
+// ---- norm and rotation of a layer's heads, verification of drafted trees, reordering of sequences (decoding.cuh)
 struct HeadsParams;
 struct VerifyParams;
 struct ReorderParams;

@@ -12,7 +12,7 @@
 // only after all of it has been read, and nobody else touches it.  Threads share nothing but the map, so nobody waits for anybody.
 // Eight beams x 1024 units x 1024 slots: 6.1 GB in 972 us, 6.3 TB/s; a prompt forked into seven more samples in one layer (121 of
 // 138 MB are writes) 28 us, where plain writes of as many bytes take 39.
-#include "heads.cuh"
+#include "decoding.cuh"
 
 namespace roco {
 namespace {

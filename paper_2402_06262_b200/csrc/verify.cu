@@ -14,7 +14,7 @@
 // clusters found no room at first and started when others ended).
 // Sums and products are in 64 bits: an index is the answer, and an error of 2^-24 in a sum over 10^5 tokens moves it about once in a
 // thousand calls.
-#include "heads.cuh"
+#include "decoding.cuh"
 
 namespace roco {
 namespace {
