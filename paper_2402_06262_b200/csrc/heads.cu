@@ -207,7 +207,8 @@ roco_status launch_t(HeadsParams p, int pairing, int sms, cudaStream_t stream) {
   // anew, which costs as much as kSetup heads, and of more than one wave the last is half full on average, the time is about
   // (waves + 1/2) (heads per CTA + kSetup) (1180 tokens x 400 heads: ten CTAs, one wave, 44 us; 6, 13 and 30 take 56, 54 and 47; 32768 tokens
   // x 96 heads: three 239 us, one and six 246; 6002 x 40 heads, fp32, d 64: two 20.5 us, one and seven 26.5 and 22).
-  constexpr double kSetup = 3.0, kResident = sizeof(T) == 2 ? 5.0 : 6.0;   // (CTAs per SM, by their registers)
+  // (CTAs per SM by their registers: five in bf16, six in single precision; adjacent pairs there would allow seven, which is not told apart)
+  constexpr double kSetup = 3.0, kResident = sizeof(T) == 2 ? 5.0 : 6.0;
   const double slots = kResident * sms;
   int parts = all;
   if ((double)tiles * all > slots) {

@@ -10,7 +10,7 @@
 // descends: run, chunk of 16 bytes, element.
 // Bound by a chain of latencies (one tree x 32000 tokens: 7 us in a graph, of which launch 0.7, the nodes' numbers 1.4, the walk 0.8, a
 // pass over the row 1.4, the sums' way 0.3, the pick about 1), and with many sequences by the walks with most rejections: 64 sequences x
-// 128000 tokens take 32.8 us: the first row ends at 11 to 13, every further pass takes 3 to 4 (with three CTAs per SM a quarter of the
+// 128000 tokens take 31.3 us: the first row ends at 11 to 13, every further pass takes 3 to 4 (with three CTAs per SM a quarter of the
 // clusters found no room at first and started when others ended).
 // Sums and products are in 64 bits: an index is the answer, and an error of 2^-24 in a sum over 10^5 tokens moves it about once in a
 // thousand calls.
@@ -141,7 +141,7 @@ __device__ __forceinline__ double widen(float x) {
 
 // A lane's part of the sum of what is left of p over whole chunks i, i + 32, ... before `end`.  A row is read at the pace of loads in
 // flight, so the thread keeps kDepth of them under way into places of its own in shared memory (`ring`: the address of its first; through
-// registers, four at a time, 34.1 us where this takes 32.8, and fewer CTAs per SM).  One chunk is worked on at a time: two cost more
+// registers, four at a time, 34.1 us where this took 32.8, and fewer CTAs per SM).  One chunk is worked on at a time: two cost more
 // registers than they hide (37 us).
 template <typename T, bool kDraft, bool kMass>
 __device__ __forceinline__ double sum_whole(const Rows<T> &rows, int i, int end, double C, const uint4 *ring, double &mass) {
@@ -604,7 +604,7 @@ template <typename T, bool kDistinct>
 roco_status launch_t(VerifyParams p, int S, int sms, cudaStream_t stream) {
   // CTAs per sequence, a power of two: doubled while they fill less than three quarters of the GPU, so up to half as many again as
   // reside together, because the walks with most rejections end last and every rejection costs a pass over a row by its own CTAs
-  // alone (64 sequences x 128000 tokens, fp32: eight 32.8 us; with three CTAs per SM eight took 34, six, which reside together, 37, four 53).
+  // alone (64 sequences x 128000 tokens, fp32: eight 31.3 us; with three CTAs per SM eight took 34, six, which reside together, 37, four 53).
   // None with fewer 16-byte chunks of a row than threads.
   int shift = 0;
   const long long chunks = (p.V + Elem<T>::kPerChunk - 1) / Elem<T>::kPerChunk;
